@@ -15,7 +15,8 @@
  * the factorized second moment of "4-bit Factor" (Sec. 4.3), rank-1 normalization for more than two
  * dimensions (App. F Alg. 4), SGD with momentum (App. E Alg. 2), stand-alone compress / decompress, the
  * quantizers the paper ablates for the second moment (Sec. 4.1, Tab. 1, App. D.3), plans (many tensors per
- * call), and the plan steps with device-resident learning rate and step number.
+ * call), the plan steps with device-resident learning rate and step number, and, for models whose weights are
+ * kept in 4 bits as well, the compressed weights' products with their gradients and the loss of distillation.
  *
  * Conventions for every call
  *   - All data pointers are DEVICE pointers unless the comment says "host".  The caller owns every
@@ -460,6 +461,80 @@ int lpmm_adamw4_plan_release(void* plan);
 /* Kernels that one step of the plan enqueues (host call; the capturable form enqueues one more in front), or LPMM_EINVAL
  * if `plan` is not a plan.  1 for a plan that holds tensors with two passes: it is stepped in one launch. */
 int lpmm_adamw4_plan_launches(const void* plan);
+
+/* ---- weights in 4 bits with group scales ---------------------------------------------------------------------------
+ *
+ * A matrix W of shape {n, k} (a linear layer's: n outputs, k inputs) whose element is value[code] * scale.
+ *   code    E2M1, the 4-bit float that gfx950 converts in hardware: 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes 0..7, their
+ *           negatives for codes 8..15.
+ *   scales  float[n][ceil(k/group)], one per group of 32, 64 or 128 elements along k (the last may be short).
+ *   codes   n rows of kp/2 bytes, kp = k rounded up to a multiple of 128, codes of the padding 0 (the products rely on
+ *           that).  8 codes make a 32-bit word, the first in the low bits; of the 16 words of 128 elements word d stands at
+ *           place (d % 4) * 4 + d / 4.  16-byte aligned.
+ * In the calls below a tensor of rows has unit stride along a row and `..._stride` elements from one row to the next (at least
+ * the row's length), LPMM_F32 or LPMM_BF16 elements, and needs no more than its elements' alignment; outputs must not
+ * overlap inputs.  Products are summed in fp32.  t == 0 is allowed and does nothing (the scales' gradient is then 0).
+ * No call needs lpmm_adamw4_init.  NaN and infinities are carried through as the formulas do. */
+#define LPMM_F32  0
+#define LPMM_BF16 1
+
+/* Bytes of {codes, scales}.  shape = {n, k}; both below 2^31, with n * kp at most 2^37. */
+int lpmm_w4_sizes(const int64_t shape[2], int group, size_t sizes[2]);
+
+/* Compress: scale = max|w| / 6 of the group (one fp32 division; 0 where the maximum is below 2^-100), code = the entry
+ * nearest to w / scale, decided exactly (no rounded quotient), ties to the smaller magnitude; -0 has code 0.  A group
+ * that holds a NaN or an infinity gets scale NaN, so that what it meets becomes NaN. */
+int lpmm_w4_quant(const void* w, int dtype, int64_t w_stride, const int64_t shape[2], int group, uint8_t* codes,
+                  float* scales, void* stream);
+
+/* Decompress: value * scale, one fp32 product, rounded once more for LPMM_BF16. */
+int lpmm_w4_dequant(const uint8_t* codes, const float* scales, const int64_t shape[2], int group, void* w, int dtype,
+                    int64_t w_stride, void* stream);
+
+/* y[t][n] = sum_k x[t][k] W[n][k]: a linear layer for t tokens, one or many. */
+int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const uint8_t* codes, const float* scales,
+                   const int64_t shape[2], int group, void* y, int64_t y_stride, void* stream);
+
+/* dx[t][k] = sum_n dy[t][n] W[n][k]: its gradient with respect to x. */
+int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, const uint8_t* codes,
+                      const float* scales, const int64_t shape[2], int group, void* dx, int64_t dx_stride,
+                      void* stream);
+
+/* dscales[n][j] = sum_t dy[t][n] sum_{k in group j} x[t][k] value[code[n][k]]: its gradient with respect to the scales,
+ * float[n][ceil(k/group)], written, not added to.  x and dy share a type.  workspace: device memory, 16-byte aligned, of
+ * the bytes that ..._workspace_bytes gives (0 means none is needed; it is also 0 for invalid arguments), contents arbitrary before and after; calls that may
+ * overlap in time need one each.  The order of all sums is fixed: equal inputs give equal bits. */
+size_t lpmm_w4_linear_dscale_workspace_bytes(int64_t t, const int64_t shape[2], int group);
+int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, int64_t x_stride, int64_t dy_stride,
+                          const uint8_t* codes, const int64_t shape[2], int group, float* dscales, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* ---- distillation from a teacher's top logits ------------------------------------------------------------------------
+ *
+ * z: student's logits, t rows of v (z_dtype, z_stride).  top: float[t][slots], index: int64[t][slots], the teacher's largest logits
+ * and where in the vocabulary they stand, both without gaps between rows.  A slot counts if 0 <= index < v (fill short lists
+ * with -1); 1 <= slots <= LPMM_DISTILL_MAX_SLOTS; an index may appear more than once.  tau: temperature, finite and > 0.
+ *   p    = softmax(top / tau) over a row's slots that count
+ *   lse  = log sum_i exp(z_i / tau)
+ *   loss = tau^2 sum_j p_j (log p_j - z[index_j] / tau + lse)            (terms with p_j = 0 are 0)
+ *   dz_i = grad * tau * (exp(z_i / tau - lse) - sum of the p_j with index_j = i)
+ * A row without slots that count (prompt, padding) has loss, lse and dz 0, whatever its logits hold, and its logits are not read;
+ * so has a row with grad == 0 its dz.  loss, lse, grad: float[t].  dz has z's type and may be z itself (same stride).
+ * workspace as above. */
+#define LPMM_DISTILL_MAX_SLOTS 1024
+size_t lpmm_distill_workspace_bytes(int64_t t, int64_t v);
+int lpmm_distill_loss(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
+                      const int64_t* index, int slots, float tau, float* loss, float* lse, void* workspace,
+                      size_t workspace_bytes, void* stream);
+/* lse: as lpmm_distill_loss wrote it for the same arguments. */
+int lpmm_distill_grad(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
+                      const int64_t* index, int slots, float tau, const float* lse, const float* grad, void* dz,
+                      int64_t dz_stride, void* stream);
+/* Both at once, for training loops that know grad beforehand (lse as above): the logits are read once where a row fits into a
+ * workgroup's registers. */
+int lpmm_distill_loss_grad(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
+                           const int64_t* index, int slots, float tau, const float* grad, float* loss, float* lse,
+                           void* dz, int64_t dz_stride, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Per-kernel timing for benchmarks, with HIP events recorded on each call's own stream.
  * lpmm_profile_begin(max_calls): from now on every lpmm_adamw4_step / _step_bf16g call in this process

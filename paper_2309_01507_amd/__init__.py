@@ -20,5 +20,7 @@ from .binding import (  # noqa: F401
     StateSgdm, new_state_sgdm, lpmm_sgdm4_state_sizes, lpmm_sgdm4_state_zero, lpmm_sgdm4_step, lpmm_sgdm4_step_bf16g,
     lpmm_sgdm32_step, lpmm_sgdm4_step_multi, make_desc_sgdm, lpmm_adamw4_step_multi_capturable,
     lpmm_sgdm4_step_multi_capturable, KIND_SGDM_4BIT, KIND_SGDM_FP32, FLAG_NO_DECAY, FLAG_DETERMINISTIC, KIND_4BIT_ND,
+    WeightsW4, new_w4, lpmm_w4_sizes, lpmm_w4_quant, lpmm_w4_dequant, lpmm_w4_linear, lpmm_w4_linear_dx,
+    lpmm_w4_linear_dscale, lpmm_distill_loss, lpmm_distill_grad, lpmm_distill_loss_grad, DISTILL_MAX_SLOTS, F32, BF16,
 )
 from .optim import AdamW4bit, SGDM4bit  # noqa: F401,E402

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 import subprocess
+import tempfile
 from dataclasses import dataclass
 from typing import Optional
 
@@ -17,8 +18,9 @@ _ROOT = os.path.dirname(_HERE)
 _SRC_DIR = os.path.join(_HERE, "csrc")
 _LIB = os.path.join(_HERE, "lpmm4.so")
 
-HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
+HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+SOURCES = ("lpmm4.hip", "w4.hip")
 
 GRAD_F32, GRAD_BF16 = 0, 1
 
@@ -33,12 +35,21 @@ def lib_path() -> str:
 
 def build_library(verbose: bool = False) -> str:
     """Cross-compile lpmm4.so for gfx950 with hipcc (works without a GPU)."""
-    cmd = ["hipcc", *HIPCC_FLAGS, os.path.join(_SRC_DIR, "lpmm4.hip"), "-o", _LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise LpmmError("hipcc failed:\n" + res.stdout + res.stderr)
-    if verbose:
-        print(" ".join(cmd))
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.splitext(src)[0] + ".o") for src in SOURCES]
+        cmds = [["hipcc", *HIPCC_FLAGS, "-c", os.path.join(_SRC_DIR, src), "-o", obj]
+                for src, obj in zip(SOURCES, objects)]
+        running = [subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for cmd in cmds]
+        said = [p.communicate()[0] for p in running]
+        link = ["hipcc", "--offload-arch=gfx950", "-shared", *objects, "-o", _LIB]
+        for p, text in zip(running, said):
+            if p.returncode != 0:
+                raise LpmmError("hipcc failed:\n" + text)
+        res = subprocess.run(link, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise LpmmError("hipcc failed:\n" + res.stdout + res.stderr)
+        if verbose:
+            print("\n".join(" ".join(cmd) for cmd in (*cmds, link)))
     return _LIB
 
 
@@ -112,6 +123,22 @@ def lib() -> ctypes.CDLL:
         L.lpmm_adamw4_step_multi.argtypes = [_VP] + [_F] * 5 + [_I64, _VP]
         L.lpmm_adamw4_plan_release.argtypes = [_VP]
         L.lpmm_adamw4_plan_launches.argtypes = [_VP]
+        L.lpmm_w4_sizes.argtypes = [_VP, ctypes.c_int, _VP]
+        L.lpmm_w4_quant.argtypes = [_VP, ctypes.c_int, _I64, _VP, ctypes.c_int, _VP, _VP, _VP]
+        L.lpmm_w4_dequant.argtypes = [_VP, _VP, _VP, ctypes.c_int, _VP, ctypes.c_int, _I64, _VP]
+        product_args = [_VP, ctypes.c_int, _I64, _I64, _VP, _VP, _VP, ctypes.c_int, _VP, _I64, _VP]
+        L.lpmm_w4_linear.argtypes = product_args
+        L.lpmm_w4_linear_dx.argtypes = product_args
+        L.lpmm_w4_linear_dscale_workspace_bytes.argtypes = [_I64, _VP, ctypes.c_int]
+        L.lpmm_w4_linear_dscale_workspace_bytes.restype = ctypes.c_size_t
+        L.lpmm_w4_linear_dscale.argtypes = [_VP, _VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, ctypes.c_int, _VP, _VP,
+                                            ctypes.c_size_t, _VP]
+        L.lpmm_distill_workspace_bytes.argtypes = [_I64, _I64]
+        L.lpmm_distill_workspace_bytes.restype = ctypes.c_size_t
+        distill_args = [_VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, ctypes.c_int, _F]
+        L.lpmm_distill_loss.argtypes = distill_args + [_VP, _VP, _VP, ctypes.c_size_t, _VP]
+        L.lpmm_distill_grad.argtypes = distill_args + [_VP, _VP, _VP, _I64, _VP]
+        L.lpmm_distill_loss_grad.argtypes = distill_args + [_VP] * 4 + [_I64, _VP, ctypes.c_size_t, _VP]
         L.lpmm_profile_begin.argtypes = [_I64]
         L.lpmm_profile_end.argtypes = [_VP, _VP]
         _lib = L
@@ -581,6 +608,234 @@ def lpmm_dequant_ablation(norm, map_, is_signed, codes, scale_a, scale_b, rows, 
     _check(lib().lpmm_dequant_ablation(int(norm), int(map_), int(is_signed), _ptr(codes), _ptr(scale_a),
                                        _ptr(scale_b), ctypes.addressof(shape), _ptr(out), _stream(stream)),
            "lpmm_dequant_ablation")
+
+
+# ---- weights in 4 bits with group scales ------------------------------------------------------------------
+
+F32, BF16 = 0, 1
+
+
+@dataclass
+class WeightsW4:
+    """A rows x cols weight matrix in 4 bits: E2M1 codes and one fp32 scale per `group` elements of a row (lpmm4.h)."""
+    rows: int
+    cols: int
+    group: int
+    codes: "object"
+    scales: "object"
+
+
+def _w4_check(w: WeightsW4, what: str) -> None:
+    if (w.codes.numel() != w.rows * ((w.cols + 127) // 128 * 64) or not w.codes.is_contiguous() or
+            w.scales.shape != (w.rows, -(-w.cols // w.group)) or not w.scales.is_contiguous()):
+        raise ValueError(f"{what}: codes or scales are not those of a {w.rows} x {w.cols} matrix with groups of {w.group}")
+
+
+def _rows(t, cols: int, what: str):
+    """(pointer, type, rows, elements from one row to the next) of a matrix argument"""
+    import torch
+    dtype = BF16 if t.dtype == torch.bfloat16 else F32 if t.dtype == torch.float32 else None
+    if dtype is None:
+        raise ValueError(f"{what} must be float32 or bfloat16")
+    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must have {cols} columns, next to each other")
+    n = t.shape[0]
+    stride = t.stride(0) if n > 1 else cols
+    if stride < cols:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), dtype, n, stride
+
+
+def _on_current(what: str, *tensors) -> None:
+    import torch
+    here = torch.cuda.current_device() if any(t.is_cuda for t in tensors) else None
+    if any(not t.is_cuda or t.device.index != here for t in tensors):
+        raise ValueError(f"{what}: all tensors must be on the current GPU")
+
+
+def _new(out, shape, dtype, device, stream, what: str):
+    """The caller's output, or one allocated on torch's current stream."""
+    import torch
+    if out is None:
+        if stream is not None:
+            raise ValueError(f"{what}: a call on a stream of its own needs its outputs (and workspace) given")
+        return torch.empty(shape, dtype=dtype, device=device)
+    if out.dtype != dtype or out.shape != torch.Size(shape):
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}")
+    return out
+
+
+def lpmm_w4_sizes(rows: int, cols: int, group: int = 128):
+    """Bytes of the codes and of the scales."""
+    sizes = (ctypes.c_size_t * 2)()
+    shape = _shape(rows, cols)
+    _check(lib().lpmm_w4_sizes(ctypes.addressof(shape), int(group), ctypes.addressof(sizes)), "lpmm_w4_sizes")
+    return [int(s) for s in sizes]
+
+
+def new_w4(rows: int, cols: int, group: int = 128, device="cuda") -> WeightsW4:
+    """Allocate (torch) room for a compressed matrix; lpmm_w4_quant fills it."""
+    import torch
+    sz = lpmm_w4_sizes(rows, cols, group)
+    return WeightsW4(rows, cols, group, torch.empty(sz[0], dtype=torch.uint8, device=device),
+                     torch.empty(rows, sz[1] // (4 * rows), dtype=torch.float32, device=device))
+
+
+def lpmm_w4_quant(w, group: int = 128, out: Optional[WeightsW4] = None, stream=None) -> WeightsW4:
+    """w: rows x cols, float32 or bfloat16.  Returns `out`, or new codes and scales."""
+    if out is None:
+        if stream is not None:
+            raise ValueError("lpmm_w4_quant: a call on a stream of its own needs `out`")
+        if w.dim() != 2:
+            raise ValueError("lpmm_w4_quant: w must be a matrix")
+        out = new_w4(w.shape[0], w.shape[1], group, w.device)
+    ptr, dtype, n, ld = _rows(w, out.cols, "w")
+    if n != out.rows or group != out.group:
+        raise ValueError("lpmm_w4_quant: out has another shape or group")
+    _w4_check(out, "out")
+    _on_current("lpmm_w4_quant", w, out.codes, out.scales)
+    shape = _shape(out.rows, out.cols)
+    _check(lib().lpmm_w4_quant(ptr, dtype, ld, ctypes.addressof(shape), group, out.codes.data_ptr(),
+                               out.scales.data_ptr(), _stream(stream)), "lpmm_w4_quant")
+    return out
+
+
+def lpmm_w4_dequant(w: WeightsW4, dtype=None, out=None, stream=None):
+    """The values as a rows x cols matrix, float32 or bfloat16 (`dtype`, or that of `out`; float32 by default)."""
+    import torch
+    _w4_check(w, "w")
+    if dtype is None:
+        dtype = torch.float32 if out is None else out.dtype
+    out = _new(out, (w.rows, w.cols), dtype, w.codes.device, stream, "out")
+    ptr, dt, n, ld = _rows(out, w.cols, "out")
+    _on_current("lpmm_w4_dequant", w.codes, w.scales, out)
+    shape = _shape(w.rows, w.cols)
+    _check(lib().lpmm_w4_dequant(w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape), w.group, ptr, dt, ld,
+                                 _stream(stream)), "lpmm_w4_dequant")
+    return out
+
+
+def _w4_product(name: str, a, w: WeightsW4, a_cols: int, out_cols: int, out, stream):
+    _w4_check(w, name)
+    ptr, dtype, t, ld = _rows(a, a_cols, name + "'s input")
+    out = _new(out, (t, out_cols), a.dtype, a.device, stream, name + "'s output")
+    optr, _, _, old = _rows(out, out_cols, name + "'s output")
+    _on_current(name, a, w.codes, w.scales, out)
+    shape = _shape(w.rows, w.cols)
+    _check(getattr(lib(), name)(ptr, dtype, t, ld, w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape),
+                                w.group, optr, old, _stream(stream)), name)
+    return out
+
+
+def lpmm_w4_linear(x, w: WeightsW4, y=None, stream=None):
+    """y = x W^T: x is tokens x cols (float32 or bfloat16), y tokens x rows of the same type."""
+    return _w4_product("lpmm_w4_linear", x, w, w.cols, w.rows, y, stream)
+
+
+def lpmm_w4_linear_dx(dy, w: WeightsW4, dx=None, stream=None):
+    """dx = dy W: the gradient of lpmm_w4_linear with respect to x."""
+    return _w4_product("lpmm_w4_linear_dx", dy, w, w.rows, w.cols, dx, stream)
+
+
+def lpmm_w4_linear_dscale(x, dy, w: WeightsW4, dscales=None, workspace=None, stream=None):
+    """The gradient of lpmm_w4_linear with respect to the scales, float32, shaped like them.  w.scales is not read."""
+    import torch
+    _w4_check(w, "lpmm_w4_linear_dscale")
+    xp, dtype, t, xld = _rows(x, w.cols, "x")
+    dyp, dy_dtype, dy_t, dyld = _rows(dy, w.rows, "dy")
+    if dy_dtype != dtype or dy_t != t:
+        raise ValueError("lpmm_w4_linear_dscale: x and dy must have the same type and number of rows")
+    dscales = _new(dscales, w.scales.shape, torch.float32, x.device, stream, "dscales")
+    if not dscales.is_contiguous():
+        raise ValueError("dscales must be contiguous")
+    shape = _shape(w.rows, w.cols)
+    need = lib().lpmm_w4_linear_dscale_workspace_bytes(t, ctypes.addressof(shape), w.group)
+    workspace = _workspace(workspace, need, x.device, stream, "lpmm_w4_linear_dscale")
+    _on_current("lpmm_w4_linear_dscale", x, dy, w.codes, dscales)
+    _check(lib().lpmm_w4_linear_dscale(xp, dyp, dtype, t, xld, dyld, w.codes.data_ptr(), ctypes.addressof(shape), w.group,
+                                       dscales.data_ptr(), _ptr(workspace), _room(workspace), _stream(stream)),
+           "lpmm_w4_linear_dscale")
+    return dscales
+
+
+def _workspace(workspace, need: int, device, stream, what: str):
+    import torch
+    if workspace is None and need:
+        if stream is not None:
+            raise ValueError(f"{what}: a call on a stream of its own needs a workspace of {need} bytes")
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace
+
+
+def _room(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+# ---- distillation from a teacher's top logits ---------------------------------------------------------------
+
+DISTILL_MAX_SLOTS = 1024
+
+
+def _distill_args(z, top, index, tau, what: str):
+    import torch
+    if z.dim() != 2:
+        raise ValueError(f"{what}: logits must be tokens x vocabulary")
+    ptr, dtype, t, ld = _rows(z, z.shape[1], "logits")
+    if (top.dtype != torch.float32 or index.dtype != torch.int64 or top.dim() != 2 or top.shape != index.shape or
+            top.shape[0] != t or not top.is_contiguous() or not index.is_contiguous()):
+        raise ValueError(f"{what}: top (float32) and index (int64) must be contiguous, {t} x slots each")
+    return (ptr, dtype, t, z.shape[1], ld, top.data_ptr(), index.data_ptr(), top.shape[1], float(tau))
+
+
+def _per_row(x, t: int, name: str):
+    import torch
+    if x.dtype != torch.float32 or x.shape != (t,) or not x.is_contiguous():
+        raise ValueError(f"{name} must be float32, contiguous, one per row")
+    return x.data_ptr()
+
+
+def lpmm_distill_loss(z, top, index, tau, loss=None, lse=None, workspace=None, stream=None):
+    """(loss, lse), one per row of the student's logits z; top, index: the teacher's largest logits and their places, -1 in
+    slots that do not count."""
+    import torch
+    args = _distill_args(z, top, index, tau, "lpmm_distill_loss")
+    t, v = z.shape
+    loss = _new(loss, (t,), torch.float32, z.device, stream, "loss")
+    lse = _new(lse, (t,), torch.float32, z.device, stream, "lse")
+    workspace = _workspace(workspace, lib().lpmm_distill_workspace_bytes(t, v), z.device, stream, "lpmm_distill_loss")
+    _on_current("lpmm_distill_loss", z, top, index, loss, lse)
+    _check(lib().lpmm_distill_loss(*args, _per_row(loss, t, "loss"), _per_row(lse, t, "lse"), _ptr(workspace),
+                                   _room(workspace), _stream(stream)), "lpmm_distill_loss")
+    return loss, lse
+
+
+def lpmm_distill_grad(z, top, index, tau, lse, grad, dz=None, stream=None):
+    """The loss's gradient with respect to z, from the gradient of each row's loss; dz may be z."""
+    args = _distill_args(z, top, index, tau, "lpmm_distill_grad")
+    t, v = z.shape
+    dz = _new(dz, (t, v), z.dtype, z.device, stream, "dz")
+    dptr, _, _, dld = _rows(dz, v, "dz")
+    _on_current("lpmm_distill_grad", z, top, index, lse, grad, dz)
+    _check(lib().lpmm_distill_grad(*args, _per_row(lse, t, "lse"), _per_row(grad, t, "grad"), dptr, dld,
+                                   _stream(stream)), "lpmm_distill_grad")
+    return dz
+
+
+def lpmm_distill_loss_grad(z, top, index, tau, grad, loss=None, lse=None, dz=None, workspace=None, stream=None):
+    """(loss, dz) in one call, for a gradient of the rows' losses that is known beforehand; dz may be z."""
+    import torch
+    args = _distill_args(z, top, index, tau, "lpmm_distill_loss_grad")
+    t, v = z.shape
+    loss = _new(loss, (t,), torch.float32, z.device, stream, "loss")
+    lse = _new(lse, (t,), torch.float32, z.device, stream, "lse")
+    dz = _new(dz, (t, v), z.dtype, z.device, stream, "dz")
+    dptr, _, _, dld = _rows(dz, v, "dz")
+    workspace = _workspace(workspace, lib().lpmm_distill_workspace_bytes(t, v), z.device, stream, "lpmm_distill_loss_grad")
+    _on_current("lpmm_distill_loss_grad", z, top, index, grad, loss, lse, dz)
+    _check(lib().lpmm_distill_loss_grad(*args, _per_row(grad, t, "grad"), _per_row(loss, t, "loss"),
+                                        _per_row(lse, t, "lse"), dptr, dld, _ptr(workspace), _room(workspace),
+                                        _stream(stream)), "lpmm_distill_loss_grad")
+    return loss, dz
 
 
 # ---- many tensors in one call ------------------------------------------------------------------------

@@ -18,6 +18,9 @@
 #include "flow.hpp"
 #include "convert.hpp"
 #include "ablation.hpp"
+#include "host_util.hpp"
+
+thread_local int lpmm::g_last_hip = 0;
 
 namespace {
 
@@ -45,7 +48,6 @@ static __device__ __align__(256) unsigned char scratch[kCounterBytes + kScratchF
 
 DeviceCtx g_ctx[kMaxDevices];
 std::mutex g_mu;
-thread_local int g_last_hip = 0;
 
 // per-kernel timing (lpmm_profile_begin / _end)
 struct Profile {
@@ -75,10 +77,6 @@ struct HostTables {
 };
 const HostTables& host_tables() { static const HostTables t; return t; }
 
-int hip_fail(hipError_t e) { g_last_hip = int(e); return LPMM_EHIP; }
-#define LPMM_HIP(call) do { hipError_t e_ = (call); if (e_ != hipSuccess) return hip_fail(e_); } while (0)
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool finite_nonneg(float x) { return std::isfinite(x) && x >= 0.0f; }
 
 int env_int(const char* name, int dflt) {

@@ -1,0 +1,368 @@
+"""4-bit weights with group scales on the GPU: compress and decompress bit for bit, the product and its gradients against
+plain 64-bit forms within bounds that follow from their roundings."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2309_01507_amd as lpmm
+import w4_util as ref
+from conftest import progress
+from w4_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+GROUPS = (32, 64, 128)
+# tokens x rows x cols: one of everything, less than and just beyond a tile, a row's padding, odd sizes
+SHAPES = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (2, 33, 96), (3, 100, 7), (7, 65, 1000), (15, 64, 257), (16, 48, 512),
+          (17, 40, 640), (31, 130, 384), (33, 257, 130), (64, 64, 64), (65, 300, 200), (77, 129, 1031), (128, 256, 256),
+          (129, 255, 896), (200, 520, 513), (333, 384, 768), (520, 260, 140)]
+
+
+def weights(rows, cols, group, seed):
+    q, packed, scales = ref.random_weights(rows, cols, group, seed)
+    w = lpmm.WeightsW4(rows, cols, group, packed.to(DEV), scales.to(DEV))
+    return w, ref.VALUES[q], scales
+
+
+def activations(t, cols, dtype, seed, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (scale * torch.randn(t, cols, generator=g) * torch.exp(0.5 * torch.randn(1, cols, generator=g))).to(dtype)
+
+
+def strided(x, extra, offset=0):
+    """The same matrix on the GPU with `extra` elements of NaN between its rows, `offset` elements off an aligned start"""
+    t, n = x.shape
+    buf = torch.full((t * (n + extra) + offset,), float("nan"), dtype=x.dtype, device=DEV)
+    view = buf[offset:].view(t, n + extra)[:, :n]
+    view.copy_(x)
+    return view
+
+
+# ---- compress, decompress ----------------------------------------------------------------------------------------------
+
+def _inputs(rows, cols, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn(rows, cols, generator=g) * torch.exp(2 * torch.randn(rows, 1, generator=g))
+    if rows > 2:
+        w[1] = 0.0
+        w[2, : cols // 2] = -0.0
+    if rows > 4:
+        w[3] *= 2.0 ** -90                       # small, but not zeros
+        w[4] = 2.0 ** -101                       # zeros
+    return w.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 31), (5, 128), (7, 129), (16, 1000), (65, 4096), (33, 1031)])
+def test_compress_and_decompress_bit_for_bit(rows, cols, group, dtype):
+    w = _inputs(rows, cols, dtype, rows * 31 + cols)
+    q, scales = ref.quantize(w, group)
+    for wd in (w.to(DEV), strided(w, 3, 1)):
+        got = lpmm.lpmm_w4_quant(wd, group)
+        assert torch.equal(got.scales.cpu(), scales)
+        assert torch.equal(got.codes.cpu(), ref.pack(q)), "codes, or padding that is not 0"
+        for out_dtype in (F32, BF16):
+            want = (ref.VALUES[q].float() * scales.repeat_interleave(group, dim=1)[:, :cols]).to(out_dtype)
+            assert torch.equal(lpmm.lpmm_w4_dequant(got, out_dtype).cpu(), want)
+            out = strided(torch.zeros(rows, cols, dtype=out_dtype), 5, 1)
+            lpmm.lpmm_w4_dequant(got, out=out)
+            assert torch.equal(out.cpu(), want)
+
+
+@pytest.mark.parametrize("group", GROUPS)
+def test_values_around_the_midpoints(group):
+    """Every midpoint times the scale and its neighbours, under scales of all kinds; the decision is exact."""
+    mids = np.array(ref.MIDPOINTS)
+    rows = []
+    for top in (6.0, 1.0, 0.37, 3.1e-7, 1.9999999, 2.0 ** -98, 1.7e29, 3.3e38, 5.5, 0.75, 2.0 ** -100):
+        s = np.float64(np.float32(np.float32(top) / np.float32(6)))
+        at = (mids * s).astype(np.float32)
+        near = [at]
+        for up in (np.float32(np.inf), np.float32(-np.inf)):
+            v = at
+            for _ in range(2):
+                v = np.nextafter(v, up, dtype=np.float32)
+                near.append(v)
+        vals = np.concatenate(near)
+        vals = np.concatenate([vals, -vals, [0.0, -0.0]]).astype(np.float32)
+        row = np.resize(vals, 2048).astype(np.float32)
+        row[::32] = np.float32(top)
+        rows.append(row)
+    w = torch.from_numpy(np.stack(rows))
+    q, scales = ref.quantize(w, group)
+    got = lpmm.lpmm_w4_quant(w.to(DEV), group)
+    assert torch.equal(got.scales.cpu(), scales) and torch.equal(got.codes.cpu(), ref.pack(q))
+
+
+def test_groups_with_nan_or_infinity_become_nan():
+    w = torch.randn(4, 256)
+    w[0, 3], w[1, 40], w[2, 70] = float("nan"), float("inf"), -float("inf")
+    got = lpmm.lpmm_w4_quant(w.to(DEV), 32)
+    bad = torch.isnan(got.scales.cpu())
+    want = torch.zeros(4, 8, dtype=torch.bool)
+    want[0, 0] = want[1, 1] = want[2, 2] = True
+    assert torch.equal(bad, want)
+    d = lpmm.lpmm_w4_dequant(got).cpu()
+    assert torch.equal(torch.isnan(d), want.repeat_interleave(32, dim=1))
+    y = lpmm.lpmm_w4_linear(torch.ones(2, 256, device=DEV), got).cpu()
+    assert torch.equal(torch.isnan(y), torch.tensor([[True, True, True, False]] * 2))
+
+
+# ---- the product and its gradients -------------------------------------------------------------------------------------
+
+def check_linear(x, w, values, scales, dtype, what, y=None):
+    full = values * ref.spread(scales, w.group, w.cols)
+    got = lpmm.lpmm_w4_linear(x, w, y)
+    xd = x.cpu().double()
+    want, mag = xd @ full.t(), xd.abs() @ full.abs().t()
+    # a sum of cols terms and one scaling per group
+    ref.assert_within(got, want, ref.bound(dtype, want, mag, w.cols + 4), what)
+
+
+def check_dx(dy, w, values, scales, dtype, what, dx=None):
+    full = values * ref.spread(scales, w.group, w.cols)
+    got = lpmm.lpmm_w4_linear_dx(dy, w, dx)
+    d = dy.cpu().double()
+    want, mag = d @ full, d.abs() @ full.abs()
+    # bf16: value * scale may be rounded to bf16 in front of the product
+    ref.assert_within(got, want, ref.bound(dtype, want, mag, w.rows + 4, 2.0 ** -8 if dtype == BF16 else 0.0), what)
+
+
+def check_dscale(x, dy, w, values, what, out=None):
+    got = lpmm.lpmm_w4_linear_dscale(x, dy, w, out)
+    xd, d = x.cpu().double(), dy.cpu().double()
+    want = ref.group_sums((d.t() @ xd) * values, w.group)
+    mag = ref.group_sums((d.abs().t() @ xd.abs()) * values.abs(), w.group)
+    ref.assert_within(got, want, ref.bound(F32, want, mag, w.group + x.shape[0] + 4), what)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("t,rows,cols", SHAPES)
+def test_product_and_gradients(t, rows, cols, group, dtype):
+    progress(f"w4 {t} x {rows} x {cols} group {group} {dtype}")
+    w, values, scales = weights(rows, cols, group, t + rows + cols)
+    x, dy = activations(t, cols, dtype, 1), activations(t, rows, dtype, 2, 1e-3)
+    check_linear(x.to(DEV), w, values, scales, dtype, "y")
+    check_dx(dy.to(DEV), w, values, scales, dtype, "dx")
+    check_dscale(x.to(DEV), dy.to(DEV), w, values, "dscales")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,rows,cols,extra,offset", [(5, 48, 256, 8, 0), (5, 48, 256, 1, 0), (19, 70, 300, 3, 1), (140, 260, 384, 5, 3),
+                                                      (140, 256, 384, 8, 0), (300, 520, 257, 7, 1), (1, 48, 256, 0, 1)])
+def test_rows_apart_and_off_alignment(t, rows, cols, extra, offset, dtype):
+    """Between the inputs' rows stand NaN; what stands between the outputs' rows stays."""
+    w, values, scales = weights(rows, cols, 64, 5)
+    x, dy = strided(activations(t, cols, dtype, 1), extra, offset), strided(activations(t, rows, dtype, 2), extra, offset)
+    y, dx = strided(torch.zeros(t, rows, dtype=dtype), extra, offset), strided(torch.zeros(t, cols, dtype=dtype), extra, offset)
+    check_linear(x, w, values, scales, dtype, "y", y)
+    check_dx(dy, w, values, scales, dtype, "dx", dx)
+    check_dscale(x, dy, w, values, "dscales")
+    for out, n in ((y, rows), (dx, cols)):
+        if extra and t > 1:
+            between = out.as_strided((t - 1, extra), (n + extra, 1), out.storage_offset() + n)
+            assert bool(torch.isnan(between).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [4, 150])
+def test_infinities_and_nan_stay_in_their_rows(t, dtype):
+    """An element that is not finite reaches what the formula lets it reach and nothing else: neither other tokens nor, through
+    the padding of a short row of codes, the same one's other sums."""
+    rows, cols = 70, 200
+    w, values, scales = weights(rows, cols, 32, 9)
+    scales = scales.abs() + 0.01                        # no 0 * infinity from a scale
+    w = lpmm.WeightsW4(rows, cols, 32, w.codes, scales.to(DEV))
+    x, dy = activations(t, cols, dtype, 1), activations(t, rows, dtype, 2)
+    x[1, 5] = float("inf")
+    x[2, 199] = float("nan")
+    dy[0, 3] = float("nan")
+    dy[3, 69] = -float("inf")
+    full = values * ref.spread(scales, 32, cols)
+    y, dx = lpmm.lpmm_w4_linear(x.to(DEV), w).cpu(), lpmm.lpmm_w4_linear_dx(dy.to(DEV), w).cpu()
+    want_y, want_dx = x.double() @ full.t(), dy.double() @ full
+    for got, want in ((y, want_y), (dx, want_dx)):
+        assert torch.equal(torch.isfinite(got), torch.isfinite(want))
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+    ds = lpmm.lpmm_w4_linear_dscale(x.to(DEV), dy.to(DEV), w).cpu()
+    want = ref.group_sums((dy.double().t() @ x.double()) * values, 32)
+    assert torch.equal(torch.isnan(ds) | torch.isinf(ds), ~torch.isfinite(want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_extreme_magnitudes(dtype):
+    """Inputs next to the largest and the smallest floats: splitting and scaling neither overflow nor lose them."""
+    rows, cols, t = 32, 128, 20
+    q = torch.randint(0, 16, (rows, cols), generator=torch.Generator().manual_seed(3))
+    values = ref.VALUES[q]
+    for size, s in ((3.0e38, 2.0 ** -20), (1.0e-30, 2.0 ** 20)):
+        scales = torch.full((rows, 1), s)
+        w = lpmm.WeightsW4(rows, cols, 128, ref.pack(q).to(DEV), scales.to(DEV))
+        x = torch.zeros(t, cols)
+        x[torch.arange(t), torch.arange(t) * 5] = size                # one element a row: no sum overflows
+        x = x.to(dtype)
+        if float(x.double().abs().max()) * 6 > 3.4e38:
+            values_ok = values.abs() <= 1.0                           # the unscaled sum would overflow beyond
+        else:
+            values_ok = torch.ones_like(values, dtype=torch.bool)
+        want = x.double() @ (values * values_ok * s).t()
+        ww = lpmm.WeightsW4(rows, cols, 128, ref.pack(torch.where(values_ok, q, torch.zeros_like(q))).to(DEV), scales.to(DEV))
+        got = lpmm.lpmm_w4_linear(x.to(DEV), ww)
+        ref.assert_within(got, want, ref.bound(dtype, want, want.abs(), 8), f"{size}")
+        del w
+
+
+def test_no_tokens():
+    w, _, _ = weights(33, 65, 32, 1)
+    x, dy = torch.empty(0, 65, device=DEV), torch.empty(0, 33, device=DEV)
+    assert lpmm.lpmm_w4_linear(x, w).shape == (0, 33)
+    assert lpmm.lpmm_w4_linear_dx(dy, w).shape == (0, 65)
+    assert torch.equal(lpmm.lpmm_w4_linear_dscale(x, dy, w, torch.full((33, 3), 7.0, device=DEV)), torch.zeros(33, 3, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_against_differences(dtype):
+    """The product is linear in x and in the scales, so a difference over a step of any size is the derivative, up to rounding."""
+    t, rows, cols, group = 37, 96, 320, 64
+    w, values, scales = weights(rows, cols, group, 21)
+    x, dy = activations(t, cols, dtype, 1), activations(t, rows, dtype, 2)
+    y = lambda a, s: lpmm.lpmm_w4_linear(a.to(DEV), lpmm.WeightsW4(rows, cols, group, w.codes, s.to(DEV))).cpu().double()
+    dx = lpmm.lpmm_w4_linear_dx(dy.to(DEV), w).cpu().double()
+    ds = lpmm.lpmm_w4_linear_dscale(x.to(DEV), dy.to(DEV), w).cpu().double()
+    g = torch.Generator().manual_seed(4)
+    u = 2.0 ** -8 if dtype == BF16 else 2.0 ** -20
+    step = torch.randint(-1, 2, x.shape, generator=g).to(dtype)
+    moved = (x.float() + 2 * step.float()).to(dtype)
+    real = moved.double() - x.double()
+    a = float(((y(moved, scales) - y(x, scales)) * dy.double()).sum())
+    b = float((dx * real).sum())
+    size = float((y(moved, scales).abs() + y(x, scales).abs()).mul(dy.double().abs()).sum()) + float((dx * real).abs().sum())
+    assert abs(a - b) <= 2 * u * size
+    step = 0.25 * torch.randint(-1, 2, scales.shape, generator=g)
+    a = float(((y(x, scales + step) - y(x, scales)) * dy.double()).sum())
+    b = float((ds * step).sum())
+    size = float((y(x, scales + step).abs() + y(x, scales).abs()).mul(dy.double().abs()).sum()) + float((ds * step).abs().sum())
+    assert abs(a - b) <= 2 * u * size
+
+
+def test_same_bits_every_time():
+    t, rows, cols = 300, 640, 1024
+    w, _, _ = weights(rows, cols, 128, 2)
+    x, dy = activations(t, cols, BF16, 1).to(DEV), activations(t, rows, BF16, 2).to(DEV)
+    run = lambda: (lpmm.lpmm_w4_linear(x, w), lpmm.lpmm_w4_linear(x[:3], w), lpmm.lpmm_w4_linear_dx(dy, w),
+                   lpmm.lpmm_w4_linear_dscale(x, dy, w))
+    first = run()
+    for _ in range(4):
+        assert all(torch.equal(a, b) for a, b in zip(first, run()))
+
+
+def test_on_another_stream_and_in_a_graph():
+    t, rows, cols = 5, 256, 512
+    w, _, _ = weights(rows, cols, 64, 2)
+    x, dy = activations(t, cols, BF16, 1).to(DEV), activations(t, rows, BF16, 2).to(DEV)
+    want = lpmm.lpmm_w4_linear(x, w), lpmm.lpmm_w4_linear_dx(dy, w), lpmm.lpmm_w4_linear_dscale(x, dy, w)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = lpmm.lpmm_w4_linear(x, w), lpmm.lpmm_w4_linear_dx(dy, w), lpmm.lpmm_w4_linear_dscale(x, dy, w)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    outs = [torch.zeros_like(a) for a in want]
+    torch.cuda.synchronize()
+    lpmm.lpmm_w4_linear(x, w, outs[0], stream=side)
+    side.synchronize()
+    assert torch.equal(outs[0], want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lpmm.lpmm_w4_linear(x, w, outs[0])
+        lpmm.lpmm_w4_linear_dx(dy, w, outs[1])
+        lpmm.lpmm_w4_linear_dscale(x, dy, w, outs[2])
+    for i in range(4):
+        x.mul_(-1.0 if i % 2 else 0.5)
+        eager = lpmm.lpmm_w4_linear(x, w), lpmm.lpmm_w4_linear_dx(dy, w), lpmm.lpmm_w4_linear_dscale(x, dy, w)
+        for o in outs:
+            o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 bytes of codes, and outputs of more than 2^32 bytes."""
+    rows, cols = 270000, 32768
+    progress("4.4 GB of codes")
+    codes = torch.randint(0, 256, (rows * cols // 2,), dtype=torch.uint8, device=DEV)
+    scales = torch.rand(rows, cols // 128, device=DEV)
+    w = lpmm.WeightsW4(rows, cols, 128, codes, scales)
+    x = torch.randn(2, cols, device=DEV)
+    y = lpmm.lpmm_w4_linear(x, w)
+    d = torch.zeros(1, rows, device=DEV)
+    picks = [0, 131071, 131072, rows - 1]
+    for i, r in enumerate(picks):
+        d[0, r] = float(i + 1)
+    dx = lpmm.lpmm_w4_linear_dx(d, w).cpu()
+    total, total_mag = torch.zeros(1, cols).double(), torch.zeros(1, cols).double()
+    for i, r in enumerate(picks):
+        values = ref.VALUES[ref.unpack(codes[r * cols // 2:(r + 1) * cols // 2], 1, cols)]
+        full = values * ref.spread(scales[r:r + 1].cpu(), 128, cols)
+        want, mag = x.cpu().double() @ full.t(), x.cpu().double().abs() @ full.abs().t()
+        ref.assert_within(y[:, r:r + 1], want, ref.bound(F32, want, mag, cols + 4), f"row {r}")
+        total += (i + 1) * full
+        total_mag += (i + 1) * full.abs()
+    ref.assert_within(dx, total, ref.bound(F32, total, total_mag, 8), "dx")
+    del codes, scales, w, y
+    progress("4.8 GB of outputs")
+    t, rows, cols = 48000, 50257, 64
+    w, values, scales = weights(rows, cols, 64, 3)
+    x = activations(t, cols, BF16, 1)
+    y = lpmm.lpmm_w4_linear(x.to(DEV), w)
+    full = values * ref.spread(scales, 64, cols)
+    for r in (0, 42734, 42735, t - 1):
+        xd = x[r:r + 1].double()
+        want, mag = xd @ full.t(), xd.abs() @ full.abs().t()
+        ref.assert_within(y[r:r + 1], want, ref.bound(BF16, want, mag, cols + 4), f"token {r}")
+
+
+def test_refusals():
+    L = lpmm.lib()
+    w, _, _ = weights(16, 128, 64, 1)
+    x, dy = torch.zeros(4, 128, device=DEV), torch.zeros(4, 16, device=DEV)
+    s = (ctypes.c_int64 * 2)(16, 128)
+    sh, xp, dp, c, sc = ctypes.addressof(s), x.data_ptr(), dy.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr()
+    ok = [xp, 0, 4, 128, c, sc, sh, 64, dp, 16, None]
+    for at, bad in ((0, None), (0, xp + 2), (1, 2), (2, -1), (3, 127), (4, None), (4, c + 8), (5, None), (5, sc + 2), (6, None), (7, 48),
+                    (8, None), (9, 15)):
+        args = list(ok)
+        args[at] = bad
+        assert L.lpmm_w4_linear(*args) == -1, (at, bad)
+    ok = [dp, 0, 4, 16, c, sc, sh, 64, xp, 128, None]
+    for at, bad in ((0, None), (1, 3), (3, 15), (4, c + 4), (7, 0), (9, 127)):
+        args = list(ok)
+        args[at] = bad
+        assert L.lpmm_w4_linear_dx(*args) == -1, (at, bad)
+    none = (ctypes.c_int64 * 2)(0, 128)
+    huge = (ctypes.c_int64 * 2)(1 << 30, 1 << 20)
+    sizes = (ctypes.c_size_t * 2)()
+    for shape in (none, huge):
+        assert L.lpmm_w4_sizes(ctypes.addressof(shape), 64, ctypes.addressof(sizes)) == -1
+        assert L.lpmm_w4_quant(xp, 0, 128, ctypes.addressof(shape), 64, c, sc, None) == -1
+        assert L.lpmm_w4_dequant(c, sc, ctypes.addressof(shape), 64, xp, 0, 128, None) == -1
+        assert L.lpmm_w4_linear_dscale_workspace_bytes(4, ctypes.addressof(shape), 64) == 0
+    assert L.lpmm_w4_linear_dscale(xp, None, 0, 4, 128, 16, c, sh, 64, sc, None, 0, None) == -1
+    torch.cuda.synchronize()
+    for call in (lambda: lpmm.lpmm_w4_linear(x[:, :64], w), lambda: lpmm.lpmm_w4_linear(x.half(), w),
+                 lambda: lpmm.lpmm_w4_linear(x.cpu(), w), lambda: lpmm.lpmm_w4_linear(x.t().contiguous().t(), w),
+                 lambda: lpmm.lpmm_w4_linear(x[:1].expand(4, 128), w), lambda: lpmm.lpmm_w4_linear(x, w, stream=torch.cuda.Stream()),
+                 lambda: lpmm.lpmm_w4_linear(x, w, torch.zeros(4, 17, device=DEV)),
+                 lambda: lpmm.lpmm_w4_linear_dscale(x, dy.bfloat16(), w), lambda: lpmm.lpmm_w4_linear_dscale(x[:3], dy, w),
+                 lambda: lpmm.lpmm_w4_linear(x, lpmm.WeightsW4(16, 128, 32, w.codes, w.scales)),
+                 lambda: lpmm.lpmm_w4_quant(x, 64, w)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(lpmm.LpmmError):
+        lpmm.lpmm_w4_quant(x, 48)
