@@ -495,15 +495,17 @@ int lpmm_w4_dequant(const uint8_t* codes, const float* scales, const int64_t sha
 int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const uint8_t* codes, const float* scales,
                    const int64_t shape[2], int group, void* y, int64_t y_stride, void* stream);
 
-/* dx[t][k] = sum_n dy[t][n] W[n][k]: its gradient with respect to x. */
+/* dx[t][k] = sum_n dy[t][n] W[n][k]: its gradient with respect to x.  In bf16 value * scale is rounded to bf16 once.  workspace:
+ * device memory, 16-byte aligned, of the bytes that ..._workspace_bytes gives (0: none is needed, as for invalid arguments), contents
+ * arbitrary before and after; calls that may overlap in time need one each.  The order of all sums is fixed: equal inputs
+ * give equal bits. */
+size_t lpmm_w4_linear_dx_workspace_bytes(int64_t t, const int64_t shape[2], int dtype);
 int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, const uint8_t* codes,
-                      const float* scales, const int64_t shape[2], int group, void* dx, int64_t dx_stride,
-                      void* stream);
+                      const float* scales, const int64_t shape[2], int group, void* dx, int64_t dx_stride, void* workspace,
+                      size_t workspace_bytes, void* stream);
 
 /* dscales[n][j] = sum_t dy[t][n] sum_{k in group j} x[t][k] value[code[n][k]]: its gradient with respect to the scales,
- * float[n][ceil(k/group)], written, not added to.  x and dy share a type.  workspace: device memory, 16-byte aligned, of
- * the bytes that ..._workspace_bytes gives (0 means none is needed; it is also 0 for invalid arguments), contents arbitrary before and after; calls that may
- * overlap in time need one each.  The order of all sums is fixed: equal inputs give equal bits. */
+ * float[n][ceil(k/group)], written, not added to.  x and dy share a type.  Workspace and order as above. */
 size_t lpmm_w4_linear_dscale_workspace_bytes(int64_t t, const int64_t shape[2], int group);
 int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, int64_t x_stride, int64_t dy_stride,
                           const uint8_t* codes, const int64_t shape[2], int group, float* dscales, void* workspace,

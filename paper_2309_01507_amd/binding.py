@@ -128,7 +128,9 @@ def lib() -> ctypes.CDLL:
         L.lpmm_w4_dequant.argtypes = [_VP, _VP, _VP, ctypes.c_int, _VP, ctypes.c_int, _I64, _VP]
         product_args = [_VP, ctypes.c_int, _I64, _I64, _VP, _VP, _VP, ctypes.c_int, _VP, _I64, _VP]
         L.lpmm_w4_linear.argtypes = product_args
-        L.lpmm_w4_linear_dx.argtypes = product_args
+        L.lpmm_w4_linear_dx.argtypes = product_args[:-1] + [_VP, ctypes.c_size_t, _VP]
+        L.lpmm_w4_linear_dx_workspace_bytes.argtypes = [_I64, _VP, ctypes.c_int]
+        L.lpmm_w4_linear_dx_workspace_bytes.restype = ctypes.c_size_t
         L.lpmm_w4_linear_dscale_workspace_bytes.argtypes = [_I64, _VP, ctypes.c_int]
         L.lpmm_w4_linear_dscale_workspace_bytes.restype = ctypes.c_size_t
         L.lpmm_w4_linear_dscale.argtypes = [_VP, _VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, ctypes.c_int, _VP, _VP,
@@ -715,26 +717,32 @@ def lpmm_w4_dequant(w: WeightsW4, dtype=None, out=None, stream=None):
     return out
 
 
-def _w4_product(name: str, a, w: WeightsW4, a_cols: int, out_cols: int, out, stream):
-    _w4_check(w, name)
-    ptr, dtype, t, ld = _rows(a, a_cols, name + "'s input")
-    out = _new(out, (t, out_cols), a.dtype, a.device, stream, name + "'s output")
-    optr, _, _, old = _rows(out, out_cols, name + "'s output")
-    _on_current(name, a, w.codes, w.scales, out)
-    shape = _shape(w.rows, w.cols)
-    _check(getattr(lib(), name)(ptr, dtype, t, ld, w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape),
-                                w.group, optr, old, _stream(stream)), name)
-    return out
-
-
 def lpmm_w4_linear(x, w: WeightsW4, y=None, stream=None):
     """y = x W^T: x is tokens x cols (float32 or bfloat16), y tokens x rows of the same type."""
-    return _w4_product("lpmm_w4_linear", x, w, w.cols, w.rows, y, stream)
+    _w4_check(w, "lpmm_w4_linear")
+    ptr, dtype, t, ld = _rows(x, w.cols, "x")
+    y = _new(y, (t, w.rows), x.dtype, x.device, stream, "y")
+    yptr, _, _, yld = _rows(y, w.rows, "y")
+    _on_current("lpmm_w4_linear", x, w.codes, w.scales, y)
+    shape = _shape(w.rows, w.cols)
+    _check(lib().lpmm_w4_linear(ptr, dtype, t, ld, w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape), w.group,
+                                yptr, yld, _stream(stream)), "lpmm_w4_linear")
+    return y
 
 
-def lpmm_w4_linear_dx(dy, w: WeightsW4, dx=None, stream=None):
+def lpmm_w4_linear_dx(dy, w: WeightsW4, dx=None, workspace=None, stream=None):
     """dx = dy W: the gradient of lpmm_w4_linear with respect to x."""
-    return _w4_product("lpmm_w4_linear_dx", dy, w, w.rows, w.cols, dx, stream)
+    _w4_check(w, "lpmm_w4_linear_dx")
+    ptr, dtype, t, ld = _rows(dy, w.rows, "dy")
+    dx = _new(dx, (t, w.cols), dy.dtype, dy.device, stream, "dx")
+    xptr, _, _, xld = _rows(dx, w.cols, "dx")
+    _on_current("lpmm_w4_linear_dx", dy, w.codes, w.scales, dx)
+    shape = _shape(w.rows, w.cols)
+    need = lib().lpmm_w4_linear_dx_workspace_bytes(t, ctypes.addressof(shape), dtype)
+    workspace = _workspace(workspace, need, dy.device, stream, "lpmm_w4_linear_dx")
+    _check(lib().lpmm_w4_linear_dx(ptr, dtype, t, ld, w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape),
+                                   w.group, xptr, xld, _ptr(workspace), _room(workspace), _stream(stream)), "lpmm_w4_linear_dx")
+    return dx
 
 
 def lpmm_w4_linear_dscale(x, dy, w: WeightsW4, dscales=None, workspace=None, stream=None):

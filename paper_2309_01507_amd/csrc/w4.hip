@@ -7,7 +7,7 @@
 #include <cmath>
 
 #include "host_util.hpp"
-#include "w4.hpp"
+#include "w4_tile.hpp"
 #include "distill.hpp"
 
 namespace {
@@ -43,6 +43,12 @@ int check_rows(const void* p, int dtype, int64_t rows, int64_t len, int64_t stri
 
 int check_codes(const uint8_t* codes) { return codes && aligned(codes, 16) ? LPMM_OK : LPMM_EINVAL; }
 int check_floats(const float* p) { return p && aligned(p, 4) ? LPMM_OK : LPMM_EINVAL; }
+
+int check_workspace(const void* p, size_t have, size_t need) {
+    if (need == 0) return LPMM_OK;
+    if (!p || !aligned(p, 16)) return LPMM_EINVAL;
+    return have < need ? LPMM_EWORKSPACE : LPMM_OK;
+}
 
 #define LPMM_TRY(call) do { const int rc_ = (call); if (rc_) return rc_; } while (0)
 
@@ -88,6 +94,35 @@ int launch_grad(const DistillArgs& a, bool bf16, hipStream_t s) {
         LPMM_HIP(hipGetLastError());
     }
     return LPMM_OK;
+}
+
+// Splits of a reduction over `steps` pieces for a launch of `blocks` workgroups: as many as bring it to `want` of them.
+int splits_for(int64_t blocks, int64_t steps, int64_t want) {
+    return int(std::max<int64_t>(1, std::min(steps, want / std::max<int64_t>(1, blocks))));
+}
+
+// The gradient of the scales: rows of W of a tile, tokens of a piece that splits are made of
+constexpr int kDscaleRows = 256, kDscaleTokens = 64;
+int dscale_splits(int64_t t, const W4Mat& m) {
+    return splits_for(div_up(m.n, kDscaleRows) * (m.words / 16), div_up(t, kDscaleTokens), 768);
+}
+
+// The gradient of the input: a large tile where it fills the GPU, else a small one with the reduction split
+struct DxPlan {
+    bool big;
+    int bt, bk, splits, n_per_split;
+};
+constexpr int kDxStep = 64;              // rows of W
+DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16) {
+    DxPlan p{};
+    p.big = bf16 && div_up(t, 256) * div_up(m.k, 256) >= 192;
+    p.bt = p.big ? 256 : bf16 ? 64 : 128;
+    p.bk = p.big ? 256 : 128;
+    const int64_t steps = div_up(m.n, kDxStep);
+    const int splits = p.big ? 1 : splits_for(div_up(t, p.bt) * div_up(m.k, p.bk), div_up(steps, 2), 512);
+    p.n_per_split = int(div_up(steps, splits)) * kDxStep;
+    p.splits = int(div_up(m.n, p.n_per_split));
+    return p;
 }
 
 }  // namespace
@@ -156,6 +191,22 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int esize = elem_size(dtype);
+    if (t > 64) {
+        const int bt = dtype == LPMM_BF16 ? 128 : 64;
+        const int64_t n_tiles = div_up(m.n, 256), t_tiles = div_up(t, bt);
+        const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
+        if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+#define LPMM_TILE(B, G, TT) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, 4, 2, 2, TT>), dim3(unsigned(blocks)), dim3(512), 0, s, m, x, \
+                                               int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
+        if (dtype == LPMM_BF16) {
+            if (group == 32) LPMM_TILE(true, 32, 2); else if (group == 64) LPMM_TILE(true, 64, 2); else LPMM_TILE(true, 128, 2);
+        } else {
+            if (group == 32) LPMM_TILE(false, 32, 1); else if (group == 64) LPMM_TILE(false, 64, 1); else LPMM_TILE(false, 128, 1);
+        }
+#undef LPMM_TILE
+        LPMM_HIP(hipGetLastError());
+        return LPMM_OK;
+    }
     constexpr int64_t kTokens = 16 * 32768;              // of a launch: grid.y
     for (int64_t at = 0; at < t; at += kTokens) {
         const int part = int(std::min(kTokens, t - at));
@@ -174,9 +225,16 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     return LPMM_OK;
 }
 
+size_t lpmm_w4_linear_dx_workspace_bytes(int64_t t, const int64_t shape[2], int dtype) {
+    W4Mat m{};
+    if (check_w4(shape, 32, &m) || t < 1 || t > kMaxTokens || (dtype != LPMM_F32 && dtype != LPMM_BF16)) return 0;
+    const DxPlan p = dx_plan(t, m, dtype == LPMM_BF16);
+    return p.splits > 1 ? size_t(p.splits) * size_t(t) * size_t(m.k) * 4 : 0;
+}
+
 int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, const uint8_t* codes,
-                      const float* scales, const int64_t shape[2], int group, void* dx, int64_t dx_stride,
-                      void* stream) {
+                      const float* scales, const int64_t shape[2], int group, void* dx, int64_t dx_stride, void* workspace,
+                      size_t workspace_bytes, void* stream) {
     W4Mat m{};
     LPMM_TRY(check_w4(shape, group, &m));
     LPMM_TRY(check_rows(dy, dtype, t, m.n, dy_stride));
@@ -184,26 +242,38 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
     LPMM_TRY(check_codes(codes));
     LPMM_TRY(check_floats(scales));
     if (t == 0) return LPMM_OK;
+    const bool bf16 = dtype == LPMM_BF16;
+    const DxPlan p = dx_plan(t, m, bf16);
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_w4_linear_dx_workspace_bytes(t, shape, dtype)));
     m.codes = reinterpret_cast<const uint32_t*>(codes);
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int esize = elem_size(dtype);
-    constexpr int64_t kTokens = 32768;                   // of a launch: grid.y
-    for (int64_t at = 0; at < t; at += kTokens) {
-        const int part = int(std::min(kTokens, t - at));
-        const void* dyp = static_cast<const char*>(dy) + at * dy_stride * esize;
-        void* dxp = static_cast<char*>(dx) + at * dx_stride * esize;
-        const dim3 grid(unsigned(div_up(m.words, 256)), unsigned(part));
-        if (dtype == LPMM_BF16) hipLaunchKernelGGL(w4_dx_kernel<true>, grid, dim3(256), 0, s, m, dyp, part, dy_stride, dxp, dx_stride, group_shift(group));
-        else hipLaunchKernelGGL(w4_dx_kernel<false>, grid, dim3(256), 0, s, m, dyp, part, dy_stride, dxp, dx_stride, group_shift(group));
+    const int64_t t_tiles = div_up(t, p.bt), k_tiles = div_up(m.k, p.bk), blocks = div_up(t_tiles * k_tiles, 8) * 8;
+    if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+    float* parts = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+    const dim3 grid(unsigned(blocks), unsigned(p.splits));
+#define LPMM_DX(B, WT, WK, TT, KT, LOGN) hipLaunchKernelGGL((w4_dx_tile_kernel<B, WT, WK, TT, KT, LOGN>), grid, dim3(64 * WT * WK), 0, s, m, dy, \
+                                                            int(t), dy_stride, dx, dx_stride, int(t_tiles), int(k_tiles), p.n_per_split, \
+                                                            parts, group_shift(group))
+    if (p.big) LPMM_DX(true, 2, 4, 4, 2, 3);
+    else if (bf16) LPMM_DX(true, 2, 4, 1, 1, 3);
+    else LPMM_DX(false, 4, 2, 1, 2, 2);
+#undef LPMM_DX
+    LPMM_HIP(hipGetLastError());
+    if (parts) {
+        const dim3 join(unsigned(div_up(t * m.k, 256)));
+        if (bf16) hipLaunchKernelGGL(w4_dx_join_kernel<true>, join, dim3(256), 0, s, parts, p.splits, int(t), m.k, dx, dx_stride);
+        else hipLaunchKernelGGL(w4_dx_join_kernel<false>, join, dim3(256), 0, s, parts, p.splits, int(t), m.k, dx, dx_stride);
         LPMM_HIP(hipGetLastError());
     }
     return LPMM_OK;
 }
 
 size_t lpmm_w4_linear_dscale_workspace_bytes(int64_t t, const int64_t shape[2], int group) {
-    (void)t; (void)shape; (void)group;
-    return 0;
+    W4Mat m{};
+    if (check_w4(shape, group, &m) || t < 1 || t > kMaxTokens) return 0;
+    const int splits = dscale_splits(t, m);
+    return splits > 1 ? size_t(splits) * m.n * m.groups * 4 : 0;
 }
 
 int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, int64_t x_stride, int64_t dy_stride,
@@ -215,14 +285,34 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
     LPMM_TRY(check_rows(dy, dtype, t, m.n, dy_stride));
     LPMM_TRY(check_codes(codes));
     LPMM_TRY(check_floats(dscales));
-    (void)workspace; (void)workspace_bytes;
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_w4_linear_dscale_workspace_bytes(t, shape, group)));
     m.codes = reinterpret_cast<const uint32_t*>(codes);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t blocks = div_up(int64_t(m.n) * m.groups, 4);
+    const int64_t n_tiles = div_up(m.n, kDscaleRows), blocks = div_up(n_tiles * (m.words / 16), 8) * 8;
     if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
-    if (dtype == LPMM_BF16) hipLaunchKernelGGL(w4_dscale_kernel<true>, dim3(unsigned(blocks)), dim3(256), 0, s, m, x, dy, int(t), x_stride, dy_stride, group_shift(group), dscales);
-    else hipLaunchKernelGGL(w4_dscale_kernel<false>, dim3(unsigned(blocks)), dim3(256), 0, s, m, x, dy, int(t), x_stride, dy_stride, group_shift(group), dscales);
+    int splits = dscale_splits(t, m);
+    const int per = int(div_up(div_up(t, kDscaleTokens), splits)) * kDscaleTokens;
+    splits = std::max(1, int(div_up(t, std::max(per, 1))));
+    const int64_t count = int64_t(m.n) * m.groups;
+    float* out = splits > 1 ? static_cast<float*>(workspace) : dscales;
+    const dim3 grid = dim3(unsigned(blocks), unsigned(splits));
+#define LPMM_DSCALE(B, G, WN, WT, NT, TT) hipLaunchKernelGGL((w4_dscale_tile_kernel<B, G, WN, WT, NT, TT>), grid, dim3(512), 0, s, m, x, dy, int(t), \
+                                                             x_stride, dy_stride, int(n_tiles), per, out, count)
+    if (dtype == LPMM_BF16) {
+        if (group == 32) LPMM_DSCALE(true, 32, 8, 1, 1, 2);
+        else if (group == 64) LPMM_DSCALE(true, 64, 4, 2, 2, 1);
+        else LPMM_DSCALE(true, 128, 4, 2, 2, 1);
+    } else {
+        if (group == 32) LPMM_DSCALE(false, 32, 8, 1, 1, 1);
+        else if (group == 64) LPMM_DSCALE(false, 64, 8, 1, 1, 1);
+        else LPMM_DSCALE(false, 128, 8, 1, 1, 1);
+    }
+#undef LPMM_DSCALE
     LPMM_HIP(hipGetLastError());
+    if (splits > 1) {
+        hipLaunchKernelGGL(w4_join_kernel, dim3(unsigned(div_up(count, 256))), dim3(256), 0, s, out, splits, count, count, dscales);
+        LPMM_HIP(hipGetLastError());
+    }
     return LPMM_OK;
 }
 

@@ -289,53 +289,4 @@ __global__ __launch_bounds__(64 * WAVES) void w4_linear_kernel(W4Mat m, const vo
     }
 }
 
-// ---- dx = dy W -----------------------------------------------------------------------------------------------------------------
-//
-// A lane takes the 8 inputs of one word and one token, and walks down the rows of W.
-template <bool BF16>
-__global__ __launch_bounds__(256) void w4_dx_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx, int64_t dx_stride,
-                                                    int group_shift) {
-    const int word = blockIdx.x * 256 + threadIdx.x;             // logical
-    const int at = word * 8, tok = blockIdx.y;
-    if (at >= m.k) return;
-    const int place = (word & ~15) + w4_place(word & 15);
-    float acc[8] = {};
-    for (int n = 0; n < m.n; ++n) {
-        const float c = w4_load1<BF16>(dy, int64_t(tok) * dy_stride + n) * m.scales[int64_t(n) * m.groups + (at >> group_shift)];
-        float v[8];
-        w4_values8(m.codes[int64_t(n) * m.words + place], v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(c, v[e], acc[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (at + e < m.k) w4_store1<BF16>(dx, int64_t(tok) * dx_stride + at + e, acc[e]);
-}
-
-// ---- gradient of the scales ------------------------------------------------------------------------------------------------------
-//
-// A wave takes one scale; its lanes share the tokens.
-template <bool BF16>
-__global__ __launch_bounds__(256) void w4_dscale_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
-                                                        int64_t dy_stride, int group_shift, float* dscales) {
-    const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (id >= int64_t(m.n) * m.groups) return;
-    const int n = int(id / m.groups), g = int(id % m.groups);
-    float acc = 0.0f;
-    for (int tok = threadIdx.x & 63; tok < t; tok += 64) {
-        float sum = 0.0f;
-        for (int w = g << (group_shift - 3); w < (g + 1) << (group_shift - 3) && w * 8 < m.k; ++w) {
-            float v[8], xx[8];
-            w4_values8(m.codes[int64_t(n) * m.words + (w & ~15) + w4_place(w & 15)], v);
-            w4_load8<BF16>(x, int64_t(tok) * x_stride + w * 8, int64_t(tok) * x_stride + m.k, xx);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(v[e], xx[e], sum);
-        }
-        acc = __builtin_fmaf(w4_load1<BF16>(dy, int64_t(tok) * dy_stride + n), sum, acc);
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) acc += __shfl_xor(acc, d);
-    if ((threadIdx.x & 63) == 0) dscales[id] = acc;
-}
-
 }  // namespace lpmm

@@ -1,0 +1,530 @@
+// The product with 4-bit weights and its gradients for many tokens: tiles through LDS and the 32x32x16 matrix instructions.
+//
+// Operand layout of v_mfma_f32_32x32x16_bf16: lane l holds, of row (A) or column (B) l % 32, the reduction's elements 8 (l / 32)
+// .. + 7; of the result column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 for i = 0..15.
+#pragma once
+
+#include "w4.hpp"
+
+namespace lpmm {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ int mfma32_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
+
+// Workgroups go round robin over the 8 XCDs; so that each XCD's L2 serves neighbouring tiles, XCD x takes the x-th eighth of them,
+// in an order that walks down `rows` in strips of 4 columns.  False: nothing to do.
+__device__ __forceinline__ bool tile_of(int id, int rows, int cols, int& row, int& col) {
+    const int total = rows * cols, per = (total + 7) >> 3;
+    const int tile = (id & 7) * per + (id >> 3);
+    if ((id >> 3) >= per || tile >= total) return false;
+    const int strip = tile / (4 * rows), rest = tile - strip * 4 * rows;
+    const int width = min(4, cols - strip * 4);
+    row = rest / width;
+    col = strip * 4 + rest % width;
+    return true;
+}
+
+// 16-byte pieces in LDS: piece o of row r of an array with 2^LOG pieces a row stands at o ^ (r, or r / 2 for rows of 8 pieces), so that
+// lanes that read the same piece of consecutive rows hit different banks.
+template <int LOG>
+__device__ __forceinline__ int lds_piece(int r, int o) {
+    constexpr int mask = (1 << LOG) - 1;
+    return (r << LOG) + (o ^ ((LOG <= 3 ? r >> 1 : r) & mask));
+}
+
+// ---- staging: octets of rows, from global memory into registers and from there into LDS ------------------------------------------
+
+// Elements as they come from memory: 8 of them
+template <bool BF16> struct RawOctet;
+template <> struct RawOctet<true> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const void* p, int64_t i, int64_t end) {
+        if (i + 8 <= end) {
+            const Vec16 q = *reinterpret_cast<const Vec16*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = q.v[e];
+        } else {
+            const uint16_t* x = static_cast<const uint16_t*>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = i + 2 * e < end ? x[i + 2 * e] : 0, hi = i + 2 * e + 1 < end ? x[i + 2 * e + 1] : 0;
+                w[e] = lo | hi << 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ void terms(uint4 out[]) const { out[0] = make_uint4(w[0], w[1], w[2], w[3]); }
+};
+template <> struct RawOctet<false> {
+    float x[8];
+    __device__ __forceinline__ void load(const void* p, int64_t i, int64_t end) { w4_load8<false>(p, i, end, x); }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+    }
+    __device__ __forceinline__ void terms(uint4 out[]) const {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t a[3], b[3];
+            split3(x[2 * e], a);
+            split3(x[2 * e + 1], b);
+#pragma unroll
+            for (int j = 0; j < 3; ++j) w[j][e] = a[j] >> 16 | b[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j) out[j] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+    }
+};
+
+__device__ __forceinline__ bf16x8 as_operand(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+// ROWS rows of 2^LOG octets, staged by THREADS threads: the octets of a thread are THREADS apart
+template <bool BF16, int ROWS, int LOG, int THREADS>
+struct Stage {
+    static constexpr int kPieces = ROWS << LOG, kOwn = kPieces / THREADS, kTerms = kW4Terms<BF16>;
+    static_assert(kPieces % THREADS == 0, "whole octets per thread");
+    RawOctet<BF16> raw[kOwn];
+    // rows row0 .. of a matrix of `rows` rows; columns col0 .. ; what lies outside is 0
+    __device__ __forceinline__ void load(const void* p, int64_t stride, int row0, int rows, int col0, int cols) {
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+            const int id = threadIdx.x + j * THREADS, r = row0 + (id >> LOG), c = col0 + (id & ((1 << LOG) - 1)) * 8;
+            if (r < rows && c < cols) raw[j].load(p, int64_t(r) * stride + c, int64_t(r) * stride + cols);
+            else raw[j].zero();
+        }
+    }
+    __device__ __forceinline__ void store(uint4* lds) const {
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+            const int id = threadIdx.x + j * THREADS;
+            uint4 t[kTerms];
+            raw[j].terms(t);
+#pragma unroll
+            for (int k = 0; k < kTerms; ++k) lds[k * kPieces + lds_piece<LOG>(id >> LOG, id & ((1 << LOG) - 1))] = t[k];
+        }
+    }
+};
+
+// ---- y = x W^T --------------------------------------------------------------------------------------------------------------------
+//
+// A workgroup of WN x WT waves takes WN NT 32 rows of W and WT TT 32 tokens.  x goes through LDS in runs of 128; codes
+// go from memory into the registers of the waves that use them and are converted there.  Each group's products are summed from 0 and
+// join the total with one multiply-add by the scale.
+template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
+__global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
+                                                                      int64_t y_stride, int n_tiles, int t_tiles) {
+    constexpr int TERMS = kW4Terms<BF16>, THREADS = 64 * WN * WT, BN = WN * NT * 32, BT = WT * TT * 32;
+    typedef Stage<BF16, BT, 4, THREADS> StageX;
+    __shared__ uint4 s_x[2][TERMS * StageX::kPieces];
+    int n_tile, t_tile;
+    if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int n0 = n_tile * BN + (wave % WN) * NT * 32, t0 = t_tile * BT, tw = (wave / WN) * TT * 32;
+    const uint32_t* codes[NT];
+    const float* scales[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+        const int n = min(n0 + b * 32 + col, m.n - 1);
+        codes[b] = m.codes + int64_t(n) * m.words + half * 4;
+        scales[b] = m.scales + int64_t(n) * m.groups;
+    }
+    constexpr int GROUPS = kW4Chunk / GROUP;             // of a run
+    uint4 q[NT][2];
+    float sc[NT][GROUPS];
+    auto load_w = [&](int run) {
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            q[b][0] = *reinterpret_cast<const uint4*>(codes[b] + run * 16);
+            q[b][1] = *reinterpret_cast<const uint4*>(codes[b] + run * 16 + 8);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int at = run * GROUPS + g;
+                sc[b][g] = at < m.groups ? scales[b][at] : 0.0f;
+            }
+        }
+    };
+    f32x16 acc[TT][NT] = {};
+    StageX stage;
+    const int runs = m.words / 16;
+    stage.load(x, x_stride, t0, t, 0, m.k);
+    load_w(0);
+    stage.store(s_x[0]);
+    __syncthreads();
+    for (int run = 0; run < runs; ++run) {
+        uint32_t w[NT][8];
+        float s_now[NT][GROUPS];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            // step s uses piece s % 2 (logical word 2 s + half), word s / 2
+            w[b][0] = q[b][0].x; w[b][1] = q[b][1].x; w[b][2] = q[b][0].y; w[b][3] = q[b][1].y;
+            w[b][4] = q[b][0].z; w[b][5] = q[b][1].z; w[b][6] = q[b][0].w; w[b][7] = q[b][1].w;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) s_now[b][g] = sc[b][g];
+        }
+        const bool more = run + 1 < runs;
+        if (more) {
+            stage.load(x, x_stride, t0, t, (run + 1) * kW4Chunk, m.k);
+            load_w(run + 1);
+        }
+        const uint4* lds = s_x[run & 1];
+        f32x16 part[TT][NT];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            if (s * 16 % GROUP == 0) {
+#pragma unroll
+                for (int a = 0; a < TT; ++a)
+#pragma unroll
+                    for (int b = 0; b < NT; ++b) part[a][b] = f32x16{};
+            }
+            bf16x8 bw[NT];
+#pragma unroll
+            for (int b = 0; b < NT; ++b) bw[b] = w4_codes_bf16(w[b][s]);
+#pragma unroll
+            for (int a = 0; a < TT; ++a)
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) {
+                    const bf16x8 ax = as_operand(lds[j * StageX::kPieces + lds_piece<4>(tw + a * 32 + col, 2 * s + half)]);
+#pragma unroll
+                    for (int b = 0; b < NT; ++b) part[a][b] = mfma32(ax, bw[b], part[a][b]);
+                }
+            if ((s + 1) * 16 % GROUP == 0) {
+#pragma unroll
+                for (int a = 0; a < TT; ++a)
+#pragma unroll
+                    for (int b = 0; b < NT; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[a][b][i] = __builtin_fmaf(s_now[b][s * 16 / GROUP], part[a][b][i], acc[a][b][i]);
+            }
+        }
+        if (more) stage.store(s_x[(run + 1) & 1]);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int a = 0; a < TT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            const int n = n0 + b * 32 + col;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int tok = t0 + tw + a * 32 + mfma32_row(i, half);
+                if (n < m.n && tok < t) w4_store1<BF16>(y, int64_t(tok) * y_stride + n, acc[a][b][i]);
+            }
+        }
+}
+
+// ---- gradient of the scales ---------------------------------------------------------------------------------------------------------
+//
+// dscales[n][g] = sum_t dy[t][n] P[t][n][g] with P the product's sum over the group before its scale: the same matrix products, and no
+// weight gradient of n x k is ever formed.  A workgroup takes WN NT 32 rows of W and a run of 128 and walks over the tokens
+// (those of split blockIdx.y); the run's codes stay converted in registers.  Here W is the A operand, so that a lane holds one token and
+// for it 4 consecutive rows of W at a time, as dy has them; the sum over the lanes' tokens waits until the end.
+template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
+__global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
+                                                                      int64_t dy_stride, int n_tiles, int t_per_split, float* out,
+                                                                      int64_t out_split) {
+    constexpr int TERMS = kW4Terms<BF16>, THREADS = 64 * WN * WT, BN = WN * NT * 32, BT = WT * TT * 32;
+    constexpr int GROUPS = kW4Chunk / GROUP, LOGD = BN == 256 ? 5 : 4;      // octets of dy a row
+    static_assert(BN == 8 << LOGD, "rows of W of a tile");
+    constexpr int DPIECE = BF16 ? 1 : 2;                                    // 16-byte pieces of an octet of dy
+    typedef Stage<BF16, BT, 4, THREADS> StageX;
+    typedef Stage<BF16, BT, LOGD, THREADS> StageD;                          // its raw octets only
+    __shared__ uint4 s_x[2][TERMS * StageX::kPieces];
+    __shared__ uint4 s_d[2][DPIECE * StageD::kPieces];
+    __shared__ float s_sum[WT][GROUPS][BN];
+    int n_tile, run;
+    if (!tile_of(blockIdx.x, n_tiles, m.words / 16, n_tile, run)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int nw = (wave % WN) * NT * 32, n0 = n_tile * BN, tw = (wave / WN) * TT * 32;
+    bf16x8 aw[NT][8];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+        const int n = min(n0 + nw + b * 32 + col, m.n - 1);
+        const uint32_t* c = m.codes + int64_t(n) * m.words + run * 16 + half * 4;
+        const uint4 q0 = *reinterpret_cast<const uint4*>(c), q1 = *reinterpret_cast<const uint4*>(c + 8);
+        const uint32_t w[8] = {q0.x, q1.x, q0.y, q1.y, q0.z, q1.z, q0.w, q1.w};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) aw[b][s] = w4_codes_bf16(w[s]);
+    }
+    f32x16 sum[GROUPS][NT] = {};
+    const int first = blockIdx.y * t_per_split, last = min(t, first + t_per_split);
+    StageX sx;
+    StageD sd;
+    auto load = [&](int tok) {
+        sx.load(x, x_stride, tok, last, run * kW4Chunk, m.k);
+        sd.load(dy, dy_stride, tok, last, n0, m.n);
+    };
+    auto store = [&](int at) {
+        sx.store(s_x[at]);
+#pragma unroll
+        for (int j = 0; j < StageD::kOwn; ++j) {
+            const int id = threadIdx.x + j * THREADS, r = id >> LOGD, o = id & ((1 << LOGD) - 1);
+            if constexpr (BF16) {
+                s_d[at][lds_piece<LOGD>(r, o)] = make_uint4(sd.raw[j].w[0], sd.raw[j].w[1], sd.raw[j].w[2], sd.raw[j].w[3]);
+            } else {
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+                    s_d[at][lds_piece<LOGD + 1>(r, 2 * o + p)] =
+                        make_uint4(__float_as_uint(sd.raw[j].x[4 * p]), __float_as_uint(sd.raw[j].x[4 * p + 1]),
+                                   __float_as_uint(sd.raw[j].x[4 * p + 2]), __float_as_uint(sd.raw[j].x[4 * p + 3]));
+            }
+        }
+    };
+    if (first < last) {
+        load(first);
+        store(0);
+    }
+    __syncthreads();
+    for (int tok = first, at = 0; tok < last; tok += BT, at ^= 1) {
+        const bool more = tok + BT < last;
+        if (more) load(tok + BT);
+#pragma unroll
+        for (int a = 0; a < TT; ++a) {
+            const int r = tw + a * 32 + col;
+            f32x16 d[NT];
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int o = (nw + b * 32) / 8 + i;                    // rows of W 8 o + 4 half .. + 3
+                    if constexpr (BF16) {
+                        const uint2 v = reinterpret_cast<const uint2*>(&s_d[at][lds_piece<LOGD>(r, o)])[half];
+                        d[b][4 * i] = __uint_as_float(v.x << 16);
+                        d[b][4 * i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+                        d[b][4 * i + 2] = __uint_as_float(v.y << 16);
+                        d[b][4 * i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+                    } else {
+                        const uint4 v = s_d[at][lds_piece<LOGD + 1>(r, 2 * o + half)];
+                        d[b][4 * i] = __uint_as_float(v.x);
+                        d[b][4 * i + 1] = __uint_as_float(v.y);
+                        d[b][4 * i + 2] = __uint_as_float(v.z);
+                        d[b][4 * i + 3] = __uint_as_float(v.w);
+                    }
+                }
+            f32x16 part[NT];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                if (s * 16 % GROUP == 0) {
+#pragma unroll
+                    for (int b = 0; b < NT; ++b) part[b] = f32x16{};
+                }
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) {
+                    const bf16x8 bx = as_operand(s_x[at][j * StageX::kPieces + lds_piece<4>(r, 2 * s + half)]);
+#pragma unroll
+                    for (int b = 0; b < NT; ++b) part[b] = mfma32(aw[b][s], bx, part[b]);
+                }
+                if ((s + 1) * 16 % GROUP == 0) {
+#pragma unroll
+                    for (int b = 0; b < NT; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            sum[s * 16 / GROUP][b][i] = __builtin_fmaf(part[b][i], d[b][i], sum[s * 16 / GROUP][b][i]);
+                }
+            }
+        }
+        if (more) store(at ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float v = sum[g][b][i];
+                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0xB1, 0xF, 0xF, false));
+                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x4E, 0xF, 0xF, false));
+                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x141, 0xF, 0xF, false));
+                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x140, 0xF, 0xF, false));
+                v += __shfl_xor(v, 16);
+                if (col == 0) s_sum[wave / WN][g][nw + b * 32 + mfma32_row(i, half)] = v;
+            }
+    __syncthreads();
+    for (int id = threadIdx.x; id < GROUPS * BN; id += THREADS) {
+        const int g = id % GROUPS, n = id / GROUPS, at = run * GROUPS + g;
+        if (n0 + n >= m.n || at >= m.groups) continue;
+        float v = s_sum[0][g][n];
+#pragma unroll
+        for (int w = 1; w < WT; ++w) v += s_sum[w][g][n];
+        out[int64_t(blockIdx.y) * out_split + int64_t(n0 + n) * m.groups + at] = v;
+    }
+}
+
+// Sum of `splits` arrays of `count` floats, `apart` from one to the next, in their order
+__global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int splits, int64_t apart, int64_t count, float* out) {
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= count) return;
+    float v = parts[i];
+    for (int s = 1; s < splits; ++s) v += parts[s * apart + i];
+    out[i] = v;
+}
+
+// ---- dx = dy W -------------------------------------------------------------------------------------------------------------------------
+//
+// The reduction runs along W's rows, whose scales differ: value * scale is formed once per workgroup, as bf16 (one rounding of half a
+// unit in the last place per weight, as large as the one of the result) or as three bf16 terms for fp32, and goes to LDS transposed, 8 rows of W
+// an octet.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a dy that is not finite meets
+// W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0 would make NaN of infinity.
+template <bool BF16, int WT, int WK, int TT, int KT, int LOGN>
+__global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
+                                                                  int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
+                                                                  float* parts, int group_shift) {
+    constexpr int TERMS = kW4Terms<BF16>, THREADS = 64 * WT * WK, BT = WT * TT * 32, BK = WK * KT * 32, BN = 8 << LOGN;
+    constexpr int DTERMS = BF16 ? 1 : 4;
+    typedef Stage<BF16, BT, LOGN, THREADS> StageD;
+    constexpr int WPIECES = BK << LOGN, TASKS = (BK / 4) << LOGN;                             // a task: 8 rows of W, 4 inputs
+    constexpr int OWN = (TASKS + THREADS - 1) / THREADS;
+    __shared__ uint4 s_d[2][DTERMS * StageD::kPieces];
+    __shared__ uint4 s_w[2][TERMS * WPIECES];
+    int t_tile, k_tile;
+    if (!tile_of(blockIdx.x, t_tiles, k_tiles, t_tile, k_tile)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int t0 = t_tile * BT, k0 = k_tile * BK, tw = (wave % WT) * TT * 32, kw = (wave / WT) * KT * 32;
+    const int first = blockIdx.y * n_per_split, last = min(m.n, first + n_per_split);
+    StageD stage;
+    uint32_t word[OWN][8];
+    float sc[OWN][8];
+    // task: octet of rows in the low bits, then which half of the word, then the word
+    auto load_w = [&](int n) {
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const int id = threadIdx.x + j * THREADS, o = id & ((1 << LOGN) - 1), wd = k0 / 8 + (id >> (LOGN + 1));
+            if (TASKS % THREADS != 0 && id >= TASKS) break;
+            const int place = (wd & ~15) + w4_place(wd & 15);
+            const int at = wd * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int row = n + o * 8 + e;
+                const bool in = row < last && at < m.k;
+                word[j][e] = in ? m.codes[int64_t(row) * m.words + place] : 0u;
+                sc[j][e] = in ? m.scales[int64_t(row) * m.groups + (at >> group_shift)] : 0.0f;
+            }
+        }
+    };
+    auto store_w = [&](uint4* lds) {
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            const int id = threadIdx.x + j * THREADS, o = id & ((1 << LOGN) - 1), upper = (id >> LOGN) & 1;
+            if (TASKS % THREADS != 0 && id >= TASKS) break;
+            const int kk = (id >> (LOGN + 1)) * 8 + upper * 4;
+            float v[8][4];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t u = upper ? word[j][e] >> 16 : word[j][e];
+                const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 0);
+                const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 1);
+                v[e][0] = a.x * sc[j][e]; v[e][1] = a.y * sc[j][e];
+                v[e][2] = b.x * sc[j][e]; v[e][3] = b.y * sc[j][e];
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[TERMS][4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (BF16) {
+                        const bf16x2 p = {static_cast<__bf16>(v[2 * e][c]), static_cast<__bf16>(v[2 * e + 1][c])};
+                        w[0][e] = __builtin_bit_cast(uint32_t, p);
+                    } else {
+                        uint32_t a[3], b[3];
+                        split3(v[2 * e][c], a);
+                        split3(v[2 * e + 1][c], b);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) w[k][e] = a[k] >> 16 | b[k];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k)
+                    lds[k * WPIECES + lds_piece<LOGN>(kk + c, o)] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+            }
+        }
+    };
+    auto store_d = [&](uint4* lds) {
+        stage.store(lds);
+        if constexpr (!BF16) {
+#pragma unroll
+            for (int j = 0; j < StageD::kOwn; ++j) {
+                const int id = threadIdx.x + j * THREADS;
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t a = __float_as_uint(stage.raw[j].x[2 * e]), b = __float_as_uint(stage.raw[j].x[2 * e + 1]);
+                    w[e] = ((a & 0x7F800000u) == 0x7F800000u ? 0u : a >> 16) | ((b & 0x7F800000u) == 0x7F800000u ? 0u : b & 0xFFFF0000u);
+                }
+                lds[3 * StageD::kPieces + lds_piece<LOGN>(id >> LOGN, id & ((1 << LOGN) - 1))] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    };
+    f32x16 acc[TT][KT] = {};
+    if (first < last) {
+        stage.load(dy, dy_stride, t0, t, first, last);
+        load_w(first);
+        store_d(s_d[0]);
+        store_w(s_w[0]);
+    }
+    __syncthreads();
+    for (int n = first, at = 0; n < last; n += BN, at ^= 1) {
+        const bool more = n + BN < last;
+        if (more) {
+            stage.load(dy, dy_stride, t0, t, n + BN, last);
+            load_w(n + BN);
+        }
+#pragma unroll
+        for (int s = 0; s < BN / 16; ++s) {
+            bf16x8 bw[KT][TERMS];
+#pragma unroll
+            for (int b = 0; b < KT; ++b)
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j)
+                    bw[b][j] = as_operand(s_w[at][j * WPIECES + lds_piece<LOGN>(kw + b * 32 + col, 2 * s + half)]);
+#pragma unroll
+            for (int a = 0; a < TT; ++a)
+#pragma unroll
+                for (int j = 0; j < DTERMS; ++j) {
+                    const bf16x8 ad = as_operand(s_d[at][j * StageD::kPieces + lds_piece<LOGN>(tw + a * 32 + col, 2 * s + half)]);
+                    // dy's terms 0, 1, 2 meet W's first 1, 2, 1 terms, the finite ones of term 0 its other two
+                    constexpr int from[4] = {0, 0, 0, 1}, to[4] = {1, 2, 1, 3};
+#pragma unroll
+                    for (int b = 0; b < KT; ++b)
+#pragma unroll
+                        for (int i = from[j]; i < to[j]; ++i) acc[a][b] = mfma32(ad, bw[b][i], acc[a][b]);
+                }
+        }
+        if (more) {
+            store_d(s_d[at ^ 1]);
+            store_w(s_w[at ^ 1]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int a = 0; a < TT; ++a)
+#pragma unroll
+        for (int b = 0; b < KT; ++b) {
+            const int k = k0 + kw + b * 32 + col;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int tok = t0 + tw + a * 32 + mfma32_row(i, half);
+                if (k < m.k && tok < t) {
+                    if (parts) parts[(int64_t(blockIdx.y) * t + tok) * m.k + k] = acc[a][b][i];
+                    else w4_store1<BF16>(dx, int64_t(tok) * dx_stride + k, acc[a][b][i]);
+                }
+            }
+        }
+}
+
+// Sum of the splits' parts (t x k each), in their order
+template <bool BF16>
+__global__ __launch_bounds__(256) void w4_dx_join_kernel(const float* parts, int splits, int t, int k, void* dx, int64_t dx_stride) {
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, count = int64_t(t) * k;
+    if (i >= count) return;
+    float v = parts[i];
+    for (int s = 1; s < splits; ++s) v += parts[s * count + i];
+    w4_store1<BF16>(dx, i / k * dx_stride + i % k, v);
+}
+
+}  // namespace lpmm

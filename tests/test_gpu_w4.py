@@ -340,7 +340,8 @@ def test_refusals():
         args = list(ok)
         args[at] = bad
         assert L.lpmm_w4_linear(*args) == -1, (at, bad)
-    ok = [dp, 0, 4, 16, c, sc, sh, 64, xp, 128, None]
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    ok = [dp, 0, 4, 16, c, sc, sh, 64, xp, 128, ws.data_ptr(), 1 << 20, None]
     for at, bad in ((0, None), (1, 3), (3, 15), (4, c + 4), (7, 0), (9, 127)):
         args = list(ok)
         args[at] = bad
