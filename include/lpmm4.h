@@ -514,7 +514,7 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
 /* ---- distillation from a teacher's top logits ------------------------------------------------------------------------
  *
  * z: student's logits, t rows of v (z_dtype, z_stride).  top: float[t][slots], index: int64[t][slots], the teacher's largest logits
- * and where in the vocabulary they stand, both without gaps between rows.  A slot counts if 0 <= index < v (fill short lists
+ * and where in the vocabulary they stand, both without gaps between rows; v is at most 2^30.  A slot counts if 0 <= index < v (fill short lists
  * with -1); 1 <= slots <= LPMM_DISTILL_MAX_SLOTS; an index may appear more than once.  tau: temperature, finite and > 0.
  *   p    = softmax(top / tau) over a row's slots that count
  *   lse  = log sum_i exp(z_i / tau)

@@ -1,16 +1,19 @@
 // Distillation from a teacher's top logits: loss and gradient (formulas: include/lpmm4.h).
 //
-// One pass over a row of logits keeps a running maximum m and the sum l of exp(z / tau - m), both in fp32 per lane, and joins the
-// lanes' pairs at the end; the gradient is exp(z / tau - lse) times a factor everywhere but at the teacher's slots, which
-// are written once more behind a barrier.  Bound by reading and writing the logits.
+// A pass over a row keeps, per lane and in fp32, the largest logit m and the sum l of exp((z - m) / tau), rescaled when m
+// rises, and joins the lanes' pairs at the end.  The gradient is a factor times exp((z - m) / tau) everywhere but at the teacher's
+// places, which are written once more behind a barrier.  Bound by reading and writing the logits.
+//
+// A row is taken in pieces of 16 bytes from its first element on, wherever that lies: gfx950 reads and writes them in one piece at any
+// alignment of an element, and so the sums' order, and with it the bits, does not depend on where a row stands.
 #pragma once
 
 #include "w4.hpp"
 
 namespace lpmm {
 
-constexpr int kDistillSlots = 1024;      // most slots of a row
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLowest = -3.402823466e38f;
 
 struct DistillArgs {
     const void* z;
@@ -19,7 +22,7 @@ struct DistillArgs {
     int v, slots;
     const float* top;
     const int64_t* index;
-    float tau, inv_tau;
+    float tau, inv_tau, c;               // c = log2(e) / tau
     const float* grad;
     float* loss;
     float* lse;
@@ -27,23 +30,38 @@ struct DistillArgs {
     int64_t dz_stride;
 };
 
-// The teacher's side of a row, in LDS: places (-1 where a slot does not count) and probabilities
+// The teacher's side of a row, in LDS: places (-1 where a slot does not count), probabilities and the student's logits there.
+// Sized by the launch, so that short lists leave room for many workgroups.
 struct DistillSlots {
-    int at[kDistillSlots];
-    float p[kDistillSlots];
+    int* at;                             // a multiple of 4 of them
+    float* p;
+    float* z;
+    int* later;                          // an earlier slot names the same place
+    int* repeats;                        // [0]: some slot is a later one
 };
+constexpr int distill_room(int slots) { return (slots + 3) / 4 * 4; }
+constexpr size_t distill_lds(int slots) { return size_t(distill_room(slots)) * 16 + 16; }
+__device__ __forceinline__ DistillSlots distill_slots(int slots) {
+    extern __shared__ __align__(16) int distill_memory[];
+    const int room = distill_room(slots);
+    return DistillSlots{distill_memory, reinterpret_cast<float*>(distill_memory + room), reinterpret_cast<float*>(distill_memory + 2 * room),
+                        distill_memory + 3 * room, distill_memory + 4 * room};
+}
 
-__device__ __forceinline__ float exp_nat(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float ln_fast(float x) { return __builtin_amdgcn_logf(x) * kLn2; }     // of sums in [1, v], 0 or not finite
 
 // (m, l) of two disjoint sets.  m starts at -FLT_MAX rather than -infinity, so that no difference is infinity - infinity
 // as long as the logits hold no +infinity.
-__device__ __forceinline__ void join_ml(float& m, float& l, float m2, float l2) {
+__device__ __forceinline__ void join_ml(float c, float& m, float& l, float m2, float l2) {
     const float top = fmaxf(m, m2);
-    l = l * exp_nat(m - top) + l2 * exp_nat(m2 - top);
+    l = l * exp2_fast((m - top) * c) + l2 * exp2_fast((m2 - top) * c);
     m = top;
 }
-constexpr float kLowest = -3.402823466e38f;
-
+__device__ __forceinline__ void wave_join_ml(float c, float& m, float& l) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) join_ml(c, m, l, __shfl_xor(m, d), __shfl_xor(l, d));
+}
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
@@ -55,156 +73,361 @@ __device__ __forceinline__ float wave_max(float x) {
     return x;
 }
 
-// One wave reads a row's slots: s.at and s.p of the row, and log p = u - log_total with u = top / tau - top_max in each lane's own
-// loop below.  Returns whether any slot counts.
-__device__ __forceinline__ bool distill_teacher(const DistillArgs& a, int64_t row, DistillSlots& s, float& u_max,
-                                                float& log_total) {
-    const int lane = threadIdx.x & 63;
-    const float* top = a.top + row * a.slots;
-    const int64_t* index = a.index + row * a.slots;
-    float m = -__builtin_inff();
+// ---- pieces of 16 bytes ----------------------------------------------------------------------------------------------------
+
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+template <bool BF16> constexpr int kPiece = BF16 ? 8 : 4;          // elements
+constexpr uint32_t kMinusInf = 0xFF800000u;
+
+// elements first .. of a row at p[row0 ..]; beyond v: -infinity
+template <bool BF16>
+__device__ __forceinline__ Vec16 piece_load(const void* p, int64_t row0, int first, int v) {
+    if (first + kPiece<BF16> <= v) {
+        if constexpr (BF16) return *reinterpret_cast<const Vec16*>(static_cast<const uint16_t*>(p) + row0 + first);
+        else return *reinterpret_cast<const Vec16*>(static_cast<const float*>(p) + row0 + first);
+    }
+    Vec16 r;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (BF16) {
+            const uint16_t* x = static_cast<const uint16_t*>(p) + row0;
+            const int i = first + 2 * w;
+            const uint32_t lo = i < v ? x[i] : kMinusInf >> 16, hi = i + 1 < v ? x[i + 1] : kMinusInf >> 16;
+            r.v[w] = lo | hi << 16;
+        } else {
+            const int i = first + w;
+            r.v[w] = i < v ? __float_as_uint(static_cast<const float*>(p)[row0 + i]) : kMinusInf;
+        }
+    }
+    return r;
+}
+template <bool BF16, bool NT>
+__device__ __forceinline__ void piece_store(void* p, int64_t row0, int first, int v, const float x[]) {
+    if (first + kPiece<BF16> <= v) {
+        Vec16 r;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (BF16) {
+                const bf16x2 two = {static_cast<__bf16>(x[2 * w]), static_cast<__bf16>(x[2 * w + 1])};
+                r.v[w] = __builtin_bit_cast(uint32_t, two);
+            } else {
+                r.v[w] = __float_as_uint(x[w]);
+            }
+        }
+        u32x4u* to = reinterpret_cast<u32x4u*>(static_cast<char*>(p) + (row0 + first) * (BF16 ? 2 : 4));
+        if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4u, r), to);
+        else *to = __builtin_bit_cast(u32x4u, r);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kPiece<BF16>; ++e)
+        if (first + e < v) w4_store1<BF16>(p, row0 + first + e, x[e]);
+}
+template <bool BF16>
+__device__ __forceinline__ void piece_values(const Vec16& r, float x[]) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (BF16) {
+            x[2 * w] = __uint_as_float(r.v[w] << 16);
+            x[2 * w + 1] = __uint_as_float(r.v[w] & 0xFFFF0000u);
+        } else {
+            x[w] = __uint_as_float(r.v[w]);
+        }
+    }
+}
+// (m, l) with a piece's elements in it
+template <bool BF16>
+__device__ __forceinline__ void piece_ml(const Vec16& r, float c, float& m, float& l) {
+    float x[kPiece<BF16>];
+    piece_values<BF16>(r, x);
+    float top = m;
+#pragma unroll
+    for (int e = 0; e < kPiece<BF16>; ++e) top = fmaxf(top, x[e]);
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPiece<BF16>; ++e) sum += exp2_fast((x[e] - top) * c);
+    l = __builtin_fmaf(l, exp2_fast((m - top) * c), sum);
+    m = top;
+}
+
+// ---- a row's slots -----------------------------------------------------------------------------------------------------------
+
+// Does any slot count?  Every wave finds out by itself, before anything of the row is read.
+__device__ __forceinline__ bool distill_any(const DistillArgs& a, int64_t row) {
     bool any = false;
+    for (int j = threadIdx.x & 63; j < a.slots; j += 64) {
+        const int64_t i = a.index[row * a.slots + j];
+        any = any || (i >= 0 && i < a.v);
+    }
+    return __ballot(any) != 0;
+}
+
+// One wave fills s, and the row's largest top / tau and the logarithm of the sum of its exponentials
+template <bool BF16>
+__device__ __forceinline__ void distill_teacher(const DistillArgs& a, int64_t row, const DistillSlots& s, float& u_max, float& log_total) {
+    const int lane = threadIdx.x & 63;
+    float m = -__builtin_inff();
+    if (lane == 0) s.repeats[0] = 0;
+    if (a.slots + lane < distill_room(a.slots)) s.at[a.slots + lane] = -1;           // read four at a time
     for (int j = lane; j < a.slots; j += 64) {
-        const int64_t i = index[j];
+        const int64_t i = a.index[row * a.slots + j];
         const bool ok = i >= 0 && i < a.v;
-        const float u = top[j] * a.inv_tau;
+        s.later[j] = 0;
+        const float u = a.top[row * a.slots + j] * a.inv_tau;
         s.at[j] = ok ? int(i) : -1;
         s.p[j] = u;
+        s.z[j] = ok ? w4_load1<BF16>(a.z, row * a.z_stride + i) : 0.0f;
         if (ok) m = fmaxf(m, u);
-        any = any || ok;
     }
-    any = __ballot(any) != 0;
     u_max = wave_max(m);
     float sum = 0.0f;
     for (int j = lane; j < a.slots; j += 64) {
-        const float e = s.at[j] >= 0 ? exp_nat(s.p[j] - u_max) : 0.0f;
+        const float e = s.at[j] >= 0 ? exp2_fast((s.p[j] - u_max) * kLog2e) : 0.0f;
         s.p[j] = e;
         sum += e;
     }
     sum = wave_sum(sum);
     const float inv = 1.0f / sum;
     for (int j = lane; j < a.slots; j += 64) s.p[j] *= inv;
-    log_total = logf(sum);
-    return any;
+    log_total = ln_fast(sum);
 }
 
-// One wave: the row's loss from its lse
-template <bool BF16>
+// One wave, the one that filled s: the row's loss.  A logit's log-probability is (z - m) / tau - log_l.
 __device__ __forceinline__ float distill_row_loss(const DistillArgs& a, int64_t row, const DistillSlots& s, float u_max,
-                                                  float log_total, float lse) {
+                                                  float log_total, float m, float log_l) {
     float sum = 0.0f;
     for (int j = threadIdx.x & 63; j < a.slots; j += 64) {
-        const int at = s.at[j];
         const float p = s.p[j];
-        if (at >= 0 && p != 0.0f) {
+        if (s.at[j] >= 0 && p != 0.0f) {
             const float log_p = (a.top[row * a.slots + j] * a.inv_tau - u_max) - log_total;
-            const float log_q = w4_load1<BF16>(a.z, row * a.z_stride + at) * a.inv_tau - lse;
+            const float log_q = (s.z[j] - m) * a.inv_tau - log_l;
             sum += p * (log_p - log_q);
         }
     }
     return a.tau * a.tau * wave_sum(sum);
 }
 
-// A workgroup takes a row.
-template <bool BF16, int THREADS>
-__global__ __launch_bounds__(THREADS) void distill_loss_kernel(const DistillArgs a) {
-    __shared__ DistillSlots s_slots;
-    __shared__ float s_m[THREADS / 64], s_l[THREADS / 64];
-    __shared__ int s_any;
-    const int64_t row = blockIdx.x;
-    const int wave = threadIdx.x >> 6;
-    float u_max = 0.0f, log_total = 0.0f;
-    if (wave == 0) {
-        const bool any = distill_teacher(a, row, s_slots, u_max, log_total);
-        if (threadIdx.x == 0) s_any = any;
-    }
-    __syncthreads();
-    if (!s_any) {
-        if (threadIdx.x == 0) a.loss[row] = a.lse[row] = 0.0f;
-        return;
-    }
-    float m = kLowest, l = 0.0f;
-    const int64_t z0 = row * a.z_stride;
-    for (int i = threadIdx.x * 8; i < a.v; i += THREADS * 8) {
-        float x[8];
-        w4_load8<BF16>(a.z, z0 + i, z0 + a.v, x);
-        float top = m;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = i + e < a.v ? x[e] * a.inv_tau : -__builtin_inff();
-            top = fmaxf(top, x[e]);
+// Marks the slots whose place an earlier one names, by the whole workgroup: a wave holds 64 slots and looks at 4 others at a time.
+template <int THREADS>
+__device__ __forceinline__ void distill_repeats(const DistillArgs& a, const DistillSlots& s) {
+    const int quads = (a.slots + 3) >> 2, pairs = ((a.slots + 63) >> 6) * quads;
+    for (int pair = threadIdx.x >> 6; pair < pairs; pair += THREADS / 64) {
+        const int block = pair / quads, i = (pair - block * quads) * 4, j = block * 64 + int(threadIdx.x & 63);
+        if (i > block * 64 + 63) continue;
+        const int at = j < a.slots ? s.at[j] : -1;
+        const int4 other = *reinterpret_cast<const int4*>(&s.at[i]);
+        const bool later = (other.x == at && i < j) || (other.y == at && i + 1 < j) || (other.z == at && i + 2 < j) ||
+                           (other.w == at && i + 3 < j);
+        if (at >= 0 && later) {
+            s.later[j] = 1;
+            s.repeats[0] = 1;
         }
-        l *= exp_nat(m - top);
-        m = top;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) l += exp_nat(x[e] - m);
     }
+}
+// The p of a place: that of slot j, the first to name it, and of all others that do, in their order
+__device__ __forceinline__ float distill_place_p(const DistillArgs& a, const DistillSlots& s, int j) {
+    float p = s.p[j];
+    if (s.repeats[0])
+        for (int i = j + 1; i < a.slots; ++i)
+            if (s.at[i] == s.at[j]) p += s.p[i];
+    return p;
+}
+
+// ---- loss ----------------------------------------------------------------------------------------------------------------------
+
+// (m, l) of the logits [first, last) of a row, by one workgroup; in every lane of wave 0
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void distill_span_ml(const DistillArgs& a, int64_t row, int first, int last, float* s_m, float* s_l,
+                                                float& m, float& l) {
+    const int64_t row0 = row * a.z_stride + first;
+    const int len = last - first;
+    m = kLowest;
+    l = 0.0f;
+    constexpr int kAhead = 4;
+    for (int i = threadIdx.x * kPiece<BF16>; i < len; i += kAhead * THREADS * kPiece<BF16>) {
+        Vec16 r[kAhead];
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const float m2 = __shfl_xor(m, d), l2 = __shfl_xor(l, d);
-        join_ml(m, l, m2, l2);
+        for (int j = 0; j < kAhead; ++j) r[j] = piece_load<BF16>(a.z, row0, i + j * THREADS * kPiece<BF16>, len);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) piece_ml<BF16>(r[j], a.c, m, l);
     }
-    if ((threadIdx.x & 63) == 0) { s_m[wave] = m; s_l[wave] = l; }
+    wave_join_ml(a.c, m, l);
+    if ((threadIdx.x & 63) == 0) { s_m[threadIdx.x >> 6] = m; s_l[threadIdx.x >> 6] = l; }
     __syncthreads();
-    if (wave == 0) {
+    if (threadIdx.x < 64) {
         m = s_m[0], l = s_l[0];
 #pragma unroll
-        for (int w = 1; w < THREADS / 64; ++w) join_ml(m, l, s_m[w], s_l[w]);
-        const float lse = m + logf(l);
-        const float loss = distill_row_loss<BF16>(a, row, s_slots, u_max, log_total, lse);
-        if (threadIdx.x == 0) { a.loss[row] = loss; a.lse[row] = lse; }
+        for (int w = 1; w < THREADS / 64; ++w) join_ml(a.c, m, l, s_m[w], s_l[w]);
     }
 }
 
-// A workgroup takes `span` logits of a row.
-constexpr int kDistillThreads = 256;
-template <bool BF16>
-__global__ __launch_bounds__(kDistillThreads) void distill_grad_kernel(const DistillArgs a, int span) {
-    __shared__ DistillSlots s_slots;
-    __shared__ int s_any;
-    constexpr int kOwn = kDistillSlots / kDistillThreads;
-    const int64_t row = blockIdx.y;
-    const int first = blockIdx.x * span, last = min(first + span, a.v);
-    const float g = a.grad[row] * a.tau;
-    const bool masked = a.grad[row] == 0.0f;
-    if (threadIdx.x < 64) {
-        float u_max, log_total;
-        const bool any = distill_teacher(a, row, s_slots, u_max, log_total);
-        if (threadIdx.x == 0) s_any = any;
-    }
-    __syncthreads();
-    const int64_t z0 = row * a.z_stride, o0 = row * a.dz_stride;
-    if (!s_any || masked) {
-        for (int i = first + threadIdx.x; i < last; i += kDistillThreads) w4_store1<BF16>(a.dz, o0 + i, 0.0f);
+// A workgroup takes a row.
+template <bool BF16, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_loss_kernel(const DistillArgs a) {
+    const DistillSlots s_slots = distill_slots(a.slots);
+    __shared__ float s_m[THREADS / 64], s_l[THREADS / 64];
+    const int64_t row = blockIdx.x;
+    if (!distill_any(a, row)) {
+        if (threadIdx.x == 0) a.loss[row] = a.lse[row] = 0.0f;
         return;
     }
-    const float lse = a.lse[row];
-    // the slots in this span, each place by the first slot that names it; read before anything is written (dz may be z)
-    float fixed[kOwn];
-    int place[kOwn];
+    float u_max = 0.0f, log_total = 0.0f, m, l;
+    if (threadIdx.x < 64) distill_teacher<BF16>(a, row, s_slots, u_max, log_total);
+    distill_span_ml<BF16, THREADS>(a, row, 0, a.v, s_m, s_l, m, l);
+    if (threadIdx.x < 64) {
+        const float log_l = ln_fast(l), loss = distill_row_loss(a, row, s_slots, u_max, log_total, m, log_l);
+        if (threadIdx.x == 0) { a.loss[row] = loss; a.lse[row] = m * a.inv_tau + log_l; }
+    }
+}
+
+// Few long rows: a workgroup takes `span` logits of a row and leaves its (m, l); a wave per row joins them.
+constexpr int kDistillThreads = 256;
+template <bool BF16>
+__global__ __launch_bounds__(kDistillThreads) void distill_part_kernel(const DistillArgs a, int span, float2* parts) {
+    __shared__ float s_m[kDistillThreads / 64], s_l[kDistillThreads / 64];
+    const int64_t row = blockIdx.y;
+    if (!distill_any(a, row)) return;
+    float m, l;
+    const int first = blockIdx.x * span;
+    distill_span_ml<BF16, kDistillThreads>(a, row, first, min(first + span, a.v), s_m, s_l, m, l);
+    if (threadIdx.x == 0) parts[row * gridDim.x + blockIdx.x] = make_float2(m, l);
+}
+template <bool BF16>
+__global__ __launch_bounds__(64) void distill_finish_kernel(const DistillArgs a, const float2* parts, int spans) {
+    const DistillSlots s_slots = distill_slots(a.slots);
+    const int64_t row = blockIdx.x;
+    if (!distill_any(a, row)) {
+        if (threadIdx.x == 0) a.loss[row] = a.lse[row] = 0.0f;
+        return;
+    }
+    float u_max, log_total, m = kLowest, l = 0.0f;
+    distill_teacher<BF16>(a, row, s_slots, u_max, log_total);
+    for (int i = threadIdx.x; i < spans; i += 64) {
+        const float2 part = parts[row * spans + i];
+        join_ml(a.c, m, l, part.x, part.y);
+    }
+    wave_join_ml(a.c, m, l);
+    const float log_l = ln_fast(l), loss = distill_row_loss(a, row, s_slots, u_max, log_total, m, log_l);
+    if (threadIdx.x == 0) { a.loss[row] = loss; a.lse[row] = m * a.inv_tau + log_l; }
+}
+
+// ---- gradient ----------------------------------------------------------------------------------------------------------------------
+
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void distill_zero(const DistillArgs& a, int64_t row0, int len) {
+    const float zero[kPiece<BF16>] = {};
+    for (int i = threadIdx.x * kPiece<BF16>; i < len; i += THREADS * kPiece<BF16>) piece_store<BF16, false>(a.dz, row0, i, len, zero);
+}
+
+// A workgroup takes kGradPieces pieces per thread of a row.
+constexpr int kGradPieces = 4;
+template <bool BF16, int THREADS> constexpr int kGradSpan = THREADS * kGradPieces * kPiece<BF16>;
+template <bool BF16, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillArgs a) {
+    const DistillSlots s_slots = distill_slots(a.slots);
+    constexpr int VEC = kPiece<BF16>;
+    const int64_t row = blockIdx.y;
+    const int first = blockIdx.x * kGradSpan<BF16, THREADS>, last = min(first + kGradSpan<BF16, THREADS>, a.v);
+    const int64_t z0 = row * a.z_stride, o0 = row * a.dz_stride;
+    const bool any = distill_any(a, row);
+    if (!any || a.grad[row] == 0.0f) {
+        distill_zero<BF16, THREADS>(a, o0 + first, last - first);
+        return;
+    }
+    Vec16 r[kGradPieces];
 #pragma unroll
-    for (int o = 0; o < kOwn; ++o) {
-        const int j = threadIdx.x + o * kDistillThreads;
-        place[o] = j < a.slots ? s_slots.at[j] : -1;
-        if (place[o] < first || place[o] >= last) place[o] = -1;
-        fixed[o] = 0.0f;
-        if (place[o] >= 0) {
-            float p = 0.0f;
-            for (int i = 0; i < a.slots; ++i)
-                if (s_slots.at[i] == place[o]) {
-                    if (i < j) { place[o] = -1; break; }
-                    p += s_slots.p[i];
-                }
-            if (place[o] >= 0) fixed[o] = g * (exp_nat(w4_load1<BF16>(a.z, z0 + place[o]) * a.inv_tau - lse) - p);
+    for (int j = 0; j < kGradPieces; ++j)
+        r[j] = piece_load<BF16>(a.z, z0, first + (j * THREADS + int(threadIdx.x)) * VEC, last);
+    if (threadIdx.x < 64) {
+        float u_max, log_total;
+        distill_teacher<BF16>(a, row, s_slots, u_max, log_total);
+    }
+    const float g = a.grad[row] * a.tau, lse = a.lse[row];
+    __syncthreads();                     // dz may be z: everything has been read (the slots' logits by the first wave)
+#pragma unroll
+    for (int j = 0; j < kGradPieces; ++j) {
+        const int at = first + (j * THREADS + int(threadIdx.x)) * VEC;
+        if (at >= last) break;
+        float x[VEC];
+        piece_values<BF16>(r[j], x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = g * exp2_fast(__builtin_fmaf(x[e], a.inv_tau, -lse) * kLog2e);
+        piece_store<BF16, true>(a.dz, o0, at, last, x);
+    }
+    distill_repeats<THREADS>(a, s_slots);
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.slots; j += THREADS) {
+        const int at = s_slots.at[j];
+        if (at >= first && at < last && !s_slots.later[j])
+            w4_store1<BF16>(a.dz, o0 + at, g * (exp2_fast(__builtin_fmaf(s_slots.z[j], a.inv_tau, -lse) * kLog2e) -
+                                                distill_place_p(a, s_slots, j)));
+    }
+}
+
+// ---- both ----------------------------------------------------------------------------------------------------------------------------
+
+// A workgroup takes a row and holds it in registers, ITEMS pieces a thread: one read, one write.  dz goes past the caches but for the
+// shortest rows (NT; 4096 x 57344 bf16 186 us, 198 through them; 65536 x 2000 bf16 200 and 183, fp32 334 and 302).
+template <bool BF16, int THREADS, int ITEMS, int WAVES>
+__global__ __launch_bounds__(THREADS, WAVES) void distill_both_kernel(const DistillArgs a) {
+    constexpr bool NT = THREADS > 64 || (BF16 && ITEMS > 4);
+    const DistillSlots s_slots = distill_slots(a.slots);
+    __shared__ float s_m[THREADS / 64], s_l[THREADS / 64];
+    constexpr int VEC = kPiece<BF16>;
+    const int64_t row = blockIdx.x;
+    const int64_t z0 = row * a.z_stride, o0 = row * a.dz_stride;
+    if (!distill_any(a, row)) {
+        distill_zero<BF16, THREADS>(a, o0, a.v);
+        if (threadIdx.x == 0) a.loss[row] = a.lse[row] = 0.0f;
+        return;
+    }
+    // a wave takes `items` KiB in a row, so that lines which two of its pieces share stay near
+    const int items = (a.v + THREADS * VEC - 1) / (THREADS * VEC);
+    const int begin = (int(threadIdx.x >> 6) * items * 64 + int(threadIdx.x & 63)) * VEC, end = min(a.v, begin + items * 64 * VEC);
+    Vec16 r[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        if (begin + j * 64 * VEC < end) r[j] = piece_load<BF16>(a.z, z0, begin + j * 64 * VEC, a.v);
+    float u_max = 0.0f, log_total = 0.0f;
+    if (threadIdx.x < 64) distill_teacher<BF16>(a, row, s_slots, u_max, log_total);
+    float m = kLowest, l = 0.0f;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        if (begin + j * 64 * VEC < end) piece_ml<BF16>(r[j], a.c, m, l);
+    wave_join_ml(a.c, m, l);
+    if ((threadIdx.x & 63) == 0) { s_m[threadIdx.x >> 6] = m; s_l[threadIdx.x >> 6] = l; }
+    __syncthreads();                     // and everything of the row has been read: dz may be z
+    m = s_m[0], l = s_l[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) join_ml(a.c, m, l, s_m[w], s_l[w]);
+    const float grad = a.grad[row], g = grad * a.tau, f = g / l;
+    if (grad == 0.0f) {
+        distill_zero<BF16, THREADS>(a, o0, a.v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            const int at = begin + j * 64 * VEC;
+            if (at < end) {
+                float x[VEC];
+                piece_values<BF16>(r[j], x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[e] = f * exp2_fast((x[e] - m) * a.c);
+                piece_store<BF16, NT>(a.dz, o0, at, a.v, x);
+            }
         }
     }
+    distill_repeats<THREADS>(a, s_slots);
+    if (threadIdx.x < 64) {
+        const float log_l = ln_fast(l), loss = distill_row_loss(a, row, s_slots, u_max, log_total, m, log_l);
+        if (threadIdx.x == 0) { a.loss[row] = loss; a.lse[row] = m * a.inv_tau + log_l; }
+    }
     __syncthreads();
-    for (int i = first + threadIdx.x; i < last; i += kDistillThreads)
-        w4_store1<BF16>(a.dz, o0 + i, g * exp_nat(w4_load1<BF16>(a.z, z0 + i) * a.inv_tau - lse));
-    __syncthreads();
-#pragma unroll
-    for (int o = 0; o < kOwn; ++o)
-        if (place[o] >= 0) w4_store1<BF16>(a.dz, o0 + place[o], fixed[o]);
+    if (grad == 0.0f) return;
+    for (int j = threadIdx.x; j < a.slots; j += THREADS) {
+        const int at = s_slots.at[j];
+        if (at >= 0 && !s_slots.later[j])
+            w4_store1<BF16>(a.dz, o0 + at, g * (exp2_fast((s_slots.z[j] - m) * a.c) / l - distill_place_p(a, s_slots, j)));
+    }
 }
 
 }  // namespace lpmm

@@ -15,6 +15,7 @@ namespace {
 using namespace lpmm;
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1 - 2 * kW4Chunk;
+constexpr int64_t kMaxVocabulary = int64_t(1) << 30;
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -54,7 +55,7 @@ int check_workspace(const void* p, size_t have, size_t need) {
 
 int check_distill(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
                   const int64_t* index, int slots, float tau, DistillArgs* a) {
-    if (v < 1 || v > kMaxDim || slots < 1 || slots > LPMM_DISTILL_MAX_SLOTS) return LPMM_EINVAL;
+    if (v < 1 || v > kMaxVocabulary || slots < 1 || slots > LPMM_DISTILL_MAX_SLOTS) return LPMM_EINVAL;
     if (!std::isfinite(tau) || !(tau > 0.0f) || !std::isfinite(1.0f / tau)) return LPMM_EINVAL;
     LPMM_TRY(check_rows(z, z_dtype, t, v, z_stride));
     if (t > 0 && (check_floats(top) || !index || !aligned(index, 8))) return LPMM_EINVAL;
@@ -67,19 +68,49 @@ int check_distill(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_st
     a->index = index;
     a->tau = tau;
     a->inv_tau = 1.0f / tau;
+    a->c = kLog2e / tau;
     return LPMM_OK;
 }
 
-int launch_loss(const DistillArgs& a, bool bf16, hipStream_t s) {
-    if (bf16) hipLaunchKernelGGL((distill_loss_kernel<true, 1024>), dim3(unsigned(a.t)), dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((distill_loss_kernel<false, 1024>), dim3(unsigned(a.t)), dim3(1024), 0, s, a);
+// Few rows that are long: the workgroups that share a row's sum; 1: one does it all
+constexpr int kSpanBytes = 32768;
+int distill_spans(int64_t t, int64_t v, int esize) {
+    if (t >= 128 || v * esize < 8 * kSpanBytes) return 1;
+    return int(std::min(div_up(v * esize, kSpanBytes), div_up(1024, t)));
+}
+
+int launch_loss(const DistillArgs& a, bool bf16, void* workspace, hipStream_t s) {
+    const int spans = distill_spans(a.t, a.v, bf16 ? 2 : 4);
+    if (spans > 1) {
+        float2* parts = static_cast<float2*>(workspace);
+        const int span = int(div_up(a.v, spans));
+        const dim3 grid(unsigned(spans), unsigned(a.t)), rows(unsigned(a.t));      // spans * span >= v > (spans - 1) * span
+        if (bf16) {
+            hipLaunchKernelGGL(distill_part_kernel<true>, grid, dim3(kDistillThreads), 0, s, a, span, parts);
+            LPMM_HIP(hipGetLastError());
+            hipLaunchKernelGGL(distill_finish_kernel<true>, rows, dim3(64), distill_lds(a.slots), s, a, parts, spans);
+        } else {
+            hipLaunchKernelGGL(distill_part_kernel<false>, grid, dim3(kDistillThreads), 0, s, a, span, parts);
+            LPMM_HIP(hipGetLastError());
+            hipLaunchKernelGGL(distill_finish_kernel<false>, rows, dim3(64), distill_lds(a.slots), s, a, parts, spans);
+        }
+        LPMM_HIP(hipGetLastError());
+        return LPMM_OK;
+    }
+    const dim3 rows(unsigned(a.t));
+    const int64_t bytes = int64_t(a.v) * (bf16 ? 2 : 4);
+#define LPMM_LOSS(B, N) hipLaunchKernelGGL((distill_loss_kernel<B, N>), rows, dim3(N), distill_lds(a.slots), s, a)
+    if (bytes <= 16384) { if (bf16) LPMM_LOSS(true, 64); else LPMM_LOSS(false, 64); }
+    else if (bytes <= 131072) { if (bf16) LPMM_LOSS(true, 256); else LPMM_LOSS(false, 256); }
+    else { if (bf16) LPMM_LOSS(true, 1024); else LPMM_LOSS(false, 1024); }
+#undef LPMM_LOSS
     LPMM_HIP(hipGetLastError());
     return LPMM_OK;
 }
 
 int launch_grad(const DistillArgs& a, bool bf16, hipStream_t s) {
-    const int span = 8192;
     constexpr int64_t kRows = 32768;                     // of a launch: grid.y
+    const bool narrow = int64_t(a.v) * (bf16 ? 2 : 4) <= 16384;      // short rows: a wave each
     for (int64_t r = 0; r < a.t; r += kRows) {
         DistillArgs b = a;
         b.z = static_cast<const char*>(a.z) + r * a.z_stride * (bf16 ? 2 : 4);
@@ -88,12 +119,38 @@ int launch_grad(const DistillArgs& a, bool bf16, hipStream_t s) {
         b.index += r * a.slots;
         b.grad += r;
         b.lse += r;
-        const dim3 grid(unsigned(div_up(a.v, span)), unsigned(std::min(kRows, a.t - r)));
-        if (bf16) hipLaunchKernelGGL(distill_grad_kernel<true>, grid, dim3(kDistillThreads), 0, s, b, span);
-        else hipLaunchKernelGGL(distill_grad_kernel<false>, grid, dim3(kDistillThreads), 0, s, b, span);
+#define LPMM_GRAD(B, N) hipLaunchKernelGGL((distill_grad_kernel<B, N>), dim3(unsigned(div_up(a.v, kGradSpan<B, N>)), \
+                                           unsigned(std::min(kRows, a.t - r))), dim3(N), distill_lds(a.slots), s, b)
+        if (narrow) { if (bf16) LPMM_GRAD(true, 64); else LPMM_GRAD(false, 64); }
+        else { if (bf16) LPMM_GRAD(true, 256); else LPMM_GRAD(false, 256); }
+#undef LPMM_GRAD
         LPMM_HIP(hipGetLastError());
     }
     return LPMM_OK;
+}
+
+// Loss and gradient with a row in a workgroup's registers: the smallest shape that holds it.  Rows share a CU three or four at a time
+// but for the longest: while one is summed up, others are read and written.  False: no shape holds it.
+bool launch_both(const DistillArgs& a, bool bf16, hipStream_t s) {
+    const int64_t pieces = div_up(a.v, bf16 ? kPiece<true> : kPiece<false>);
+    const dim3 rows(unsigned(a.t));
+#define LPMM_BOTH(N, I, W) if (pieces <= (N) * (I)) { \
+        if (bf16) hipLaunchKernelGGL((distill_both_kernel<true, N, I, W>), rows, dim3(N), distill_lds(a.slots), s, a); \
+        else hipLaunchKernelGGL((distill_both_kernel<false, N, I, W>), rows, dim3(N), distill_lds(a.slots), s, a); \
+        return true; }
+    LPMM_BOTH(64, 4, 8)
+    LPMM_BOTH(64, 8, 4)
+    LPMM_BOTH(256, 4, 8)
+    LPMM_BOTH(256, 8, 4)
+    LPMM_BOTH(256, 16, 3)
+    // 50257 bf16 logits: 4096 rows 205 us with 256 threads, 225 with 512; 300 rows, which do not fill the GPU, 22 and 19
+    if (a.t >= 1024) LPMM_BOTH(256, 25, 3)
+    LPMM_BOTH(512, 13, 4)
+    LPMM_BOTH(512, 16, 4)
+    LPMM_BOTH(1024, 13, 4)
+    LPMM_BOTH(1024, 16, 4)
+#undef LPMM_BOTH
+    return false;
 }
 
 // Splits of a reduction over `steps` pieces for a launch of `blocks` workgroups: as many as bring it to `want` of them.
@@ -317,8 +374,9 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
 }
 
 size_t lpmm_distill_workspace_bytes(int64_t t, int64_t v) {
-    (void)t; (void)v;
-    return 0;
+    if (t < 1 || t > kMaxTokens || v < 1 || v > kMaxVocabulary) return 0;
+    const int spans = std::max(distill_spans(t, v, 2), distill_spans(t, v, 4));
+    return spans > 1 ? size_t(t) * spans * sizeof(float2) : 0;
 }
 
 int lpmm_distill_loss(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
@@ -329,10 +387,10 @@ int lpmm_distill_loss(const void* z, int z_dtype, int64_t t, int64_t v, int64_t 
     if (t == 0) return LPMM_OK;
     LPMM_TRY(check_floats(loss));
     LPMM_TRY(check_floats(lse));
-    (void)workspace; (void)workspace_bytes;
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_distill_workspace_bytes(t, v)));
     a.loss = loss;
     a.lse = lse;
-    return launch_loss(a, z_dtype == LPMM_BF16, static_cast<hipStream_t>(stream));
+    return launch_loss(a, z_dtype == LPMM_BF16, workspace, static_cast<hipStream_t>(stream));
 }
 
 int lpmm_distill_grad(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
@@ -363,7 +421,7 @@ int lpmm_distill_loss_grad(const void* z, int z_dtype, int64_t t, int64_t v, int
     LPMM_TRY(check_floats(loss));
     LPMM_TRY(check_floats(lse));
     LPMM_TRY(check_floats(grad));
-    (void)workspace; (void)workspace_bytes;
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_distill_workspace_bytes(t, v)));
     a.loss = loss;
     a.lse = lse;
     a.grad = grad;
@@ -371,7 +429,11 @@ int lpmm_distill_loss_grad(const void* z, int z_dtype, int64_t t, int64_t v, int
     a.dz_stride = dz_stride;
     const bool bf16 = z_dtype == LPMM_BF16;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    LPMM_TRY(launch_loss(a, bf16, s));
+    if (launch_both(a, bf16, s)) {
+        LPMM_HIP(hipGetLastError());
+        return LPMM_OK;
+    }
+    LPMM_TRY(launch_loss(a, bf16, workspace, s));
     return launch_grad(a, bf16, s);
 }
 
