@@ -248,6 +248,19 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int esize = elem_size(dtype);
+    // 16-byte boundaries, whole runs, offsets within a tile below 2^31
+    const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22);
+    if (t > 64 && direct) {
+        const int64_t n_tiles = div_up(m.n, 128), t_tiles = div_up(t, 128);
+        const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
+        if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+#define LPMM_DIRECT(G) hipLaunchKernelGGL((w4_linear_direct_kernel<G, 2, 2, 2, 2>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, \
+                                          int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
+        if (group == 32) LPMM_DIRECT(32); else if (group == 64) LPMM_DIRECT(64); else LPMM_DIRECT(128);
+#undef LPMM_DIRECT
+        LPMM_HIP(hipGetLastError());
+        return LPMM_OK;
+    }
     if (t > 64) {
         const int bt = dtype == LPMM_BF16 ? 128 : 64;
         const int64_t n_tiles = div_up(m.n, 256), t_tiles = div_up(t, bt);

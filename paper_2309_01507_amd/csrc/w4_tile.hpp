@@ -218,6 +218,141 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
         }
 }
 
+// ---- straight from memory into LDS -------------------------------------------------------------------------------------------------
+
+// 16 bytes a lane from `from` to lane * 16 bytes behind `to` (the same in all lanes of the wave)
+__device__ __forceinline__ void load_to_lds(const void* from, uint4* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from),
+                                     (__attribute__((address_space(3))) uint32_t*)(to), 16, 0, 0);
+}
+
+// ROWS rows of 2^LOG octets of bf16, staged by WAVES waves a KiB at a time.  A lane's octet of a row is the one that lds_piece puts at
+// the lane's place, so the swizzle costs nothing.  Rows beyond the matrix repeat its last one.  Offsets fit 32 bits (the launch sees to it).
+template <int ROWS, int LOG, int WAVES>
+struct StageDirect {
+    static constexpr int kPieces = ROWS << LOG, kOwn = kPieces / 64 / WAVES, kRowsAtOnce = 64 >> LOG;
+    static_assert(kPieces % (64 * WAVES) == 0, "whole KiB per wave");
+    uint32_t off[kOwn];                                        // bytes from the first row's first octet
+    __device__ __forceinline__ void setup(int64_t stride, int row0, int rows) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+            const int r = (j * WAVES + wave) * kRowsAtOnce + (lane >> LOG);
+            const int o = lds_piece<LOG>(r, lane & ((1 << LOG) - 1)) - (r << LOG);      // an involution
+            off[j] = uint32_t(min(r, rows - 1 - row0)) * uint32_t(stride * 2) + o * 16;
+        }
+    }
+    // from: the first row's first octet
+    __device__ __forceinline__ void load(const char* from, uint4* lds) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) load_to_lds(from + off[j], lds + (j * WAVES + wave) * 64);
+    }
+};
+
+// 0 in registers that the compiler does not know to be 0: the C operand of a sum's first product, which saves clearing the sum
+__device__ __forceinline__ f32x16 opaque_zero() {
+    f32x16 z = {};
+    asm volatile("" : "+v"(z));
+    return z;
+}
+
+// The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Two workgroups of 4 waves share a CU, so that one computes
+// while the other waits at its barrier.
+template <int GROUP, int WN, int WT, int NT, int TT>
+__global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
+                                                                        int64_t y_stride, int n_tiles, int t_tiles) {
+    constexpr int BN = WN * NT * 32, BT = WT * TT * 32, GROUPS = kW4Chunk / GROUP;
+    typedef StageDirect<BT, 4, WN * WT> StageX;
+    __shared__ uint4 s_x0[StageX::kPieces];
+    __shared__ uint4 s_x1[StageX::kPieces];                    // two objects: what is loaded into one is no reason to wait for reads of the other
+    int n_tile, t_tile;
+    if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int n0 = n_tile * BN + (wave % WN) * NT * 32, t0 = t_tile * BT, tw = (wave / WN) * TT * 32;
+    const uint32_t* codes[NT];
+    const float* scales[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+        const int n = min(n0 + b * 32 + col, m.n - 1);
+        codes[b] = m.codes + int64_t(n) * m.words + half * 4;
+        scales[b] = m.scales + int64_t(n) * m.groups;
+    }
+    uint4 q[NT][2];
+    float sc[NT][GROUPS];
+    auto load_w = [&](int run) {
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            q[b][0] = *reinterpret_cast<const uint4*>(codes[b] + run * 16);
+            q[b][1] = *reinterpret_cast<const uint4*>(codes[b] + run * 16 + 8);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][run * GROUPS + g];
+        }
+    };
+    f32x16 acc[TT][NT] = {};
+    const f32x16 zero = opaque_zero();
+    StageX stage;
+    stage.setup(x_stride, t0, t);
+    const char* from = static_cast<const char*>(x) + int64_t(t0) * x_stride * 2;
+    const int runs = m.words / 16;
+    auto step = [&](int run, const uint4* now, uint4* next) {
+        uint32_t w[NT][8];
+        float s_now[NT][GROUPS];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            w[b][0] = q[b][0].x; w[b][1] = q[b][1].x; w[b][2] = q[b][0].y; w[b][3] = q[b][1].y;
+            w[b][4] = q[b][0].z; w[b][5] = q[b][1].z; w[b][6] = q[b][0].w; w[b][7] = q[b][1].w;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) s_now[b][g] = sc[b][g];
+        }
+        if (run + 1 < runs) {
+            stage.load(from + (run + 1) * (kW4Chunk * 2), next);
+            load_w(run + 1);
+        }
+        f32x16 part[TT][NT];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            bf16x8 bw[NT];
+#pragma unroll
+            for (int b = 0; b < NT; ++b) bw[b] = w4_codes_bf16(w[b][s]);
+#pragma unroll
+            for (int a = 0; a < TT; ++a) {
+                const bf16x8 ax = as_operand(now[lds_piece<4>(tw + a * 32 + col, 2 * s + half)]);
+#pragma unroll
+                for (int b = 0; b < NT; ++b) part[a][b] = mfma32(ax, bw[b], s * 16 % GROUP == 0 ? zero : part[a][b]);
+            }
+            if ((s + 1) * 16 % GROUP == 0) {
+#pragma unroll
+                for (int a = 0; a < TT; ++a)
+#pragma unroll
+                    for (int b = 0; b < NT; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[a][b][i] = __builtin_fmaf(s_now[b][s * 16 / GROUP], part[a][b][i], acc[a][b][i]);
+            }
+        }
+        __syncthreads();
+    };
+    stage.load(from, s_x0);
+    load_w(0);
+    __syncthreads();
+    for (int run = 0; run < runs; run += 2) {
+        step(run, s_x0, s_x1);
+        if (run + 1 < runs) step(run + 1, s_x1, s_x0);
+    }
+#pragma unroll
+    for (int a = 0; a < TT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            const int n = n0 + b * 32 + col;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int tok = t0 + tw + a * 32 + mfma32_row(i, half);
+                if (n < m.n && tok < t) w4_store1<true>(y, int64_t(tok) * y_stride + n, acc[a][b][i]);
+            }
+        }
+}
+
 // ---- gradient of the scales ---------------------------------------------------------------------------------------------------------
 //
 // dscales[n][g] = sum_t dy[t][n] P[t][n][g] with P the product's sum over the group before its scale: the same matrix products, and no
