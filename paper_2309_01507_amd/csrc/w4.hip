@@ -249,7 +249,7 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int esize = elem_size(dtype);
     // 16-byte boundaries, whole runs, offsets within a tile below 2^31
-    const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22);
+    const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22) && m.k < (1 << 22);
     if (t > 64 && direct) {
         const int64_t n_tiles = div_up(m.n, 128), t_tiles = div_up(t, 128);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;

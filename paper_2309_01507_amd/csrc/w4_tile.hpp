@@ -28,12 +28,11 @@ __device__ __forceinline__ bool tile_of(int id, int rows, int cols, int& row, in
     return true;
 }
 
-// 16-byte pieces in LDS: piece o of row r of an array with 2^LOG pieces a row stands at o ^ (r, or r / 2 for rows of 8 pieces), so that
-// lanes that read the same piece of consecutive rows hit different banks.
+// 16-byte pieces in LDS: piece o of row r of an array with 2^LOG pieces a row stands at o ^ (r divided by the rows that make 256 bytes), so
+// that lanes that read the same piece of 16 consecutive rows hit all banks.
 template <int LOG>
 __device__ __forceinline__ int lds_piece(int r, int o) {
-    constexpr int mask = (1 << LOG) - 1;
-    return (r << LOG) + (o ^ ((LOG <= 3 ? r >> 1 : r) & mask));
+    return (r << LOG) + (o ^ ((r >> (LOG < 4 ? 4 - LOG : 0)) & ((1 << LOG) - 1)));
 }
 
 // ---- staging: octets of rows, from global memory into registers and from there into LDS ------------------------------------------
@@ -233,13 +232,14 @@ struct StageDirect {
     static constexpr int kPieces = ROWS << LOG, kOwn = kPieces / 64 / WAVES, kRowsAtOnce = 64 >> LOG;
     static_assert(kPieces % (64 * WAVES) == 0, "whole KiB per wave");
     uint32_t off[kOwn];                                        // bytes from the first row's first octet
+    // stride: bytes
     __device__ __forceinline__ void setup(int64_t stride, int row0, int rows) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
             const int r = (j * WAVES + wave) * kRowsAtOnce + (lane >> LOG);
             const int o = lds_piece<LOG>(r, lane & ((1 << LOG) - 1)) - (r << LOG);      // an involution
-            off[j] = uint32_t(min(r, rows - 1 - row0)) * uint32_t(stride * 2) + o * 16;
+            off[j] = uint32_t(min(r, rows - 1 - row0)) * uint32_t(stride) + o * 16;
         }
     }
     // from: the first row's first octet
@@ -257,94 +257,113 @@ __device__ __forceinline__ f32x16 opaque_zero() {
     return z;
 }
 
-// The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Two workgroups of 4 waves share a CU, so that one computes
-// while the other waits at its barrier.
+// The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Tokens and codes are loaded straight into LDS, a run ahead:
+// codes that each wave loaded for itself came in pieces of 32 bytes a row, twice, and a scale a line.  A lane loads the scales of four groups
+// at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at its barrier.
 template <int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                         int64_t y_stride, int n_tiles, int t_tiles) {
-    constexpr int BN = WN * NT * 32, BT = WT * TT * 32, GROUPS = kW4Chunk / GROUP;
-    typedef StageDirect<BT, 4, WN * WT> StageX;
+    constexpr int BN = WN * NT * 32, BT = WT * TT * 32, GROUPS = kW4Chunk / GROUP, WAVES = WN * WT;
+    constexpr int QUAD = GROUP / 32;                           // runs that four groups make
+    typedef StageDirect<BT, 4, WAVES> StageX;
+    typedef StageDirect<BN, 2, WAVES> StageW;
     __shared__ uint4 s_x0[StageX::kPieces];
-    __shared__ uint4 s_x1[StageX::kPieces];                    // two objects: what is loaded into one is no reason to wait for reads of the other
+    __shared__ uint4 s_x1[StageX::kPieces];                    // objects of their own: what is loaded into one is no reason to wait in front
+    __shared__ uint4 s_w0[StageW::kPieces];                    // of reading another
+    __shared__ uint4 s_w1[StageW::kPieces];
     int n_tile, t_tile;
     if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
-    const int n0 = n_tile * BN + (wave % WN) * NT * 32, t0 = t_tile * BT, tw = (wave / WN) * TT * 32;
-    const uint32_t* codes[NT];
+    const int n0 = n_tile * BN, nw = (wave % WN) * NT * 32, t0 = t_tile * BT, tw = (wave / WN) * TT * 32;
     const float* scales[NT];
 #pragma unroll
-    for (int b = 0; b < NT; ++b) {
-        const int n = min(n0 + b * 32 + col, m.n - 1);
-        codes[b] = m.codes + int64_t(n) * m.words + half * 4;
-        scales[b] = m.scales + int64_t(n) * m.groups;
-    }
-    uint4 q[NT][2];
-    float sc[NT][GROUPS];
-    auto load_w = [&](int run) {
+    for (int b = 0; b < NT; ++b) scales[b] = m.scales + int64_t(min(n0 + nw + b * 32 + col, m.n - 1)) * m.groups;
+    float sc[NT][4], sc_next[NT][4];
+    auto load_scales = [&](int g) {
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
-            q[b][0] = *reinterpret_cast<const uint4*>(codes[b] + run * 16);
-            q[b][1] = *reinterpret_cast<const uint4*>(codes[b] + run * 16 + 8);
+            if (g + 4 <= m.groups) {
+                const Vec16f v = *reinterpret_cast<const Vec16f*>(scales[b] + g);
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][run * GROUPS + g];
+                for (int i = 0; i < 4; ++i) sc_next[b][i] = v.v[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc_next[b][i] = g + i < m.groups ? scales[b][g + i] : 0.0f;
+            }
         }
     };
     f32x16 acc[TT][NT] = {};
     const f32x16 zero = opaque_zero();
-    StageX stage;
-    stage.setup(x_stride, t0, t);
-    const char* from = static_cast<const char*>(x) + int64_t(t0) * x_stride * 2;
+    StageX stage_x;
+    StageW stage_w;
+    stage_x.setup(x_stride * 2, t0, t);
+    stage_w.setup(int64_t(m.words) * 4, n0, m.n);
+    const char* from_x = static_cast<const char*>(x) + int64_t(t0) * x_stride * 2;
+    const char* from_w = reinterpret_cast<const char*>(m.codes) + int64_t(n0) * m.words * 4;
     const int runs = m.words / 16;
-    auto step = [&](int run, const uint4* now, uint4* next) {
-        uint32_t w[NT][8];
-        float s_now[NT][GROUPS];
+    auto step = [&](int run, const uint4* now_x, const uint4* now_w, uint4* next_x, uint4* next_w) {
+        if (run % QUAD == 0) {
 #pragma unroll
-        for (int b = 0; b < NT; ++b) {
-            w[b][0] = q[b][0].x; w[b][1] = q[b][1].x; w[b][2] = q[b][0].y; w[b][3] = q[b][1].y;
-            w[b][4] = q[b][0].z; w[b][5] = q[b][1].z; w[b][6] = q[b][0].w; w[b][7] = q[b][1].w;
+            for (int b = 0; b < NT; ++b)
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) s_now[b][g] = sc[b][g];
+                for (int i = 0; i < 4; ++i) sc[b][i] = sc_next[b][i];
         }
         if (run + 1 < runs) {
-            stage.load(from + (run + 1) * (kW4Chunk * 2), next);
-            load_w(run + 1);
+            stage_x.load(from_x + (run + 1) * (kW4Chunk * 2), next_x);
+            stage_w.load(from_w + (run + 1) * (kW4Chunk / 2), next_w);
+            if ((run + 1) % QUAD == 0) load_scales((run + 1) * GROUPS);
+        }
+        uint4 q[NT][2];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            q[b][0] = now_w[lds_piece<2>(nw + b * 32 + col, half)];
+            q[b][1] = now_w[lds_piece<2>(nw + b * 32 + col, half + 2)];
         }
         f32x16 part[TT][NT];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             bf16x8 bw[NT];
 #pragma unroll
-            for (int b = 0; b < NT; ++b) bw[b] = w4_codes_bf16(w[b][s]);
+            for (int b = 0; b < NT; ++b) {
+                const uint4 v = q[b][s & 1];                   // logical word 2 s + half
+                bw[b] = w4_codes_bf16(s < 2 ? v.x : s < 4 ? v.y : s < 6 ? v.z : v.w);
+            }
 #pragma unroll
             for (int a = 0; a < TT; ++a) {
-                const bf16x8 ax = as_operand(now[lds_piece<4>(tw + a * 32 + col, 2 * s + half)]);
+                const bf16x8 ax = as_operand(now_x[lds_piece<4>(tw + a * 32 + col, 2 * s + half)]);
 #pragma unroll
                 for (int b = 0; b < NT; ++b) part[a][b] = mfma32(ax, bw[b], s * 16 % GROUP == 0 ? zero : part[a][b]);
             }
             if ((s + 1) * 16 % GROUP == 0) {
+                const int at = run % QUAD * GROUPS;            // of the four
 #pragma unroll
-                for (int a = 0; a < TT; ++a)
+                for (int b = 0; b < NT; ++b) {
+                    const int g = s * 16 / GROUP;
+                    float scale = sc[b][g];
 #pragma unroll
-                    for (int b = 0; b < NT; ++b)
+                    for (int i = GROUPS; i + g < 4; i += GROUPS) scale = at == i ? sc[b][i + g] : scale;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            acc[a][b][i] = __builtin_fmaf(s_now[b][s * 16 / GROUP], part[a][b][i], acc[a][b][i]);
+                    for (int a = 0; a < TT; ++a)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[a][b][i] = __builtin_fmaf(scale, part[a][b][i], acc[a][b][i]);
+                }
             }
         }
         __syncthreads();
     };
-    stage.load(from, s_x0);
-    load_w(0);
+    stage_x.load(from_x, s_x0);
+    stage_w.load(from_w, s_w0);
+    load_scales(0);
     __syncthreads();
     for (int run = 0; run < runs; run += 2) {
-        step(run, s_x0, s_x1);
-        if (run + 1 < runs) step(run + 1, s_x1, s_x0);
+        step(run, s_x0, s_w0, s_x1, s_w1);
+        if (run + 1 < runs) step(run + 1, s_x1, s_w1, s_x0, s_w0);
     }
 #pragma unroll
     for (int a = 0; a < TT; ++a)
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
-            const int n = n0 + b * 32 + col;
+            const int n = n0 + nw + b * 32 + col;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int tok = t0 + tw + a * 32 + mfma32_row(i, half);
