@@ -9,6 +9,7 @@
 namespace lpmm {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));      // 16 bytes at the alignment of a float
 
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -219,34 +220,55 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
 
 // ---- straight from memory into LDS -------------------------------------------------------------------------------------------------
 
-// 16 bytes a lane from `from` to lane * 16 bytes behind `to` (the same in all lanes of the wave)
-__device__ __forceinline__ void load_to_lds(const void* from, uint4* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from),
-                                     (__attribute__((address_space(3))) uint32_t*)(to), 16, 0, 0);
-}
+// Loads go through a buffer descriptor: the lane's part of an address is a 32-bit offset that stays, what moves is a scalar, and what lies
+// beyond the end arrives as 0.  Offsets are below 2^31 (the launch sees to it).
+struct Buffer {
+    const void* start;
+    int bytes;
+    __device__ __forceinline__ void set(const void* p, int64_t length) {
+        start = p;
+        bytes = int(length < 0x7FFFFFFF ? length : 0x7FFFFFFF);
+    }
+    // 16 (or 4) bytes a lane from lane offset `off` + `at` to lane * 16 (4) bytes behind `to`, which is the same in all lanes.  The
+    // descriptor's type exists in device code only.
+    __device__ __forceinline__ void to_lds16(uint32_t off, int at, void* to) const {
+#ifdef __HIP_DEVICE_COMPILE__
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(start), 0, bytes, 0x00020000),
+                                                 (__attribute__((address_space(3))) void*)(to), 16, off, at, 0, 0);
+#endif
+    }
+    __device__ __forceinline__ void to_lds4(uint32_t off, int at, void* to) const {
+#ifdef __HIP_DEVICE_COMPILE__
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(start), 0, bytes, 0x00020000),
+                                                 (__attribute__((address_space(3))) void*)(to), 4, off, at, 0, 0);
+#endif
+    }
+};
 
-// ROWS rows of 2^LOG octets of bf16, staged by WAVES waves a KiB at a time.  A lane's octet of a row is the one that lds_piece puts at
-// the lane's place, so the swizzle costs nothing.  Rows beyond the matrix repeat its last one.  Offsets fit 32 bits (the launch sees to it).
+// ROWS rows of 2^LOG octets of bf16 (16 bytes), staged by WAVES waves a KiB at a time.  A lane's octet of a row is the one that lds_piece
+// puts at the lane's place, so the swizzle costs nothing.
 template <int ROWS, int LOG, int WAVES>
 struct StageDirect {
     static constexpr int kPieces = ROWS << LOG, kOwn = kPieces / 64 / WAVES, kRowsAtOnce = 64 >> LOG;
     static_assert(kPieces % (64 * WAVES) == 0, "whole KiB per wave");
-    uint32_t off[kOwn];                                        // bytes from the first row's first octet
-    // stride: bytes
-    __device__ __forceinline__ void setup(int64_t stride, int row0, int rows) {
+    Buffer buffer;
+    uint32_t off[kOwn];                                        // bytes
+    // stride: bytes from one row to the next; rows: of the matrix from `first` on; those beyond arrive as 0
+    __device__ __forceinline__ void setup(const void* first, int64_t stride, int64_t rows) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        buffer.set(first, rows < ROWS ? rows * stride : ROWS * stride);
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
             const int r = (j * WAVES + wave) * kRowsAtOnce + (lane >> LOG);
-            const int o = lds_piece<LOG>(r, lane & ((1 << LOG) - 1)) - (r << LOG);      // an involution
-            off[j] = uint32_t(min(r, rows - 1 - row0)) * uint32_t(stride) + o * 16;
+            off[j] = uint32_t(r) * uint32_t(stride) + (lds_piece<LOG>(r, lane & ((1 << LOG) - 1)) - (r << LOG)) * 16;    // an involution
         }
     }
-    // from: the first row's first octet
-    __device__ __forceinline__ void load(const char* from, uint4* lds) const {
+    // at: bytes from a row's start
+    __device__ __forceinline__ void load(int at, uint4* lds) const {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) load_to_lds(from + off[j], lds + (j * WAVES + wave) * 64);
+        for (int j = 0; j < kOwn; ++j)
+            buffer.to_lds16(off[j], at, lds + (j * WAVES + wave) * 64);
     }
 };
 
@@ -257,9 +279,9 @@ __device__ __forceinline__ f32x16 opaque_zero() {
     return z;
 }
 
-// The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Tokens and codes are loaded straight into LDS, a run ahead:
-// codes that each wave loaded for itself came in pieces of 32 bytes a row, twice, and a scale a line.  A lane loads the scales of four groups
-// at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at its barrier.
+// The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Tokens and codes are loaded straight into LDS, a run ahead;
+// a lane loads the scales of four groups at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at its
+// barrier.
 template <int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                         int64_t y_stride, int n_tiles, int t_tiles) {
@@ -267,50 +289,44 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
     constexpr int QUAD = GROUP / 32;                           // runs that four groups make
     typedef StageDirect<BT, 4, WAVES> StageX;
     typedef StageDirect<BN, 2, WAVES> StageW;
-    __shared__ uint4 s_x0[StageX::kPieces];
-    __shared__ uint4 s_x1[StageX::kPieces];                    // objects of their own: what is loaded into one is no reason to wait in front
-    __shared__ uint4 s_w0[StageW::kPieces];                    // of reading another
-    __shared__ uint4 s_w1[StageW::kPieces];
+    __shared__ uint4 s_x0[StageX::kPieces], s_x1[StageX::kPieces];       // objects of their own: what is loaded into one is no reason to wait in
+    __shared__ uint4 s_w0[StageW::kPieces], s_w1[StageW::kPieces];       // front of reading another
     int n_tile, t_tile;
     if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const int n0 = n_tile * BN, nw = (wave % WN) * NT * 32, t0 = t_tile * BT, tw = (wave / WN) * TT * 32;
+    StageX stage_x;
+    StageW stage_w;
+    stage_x.setup(static_cast<const char*>(x) + int64_t(t0) * x_stride * 2, x_stride * 2, t - t0);
+    stage_w.setup(m.codes + int64_t(n0) * m.words, int64_t(m.words) * 4, m.n - n0);
     const float* scales[NT];
 #pragma unroll
     for (int b = 0; b < NT; ++b) scales[b] = m.scales + int64_t(min(n0 + nw + b * 32 + col, m.n - 1)) * m.groups;
-    float sc[NT][4], sc_next[NT][4];
+    f32x4 sc[NT], sc_next[NT];
     auto load_scales = [&](int g) {
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
             if (g + 4 <= m.groups) {
-                const Vec16f v = *reinterpret_cast<const Vec16f*>(scales[b] + g);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sc_next[b][i] = v.v[i];
+                sc_next[b] = *reinterpret_cast<const f32x4u*>(scales[b] + g);
             } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sc_next[b][i] = g + i < m.groups ? scales[b][g + i] : 0.0f;
+                sc_next[b].x = scales[b][g];
+                sc_next[b].y = g + 1 < m.groups ? scales[b][g + 1] : 0.0f;
+                sc_next[b].z = g + 2 < m.groups ? scales[b][g + 2] : 0.0f;
+                sc_next[b].w = 0.0f;
             }
         }
     };
     f32x16 acc[TT][NT] = {};
     const f32x16 zero = opaque_zero();
-    StageX stage_x;
-    StageW stage_w;
-    stage_x.setup(x_stride * 2, t0, t);
-    stage_w.setup(int64_t(m.words) * 4, n0, m.n);
-    const char* from_x = static_cast<const char*>(x) + int64_t(t0) * x_stride * 2;
-    const char* from_w = reinterpret_cast<const char*>(m.codes) + int64_t(n0) * m.words * 4;
     const int runs = m.words / 16;
-    auto step = [&](int run, const uint4* now_x, const uint4* now_w, uint4* next_x, uint4* next_w) {
+    auto step = [&](bool more, int run, const uint4* now_x, const uint4* now_w, uint4* next_x, uint4* next_w) {
         if (run % QUAD == 0) {
 #pragma unroll
-            for (int b = 0; b < NT; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sc[b][i] = sc_next[b][i];
+            for (int b = 0; b < NT; ++b) sc[b] = sc_next[b];
         }
-        if (run + 1 < runs) {
-            stage_x.load(from_x + (run + 1) * (kW4Chunk * 2), next_x);
-            stage_w.load(from_w + (run + 1) * (kW4Chunk / 2), next_w);
+        if (more) {
+            stage_x.load((run + 1) * (kW4Chunk * 2), next_x);
+            stage_w.load((run + 1) * (kW4Chunk / 2), next_w);
             if ((run + 1) % QUAD == 0) load_scales((run + 1) * GROUPS);
         }
         uint4 q[NT][2];
@@ -335,30 +351,34 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
                 for (int b = 0; b < NT; ++b) part[a][b] = mfma32(ax, bw[b], s * 16 % GROUP == 0 ? zero : part[a][b]);
             }
             if ((s + 1) * 16 % GROUP == 0) {
-                const int at = run % QUAD * GROUPS;            // of the four
+                const int at = run % QUAD * GROUPS + s * 16 / GROUP;     // of the four; the same in all lanes
 #pragma unroll
                 for (int b = 0; b < NT; ++b) {
-                    const int g = s * 16 / GROUP;
-                    float scale = sc[b][g];
-#pragma unroll
-                    for (int i = GROUPS; i + g < 4; i += GROUPS) scale = at == i ? sc[b][i + g] : scale;
+                    const float scale = at < 2 ? (at < 1 ? sc[b].x : sc[b].y) : (at < 3 ? sc[b].z : sc[b].w);
 #pragma unroll
                     for (int a = 0; a < TT; ++a)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[a][b][i] = __builtin_fmaf(scale, part[a][b][i], acc[a][b][i]);
+                        for (int i = 0; i < 16; ++i) {
+                            float sum = __builtin_fmaf(scale, part[a][b][i], acc[a][b][i]);
+                            if (GROUPS > 1) asm volatile("" : "+v"(sum));      // here: further down the sums of all groups would be held
+                            acc[a][b][i] = sum;
+                        }
                 }
             }
         }
         __syncthreads();
     };
-    stage_x.load(from_x, s_x0);
-    stage_w.load(from_w, s_w0);
+    stage_x.load(0, s_x0);
+    stage_w.load(0, s_w0);
     load_scales(0);
     __syncthreads();
-    for (int run = 0; run < runs; run += 2) {
-        step(run, s_x0, s_w0, s_x1, s_w1);
-        if (run + 1 < runs) step(run + 1, s_x1, s_w1, s_x0, s_w0);
+    int run = 0;
+    for (; run + 2 < runs; run += 2) {
+        step(true, run, s_x0, s_w0, s_x1, s_w1);
+        step(true, run + 1, s_x1, s_w1, s_x0, s_w0);
     }
+    step(run + 1 < runs, run, s_x0, s_w0, s_x1, s_w1);
+    if (run + 1 < runs) step(false, run + 1, s_x1, s_w1, s_x0, s_w0);
 #pragma unroll
     for (int a = 0; a < TT; ++a)
 #pragma unroll
