@@ -627,37 +627,71 @@ class WeightsW4:
     scales: "object"
 
 
-def _w4_check(w: WeightsW4, what: str) -> None:
-    if (w.codes.numel() != w.rows * ((w.cols + 127) // 128 * 64) or not w.codes.is_contiguous() or
-            w.scales.shape != (w.rows, -(-w.cols // w.group)) or not w.scales.is_contiguous()):
-        raise ValueError(f"{what}: codes or scales are not those of a {w.rows} x {w.cols} matrix with groups of {w.group}")
+def _load_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _w4_check(w: WeightsW4, what: str):
+    codes, scales, rows, cols = w.codes, w.scales, w.rows, w.cols
+    if (codes.numel() != rows * ((cols + 127) // 128 * 64) or scales.shape != (rows, -(-cols // w.group)) or
+            not codes.is_contiguous() or not scales.is_contiguous()):
+        raise ValueError(f"{what}: codes or scales are not those of a {rows} x {cols} matrix with groups of {w.group}")
+    return codes, scales
 
 
 def _rows(t, cols: int, what: str):
     """(pointer, type, rows, elements from one row to the next) of a matrix argument"""
-    import torch
-    dtype = BF16 if t.dtype == torch.bfloat16 else F32 if t.dtype == torch.float32 else None
-    if dtype is None:
+    torch = _torch or _load_torch()
+    dtype = t.dtype
+    if dtype is torch.bfloat16:
+        dtype = BF16
+    elif dtype is torch.float32:
+        dtype = F32
+    else:
         raise ValueError(f"{what} must be float32 or bfloat16")
-    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what} must have {cols} columns, next to each other")
-    n = t.shape[0]
-    stride = t.stride(0) if n > 1 else cols
-    if stride < cols:
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != cols:
+        raise ValueError(f"{what} must have {cols} columns")
+    n = shape[0]
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{what}: a row's elements must be next to each other")
+    if n <= 1:
+        ld = cols
+    elif ld < cols:
         raise ValueError(f"{what}: rows overlap")
-    return t.data_ptr(), dtype, n, stride
+    return t.data_ptr(), dtype, n, ld
 
 
 def _on_current(what: str, *tensors) -> None:
-    import torch
-    here = torch.cuda.current_device() if any(t.is_cuda for t in tensors) else None
-    if any(not t.is_cuda or t.device.index != here for t in tensors):
+    here = tensors[0].get_device()
+    if here < 0 or here != (_torch or _load_torch())._C._cuda_getDevice():
         raise ValueError(f"{what}: all tensors must be on the current GPU")
+    for t in tensors:
+        if t.get_device() != here:
+            raise ValueError(f"{what}: all tensors must be on the current GPU")
+
+
+def _matrix_out(out, like, rows: int, cols: int, stream, what: str):
+    """(tensor, pointer, elements from one row to the next) of the caller's output, or of one allocated on torch's current stream"""
+    if out is None:
+        if stream is not None:
+            raise ValueError(f"{what}: a call on a stream of its own needs its outputs (and workspace) given")
+        out = like.new_empty((rows, cols))
+        return out, out.data_ptr(), cols
+    if out.dtype != like.dtype or out.shape != (rows, cols):
+        raise ValueError(f"{what} must be {like.dtype} of shape {(rows, cols)}")
+    ptr, _, _, ld = _rows(out, cols, what)
+    return out, ptr, ld
 
 
 def _new(out, shape, dtype, device, stream, what: str):
     """The caller's output, or one allocated on torch's current stream."""
-    import torch
+    torch = _torch or _load_torch()
     if out is None:
         if stream is not None:
             raise ValueError(f"{what}: a call on a stream of its own needs its outputs (and workspace) given")
@@ -719,59 +753,61 @@ def lpmm_w4_dequant(w: WeightsW4, dtype=None, out=None, stream=None):
 
 def lpmm_w4_linear(x, w: WeightsW4, y=None, stream=None):
     """y = x W^T: x is tokens x cols (float32 or bfloat16), y tokens x rows of the same type."""
-    _w4_check(w, "lpmm_w4_linear")
+    codes, scales = _w4_check(w, "lpmm_w4_linear")
     ptr, dtype, t, ld = _rows(x, w.cols, "x")
-    y = _new(y, (t, w.rows), x.dtype, x.device, stream, "y")
-    yptr, _, _, yld = _rows(y, w.rows, "y")
-    _on_current("lpmm_w4_linear", x, w.codes, w.scales, y)
-    shape = _shape(w.rows, w.cols)
-    _check(lib().lpmm_w4_linear(ptr, dtype, t, ld, w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape), w.group,
-                                yptr, yld, _stream(stream)), "lpmm_w4_linear")
+    y, yptr, yld = _matrix_out(y, x, t, w.rows, stream, "y")
+    _on_current("lpmm_w4_linear", x, codes, scales, y)
+    shape = _SHAPE(w.rows, w.cols)
+    _check((_lib or lib()).lpmm_w4_linear(ptr, dtype, t, ld, codes.data_ptr(), scales.data_ptr(), ctypes.addressof(shape),
+                                          w.group, yptr, yld, _stream(stream)), "lpmm_w4_linear")
     return y
 
 
 def lpmm_w4_linear_dx(dy, w: WeightsW4, dx=None, workspace=None, stream=None):
     """dx = dy W: the gradient of lpmm_w4_linear with respect to x."""
-    _w4_check(w, "lpmm_w4_linear_dx")
+    codes, scales = _w4_check(w, "lpmm_w4_linear_dx")
     ptr, dtype, t, ld = _rows(dy, w.rows, "dy")
-    dx = _new(dx, (t, w.cols), dy.dtype, dy.device, stream, "dx")
-    xptr, _, _, xld = _rows(dx, w.cols, "dx")
-    _on_current("lpmm_w4_linear_dx", dy, w.codes, w.scales, dx)
-    shape = _shape(w.rows, w.cols)
-    need = lib().lpmm_w4_linear_dx_workspace_bytes(t, ctypes.addressof(shape), dtype)
-    workspace = _workspace(workspace, need, dy.device, stream, "lpmm_w4_linear_dx")
-    _check(lib().lpmm_w4_linear_dx(ptr, dtype, t, ld, w.codes.data_ptr(), w.scales.data_ptr(), ctypes.addressof(shape),
-                                   w.group, xptr, xld, _ptr(workspace), _room(workspace), _stream(stream)), "lpmm_w4_linear_dx")
+    dx, xptr, xld = _matrix_out(dx, dy, t, w.cols, stream, "dx")
+    _on_current("lpmm_w4_linear_dx", dy, codes, scales, dx)
+    shape = _SHAPE(w.rows, w.cols)
+    L = _lib or lib()
+    need = L.lpmm_w4_linear_dx_workspace_bytes(t, ctypes.addressof(shape), dtype)
+    workspace = _workspace(workspace, need, dy, stream, "lpmm_w4_linear_dx")
+    _check(L.lpmm_w4_linear_dx(ptr, dtype, t, ld, codes.data_ptr(), scales.data_ptr(), ctypes.addressof(shape), w.group,
+                               xptr, xld, _ptr(workspace), _room(workspace), _stream(stream)), "lpmm_w4_linear_dx")
     return dx
 
 
 def lpmm_w4_linear_dscale(x, dy, w: WeightsW4, dscales=None, workspace=None, stream=None):
     """The gradient of lpmm_w4_linear with respect to the scales, float32, shaped like them.  w.scales is not read."""
-    import torch
-    _w4_check(w, "lpmm_w4_linear_dscale")
+    torch = _torch or _load_torch()
+    codes, scales = _w4_check(w, "lpmm_w4_linear_dscale")
     xp, dtype, t, xld = _rows(x, w.cols, "x")
     dyp, dy_dtype, dy_t, dyld = _rows(dy, w.rows, "dy")
     if dy_dtype != dtype or dy_t != t:
         raise ValueError("lpmm_w4_linear_dscale: x and dy must have the same type and number of rows")
-    dscales = _new(dscales, w.scales.shape, torch.float32, x.device, stream, "dscales")
+    dscales = _new(dscales, scales.shape, torch.float32, x.device, stream, "dscales")
     if not dscales.is_contiguous():
         raise ValueError("dscales must be contiguous")
-    shape = _shape(w.rows, w.cols)
-    need = lib().lpmm_w4_linear_dscale_workspace_bytes(t, ctypes.addressof(shape), w.group)
-    workspace = _workspace(workspace, need, x.device, stream, "lpmm_w4_linear_dscale")
-    _on_current("lpmm_w4_linear_dscale", x, dy, w.codes, dscales)
-    _check(lib().lpmm_w4_linear_dscale(xp, dyp, dtype, t, xld, dyld, w.codes.data_ptr(), ctypes.addressof(shape), w.group,
-                                       dscales.data_ptr(), _ptr(workspace), _room(workspace), _stream(stream)),
+    _on_current("lpmm_w4_linear_dscale", x, dy, codes, dscales)
+    shape = _SHAPE(w.rows, w.cols)
+    L = _lib or lib()
+    need = L.lpmm_w4_linear_dscale_workspace_bytes(t, ctypes.addressof(shape), w.group)
+    workspace = _workspace(workspace, need, x, stream, "lpmm_w4_linear_dscale")
+    _check(L.lpmm_w4_linear_dscale(xp, dyp, dtype, t, xld, dyld, codes.data_ptr(), ctypes.addressof(shape), w.group,
+                                   dscales.data_ptr(), _ptr(workspace), _room(workspace), _stream(stream)),
            "lpmm_w4_linear_dscale")
     return dscales
 
 
-def _workspace(workspace, need: int, device, stream, what: str):
-    import torch
-    if workspace is None and need:
-        if stream is not None:
-            raise ValueError(f"{what}: a call on a stream of its own needs a workspace of {need} bytes")
-        return torch.empty(need, dtype=torch.uint8, device=device)
+def _workspace(workspace, need: int, like, stream, what: str):
+    if workspace is None:
+        if need:
+            if stream is not None:
+                raise ValueError(f"{what}: a call on a stream of its own needs a workspace of {need} bytes")
+            return like.new_empty(need, dtype=_torch.uint8)
+    elif workspace.get_device() != like.get_device():
+        raise ValueError(f"{what}: the workspace must be on the current GPU")
     return workspace
 
 
@@ -785,35 +821,44 @@ DISTILL_MAX_SLOTS = 1024
 
 
 def _distill_args(z, top, index, tau, what: str):
-    import torch
+    torch = _torch or _load_torch()
     if z.dim() != 2:
         raise ValueError(f"{what}: logits must be tokens x vocabulary")
-    ptr, dtype, t, ld = _rows(z, z.shape[1], "logits")
-    if (top.dtype != torch.float32 or index.dtype != torch.int64 or top.dim() != 2 or top.shape != index.shape or
+    t, v = z.shape
+    ptr, dtype, _, ld = _rows(z, v, "logits")
+    if (top.dtype is not torch.float32 or index.dtype is not torch.int64 or top.dim() != 2 or top.shape != index.shape or
             top.shape[0] != t or not top.is_contiguous() or not index.is_contiguous()):
         raise ValueError(f"{what}: top (float32) and index (int64) must be contiguous, {t} x slots each")
-    return (ptr, dtype, t, z.shape[1], ld, top.data_ptr(), index.data_ptr(), top.shape[1], float(tau))
+    return (ptr, dtype, t, v, ld, top.data_ptr(), index.data_ptr(), top.shape[1], tau)
 
 
 def _per_row(x, t: int, name: str):
-    import torch
-    if x.dtype != torch.float32 or x.shape != (t,) or not x.is_contiguous():
+    if x.dtype is not _torch.float32 or x.shape != (t,) or not x.is_contiguous():
         raise ValueError(f"{name} must be float32, contiguous, one per row")
     return x.data_ptr()
+
+
+def _row_out(x, like, t: int, stream, name: str):
+    if x is None:
+        if stream is not None:
+            raise ValueError(f"{name}: a call on a stream of its own needs its outputs (and workspace) given")
+        x = like.new_empty(t, dtype=_torch.float32)
+        return x, x.data_ptr()
+    return x, _per_row(x, t, name)
 
 
 def lpmm_distill_loss(z, top, index, tau, loss=None, lse=None, workspace=None, stream=None):
     """(loss, lse), one per row of the student's logits z; top, index: the teacher's largest logits and their places, -1 in
     slots that do not count."""
-    import torch
     args = _distill_args(z, top, index, tau, "lpmm_distill_loss")
     t, v = z.shape
-    loss = _new(loss, (t,), torch.float32, z.device, stream, "loss")
-    lse = _new(lse, (t,), torch.float32, z.device, stream, "lse")
-    workspace = _workspace(workspace, lib().lpmm_distill_workspace_bytes(t, v), z.device, stream, "lpmm_distill_loss")
+    loss, loss_ptr = _row_out(loss, top, t, stream, "loss")
+    lse, lse_ptr = _row_out(lse, top, t, stream, "lse")
+    L = _lib or lib()
+    workspace = _workspace(workspace, L.lpmm_distill_workspace_bytes(t, v), z, stream, "lpmm_distill_loss")
     _on_current("lpmm_distill_loss", z, top, index, loss, lse)
-    _check(lib().lpmm_distill_loss(*args, _per_row(loss, t, "loss"), _per_row(lse, t, "lse"), _ptr(workspace),
-                                   _room(workspace), _stream(stream)), "lpmm_distill_loss")
+    _check(L.lpmm_distill_loss(*args, loss_ptr, lse_ptr, _ptr(workspace), _room(workspace), _stream(stream)),
+           "lpmm_distill_loss")
     return loss, lse
 
 
@@ -821,28 +866,25 @@ def lpmm_distill_grad(z, top, index, tau, lse, grad, dz=None, stream=None):
     """The loss's gradient with respect to z, from the gradient of each row's loss; dz may be z."""
     args = _distill_args(z, top, index, tau, "lpmm_distill_grad")
     t, v = z.shape
-    dz = _new(dz, (t, v), z.dtype, z.device, stream, "dz")
-    dptr, _, _, dld = _rows(dz, v, "dz")
+    dz, dptr, dld = _matrix_out(dz, z, t, v, stream, "dz")
     _on_current("lpmm_distill_grad", z, top, index, lse, grad, dz)
-    _check(lib().lpmm_distill_grad(*args, _per_row(lse, t, "lse"), _per_row(grad, t, "grad"), dptr, dld,
-                                   _stream(stream)), "lpmm_distill_grad")
+    _check((_lib or lib()).lpmm_distill_grad(*args, _per_row(lse, t, "lse"), _per_row(grad, t, "grad"), dptr, dld,
+                                             _stream(stream)), "lpmm_distill_grad")
     return dz
 
 
 def lpmm_distill_loss_grad(z, top, index, tau, grad, loss=None, lse=None, dz=None, workspace=None, stream=None):
     """(loss, dz) in one call, for a gradient of the rows' losses that is known beforehand; dz may be z."""
-    import torch
     args = _distill_args(z, top, index, tau, "lpmm_distill_loss_grad")
     t, v = z.shape
-    loss = _new(loss, (t,), torch.float32, z.device, stream, "loss")
-    lse = _new(lse, (t,), torch.float32, z.device, stream, "lse")
-    dz = _new(dz, (t, v), z.dtype, z.device, stream, "dz")
-    dptr, _, _, dld = _rows(dz, v, "dz")
-    workspace = _workspace(workspace, lib().lpmm_distill_workspace_bytes(t, v), z.device, stream, "lpmm_distill_loss_grad")
+    loss, loss_ptr = _row_out(loss, top, t, stream, "loss")
+    lse, lse_ptr = _row_out(lse, top, t, stream, "lse")
+    dz, dptr, dld = _matrix_out(dz, z, t, v, stream, "dz")
+    L = _lib or lib()
+    workspace = _workspace(workspace, L.lpmm_distill_workspace_bytes(t, v), z, stream, "lpmm_distill_loss_grad")
     _on_current("lpmm_distill_loss_grad", z, top, index, grad, loss, lse, dz)
-    _check(lib().lpmm_distill_loss_grad(*args, _per_row(grad, t, "grad"), _per_row(loss, t, "loss"),
-                                        _per_row(lse, t, "lse"), dptr, dld, _ptr(workspace), _room(workspace),
-                                        _stream(stream)), "lpmm_distill_loss_grad")
+    _check(L.lpmm_distill_loss_grad(*args, _per_row(grad, t, "grad"), loss_ptr, lse_ptr, dptr, dld, _ptr(workspace),
+                                    _room(workspace), _stream(stream)), "lpmm_distill_loss_grad")
     return loss, dz
 
 

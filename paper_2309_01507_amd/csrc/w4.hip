@@ -250,6 +250,17 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     const int esize = elem_size(dtype);
     // 16-byte boundaries, whole runs, offsets within a tile below 2^31
     const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22) && m.k < (1 << 22);
+    // Tiles of 64 x 64 with the runs split among a workgroup's waves while there are no more than two for each CU (4096 x 4096, us, with these and
+    // with tiles of 128 x 128: 64 tokens 14 and 32, 256 15 and 33, 512 27 and 36, 768 42 and 36)
+    if (t > 32 && direct && div_up(m.n, 64) * div_up(t, 64) <= 512) {
+        const int64_t n_tiles = div_up(m.n, 64), t_tiles = div_up(t, 64), blocks = div_up(n_tiles * t_tiles, 8) * 8;
+#define LPMM_SPLIT(G) hipLaunchKernelGGL((w4_linear_split_kernel<G, 2, 2>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, y, \
+                                         y_stride, int(n_tiles), int(t_tiles))
+        if (group == 32) LPMM_SPLIT(32); else if (group == 64) LPMM_SPLIT(64); else LPMM_SPLIT(128);
+#undef LPMM_SPLIT
+        LPMM_HIP(hipGetLastError());
+        return LPMM_OK;
+    }
     if (t > 64 && direct) {
         const int64_t n_tiles = div_up(m.n, 128), t_tiles = div_up(t, 128);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
@@ -277,19 +288,27 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
+    // 16, 32 or 64 tokens a workgroup; as many runs a wave as cover a row with 8 waves, up to what registers hold; 16 waves for longer rows
+    const int mt = t <= 16 ? 1 : t <= 32 || dtype == LPMM_F32 ? 2 : 4, runs = m.words / 16;
     constexpr int64_t kTokens = 16 * 32768;              // of a launch: grid.y
     for (int64_t at = 0; at < t; at += kTokens) {
         const int part = int(std::min(kTokens, t - at));
         const void* xp = static_cast<const char*>(x) + at * x_stride * esize;
         void* yp = static_cast<char*>(y) + at * y_stride * esize;
-        const dim3 grid(unsigned(div_up(m.n, 16)), unsigned(div_up(part, 16)));
-#define LPMM_LINEAR(B, G) hipLaunchKernelGGL((w4_linear_kernel<B, G, 4>), grid, dim3(256), 0, s, m, xp, part, x_stride, yp, y_stride)
+        const int64_t tiles = div_up(m.n, 16), groups_t = div_up(part, 16 * mt);
+#define LPMM_FEW(B, G, MT, W, A, S, E) hipLaunchKernelGGL((w4_linear_kernel<B, G, MT, W, A, S, E>), dim3(unsigned(std::min<int64_t>(tiles, 256 * 4 * S / W)), \
+                                                          unsigned(groups_t)), dim3(64 * W), 0, s, m, xp, part, x_stride, yp, y_stride)
+#define LPMM_FEW_G(B, MT, W, A, S, E) { if (group == 32) LPMM_FEW(B, 32, MT, W, A, S, E); else if (group == 64) LPMM_FEW(B, 64, MT, W, A, S, E); else LPMM_FEW(B, 128, MT, W, A, S, E); }
         if (dtype == LPMM_BF16) {
-            if (group == 32) LPMM_LINEAR(true, 32); else if (group == 64) LPMM_LINEAR(true, 64); else LPMM_LINEAR(true, 128);
+            if (mt == 1) { if (runs <= 8) LPMM_FEW_G(true, 1, 8, 1, 4, true) else if (runs <= 16) LPMM_FEW_G(true, 1, 8, 2, 4, true) else LPMM_FEW_G(true, 1, 16, 2, 4, true) }
+            else if (mt == 2) { if (runs <= 8) LPMM_FEW_G(true, 2, 8, 1, 4, true) else LPMM_FEW_G(true, 2, 16, 1, 4, true) }
+            else LPMM_FEW_G(true, 4, 8, 1, 2, true)
         } else {
-            if (group == 32) LPMM_LINEAR(false, 32); else if (group == 64) LPMM_LINEAR(false, 64); else LPMM_LINEAR(false, 128);
+            if (mt == 1) { if (runs <= 8) LPMM_FEW_G(false, 1, 8, 1, 4, true) else if (runs <= 16) LPMM_FEW_G(false, 1, 16, 1, 4, true) else { if (tiles >= 1024) LPMM_FEW_G(false, 1, 8, 4, 2, false) else LPMM_FEW_G(false, 1, 16, 1, 4, true) } }
+            else LPMM_FEW_G(false, 2, 8, 1, 2, true)
         }
-#undef LPMM_LINEAR
+#undef LPMM_FEW_G
+#undef LPMM_FEW
         LPMM_HIP(hipGetLastError());
     }
     return LPMM_OK;

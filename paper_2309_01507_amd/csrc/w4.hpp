@@ -188,16 +188,57 @@ __device__ __forceinline__ bf16x8 w4_codes_bf16(uint32_t word) {
     return u.v;
 }
 
-// A float as three bf16 numbers with that sum: the upper 8 bits of the significand, of what is left, and of what is left then (24
-// bits in all), cut off, not rounded, so that nothing overflows.  Infinities and NaN stand in the first, with nothing left.
-__device__ __forceinline__ void split3(float x, uint32_t out[3]) {
+// Floats as three bf16 numbers each with that sum, exactly: the value rounded to 8 bits of significand, what is left (at most 16 bits)
+// rounded to 8, and what is left then.  Two at a time, packed.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const bf16x2 p = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+    return __builtin_bit_cast(uint32_t, p);
+}
+__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ void split3_pair(float a, float b, uint32_t out[3]) {
+    out[0] = pack_bf16(a, b);
+    a -= low_bf16(out[0]);
+    b -= high_bf16(out[0]);
+    out[1] = pack_bf16(a, b);
+    out[2] = pack_bf16(a - low_bf16(out[1]), b - high_bf16(out[1]));
+}
+// The same where values may be too large to round up, infinite or NaN: cut off instead of rounded, nothing left of what is not finite
+__device__ __forceinline__ void split3_any(float x, uint32_t out[3]) {
     const uint32_t hi = __float_as_uint(x) & 0xFFFF0000u;
-    float r = x - __uint_as_float(hi);
-    if ((hi & 0x7F800000u) == 0x7F800000u) r = 0.0f;
+    const bool finite = (hi & 0x7F800000u) != 0x7F800000u;
+    const float r = finite ? x - __uint_as_float(hi) : 0.0f;
     const uint32_t mid = __float_as_uint(r) & 0xFFFF0000u;
-    out[0] = hi | ((__float_as_uint(x) & 0xFFFFu) != 0 && (hi & 0x7FFFFFFFu) == 0x7F800000u ? 0x00400000u : 0u);   // a NaN stays one
+    out[0] = hi | (!finite && (__float_as_uint(x) & 0xFFFFu) != 0 ? 0x00400000u : 0u);       // a NaN stays one
     out[1] = mid;
     out[2] = __float_as_uint(r - __uint_as_float(mid)) & 0xFFFF0000u;
+}
+// 8 floats as words of 2 for each of the three terms
+__device__ __forceinline__ void split3_8(const float x[8], uint32_t out[3][4]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t a = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+        most = a > most ? a : most;
+    }
+    if (__builtin_expect(most < 0x7F000000u, 1)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t w[3];
+            split3_pair(x[2 * e], x[2 * e + 1], w);
+#pragma unroll
+            for (int j = 0; j < 3; ++j) out[j][e] = w[j];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t a[3], b[3];
+            split3_any(x[2 * e], a);
+            split3_any(x[2 * e + 1], b);
+#pragma unroll
+            for (int j = 0; j < 3; ++j) out[j][e] = a[j] >> 16 | b[j];
+        }
+    }
 }
 
 template <bool BF16> constexpr int kW4Terms = BF16 ? 1 : 3;
@@ -223,69 +264,134 @@ __device__ __forceinline__ void w4_operand8(const void* p, int64_t i, int64_t en
     } else {
         float x[8];
         w4_load8<false>(p, i, end, x);
-        union { uint32_t w[4]; bf16x8 v; } u[3];
+        uint32_t w[3][4];
+        split3_8(x, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t a[3], b[3];
-            split3(x[2 * e], a);
-            split3(x[2 * e + 1], b);
-#pragma unroll
-            for (int j = 0; j < 3; ++j) u[j].w[e] = a[j] >> 16 | b[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 3; ++j) out[j] = u[j].v;
+        for (int j = 0; j < 3; ++j) out[j] = __builtin_bit_cast(bf16x8, make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]));
     }
 }
 
 // ---- y = x W^T ---------------------------------------------------------------------------------------------------------------
 //
-// A workgroup takes 16 rows of W and 16 tokens; its waves share the runs of 128 and add up in LDS.  A lane's 16 bytes of
-// codes are its operands of four 16x16x32 products: lane l holds row l % 16, and its word s the elements 32 s + 8 (l / 16) .. + 7.
-template <bool BF16, int GROUP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void w4_linear_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
-                                                               int64_t y_stride) {
-    constexpr int TERMS = kW4Terms<BF16>;
-    __shared__ f32x4 s_part[WAVES][64];
+// Few tokens (MT 16).  A workgroup takes tiles of 16 rows of W, one after the other; its waves share the runs of 128 in pieces of A next to each
+// other and add up in LDS.  A lane's 16 bytes of codes are its operands of four 16x16x32 products: lane l holds row l % 16, and its word s
+// the elements 32 s + 8 (l / 16) .. + 7.  The operands of x stay in registers from tile to tile where the waves cover a row at once
+// (K <= 128 A WAVES); the next tile's codes are requested before this one's are used (EARLY: where registers
+// hold them).  Bound by the latency of one round trip for few
+// tiles, by reading the codes for many.
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));      // 16 and 8 bytes at the alignment of a float
+typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
+
+template <bool BF16, int GROUP, int MT, int WAVES, int A, int SIMD_WAVES, bool EARLY>
+__global__ __launch_bounds__(64 * WAVES, SIMD_WAVES) void w4_linear_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
+                                                                  int64_t y_stride) {
+    constexpr int TERMS = kW4Terms<BF16>, GROUPS = kW4Chunk / GROUP, SCALES = GROUPS * A;
+    __shared__ f32x4 s_part[2][WAVES][MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-    const int n = blockIdx.x * 16 + col, tok = blockIdx.y * 16 + col;
-    const int row = n < m.n ? n : m.n - 1;
-    const uint32_t* w = m.codes + int64_t(row) * m.words + quarter * 4;
-    const float* sc = m.scales + int64_t(row) * m.groups;
-    const int64_t x0 = int64_t(tok) * x_stride;
-    f32x4 acc = {0, 0, 0, 0};
-    for (int run = wave; run < m.words / 16; run += WAVES) {
-        const uint4 q = *reinterpret_cast<const uint4*>(w + run * 16);
-        const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-        f32x4 part = {0, 0, 0, 0};
+    const int tok0 = blockIdx.y * (MT * 16), tiles = (m.n + 15) >> 4, runs = m.words / 16;
+    const int chunks = (runs + WAVES * A - 1) / (WAVES * A);
+    uint4 q[A];
+    float sc[SCALES];
+    auto load_w = [&](int tile, int chunk) {
+        const int row = min(tile * 16 + col, m.n - 1), run0 = (chunk * WAVES + wave) * A;
+        const uint32_t* w = m.codes + int64_t(row) * m.words + quarter * 4;
+        const float* scale = m.scales + int64_t(row) * m.groups;
+        const int g0 = run0 * GROUPS;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int at = run * kW4Chunk + s * 32 + quarter * 8;
-            bf16x8 a[TERMS] = {};
-            if (tok < t) w4_operand8<BF16>(x, x0 + at, x0 + m.k, a);
-            const bf16x8 b = w4_codes_bf16(words[s]);
+        for (int u = 0; u < A; ++u) q[u] = run0 + u < runs ? *reinterpret_cast<const uint4*>(w + (run0 + u) * 16) : make_uint4(0, 0, 0, 0);
+        if (g0 + SCALES <= m.groups) {
+            if constexpr (SCALES >= 4) {
 #pragma unroll
-            for (int j = 0; j < TERMS; ++j) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j], b, part, 0, 0, 0);
-            if ((s + 1) * 32 % GROUP == 0) {
-                const int g = (run * kW4Chunk + s * 32) / GROUP;
-                const float scale = g < m.groups ? sc[g] : 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(scale, part[i], acc[i]);
-                part = f32x4{0, 0, 0, 0};
+                for (int i = 0; i < SCALES; i += 4) {
+                    const f32x4u v = *reinterpret_cast<const f32x4u*>(scale + g0 + i);
+                    sc[i] = v.x; sc[i + 1] = v.y; sc[i + 2] = v.z; sc[i + 3] = v.w;
+                }
+            } else if constexpr (SCALES == 2) {
+                const f32x2u v = *reinterpret_cast<const f32x2u*>(scale + g0);
+                sc[0] = v.x; sc[1] = v.y;
+            } else {
+                sc[0] = scale[g0];
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < SCALES; ++i) sc[i] = g0 + i < m.groups ? scale[g0 + i] : 0.0f;
         }
-    }
-    s_part[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0) {
+    };
+    bf16x8 a[A][4][MT][TERMS];
+    auto load_x = [&](int chunk) {
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) acc += s_part[i][lane];
-        if (n < m.n) {
+        for (int u = 0; u < A; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int tt = blockIdx.y * 16 + quarter * 4 + i;
-                if (tt < t) w4_store1<BF16>(y, int64_t(tt) * y_stride + n, acc[i]);
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int b = 0; b < MT; ++b) {
+                    const int at = ((chunk * WAVES + wave) * A + u) * kW4Chunk + s * 32 + quarter * 8, tok = tok0 + b * 16 + col;
+#pragma unroll
+                    for (int j = 0; j < TERMS; ++j) a[u][s][b][j] = bf16x8{};
+                    if (tok < t && at < m.k) w4_operand8<BF16>(x, int64_t(tok) * x_stride + at, int64_t(tok) * x_stride + m.k, a[u][s][b]);
+                }
+    };
+    f32x4 acc[MT] = {};
+    int tile = blockIdx.x, chunk = 0, buffer = 0;
+    load_w(tile, 0);
+    load_x(0);
+    while (true) {
+        uint4 q_now[A];
+        float sc_now[SCALES];
+#pragma unroll
+        for (int u = 0; u < A; ++u) q_now[u] = q[u];
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) sc_now[i] = sc[i];
+        const bool end = chunk + 1 == chunks;
+        const int next = end ? tile + int(gridDim.x) : tile, next_chunk = end ? 0 : chunk + 1;
+        if (EARLY && next < tiles) load_w(next, next_chunk);
+#pragma unroll
+        for (int u = 0; u < A; ++u) {
+            const uint32_t words[4] = {q_now[u].x, q_now[u].y, q_now[u].z, q_now[u].w};
+            f32x4 part[MT];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const bf16x8 v = w4_codes_bf16(words[s]);
+#pragma unroll
+                for (int b = 0; b < MT; ++b) {
+                    if (s * 32 % GROUP == 0) part[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < TERMS; ++j) part[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u][s][b][j], v, part[b], 0, 0, 0);
+                    if ((s + 1) * 32 % GROUP == 0) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[b][i] = __builtin_fmaf(sc_now[u * GROUPS + s * 32 / GROUP], part[b][i], acc[b][i]);
+                    }
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);         // codes of later runs are not converted ahead, into registers that are not there
         }
+        if (!EARLY && next < tiles) load_w(next, next_chunk);
+        if (chunks > 1 && next < tiles) load_x(next_chunk);
+        if (end) {
+#pragma unroll
+            for (int b = 0; b < MT; ++b) {
+                s_part[buffer][wave][b][lane] = acc[b];
+                acc[b] = f32x4{0, 0, 0, 0};
+            }
+            __syncthreads();               // the other buffer is written next, and this one only behind the next barrier
+            if (wave < MT) {               // a wave adds up 16 tokens
+                f32x4 sum = s_part[buffer][0][wave][lane];
+#pragma unroll
+                for (int i = 1; i < WAVES; ++i) sum += s_part[buffer][i][wave][lane];
+                const int n = tile * 16 + col;
+                if (n < m.n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int tok = tok0 + wave * 16 + quarter * 4 + i;
+                        if (tok < t) w4_store1<BF16>(y, int64_t(tok) * y_stride + n, sum[i]);
+                    }
+                }
+            }
+            buffer ^= 1;
+        }
+        if (next >= tiles) break;
+        tile = next;
+        chunk = next_chunk;
     }
 }
 

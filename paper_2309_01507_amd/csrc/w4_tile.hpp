@@ -9,11 +9,11 @@
 namespace lpmm {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));      // 16 bytes at the alignment of a float
 
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }      // as a scalar
 __device__ __forceinline__ int mfma32_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 
 // Workgroups go round robin over the 8 XCDs; so that each XCD's L2 serves neighbouring tiles, XCD x takes the x-th eighth of them,
@@ -60,22 +60,23 @@ template <> struct RawOctet<true> {
     __device__ __forceinline__ void terms(uint4 out[]) const { out[0] = make_uint4(w[0], w[1], w[2], w[3]); }
 };
 template <> struct RawOctet<false> {
-    float x[8];
-    __device__ __forceinline__ void load(const void* p, int64_t i, int64_t end) { w4_load8<false>(p, i, end, x); }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-    }
-    __device__ __forceinline__ void terms(uint4 out[]) const {
-        uint32_t w[3][4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t a[3], b[3];
-            split3(x[2 * e], a);
-            split3(x[2 * e + 1], b);
-#pragma unroll
-            for (int j = 0; j < 3; ++j) w[j][e] = a[j] >> 16 | b[j];
+    f32x4 lo, hi;
+    __device__ __forceinline__ void load(const void* p, int64_t i, int64_t end) {
+        const float* x = static_cast<const float*>(p) + i;
+        if (i + 8 <= end) {
+            lo = *reinterpret_cast<const f32x4u*>(x);
+            hi = *reinterpret_cast<const f32x4u*>(x + 4);
+        } else {
+            const int64_t left = end - i;
+            lo = f32x4{left > 0 ? x[0] : 0.0f, left > 1 ? x[1] : 0.0f, left > 2 ? x[2] : 0.0f, left > 3 ? x[3] : 0.0f};
+            hi = f32x4{left > 4 ? x[4] : 0.0f, left > 5 ? x[5] : 0.0f, left > 6 ? x[6] : 0.0f, 0.0f};
         }
+    }
+    __device__ __forceinline__ void zero() { lo = hi = f32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void terms(uint4 out[]) const {
+        const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        uint32_t w[3][4];
+        split3_8(x, w);
 #pragma unroll
         for (int j = 0; j < 3; ++j) out[j] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
     }
@@ -254,8 +255,9 @@ struct StageDirect {
     Buffer buffer;
     uint32_t off[kOwn];                                        // bytes
     // stride: bytes from one row to the next; rows: of the matrix from `first` on; those beyond arrive as 0
-    __device__ __forceinline__ void setup(const void* first, int64_t stride, int64_t rows) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // wave: of the WAVES
+    __device__ __forceinline__ void setup(const void* first, int64_t stride, int64_t rows, int wave) {
+        const int lane = threadIdx.x & 63;
         buffer.set(first, rows < ROWS ? rows * stride : ROWS * stride);
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
@@ -264,8 +266,7 @@ struct StageDirect {
         }
     }
     // at: bytes from a row's start
-    __device__ __forceinline__ void load(int at, uint4* lds) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __device__ __forceinline__ void load(int at, uint4* lds, int wave) const {
 #pragma unroll
         for (int j = 0; j < kOwn; ++j)
             buffer.to_lds16(off[j], at, lds + (j * WAVES + wave) * 64);
@@ -293,12 +294,12 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
     __shared__ uint4 s_w0[StageW::kPieces], s_w1[StageW::kPieces];       // front of reading another
     int n_tile, t_tile;
     if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
     const int n0 = n_tile * BN, nw = (wave % WN) * NT * 32, t0 = t_tile * BT, tw = (wave / WN) * TT * 32;
     StageX stage_x;
     StageW stage_w;
-    stage_x.setup(static_cast<const char*>(x) + int64_t(t0) * x_stride * 2, x_stride * 2, t - t0);
-    stage_w.setup(m.codes + int64_t(n0) * m.words, int64_t(m.words) * 4, m.n - n0);
+    stage_x.setup(static_cast<const char*>(x) + int64_t(t0) * x_stride * 2, x_stride * 2, t - t0, wave);
+    stage_w.setup(m.codes + int64_t(n0) * m.words, int64_t(m.words) * 4, m.n - n0, wave);
     const float* scales[NT];
 #pragma unroll
     for (int b = 0; b < NT; ++b) scales[b] = m.scales + int64_t(min(n0 + nw + b * 32 + col, m.n - 1)) * m.groups;
@@ -325,8 +326,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
             for (int b = 0; b < NT; ++b) sc[b] = sc_next[b];
         }
         if (more) {
-            stage_x.load((run + 1) * (kW4Chunk * 2), next_x);
-            stage_w.load((run + 1) * (kW4Chunk / 2), next_w);
+            stage_x.load((run + 1) * (kW4Chunk * 2), next_x, wave);
+            stage_w.load((run + 1) * (kW4Chunk / 2), next_w, wave);
             if ((run + 1) % QUAD == 0) load_scales((run + 1) * GROUPS);
         }
         uint4 q[NT][2];
@@ -368,8 +369,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
         }
         __syncthreads();
     };
-    stage_x.load(0, s_x0);
-    stage_w.load(0, s_w0);
+    stage_x.load(0, s_x0, wave);
+    stage_w.load(0, s_w0, wave);
     load_scales(0);
     __syncthreads();
     int run = 0;
@@ -390,6 +391,110 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
                 if (n < m.n && tok < t) w4_store1<true>(y, int64_t(tok) * y_stride + n, acc[a][b][i]);
             }
         }
+}
+
+// The same for fewer tokens than fill the GPU with such tiles: a tile of NT 32 rows of W and TT 32 tokens per workgroup, whose 4 waves share the
+// runs.  Each wave stages its own runs in its own part of LDS, one ahead, and waits for nobody until the sums are joined.
+template <int GROUP, int NT, int TT>
+__global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
+                                                              int n_tiles, int t_tiles) {
+    constexpr int BN = NT * 32, BT = TT * 32, GROUPS = kW4Chunk / GROUP, WAVES = 4;
+    typedef StageDirect<BT, 4, 1> StageX;
+    typedef StageDirect<BN, 2, 1> StageW;
+    constexpr int PIECES = StageX::kPieces + StageW::kPieces;
+    static_assert(PIECES * 16 >= NT * TT * 16 * 64 * 4, "room for a wave's sums");
+    __shared__ uint4 s_a[WAVES][PIECES];
+    __shared__ uint4 s_b[WAVES][PIECES];
+    int n_tile, t_tile;
+    if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
+    const int n0 = n_tile * BN, t0 = t_tile * BT;
+    StageX stage_x;
+    StageW stage_w;
+    stage_x.setup(static_cast<const char*>(x) + int64_t(t0) * x_stride * 2, x_stride * 2, t - t0, 0);
+    stage_w.setup(m.codes + int64_t(n0) * m.words, int64_t(m.words) * 4, m.n - n0, 0);
+    const float* scales[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) scales[b] = m.scales + int64_t(min(n0 + b * 32 + col, m.n - 1)) * m.groups;
+    float sc[NT][GROUPS];
+    f32x16 acc[TT][NT] = {};
+    const f32x16 zero = opaque_zero();
+    const int runs = m.words / 16;
+    auto load = [&](int run, uint4* lds) {
+        stage_x.load(run * (kW4Chunk * 2), lds, 0);
+        stage_w.load(run * (kW4Chunk / 2), lds + StageX::kPieces, 0);
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][run * GROUPS + g];
+    };
+    auto step = [&](int run, const uint4* now, uint4* next) {
+        float scale[NT][GROUPS];
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) scale[b][g] = sc[b][g];
+        if (run + WAVES < runs) load(run + WAVES, next);
+        const uint4* now_w = now + StageX::kPieces;
+        uint4 q[NT][2];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            q[b][0] = now_w[lds_piece<2>(b * 32 + col, half)];
+            q[b][1] = now_w[lds_piece<2>(b * 32 + col, half + 2)];
+        }
+        f32x16 part[TT][NT];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            bf16x8 bw[NT];
+#pragma unroll
+            for (int b = 0; b < NT; ++b) {
+                const uint4 v = q[b][s & 1];                   // logical word 2 s + half
+                bw[b] = w4_codes_bf16(s < 2 ? v.x : s < 4 ? v.y : s < 6 ? v.z : v.w);
+            }
+#pragma unroll
+            for (int a = 0; a < TT; ++a) {
+                const bf16x8 ax = as_operand(now[lds_piece<4>(a * 32 + col, 2 * s + half)]);
+#pragma unroll
+                for (int b = 0; b < NT; ++b) part[a][b] = mfma32(ax, bw[b], s * 16 % GROUP == 0 ? zero : part[a][b]);
+            }
+            if ((s + 1) * 16 % GROUP == 0) {
+#pragma unroll
+                for (int b = 0; b < NT; ++b)
+#pragma unroll
+                    for (int a = 0; a < TT; ++a)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float sum = __builtin_fmaf(scale[b][s * 16 / GROUP], part[a][b][i], acc[a][b][i]);
+                            if (GROUPS > 1) asm volatile("" : "+v"(sum));      // here: further down the sums of all groups would be held
+                            acc[a][b][i] = sum;
+                        }
+            }
+        }
+    };
+    if (wave < runs) load(wave, s_a[wave]);
+    for (int run = wave; run < runs; run += 2 * WAVES) {
+        step(run, s_a[wave], s_b[wave]);
+        if (run + WAVES < runs) step(run + WAVES, s_b[wave], s_a[wave]);
+    }
+    // sums through LDS: the wave's part of s_a is free, but loads into it may still be on their way
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);              // vmcnt(0)
+    float* mine = reinterpret_cast<float*>(s_a[wave]);
+#pragma unroll
+    for (int a = 0; a < TT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mine[((a * NT + b) * 16 + i) * 64 + lane] = acc[a][b][i];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NT * TT * 16 / WAVES; ++j) {
+        const int id = wave * (NT * TT * 16 / WAVES) + j, i = id & 15, b = (id >> 4) % NT, a = (id >> 4) / NT;
+        float v = reinterpret_cast<const float*>(s_a[0])[id * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += reinterpret_cast<const float*>(s_a[w])[id * 64 + lane];
+        const int n = n0 + b * 32 + col, tok = t0 + a * 32 + mfma32_row(i, half);
+        if (n < m.n && tok < t) w4_store1<true>(y, int64_t(tok) * y_stride + n, v);
+    }
 }
 
 // ---- gradient of the scales ---------------------------------------------------------------------------------------------------------
@@ -441,11 +546,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
             if constexpr (BF16) {
                 s_d[at][lds_piece<LOGD>(r, o)] = make_uint4(sd.raw[j].w[0], sd.raw[j].w[1], sd.raw[j].w[2], sd.raw[j].w[3]);
             } else {
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-                    s_d[at][lds_piece<LOGD + 1>(r, 2 * o + p)] =
-                        make_uint4(__float_as_uint(sd.raw[j].x[4 * p]), __float_as_uint(sd.raw[j].x[4 * p + 1]),
-                                   __float_as_uint(sd.raw[j].x[4 * p + 2]), __float_as_uint(sd.raw[j].x[4 * p + 3]));
+                s_d[at][lds_piece<LOGD + 1>(r, 2 * o)] = __builtin_bit_cast(uint4, sd.raw[j].lo);
+                s_d[at][lds_piece<LOGD + 1>(r, 2 * o + 1)] = __builtin_bit_cast(uint4, sd.raw[j].hi);
             }
         }
     };
@@ -569,13 +671,13 @@ __global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, co
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
             const int id = threadIdx.x + j * THREADS, o = id & ((1 << LOGN) - 1), wd = k0 / 8 + (id >> (LOGN + 1));
-            if (TASKS % THREADS != 0 && id >= TASKS) break;
             const int place = (wd & ~15) + w4_place(wd & 15);
             const int at = wd * 8;
+            const bool mine = TASKS % THREADS == 0 || id < TASKS;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int row = n + o * 8 + e;
-                const bool in = row < last && at < m.k;
+                const bool in = mine && row < last && at < m.k;
                 word[j][e] = in ? m.codes[int64_t(row) * m.words + place] : 0u;
                 sc[j][e] = in ? m.scales[int64_t(row) * m.groups + (at >> group_shift)] : 0.0f;
             }
@@ -585,7 +687,6 @@ __global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, co
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
             const int id = threadIdx.x + j * THREADS, o = id & ((1 << LOGN) - 1), upper = (id >> LOGN) & 1;
-            if (TASKS % THREADS != 0 && id >= TASKS) break;
             const int kk = (id >> (LOGN + 1)) * 8 + upper * 4;
             float v[8][4];
 #pragma unroll
@@ -599,19 +700,14 @@ __global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, co
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t w[TERMS][4];
+                if constexpr (BF16) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (BF16) {
-                        const bf16x2 p = {static_cast<__bf16>(v[2 * e][c]), static_cast<__bf16>(v[2 * e + 1][c])};
-                        w[0][e] = __builtin_bit_cast(uint32_t, p);
-                    } else {
-                        uint32_t a[3], b[3];
-                        split3(v[2 * e][c], a);
-                        split3(v[2 * e + 1][c], b);
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) w[k][e] = a[k] >> 16 | b[k];
-                    }
+                    for (int e = 0; e < 4; ++e) w[0][e] = pack_bf16(v[2 * e][c], v[2 * e + 1][c]);
+                } else {
+                    const float column[8] = {v[0][c], v[1][c], v[2][c], v[3][c], v[4][c], v[5][c], v[6][c], v[7][c]};
+                    split3_8(column, w);
                 }
+                if (TASKS % THREADS != 0 && id >= TASKS) continue;
 #pragma unroll
                 for (int k = 0; k < TERMS; ++k)
                     lds[k * WPIECES + lds_piece<LOGN>(kk + c, o)] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
@@ -624,11 +720,13 @@ __global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, co
 #pragma unroll
             for (int j = 0; j < StageD::kOwn; ++j) {
                 const int id = threadIdx.x + j * THREADS;
-                uint32_t w[4];
+                uint4 t[3];
+                stage.raw[j].terms(t);
+                uint32_t w[4] = {t[0].x, t[0].y, t[0].z, t[0].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t a = __float_as_uint(stage.raw[j].x[2 * e]), b = __float_as_uint(stage.raw[j].x[2 * e + 1]);
-                    w[e] = ((a & 0x7F800000u) == 0x7F800000u ? 0u : a >> 16) | ((b & 0x7F800000u) == 0x7F800000u ? 0u : b & 0xFFFF0000u);
+                    if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+                    if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
                 }
                 lds[3 * StageD::kPieces + lds_piece<LOGN>(id >> LOGN, id & ((1 << LOGN) - 1))] = make_uint4(w[0], w[1], w[2], w[3]);
             }
