@@ -164,23 +164,26 @@ int dscale_splits(int64_t t, const W4Mat& m) {
     return splits_for(div_up(m.n, kDscaleRows) * (m.words / 16), div_up(t, kDscaleTokens), 768);
 }
 
-// The gradient of the input: a large tile where it fills the GPU, else a small one with the reduction split
+// The gradient of the input: large tiles of 256 tokens by 128 inputs, for few tokens small ones, the reduction split where that fills the GPU
 struct DxPlan {
-    bool big;
-    int bt, bk, splits, n_per_split;
+    bool direct;
+    int bt, splits, n_per_split;
 };
-constexpr int kDxStep = 64;              // rows of W
-DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16) {
+constexpr int kDxStep = 64;              // rows of W that splits are made of
+bool dx_aligned(const void* dy, int dtype, int64_t dy_stride, const W4Mat& m) {
+    return dtype == LPMM_BF16 && m.n % 32 == 0 && aligned(dy, 16) && dy_stride % 8 == 0 && dy_stride < (1 << 21);
+}
+DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     DxPlan p{};
-    p.big = bf16 && div_up(t, 256) * div_up(m.k, 256) >= 192;
-    p.bt = p.big ? 256 : bf16 ? 64 : 128;
-    p.bk = p.big ? 256 : 128;
+    p.direct = aligned_rows && t > 128;
+    p.bt = p.direct ? 256 : bf16 ? 64 : 128;
     const int64_t steps = div_up(m.n, kDxStep);
-    const int splits = p.big ? 1 : splits_for(div_up(t, p.bt) * div_up(m.k, p.bk), div_up(steps, 2), 512);
+    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), div_up(steps, 2), 512);
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
     p.splits = int(div_up(m.n, p.n_per_split));
     return p;
 }
+size_t dx_bytes(int64_t t, const W4Mat& m, const DxPlan& p) { return p.splits > 1 ? size_t(p.splits) * size_t(t) * size_t(m.k) * 4 : 0; }
 
 }  // namespace
 
@@ -317,8 +320,8 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
 size_t lpmm_w4_linear_dx_workspace_bytes(int64_t t, const int64_t shape[2], int dtype) {
     W4Mat m{};
     if (check_w4(shape, 32, &m) || t < 1 || t > kMaxTokens || (dtype != LPMM_F32 && dtype != LPMM_BF16)) return 0;
-    const DxPlan p = dx_plan(t, m, dtype == LPMM_BF16);
-    return p.splits > 1 ? size_t(p.splits) * size_t(t) * size_t(m.k) * 4 : 0;
+    const bool bf16 = dtype == LPMM_BF16;
+    return std::max(dx_bytes(t, m, dx_plan(t, m, bf16, false)), dx_bytes(t, m, dx_plan(t, m, bf16, bf16)));
 }
 
 int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, const uint8_t* codes,
@@ -332,21 +335,24 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
     LPMM_TRY(check_floats(scales));
     if (t == 0) return LPMM_OK;
     const bool bf16 = dtype == LPMM_BF16;
-    const DxPlan p = dx_plan(t, m, bf16);
-    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_w4_linear_dx_workspace_bytes(t, shape, dtype)));
+    const DxPlan p = dx_plan(t, m, bf16, dx_aligned(dy, dtype, dy_stride, m));
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, dx_bytes(t, m, p)));
     m.codes = reinterpret_cast<const uint32_t*>(codes);
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t t_tiles = div_up(t, p.bt), k_tiles = div_up(m.k, p.bk), blocks = div_up(t_tiles * k_tiles, 8) * 8;
+    const int64_t t_tiles = div_up(t, p.bt), k_tiles = div_up(m.k, kW4Chunk), blocks = div_up(t_tiles * k_tiles, 8) * 8;
     if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
     float* parts = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
     const dim3 grid(unsigned(blocks), unsigned(p.splits));
 #define LPMM_DX(B, WT, WK, TT, KT, LOGN) hipLaunchKernelGGL((w4_dx_tile_kernel<B, WT, WK, TT, KT, LOGN>), grid, dim3(64 * WT * WK), 0, s, m, dy, \
                                                             int(t), dy_stride, dx, dx_stride, int(t_tiles), int(k_tiles), p.n_per_split, \
                                                             parts, group_shift(group))
-    if (p.big) LPMM_DX(true, 2, 4, 4, 2, 3);
+#define LPMM_DX_DIRECT(P) hipLaunchKernelGGL(w4_dx_direct_kernel<P>, grid, dim3(256), 0, s, m, dy, int(t), dy_stride, dx, dx_stride, int(t_tiles), \
+                                             int(k_tiles), p.n_per_split, parts, group_shift(group))
+    if (p.direct) { if (parts) LPMM_DX_DIRECT(true); else LPMM_DX_DIRECT(false); }
     else if (bf16) LPMM_DX(true, 2, 4, 1, 1, 3);
     else LPMM_DX(false, 4, 2, 1, 2, 2);
+#undef LPMM_DX_DIRECT
 #undef LPMM_DX
     LPMM_HIP(hipGetLastError());
     if (parts) {
@@ -385,6 +391,14 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
     const int64_t count = int64_t(m.n) * m.groups;
     float* out = splits > 1 ? static_cast<float*>(workspace) : dscales;
     const dim3 grid = dim3(unsigned(blocks), unsigned(splits));
+    const bool direct = dtype == LPMM_BF16 && aligned(x, 16) && aligned(dy, 16) && x_stride % 8 == 0 && dy_stride % 8 == 0 &&
+                        x_stride < (1 << 24) && dy_stride < (1 << 24);
+    if (direct) {
+#define LPMM_DSCALE_DIRECT(G) hipLaunchKernelGGL(w4_dscale_direct_kernel<G>, grid, dim3(256), 0, s, m, x, dy, int(t), x_stride, dy_stride, int(n_tiles), \
+                                                 per, out, count)
+        if (group == 32) LPMM_DSCALE_DIRECT(32); else if (group == 64) LPMM_DSCALE_DIRECT(64); else LPMM_DSCALE_DIRECT(128);
+#undef LPMM_DSCALE_DIRECT
+    } else
 #define LPMM_DSCALE(B, G, WN, WT, NT, TT) hipLaunchKernelGGL((w4_dscale_tile_kernel<B, G, WN, WT, NT, TT>), grid, dim3(512), 0, s, m, x, dy, int(t), \
                                                              x_stride, dy_stride, int(n_tiles), per, out, count)
     if (dtype == LPMM_BF16) {

@@ -36,6 +36,9 @@ __device__ __forceinline__ int lds_piece(int r, int o) {
     return (r << LOG) + (o ^ ((r >> (LOG < 4 ? 4 - LOG : 0)) & ((1 << LOG) - 1)));
 }
 
+// The same for arrays that are read transposed, four rows by 64 bytes at a time: the four rows' pieces hit all banks.
+__device__ __forceinline__ int lds_piece_tr(int log, int r, int o) { return (r << log) + (o ^ ((r & 3) << 2)); }
+
 // ---- staging: octets of rows, from global memory into registers and from there into LDS ------------------------------------------
 
 // Elements as they come from memory: 8 of them
@@ -248,7 +251,7 @@ struct Buffer {
 
 // ROWS rows of 2^LOG octets of bf16 (16 bytes), staged by WAVES waves a KiB at a time.  A lane's octet of a row is the one that lds_piece
 // puts at the lane's place, so the swizzle costs nothing.
-template <int ROWS, int LOG, int WAVES>
+template <int ROWS, int LOG, int WAVES, bool TR = false>
 struct StageDirect {
     static constexpr int kPieces = ROWS << LOG, kOwn = kPieces / 64 / WAVES, kRowsAtOnce = 64 >> LOG;
     static_assert(kPieces % (64 * WAVES) == 0, "whole KiB per wave");
@@ -262,8 +265,13 @@ struct StageDirect {
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
             const int r = (j * WAVES + wave) * kRowsAtOnce + (lane >> LOG);
-            off[j] = uint32_t(r) * uint32_t(stride) + (lds_piece<LOG>(r, lane & ((1 << LOG) - 1)) - (r << LOG)) * 16;    // an involution
+            const int o = lane & ((1 << LOG) - 1);
+            off[j] = uint32_t(r) * uint32_t(stride) + ((TR ? lds_piece_tr(LOG, r, o) : lds_piece<LOG>(r, o)) - (r << LOG)) * 16;   // involutions
         }
+    }
+    // other rows of the same matrix: `first` has moved
+    __device__ __forceinline__ void move(const void* first, int64_t stride, int64_t rows) {
+        buffer.set(first, rows < ROWS ? rows * stride : ROWS * stride);
     }
     // at: bytes from a row's start
     __device__ __forceinline__ void load(int at, uint4* lds, int wave) const {
@@ -272,6 +280,24 @@ struct StageDirect {
             buffer.to_lds16(off[j], at, lds + (j * WAVES + wave) * 64);
     }
 };
+
+// An operand whose reduction runs down the rows of an array in LDS (2^LOG pieces a row, staged with TR): rows `row` + 8 half .. + 7, column
+// cols + lane % 32.  A transposed read gives each of 16 lanes a column of 4 rows by 16 columns that their addresses make up.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+template <int LOG>
+__device__ __forceinline__ bf16x8 operand_tr(const uint4* lds, int row, int cols) {
+    const int lane = threadIdx.x & 63, half = lane >> 5, sub = lane & 15;
+    union { s16x4 q[2]; bf16x8 v; } u;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int r = row + 8 * half + 4 * j + (sub >> 2), piece = (cols >> 3) + 2 * ((lane >> 4) & 1) + ((sub >> 1) & 1);
+        const char* at = reinterpret_cast<const char*>(lds + lds_piece_tr(LOG, r, piece)) + (sub & 1) * 8;
+#ifdef __HIP_DEVICE_COMPILE__
+        u.q[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at));
+#endif
+    }
+    return u.v;
+}
 
 // 0 in registers that the compiler does not know to be 0: the C operand of a sum's first product, which saves clearing the sum
 __device__ __forceinline__ f32x16 opaque_zero() {
@@ -632,6 +658,113 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
     }
 }
 
+// The same for bf16 on 16-byte boundaries, the other way round: dy^T x is summed over the tokens by the matrix unit alone, in tiles of 256 rows of
+// W by a run of 128 that are never written, and at the end multiplied by the codes and added up over the groups.  (With the product over the
+// inputs first, 4096 tokens and 11008 x 4096 took 603 us: a multiply-add a product and token, and dy's conversion.)  Both operands'
+// reduction runs down the rows of their arrays, hence the transposed reads.
+template <int GROUP>
+__global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
+                                                               int64_t dy_stride, int n_tiles, int t_per_split, float* out,
+                                                               int64_t out_split) {
+    constexpr int STEP = 32, NT = 4, KT = 2;                   // tokens of a step; tiles of a wave: 128 rows of W by 64 inputs
+    typedef StageDirect<STEP, 5, 4, true> StageD;              // 256 rows of W
+    typedef StageDirect<STEP, 4, 4, true> StageX;              // 128 inputs
+    __shared__ uint4 s_d0[StageD::kPieces], s_d1[StageD::kPieces], s_x0[StageX::kPieces], s_x1[StageX::kPieces];
+    __shared__ float s_sum[2][256];
+    int n_tile, run;
+    if (!tile_of(blockIdx.x, n_tiles, m.words / 16, n_tile, run)) return;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
+    const int n0 = n_tile * 256, nw = (wave & 1) * 128, k0 = run * kW4Chunk, kw = (wave >> 1) * 64;
+    const int first = blockIdx.y * t_per_split, last = min(t, first + t_per_split);
+    const char* from_d = static_cast<const char*>(dy) + (int64_t(first) * dy_stride + n0) * 2;
+    const char* from_x = static_cast<const char*>(x) + (int64_t(first) * x_stride + k0) * 2;
+    // a descriptor ends with the 32-bit word of the last row's last element (words are checked as a whole)
+    const int64_t cut_d = int64_t(dy_stride - (m.n - n0)) * 2 & ~int64_t(3), cut_x = int64_t(x_stride - (m.k - k0)) * 2 & ~int64_t(3);
+    StageD stage_d;
+    StageX stage_x;
+    stage_d.setup(from_d, dy_stride * 2, last - first, wave);
+    stage_x.setup(from_x, x_stride * 2, last - first, wave);
+    auto load = [&](int tok, uint4* lds_d, uint4* lds_x) {
+        const int64_t left = last - tok;
+        stage_d.buffer.set(from_d + int64_t(tok - first) * dy_stride * 2, min(left, int64_t(STEP)) * dy_stride * 2 - cut_d);
+        stage_x.buffer.set(from_x + int64_t(tok - first) * x_stride * 2, min(left, int64_t(STEP)) * x_stride * 2 - cut_x);
+        stage_d.load(0, lds_d, wave);
+        stage_x.load(0, lds_x, wave);
+    };
+    f32x16 acc[NT][KT] = {};
+    auto step = [&](bool more, int tok, const uint4* now_d, const uint4* now_x, uint4* next_d, uint4* next_x) {
+        if (more) load(tok + STEP, next_d, next_x);
+#pragma unroll
+        for (int s = 0; s < STEP / 16; ++s) {
+            bf16x8 a[NT], b[KT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) a[i] = operand_tr<5>(now_d, s * 16, nw + i * 32);
+#pragma unroll
+            for (int j = 0; j < KT; ++j) b[j] = operand_tr<4>(now_x, s * 16, kw + j * 32);
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < KT; ++j) acc[i][j] = mfma32(a[i], b[j], acc[i][j]);
+        }
+        __syncthreads();
+    };
+    if (first < last) {
+        load(first, s_d0, s_x0);
+        __syncthreads();
+        int tok = first;
+        for (; tok + 2 * STEP < last; tok += 2 * STEP) {
+            step(true, tok, s_d0, s_x0, s_d1, s_x1);
+            step(true, tok + STEP, s_d1, s_x1, s_d0, s_x0);
+        }
+        step(tok + STEP < last, tok, s_d0, s_x0, s_d1, s_x1);
+        if (tok + STEP < last) step(false, tok + STEP, s_d1, s_x1, s_d0, s_x0);
+    }
+    // times the codes, summed over the group: within the wave's two tiles, its 32 lanes, and for groups of 128 the two waves
+    const int shift = (col & 7) * 4;
+    bool in[KT];
+    const uint32_t* codes[KT];
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+        const int word = (kw + j * 32 + col) >> 3;
+        in[j] = k0 + kw + j * 32 + col < m.k;
+        codes[j] = m.codes + run * 16 + w4_place(word);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int row = nw + i * 32 + mfma32_row(e, half), n = n0 + row;
+            float v[KT];
+#pragma unroll
+            for (int j = 0; j < KT; ++j) {
+                const uint32_t word = codes[j][int64_t(min(n, m.n - 1)) * m.words];
+                const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word >> shift, 1.0f, 0);
+                v[j] = in[j] ? acc[i][j][e] * c.x : 0.0f;
+            }
+            if constexpr (GROUP > 32) v[0] += v[1];
+#pragma unroll
+            for (int j = 0; j < (GROUP > 32 ? 1 : KT); ++j) {
+                float sum = v[j];
+                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0xB1, 0xF, 0xF, false));
+                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0x4E, 0xF, 0xF, false));
+                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0x141, 0xF, 0xF, false));
+                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0x140, 0xF, 0xF, false));
+                sum += __shfl_xor(sum, 16);
+                if (GROUP == 128) {
+                    if (col == 0) s_sum[wave >> 1][row] = sum;
+                } else {
+                    const int at = (k0 + kw + j * 32) / GROUP;
+                    if (col == 0 && n < m.n && at < m.groups) out[int64_t(blockIdx.y) * out_split + int64_t(n) * m.groups + at] = sum;
+                }
+            }
+        }
+    if constexpr (GROUP == 128) {
+        __syncthreads();
+        const int n = n0 + int(threadIdx.x);
+        if (n < m.n) out[int64_t(blockIdx.y) * out_split + int64_t(n) * m.groups + run] = s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x];
+    }
+}
+
 // Sum of `splits` arrays of `count` floats, `apart` from one to the next, in their order
 __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int splits, int64_t apart, int64_t count, float* out) {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
@@ -784,6 +917,95 @@ __global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, co
                 if (k < m.k && tok < t) {
                     if (parts) parts[(int64_t(blockIdx.y) * t + tok) * m.k + k] = acc[a][b][i];
                     else w4_store1<BF16>(dx, int64_t(tok) * dx_stride + k, acc[a][b][i]);
+                }
+            }
+        }
+}
+
+// The same for bf16 tokens on 16-byte boundaries and rows of W in whole steps of 32: dy straight into LDS, value * scale as it stands in W, so that
+// a lane converts a word at a time; the transposition is the reads'.
+template <bool PARTS>
+__global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx, int64_t dx_stride,
+                                                           int t_tiles, int k_tiles, int n_per_split, float* parts, int group_shift) {
+    constexpr int STEP = 32, TT = 4, KT = 2;                   // rows of W of a step; tiles of a wave: 128 tokens by 64 inputs
+    typedef StageDirect<256, 2, 4> StageD;                     // 256 tokens, 32 rows of W
+    constexpr int WPIECES = STEP << 4;                         // of 128 inputs
+    __shared__ uint4 s_d0[StageD::kPieces], s_d1[StageD::kPieces], s_w0[WPIECES], s_w1[WPIECES];
+    int t_tile, k_tile;
+    if (!tile_of(blockIdx.x, t_tiles, k_tiles, t_tile, k_tile)) return;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
+    const int t0 = t_tile * 256, tw = (wave & 1) * 128, kw = (wave >> 1) * 64;
+    const int first = blockIdx.y * n_per_split, last = min(m.n, first + n_per_split);
+    StageD stage_d;
+    stage_d.setup(static_cast<const char*>(dy) + int64_t(t0) * dy_stride * 2, dy_stride * 2, t - t0, wave);
+    // a thread converts two words of a step: rows r and r + 16, word d
+    const int d = threadIdx.x & 15, r = threadIdx.x >> 4, at = k_tile * kW4Chunk + d * 8;
+    const uint32_t* codes = m.codes + int64_t(r) * m.words + k_tile * 16 + w4_place(d);
+    const float* scales = m.scales + int64_t(r) * m.groups + min(at >> group_shift, m.groups - 1);     // beyond the last group all codes are 0
+    uint32_t word[2];
+    float sc[2];
+    auto load = [&](int n, uint4* lds) {
+        stage_d.load(n * 2, lds, wave);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            word[j] = codes[int64_t(n + 16 * j) * m.words];
+            sc[j] = scales[int64_t(n + 16 * j) * m.groups];
+        }
+    };
+    auto convert = [&](uint4* lds) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float v[8];
+            w4_values8(word[j], v);
+            uint4 p;
+            p.x = pack_bf16(v[0] * sc[j], v[1] * sc[j]);
+            p.y = pack_bf16(v[2] * sc[j], v[3] * sc[j]);
+            p.z = pack_bf16(v[4] * sc[j], v[5] * sc[j]);
+            p.w = pack_bf16(v[6] * sc[j], v[7] * sc[j]);
+            lds[lds_piece_tr(4, r + 16 * j, d)] = p;
+        }
+    };
+    f32x16 acc[TT][KT] = {};
+    auto step = [&](bool more, int n, const uint4* now_d, const uint4* now_w, uint4* next_d, uint4* next_w) {
+        if (more) load(n + STEP, next_d);
+#pragma unroll
+        for (int s = 0; s < STEP / 16; ++s) {
+            bf16x8 a[TT], b[KT];
+#pragma unroll
+            for (int i = 0; i < TT; ++i) a[i] = as_operand(now_d[lds_piece<2>(tw + i * 32 + col, 2 * s + half)]);
+#pragma unroll
+            for (int j = 0; j < KT; ++j) b[j] = operand_tr<4>(now_w, s * 16, kw + j * 32);
+#pragma unroll
+            for (int i = 0; i < TT; ++i)
+#pragma unroll
+                for (int j = 0; j < KT; ++j) acc[i][j] = mfma32(a[i], b[j], acc[i][j]);
+        }
+        if (more) convert(next_w);
+        __syncthreads();
+    };
+    if (first < last) {
+        load(first, s_d0);
+        convert(s_w0);
+        __syncthreads();
+        int n = first;
+        for (; n + 2 * STEP < last; n += 2 * STEP) {
+            step(true, n, s_d0, s_w0, s_d1, s_w1);
+            step(true, n + STEP, s_d1, s_w1, s_d0, s_w0);
+        }
+        step(n + STEP < last, n, s_d0, s_w0, s_d1, s_w1);
+        if (n + STEP < last) step(false, n + STEP, s_d1, s_w1, s_d0, s_w0);
+    }
+#pragma unroll
+    for (int i = 0; i < TT; ++i)
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+            const int k = k_tile * kW4Chunk + kw + j * 32 + col;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int tok = t0 + tw + i * 32 + mfma32_row(e, half);
+                if (k < m.k && tok < t) {
+                    if constexpr (PARTS) parts[(int64_t(blockIdx.y) * t + tok) * m.k + k] = acc[i][j][e];
+                    else w4_store1<true>(dx, int64_t(tok) * dx_stride + k, acc[i][j][e]);
                 }
             }
         }
