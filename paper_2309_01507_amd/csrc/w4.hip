@@ -178,7 +178,7 @@ DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     p.direct = aligned_rows && t > 128;
     p.bt = p.direct ? 256 : bf16 ? 64 : 128;
     const int64_t steps = div_up(m.n, kDxStep);
-    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), div_up(steps, 2), 512);
+    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), div_up(steps, 2), bf16 ? 512 : 256);
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
     p.splits = int(div_up(m.n, p.n_per_split));
     return p;
@@ -344,14 +344,14 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
     if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
     float* parts = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
     const dim3 grid(unsigned(blocks), unsigned(p.splits));
-#define LPMM_DX(B, WT, WK, TT, KT, LOGN) hipLaunchKernelGGL((w4_dx_tile_kernel<B, WT, WK, TT, KT, LOGN>), grid, dim3(64 * WT * WK), 0, s, m, dy, \
+#define LPMM_DX(B, WT, TT) hipLaunchKernelGGL((w4_dx_tile_kernel<B, WT, TT>), grid, dim3(128 * WT), 0, s, m, dy, \
                                                             int(t), dy_stride, dx, dx_stride, int(t_tiles), int(k_tiles), p.n_per_split, \
                                                             parts, group_shift(group))
 #define LPMM_DX_DIRECT(P) hipLaunchKernelGGL(w4_dx_direct_kernel<P>, grid, dim3(256), 0, s, m, dy, int(t), dy_stride, dx, dx_stride, int(t_tiles), \
                                              int(k_tiles), p.n_per_split, parts, group_shift(group))
     if (p.direct) { if (parts) LPMM_DX_DIRECT(true); else LPMM_DX_DIRECT(false); }
-    else if (bf16) LPMM_DX(true, 2, 4, 1, 1, 3);
-    else LPMM_DX(false, 4, 2, 1, 2, 2);
+    else if (bf16) LPMM_DX(true, 2, 1);
+    else LPMM_DX(false, 4, 1);
 #undef LPMM_DX_DIRECT
 #undef LPMM_DX
     LPMM_HIP(hipGetLastError());
@@ -392,7 +392,7 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
     float* out = splits > 1 ? static_cast<float*>(workspace) : dscales;
     const dim3 grid = dim3(unsigned(blocks), unsigned(splits));
     const bool direct = dtype == LPMM_BF16 && aligned(x, 16) && aligned(dy, 16) && x_stride % 8 == 0 && dy_stride % 8 == 0 &&
-                        x_stride < (1 << 24) && dy_stride < (1 << 24);
+                        x_stride < (1 << 24) && dy_stride < (1 << 24) && m.k < (1 << 23);
     if (direct) {
 #define LPMM_DSCALE_DIRECT(G) hipLaunchKernelGGL(w4_dscale_direct_kernel<G>, grid, dim3(256), 0, s, m, x, dy, int(t), x_stride, dy_stride, int(n_tiles), \
                                                  per, out, count)

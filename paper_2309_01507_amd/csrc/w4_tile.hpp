@@ -720,14 +720,19 @@ __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const
         if (tok + STEP < last) step(false, tok + STEP, s_d1, s_x1, s_d0, s_x0);
     }
     // times the codes, summed over the group: within the wave's two tiles, its 32 lanes, and for groups of 128 the two waves
+    StageDirect<256, 2, 4> stage_w;
+    static_assert(StageDirect<256, 2, 4>::kPieces <= StageD::kPieces, "room for the codes");
+    stage_w.setup(m.codes + int64_t(n0) * m.words + run * 16, int64_t(m.words) * 4, m.n - n0, wave);
+    stage_w.buffer.set(stage_w.buffer.start, int64_t(min(m.n - n0, 256) - 1) * m.words * 4 + kW4Chunk / 2);
+    stage_w.load(0, s_d0, wave);
+    __syncthreads();
     const int shift = (col & 7) * 4;
     bool in[KT];
-    const uint32_t* codes[KT];
+    int place[KT];
 #pragma unroll
     for (int j = 0; j < KT; ++j) {
-        const int word = (kw + j * 32 + col) >> 3;
         in[j] = k0 + kw + j * 32 + col < m.k;
-        codes[j] = m.codes + run * 16 + w4_place(word);
+        place[j] = w4_place((kw + j * 32 + col) >> 3);
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
@@ -737,7 +742,7 @@ __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const
             float v[KT];
 #pragma unroll
             for (int j = 0; j < KT; ++j) {
-                const uint32_t word = codes[j][int64_t(min(n, m.n - 1)) * m.words];
+                const uint32_t word = reinterpret_cast<const uint32_t*>(s_d0 + lds_piece<2>(row, place[j] >> 2))[place[j] & 3];
                 const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word >> shift, 1.0f, 0);
                 v[j] = in[j] ? acc[i][j][e] * c.x : 0.0f;
             }
@@ -777,121 +782,95 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 // ---- dx = dy W -------------------------------------------------------------------------------------------------------------------------
 //
 // The reduction runs along W's rows, whose scales differ: value * scale is formed once per workgroup, as bf16 (one rounding of half a
-// unit in the last place per weight, as large as the one of the result) or as three bf16 terms for fp32, and goes to LDS transposed, 8 rows of W
-// an octet.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a dy that is not finite meets
-// W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0 would make NaN of infinity.
-template <bool BF16, int WT, int WK, int TT, int KT, int LOGN>
-__global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
-                                                                  int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
-                                                                  float* parts, int group_shift) {
-    constexpr int TERMS = kW4Terms<BF16>, THREADS = 64 * WT * WK, BT = WT * TT * 32, BK = WK * KT * 32, BN = 8 << LOGN;
-    constexpr int DTERMS = BF16 ? 1 : 4;
-    typedef Stage<BF16, BT, LOGN, THREADS> StageD;
-    constexpr int WPIECES = BK << LOGN, TASKS = (BK / 4) << LOGN;                             // a task: 8 rows of W, 4 inputs
-    constexpr int OWN = (TASKS + THREADS - 1) / THREADS;
+// unit in the last place per weight, as large as the one of the result) or as three bf16 terms for fp32, and goes to LDS as it stands in W, a
+// lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a
+// dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
+// would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.
+template <bool BF16, int WT, int TT>
+__global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
+                                                              int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
+                                                              float* parts, int group_shift) {
+    constexpr int TERMS = kW4Terms<BF16>, DTERMS = BF16 ? 1 : 4, WK = 2, KT = 2, THREADS = 64 * WT * WK, BT = WT * TT * 32, STEP = 32;
+    constexpr int WPIECES = STEP << 4, OWN = WPIECES / THREADS, ROWS = STEP / OWN;            // of 128 inputs; a word makes a piece
+    typedef Stage<BF16, BT, 2, THREADS> StageD;
     __shared__ uint4 s_d[2][DTERMS * StageD::kPieces];
     __shared__ uint4 s_w[2][TERMS * WPIECES];
     int t_tile, k_tile;
     if (!tile_of(blockIdx.x, t_tiles, k_tiles, t_tile, k_tile)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
-    const int t0 = t_tile * BT, k0 = k_tile * BK, tw = (wave % WT) * TT * 32, kw = (wave / WT) * KT * 32;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
+    const int t0 = t_tile * BT, tw = (wave % WT) * TT * 32, kw = (wave / WT) * KT * 32;
     const int first = blockIdx.y * n_per_split, last = min(m.n, first + n_per_split);
+    const int d = threadIdx.x & 15, r = threadIdx.x >> 4, at = k_tile * kW4Chunk + d * 8;
+    const uint32_t* codes = m.codes + k_tile * 16 + w4_place(d);
+    const float* scales = m.scales + min(at >> group_shift, m.groups - 1);                    // beyond the last group all codes are 0
     StageD stage;
-    uint32_t word[OWN][8];
-    float sc[OWN][8];
-    // task: octet of rows in the low bits, then which half of the word, then the word
-    auto load_w = [&](int n) {
+    uint32_t word[OWN];
+    float sc[OWN];
+    auto load = [&](int n) {
+        stage.load(dy, dy_stride, t0, t, n, last);
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
-            const int id = threadIdx.x + j * THREADS, o = id & ((1 << LOGN) - 1), wd = k0 / 8 + (id >> (LOGN + 1));
-            const int place = (wd & ~15) + w4_place(wd & 15);
-            const int at = wd * 8;
-            const bool mine = TASKS % THREADS == 0 || id < TASKS;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int row = n + o * 8 + e;
-                const bool in = mine && row < last && at < m.k;
-                word[j][e] = in ? m.codes[int64_t(row) * m.words + place] : 0u;
-                sc[j][e] = in ? m.scales[int64_t(row) * m.groups + (at >> group_shift)] : 0.0f;
-            }
+            const int row = n + r + j * ROWS;
+            word[j] = row < last ? codes[int64_t(row) * m.words] : 0u;
+            sc[j] = row < last ? scales[int64_t(row) * m.groups] : 0.0f;
         }
     };
-    auto store_w = [&](uint4* lds) {
-#pragma unroll
-        for (int j = 0; j < OWN; ++j) {
-            const int id = threadIdx.x + j * THREADS, o = id & ((1 << LOGN) - 1), upper = (id >> LOGN) & 1;
-            const int kk = (id >> (LOGN + 1)) * 8 + upper * 4;
-            float v[8][4];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t u = upper ? word[j][e] >> 16 : word[j][e];
-                const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 0);
-                const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, 1.0f, 1);
-                v[e][0] = a.x * sc[j][e]; v[e][1] = a.y * sc[j][e];
-                v[e][2] = b.x * sc[j][e]; v[e][3] = b.y * sc[j][e];
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t w[TERMS][4];
-                if constexpr (BF16) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[0][e] = pack_bf16(v[2 * e][c], v[2 * e + 1][c]);
-                } else {
-                    const float column[8] = {v[0][c], v[1][c], v[2][c], v[3][c], v[4][c], v[5][c], v[6][c], v[7][c]};
-                    split3_8(column, w);
-                }
-                if (TASKS % THREADS != 0 && id >= TASKS) continue;
-#pragma unroll
-                for (int k = 0; k < TERMS; ++k)
-                    lds[k * WPIECES + lds_piece<LOGN>(kk + c, o)] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-            }
-        }
-    };
-    auto store_d = [&](uint4* lds) {
-        stage.store(lds);
+    auto store = [&](uint4* lds_d, uint4* lds_w) {
+        stage.store(lds_d);
         if constexpr (!BF16) {
 #pragma unroll
             for (int j = 0; j < StageD::kOwn; ++j) {
                 const int id = threadIdx.x + j * THREADS;
-                uint4 t[3];
-                stage.raw[j].terms(t);
-                uint32_t w[4] = {t[0].x, t[0].y, t[0].z, t[0].w};
+                uint4 f[3];
+                stage.raw[j].terms(f);
+                uint32_t w[4] = {f[0].x, f[0].y, f[0].z, f[0].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
                     if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
                 }
-                lds[3 * StageD::kPieces + lds_piece<LOGN>(id >> LOGN, id & ((1 << LOGN) - 1))] = make_uint4(w[0], w[1], w[2], w[3]);
+                lds_d[3 * StageD::kPieces + lds_piece<2>(id >> 2, id & 3)] = make_uint4(w[0], w[1], w[2], w[3]);
             }
+        }
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) {
+            float v[8];
+            w4_values8(word[j], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= sc[j];
+            uint32_t w[3][4];
+            if constexpr (BF16) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[0][e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+            } else {
+                split3_8(v, w);
+            }
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+                lds_w[k * WPIECES + lds_piece_tr(4, r + j * ROWS, d)] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
         }
     };
     f32x16 acc[TT][KT] = {};
     if (first < last) {
-        stage.load(dy, dy_stride, t0, t, first, last);
-        load_w(first);
-        store_d(s_d[0]);
-        store_w(s_w[0]);
+        load(first);
+        store(s_d[0], s_w[0]);
     }
     __syncthreads();
-    for (int n = first, at = 0; n < last; n += BN, at ^= 1) {
-        const bool more = n + BN < last;
-        if (more) {
-            stage.load(dy, dy_stride, t0, t, n + BN, last);
-            load_w(n + BN);
-        }
+    for (int n = first, now = 0; n < last; n += STEP, now ^= 1) {
+        const bool more = n + STEP < last;
+        if (more) load(n + STEP);
 #pragma unroll
-        for (int s = 0; s < BN / 16; ++s) {
+        for (int s = 0; s < STEP / 16; ++s) {
             bf16x8 bw[KT][TERMS];
 #pragma unroll
             for (int b = 0; b < KT; ++b)
 #pragma unroll
-                for (int j = 0; j < TERMS; ++j)
-                    bw[b][j] = as_operand(s_w[at][j * WPIECES + lds_piece<LOGN>(kw + b * 32 + col, 2 * s + half)]);
+                for (int j = 0; j < TERMS; ++j) bw[b][j] = operand_tr<4>(s_w[now] + j * WPIECES, s * 16, kw + b * 32);
 #pragma unroll
             for (int a = 0; a < TT; ++a)
 #pragma unroll
                 for (int j = 0; j < DTERMS; ++j) {
-                    const bf16x8 ad = as_operand(s_d[at][j * StageD::kPieces + lds_piece<LOGN>(tw + a * 32 + col, 2 * s + half)]);
+                    const bf16x8 ad = as_operand(s_d[now][j * StageD::kPieces + lds_piece<2>(tw + a * 32 + col, 2 * s + half)]);
                     // dy's terms 0, 1, 2 meet W's first 1, 2, 1 terms, the finite ones of term 0 its other two
                     constexpr int from[4] = {0, 0, 0, 1}, to[4] = {1, 2, 1, 3};
 #pragma unroll
@@ -900,17 +879,14 @@ __global__ __launch_bounds__(64 * WT * WK, 2) void w4_dx_tile_kernel(W4Mat m, co
                         for (int i = from[j]; i < to[j]; ++i) acc[a][b] = mfma32(ad, bw[b][i], acc[a][b]);
                 }
         }
-        if (more) {
-            store_d(s_d[at ^ 1]);
-            store_w(s_w[at ^ 1]);
-        }
+        if (more) store(s_d[now ^ 1], s_w[now ^ 1]);
         __syncthreads();
     }
 #pragma unroll
     for (int a = 0; a < TT; ++a)
 #pragma unroll
         for (int b = 0; b < KT; ++b) {
-            const int k = k0 + kw + b * 32 + col;
+            const int k = k_tile * kW4Chunk + kw + b * 32 + col;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int tok = t0 + tw + a * 32 + mfma32_row(i, half);
