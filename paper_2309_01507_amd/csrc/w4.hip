@@ -176,9 +176,9 @@ bool dx_aligned(const void* dy, int dtype, int64_t dy_stride, const W4Mat& m) {
 DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     DxPlan p{};
     p.direct = aligned_rows && t > 128;
-    p.bt = p.direct ? 256 : bf16 ? 64 : 128;
+    p.bt = p.direct ? (div_up(t, 256) * div_up(m.k, kW4Chunk) >= 512 ? 256 : 128) : bf16 ? 64 : 128;
     const int64_t steps = div_up(m.n, kDxStep);
-    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), div_up(steps, 2), bf16 ? 512 : 256);
+    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), div_up(steps, 2), 512);
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
     p.splits = int(div_up(m.n, p.n_per_split));
     return p;
@@ -276,16 +276,17 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         return LPMM_OK;
     }
     if (t > 64) {
-        const int bt = dtype == LPMM_BF16 ? 128 : 64;
-        const int64_t n_tiles = div_up(m.n, 256), t_tiles = div_up(t, bt);
+        // bf16: two buffers; fp32, three times as large: one, and several workgroups a CU
+        const bool bf16 = dtype == LPMM_BF16;
+        const int64_t n_tiles = div_up(m.n, bf16 ? 256 : 128), t_tiles = div_up(t, bf16 ? 128 : 64);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
-#define LPMM_TILE(B, G, TT) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, 4, 2, 2, TT>), dim3(unsigned(blocks)), dim3(512), 0, s, m, x, \
-                                               int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
-        if (dtype == LPMM_BF16) {
-            if (group == 32) LPMM_TILE(true, 32, 2); else if (group == 64) LPMM_TILE(true, 64, 2); else LPMM_TILE(true, 128, 2);
+#define LPMM_TILE(B, G, WN, TT, BUF) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, WN, 2, 2, TT, BUF>), dim3(unsigned(blocks)), dim3(128 * WN), 0, s, m, x, \
+                                                        int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
+        if (bf16) {
+            if (group == 32) LPMM_TILE(true, 32, 4, 2, 2); else if (group == 64) LPMM_TILE(true, 64, 4, 2, 2); else LPMM_TILE(true, 128, 4, 2, 2);
         } else {
-            if (group == 32) LPMM_TILE(false, 32, 1); else if (group == 64) LPMM_TILE(false, 64, 1); else LPMM_TILE(false, 128, 1);
+            if (group == 32) LPMM_TILE(false, 32, 2, 1, 1); else if (group == 64) LPMM_TILE(false, 64, 2, 1, 1); else LPMM_TILE(false, 128, 2, 1, 1);
         }
 #undef LPMM_TILE
         LPMM_HIP(hipGetLastError());
@@ -347,9 +348,10 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
 #define LPMM_DX(B, WT, TT) hipLaunchKernelGGL((w4_dx_tile_kernel<B, WT, TT>), grid, dim3(128 * WT), 0, s, m, dy, \
                                                             int(t), dy_stride, dx, dx_stride, int(t_tiles), int(k_tiles), p.n_per_split, \
                                                             parts, group_shift(group))
-#define LPMM_DX_DIRECT(P) hipLaunchKernelGGL(w4_dx_direct_kernel<P>, grid, dim3(256), 0, s, m, dy, int(t), dy_stride, dx, dx_stride, int(t_tiles), \
+#define LPMM_DX_DIRECT(P, TT) hipLaunchKernelGGL((w4_dx_direct_kernel<P, TT>), grid, dim3(256), 0, s, m, dy, int(t), dy_stride, dx, dx_stride, int(t_tiles), \
                                              int(k_tiles), p.n_per_split, parts, group_shift(group))
-    if (p.direct) { if (parts) LPMM_DX_DIRECT(true); else LPMM_DX_DIRECT(false); }
+    if (p.direct && p.bt == 256) LPMM_DX_DIRECT(false, 4);          // as many tiles need no splits
+    else if (p.direct) { if (parts) LPMM_DX_DIRECT(true, 2); else LPMM_DX_DIRECT(false, 2); }
     else if (bf16) LPMM_DX(true, 2, 1);
     else LPMM_DX(false, 4, 1);
 #undef LPMM_DX_DIRECT

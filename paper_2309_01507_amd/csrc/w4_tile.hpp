@@ -119,12 +119,12 @@ struct Stage {
 // A workgroup of WN x WT waves takes WN NT 32 rows of W and WT TT 32 tokens.  x goes through LDS in runs of 128; codes
 // go from memory into the registers of the waves that use them and are converted there.  Each group's products are summed from 0 and
 // join the total with one multiply-add by the scale.
-template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
+template <bool BF16, int GROUP, int WN, int WT, int NT, int TT, int BUFFERS>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                       int64_t y_stride, int n_tiles, int t_tiles) {
     constexpr int TERMS = kW4Terms<BF16>, THREADS = 64 * WN * WT, BN = WN * NT * 32, BT = WT * TT * 32;
     typedef Stage<BF16, BT, 4, THREADS> StageX;
-    __shared__ uint4 s_x[2][TERMS * StageX::kPieces];
+    __shared__ uint4 s_x[BUFFERS][TERMS * StageX::kPieces];
     int n_tile, t_tile;
     if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
             stage.load(x, x_stride, t0, t, (run + 1) * kW4Chunk, m.k);
             load_w(run + 1);
         }
-        const uint4* lds = s_x[run & 1];
+        const uint4* lds = s_x[run & (BUFFERS - 1)];
         f32x16 part[TT][NT];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
@@ -202,11 +202,15 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
 #pragma unroll
                     for (int b = 0; b < NT; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            acc[a][b][i] = __builtin_fmaf(s_now[b][s * 16 / GROUP], part[a][b][i], acc[a][b][i]);
+                        for (int i = 0; i < 16; ++i) {
+                            float sum = __builtin_fmaf(s_now[b][s * 16 / GROUP], part[a][b][i], acc[a][b][i]);
+                            if (GROUPS > 1) asm volatile("" : "+v"(sum));      // here: further down the sums of all groups would be held
+                            acc[a][b][i] = sum;
+                        }
             }
         }
-        if (more) stage.store(s_x[(run + 1) & 1]);
+        if (BUFFERS == 1) __syncthreads();                     // read before it is written
+        if (more) stage.store(s_x[(run + 1) & (BUFFERS - 1)]);
         __syncthreads();
     }
 #pragma unroll
@@ -625,8 +629,11 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
 #pragma unroll
                     for (int b = 0; b < NT; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            sum[s * 16 / GROUP][b][i] = __builtin_fmaf(part[b][i], d[b][i], sum[s * 16 / GROUP][b][i]);
+                        for (int i = 0; i < 16; ++i) {
+                            float total = __builtin_fmaf(part[b][i], d[b][i], sum[s * 16 / GROUP][b][i]);
+                            if (GROUPS > 1) asm volatile("" : "+v"(total));
+                            sum[s * 16 / GROUP][b][i] = total;
+                        }
                 }
             }
         }
@@ -900,17 +907,17 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
 
 // The same for bf16 tokens on 16-byte boundaries and rows of W in whole steps of 32: dy straight into LDS, value * scale as it stands in W, so that
 // a lane converts a word at a time; the transposition is the reads'.
-template <bool PARTS>
+template <bool PARTS, int TT>
 __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx, int64_t dx_stride,
                                                            int t_tiles, int k_tiles, int n_per_split, float* parts, int group_shift) {
-    constexpr int STEP = 32, TT = 4, KT = 2;                   // rows of W of a step; tiles of a wave: 128 tokens by 64 inputs
-    typedef StageDirect<256, 2, 4> StageD;                     // 256 tokens, 32 rows of W
+    constexpr int STEP = 32, KT = 2;                           // rows of W of a step; tiles of a wave: 32 TT tokens by 64 inputs
+    typedef StageDirect<64 * TT, 2, 4> StageD;                 // tokens by 32 rows of W
     constexpr int WPIECES = STEP << 4;                         // of 128 inputs
     __shared__ uint4 s_d0[StageD::kPieces], s_d1[StageD::kPieces], s_w0[WPIECES], s_w1[WPIECES];
     int t_tile, k_tile;
     if (!tile_of(blockIdx.x, t_tiles, k_tiles, t_tile, k_tile)) return;
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
-    const int t0 = t_tile * 256, tw = (wave & 1) * 128, kw = (wave >> 1) * 64;
+    const int t0 = t_tile * (64 * TT), tw = (wave & 1) * (32 * TT), kw = (wave >> 1) * 64;
     const int first = blockIdx.y * n_per_split, last = min(m.n, first + n_per_split);
     StageD stage_d;
     stage_d.setup(static_cast<const char*>(dy) + int64_t(t0) * dy_stride * 2, dy_stride * 2, t - t0, wave);
