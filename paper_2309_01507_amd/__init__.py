@@ -24,3 +24,4 @@ from .binding import (  # noqa: F401
     lpmm_w4_linear_dscale, lpmm_distill_loss, lpmm_distill_grad, lpmm_distill_loss_grad, DISTILL_MAX_SLOTS, F32, BF16,
 )
 from .optim import AdamW4bit, SGDM4bit  # noqa: F401,E402
+from .w4 import W4Linear, w4_linear, distill_loss  # noqa: F401,E402

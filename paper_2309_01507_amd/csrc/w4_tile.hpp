@@ -701,6 +701,7 @@ __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const
     f32x16 acc[NT][KT] = {};
     auto step = [&](bool more, int tok, const uint4* now_d, const uint4* now_x, uint4* next_d, uint4* next_x) {
         if (more) load(tok + STEP, next_d, next_x);
+        __builtin_amdgcn_sched_barrier(0);                     // requested here, not at the step's end
 #pragma unroll
         for (int s = 0; s < STEP / 16; ++s) {
             bf16x8 a[NT], b[KT];
@@ -951,6 +952,7 @@ __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const voi
     f32x16 acc[TT][KT] = {};
     auto step = [&](bool more, int n, const uint4* now_d, const uint4* now_w, uint4* next_d, uint4* next_w) {
         if (more) load(n + STEP, next_d);
+        __builtin_amdgcn_sched_barrier(0);                     // requested here, not at the step's end
 #pragma unroll
         for (int s = 0; s < STEP / 16; ++s) {
             bf16x8 a[TT], b[KT];
