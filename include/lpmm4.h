@@ -473,12 +473,13 @@ int lpmm_adamw4_plan_launches(const void* plan);
  *           place (d % 4) * 4 + d / 4.  16-byte aligned.
  * In the calls below a tensor of rows has unit stride along a row and `..._stride` elements from one row to the next (at least
  * the row's length), LPMM_F32 or LPMM_BF16 elements, and needs no more than its elements' alignment; outputs must not
- * overlap inputs.  Products are summed in fp32.  t == 0 is allowed and does nothing (the scales' gradient is then 0).
+ * overlap inputs.  Products are summed in fp32, each group before its scale is applied; what a group of x and codes adds up to must
+ * be within fp32's range for that.  t is below 2^24; t == 0 is allowed and does nothing (the scales' gradient is then 0).
  * No call needs lpmm_adamw4_init.  NaN and infinities are carried through as the formulas do. */
 #define LPMM_F32  0
 #define LPMM_BF16 1
 
-/* Bytes of {codes, scales}.  shape = {n, k}; both below 2^31, with n * kp at most 2^37. */
+/* Bytes of {codes, scales}.  shape = {n, k}; both at most 2^30, with n * kp at most 2^34. */
 int lpmm_w4_sizes(const int64_t shape[2], int group, size_t sizes[2]);
 
 /* Compress: scale = max|w| / 6 of the group (one fp32 division; 0 where the maximum is below 2^-100), code = the entry

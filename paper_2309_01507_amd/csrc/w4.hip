@@ -14,9 +14,9 @@ namespace {
 
 using namespace lpmm;
 
-constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1 - 2 * kW4Chunk;
-constexpr int64_t kMaxVocabulary = int64_t(1) << 30;
-constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxDim = int64_t(1) << 30;
+// A launch has fewer than 2^32 threads
+constexpr int64_t kMaxTokens = (int64_t(1) << 24) - 1, kMaxWeights = int64_t(1) << 34, kMaxBlocks = (int64_t(1) << 23) - 1;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int group_shift(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
@@ -26,7 +26,7 @@ int check_w4(const int64_t* shape, int group, W4Mat* m) {
     if (!shape || (group != 32 && group != 64 && group != 128)) return LPMM_EINVAL;
     if (shape[0] < 1 || shape[1] < 1 || shape[0] > kMaxDim || shape[1] > kMaxDim) return LPMM_EINVAL;
     const int64_t kp = div_up(shape[1], kW4Chunk) * kW4Chunk;
-    if (shape[0] > (int64_t(1) << 37) / kp) return LPMM_EINVAL;
+    if (shape[0] > kMaxWeights / kp) return LPMM_EINVAL;
     m->n = int(shape[0]);
     m->k = int(shape[1]);
     m->words = int(kp / 8);
@@ -37,7 +37,7 @@ int check_w4(const int64_t* shape, int group, W4Mat* m) {
 // `rows` rows of `len` elements, `stride` apart
 int check_rows(const void* p, int dtype, int64_t rows, int64_t len, int64_t stride) {
     if (dtype != LPMM_F32 && dtype != LPMM_BF16) return LPMM_EINVAL;
-    if (rows < 0 || rows > kMaxTokens || stride < len || stride > (int64_t(1) << 40)) return LPMM_EINVAL;
+    if (rows < 0 || rows > kMaxDim || stride < len || stride > (int64_t(1) << 40)) return LPMM_EINVAL;
     if (rows > 0 && (!p || !aligned(p, elem_size(dtype)))) return LPMM_EINVAL;
     return LPMM_OK;
 }
@@ -55,7 +55,7 @@ int check_workspace(const void* p, size_t have, size_t need) {
 
 int check_distill(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
                   const int64_t* index, int slots, float tau, DistillArgs* a) {
-    if (v < 1 || v > kMaxVocabulary || slots < 1 || slots > LPMM_DISTILL_MAX_SLOTS) return LPMM_EINVAL;
+    if (t > kMaxTokens || v < 1 || v > kMaxDim || slots < 1 || slots > LPMM_DISTILL_MAX_SLOTS) return LPMM_EINVAL;
     if (!std::isfinite(tau) || !(tau > 0.0f) || !std::isfinite(1.0f / tau)) return LPMM_EINVAL;
     LPMM_TRY(check_rows(z, z_dtype, t, v, z_stride));
     if (t > 0 && (check_floats(top) || !index || !aligned(index, 8))) return LPMM_EINVAL;
@@ -176,9 +176,14 @@ bool dx_aligned(const void* dy, int dtype, int64_t dy_stride, const W4Mat& m) {
 DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     DxPlan p{};
     p.direct = aligned_rows && t > 128;
-    p.bt = p.direct ? (div_up(t, 256) * div_up(m.k, kW4Chunk) >= 512 ? 256 : 128) : bf16 ? 64 : 128;
+    p.bt = p.direct ? (div_up(t, 256) * div_up(m.k, kW4Chunk) >= 512 ? 256 : 128)
+         : !bf16 && div_up(t, 128) * div_up(m.k, kW4Chunk) >= 256 ? 128 : 64;
     const int64_t steps = div_up(m.n, kDxStep);
-    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), div_up(steps, 2), 512);
+    // A step takes a workgroup about 0.9 us (fp32: 2), each further split the join 0.2 us and the time of writing and reading a part at 3 TB/s
+    // (333 x 2304 x 768 bf16: 18 splits 21 us, 5 splits 15)
+    const double step_us = bf16 ? 0.9 : 2.0, split_us = 0.2 + double(t) * m.k * 8 / 3e6;
+    const int64_t worth = std::max<int64_t>(1, int64_t(std::sqrt(double(steps) * step_us / split_us)));
+    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), std::min(div_up(steps, 2), worth), 512);
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
     p.splits = int(div_up(m.n, p.n_per_split));
     return p;
@@ -242,6 +247,7 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
                    const int64_t shape[2], int group, void* y, int64_t y_stride, void* stream) {
     W4Mat m{};
     LPMM_TRY(check_w4(shape, group, &m));
+    if (t > kMaxTokens) return LPMM_EINVAL;
     LPMM_TRY(check_rows(x, dtype, t, m.k, x_stride));
     LPMM_TRY(check_rows(y, dtype, t, m.n, y_stride));
     LPMM_TRY(check_codes(codes));
@@ -250,7 +256,6 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     m.codes = reinterpret_cast<const uint32_t*>(codes);
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int esize = elem_size(dtype);
     // 16-byte boundaries, whole runs, offsets within a tile below 2^31
     const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22) && m.k < (1 << 22);
     // Tiles of 64 x 64 with the runs split among a workgroup's waves while there are no more than two for each CU (4096 x 4096, us, with these and
@@ -267,7 +272,7 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     if (t > 64 && direct) {
         const int64_t n_tiles = div_up(m.n, 128), t_tiles = div_up(t, 128);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
-        if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+        if (blocks > kMaxBlocks) return LPMM_EINVAL;
 #define LPMM_DIRECT(G) hipLaunchKernelGGL((w4_linear_direct_kernel<G, 2, 2, 2, 2>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, \
                                           int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
         if (group == 32) LPMM_DIRECT(32); else if (group == 64) LPMM_DIRECT(64); else LPMM_DIRECT(128);
@@ -275,12 +280,12 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
+    const bool bf16 = dtype == LPMM_BF16;
     if (t > 64) {
         // bf16: two buffers; fp32, three times as large: one, and several workgroups a CU
-        const bool bf16 = dtype == LPMM_BF16;
         const int64_t n_tiles = div_up(m.n, bf16 ? 256 : 128), t_tiles = div_up(t, bf16 ? 128 : 64);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
-        if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+        if (blocks > kMaxBlocks) return LPMM_EINVAL;
 #define LPMM_TILE(B, G, WN, TT, BUF) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, WN, 2, 2, TT, BUF>), dim3(unsigned(blocks)), dim3(128 * WN), 0, s, m, x, \
                                                         int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
         if (bf16) {
@@ -292,29 +297,34 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
-    // 16, 32 or 64 tokens a workgroup; as many runs a wave as cover a row with 8 waves, up to what registers hold; 16 waves for longer rows
-    const int mt = t <= 16 ? 1 : t <= 32 || dtype == LPMM_F32 ? 2 : 4, runs = m.words / 16;
-    constexpr int64_t kTokens = 16 * 32768;              // of a launch: grid.y
-    for (int64_t at = 0; at < t; at += kTokens) {
-        const int part = int(std::min(kTokens, t - at));
-        const void* xp = static_cast<const char*>(x) + at * x_stride * esize;
-        void* yp = static_cast<char*>(y) + at * y_stride * esize;
-        const int64_t tiles = div_up(m.n, 16), groups_t = div_up(part, 16 * mt);
+    // At most 64 tokens: 16, 32 or 64 a workgroup; as many runs a wave as cover a row with 8 or 16 waves, up to what registers hold
+    // (S waves a SIMD; E: the next tile's codes ahead of this one's products)
+    const int mt = t <= 16 ? 1 : t <= 32 || !bf16 ? 2 : 4, runs = m.words / 16;
+    const int64_t tiles = div_up(m.n, 16), groups_t = div_up(t, 16 * mt);
 #define LPMM_FEW(B, G, MT, W, A, S, E) hipLaunchKernelGGL((w4_linear_kernel<B, G, MT, W, A, S, E>), dim3(unsigned(std::min<int64_t>(tiles, 256 * 4 * S / W)), \
-                                                          unsigned(groups_t)), dim3(64 * W), 0, s, m, xp, part, x_stride, yp, y_stride)
+                                                          unsigned(groups_t)), dim3(64 * W), 0, s, m, x, int(t), x_stride, y, y_stride)
 #define LPMM_FEW_G(B, MT, W, A, S, E) { if (group == 32) LPMM_FEW(B, 32, MT, W, A, S, E); else if (group == 64) LPMM_FEW(B, 64, MT, W, A, S, E); else LPMM_FEW(B, 128, MT, W, A, S, E); }
-        if (dtype == LPMM_BF16) {
-            if (mt == 1) { if (runs <= 8) LPMM_FEW_G(true, 1, 8, 1, 4, true) else if (runs <= 16) LPMM_FEW_G(true, 1, 8, 2, 4, true) else LPMM_FEW_G(true, 1, 16, 2, 4, true) }
-            else if (mt == 2) { if (runs <= 8) LPMM_FEW_G(true, 2, 8, 1, 4, true) else LPMM_FEW_G(true, 2, 16, 1, 4, true) }
-            else LPMM_FEW_G(true, 4, 8, 1, 2, true)
+    if (bf16) {
+        if (mt == 1) {
+            if (runs <= 8) LPMM_FEW_G(true, 1, 8, 1, 4, true)
+            else if (runs <= 16) LPMM_FEW_G(true, 1, 8, 2, 4, true)
+            else LPMM_FEW_G(true, 1, 16, 2, 4, true)
+        } else if (mt == 2) {
+            if (runs <= 8) LPMM_FEW_G(true, 2, 8, 1, 4, true)
+            else LPMM_FEW_G(true, 2, 16, 1, 4, true)
         } else {
-            if (mt == 1) { if (runs <= 8) LPMM_FEW_G(false, 1, 8, 1, 4, true) else if (runs <= 16) LPMM_FEW_G(false, 1, 16, 1, 4, true) else { if (tiles >= 1024) LPMM_FEW_G(false, 1, 8, 4, 2, false) else LPMM_FEW_G(false, 1, 16, 1, 4, true) } }
-            else LPMM_FEW_G(false, 2, 8, 1, 2, true)
+            LPMM_FEW_G(true, 4, 8, 1, 2, true)
         }
+    } else if (mt == 1) {
+        if (runs <= 8) LPMM_FEW_G(false, 1, 8, 1, 4, true)
+        else if (runs > 16 && tiles >= 1024) LPMM_FEW_G(false, 1, 8, 4, 2, false)      // 7 x 32000 x 4096, groups of 64: 53 us, with (16, 1, 4) 66
+        else LPMM_FEW_G(false, 1, 16, 1, 4, true)                                      // 1 x 4096 x 4096: 9 us, with (16, 2, 4) 17
+    } else {
+        LPMM_FEW_G(false, 2, 8, 1, 2, true)
+    }
 #undef LPMM_FEW_G
 #undef LPMM_FEW
-        LPMM_HIP(hipGetLastError());
-    }
+    LPMM_HIP(hipGetLastError());
     return LPMM_OK;
 }
 
@@ -330,6 +340,7 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
                       size_t workspace_bytes, void* stream) {
     W4Mat m{};
     LPMM_TRY(check_w4(shape, group, &m));
+    if (t > kMaxTokens) return LPMM_EINVAL;
     LPMM_TRY(check_rows(dy, dtype, t, m.n, dy_stride));
     LPMM_TRY(check_rows(dx, dtype, t, m.k, dx_stride));
     LPMM_TRY(check_codes(codes));
@@ -342,7 +353,7 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int64_t t_tiles = div_up(t, p.bt), k_tiles = div_up(m.k, kW4Chunk), blocks = div_up(t_tiles * k_tiles, 8) * 8;
-    if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+    if (blocks > kMaxBlocks) return LPMM_EINVAL;
     float* parts = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
     const dim3 grid(unsigned(blocks), unsigned(p.splits));
 #define LPMM_DX(B, WT, TT) hipLaunchKernelGGL((w4_dx_tile_kernel<B, WT, TT>), grid, dim3(128 * WT), 0, s, m, dy, \
@@ -353,7 +364,8 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
     if (p.direct && p.bt == 256) LPMM_DX_DIRECT(false, 4);          // as many tiles need no splits
     else if (p.direct) { if (parts) LPMM_DX_DIRECT(true, 2); else LPMM_DX_DIRECT(false, 2); }
     else if (bf16) LPMM_DX(true, 2, 1);
-    else LPMM_DX(false, 4, 1);
+    else if (p.bt == 128) LPMM_DX(false, 4, 1);
+    else LPMM_DX(false, 2, 1);
 #undef LPMM_DX_DIRECT
 #undef LPMM_DX
     LPMM_HIP(hipGetLastError());
@@ -378,6 +390,7 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
                           size_t workspace_bytes, void* stream) {
     W4Mat m{};
     LPMM_TRY(check_w4(shape, group, &m));
+    if (t > kMaxTokens) return LPMM_EINVAL;
     LPMM_TRY(check_rows(x, dtype, t, m.k, x_stride));
     LPMM_TRY(check_rows(dy, dtype, t, m.n, dy_stride));
     LPMM_TRY(check_codes(codes));
@@ -386,7 +399,7 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
     m.codes = reinterpret_cast<const uint32_t*>(codes);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int64_t n_tiles = div_up(m.n, kDscaleRows), blocks = div_up(n_tiles * (m.words / 16), 8) * 8;
-    if (blocks > 0x7FFFFFFF) return LPMM_EINVAL;
+    if (blocks > kMaxBlocks) return LPMM_EINVAL;
     int splits = dscale_splits(t, m);
     const int per = int(div_up(div_up(t, kDscaleTokens), splits)) * kDscaleTokens;
     splits = std::max(1, int(div_up(t, std::max(per, 1))));
@@ -422,7 +435,7 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
 }
 
 size_t lpmm_distill_workspace_bytes(int64_t t, int64_t v) {
-    if (t < 1 || t > kMaxTokens || v < 1 || v > kMaxVocabulary) return 0;
+    if (t < 1 || t > kMaxTokens || v < 1 || v > kMaxDim) return 0;
     const int spans = std::max(distill_spans(t, v, 2), distill_spans(t, v, 4));
     return spans > 1 ? size_t(t) * spans * sizeof(float2) : 0;
 }

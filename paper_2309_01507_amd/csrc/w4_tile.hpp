@@ -273,10 +273,6 @@ struct StageDirect {
             off[j] = uint32_t(r) * uint32_t(stride) + ((TR ? lds_piece_tr(LOG, r, o) : lds_piece<LOG>(r, o)) - (r << LOG)) * 16;   // involutions
         }
     }
-    // other rows of the same matrix: `first` has moved
-    __device__ __forceinline__ void move(const void* first, int64_t stride, int64_t rows) {
-        buffer.set(first, rows < ROWS ? rows * stride : ROWS * stride);
-    }
     // at: bytes from a row's start
     __device__ __forceinline__ void load(int at, uint4* lds, int wave) const {
 #pragma unroll
@@ -458,13 +454,18 @@ __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const 
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][run * GROUPS + g];
     };
-    auto step = [&](int run, const uint4* now, uint4* next) {
+    auto step = [&](bool more, int run, const uint4* now, uint4* next) {
+        // No barrier here: this run's loads have landed and the last one's reads are done, before the next one's loads go out.  Nothing crosses.
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_sched_barrier(0);
         float scale[NT][GROUPS];
 #pragma unroll
         for (int b = 0; b < NT; ++b)
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) scale[b][g] = sc[b][g];
-        if (run + WAVES < runs) load(run + WAVES, next);
+        if (more) load(run + WAVES, next);
+        __builtin_amdgcn_sched_barrier(0);
         const uint4* now_w = now + StageX::kPieces;
         uint4 q[NT][2];
 #pragma unroll
@@ -501,10 +502,15 @@ __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const 
             }
         }
     };
-    if (wave < runs) load(wave, s_a[wave]);
-    for (int run = wave; run < runs; run += 2 * WAVES) {
-        step(run, s_a[wave], s_b[wave]);
-        if (run + WAVES < runs) step(run + WAVES, s_b[wave], s_a[wave]);
+    if (wave < runs) {
+        load(wave, s_a[wave]);
+        int run = wave;
+        for (; run + 2 * WAVES < runs; run += 2 * WAVES) {     // no conditions here: a load that may not have been made is waited for with all others
+            step(true, run, s_a[wave], s_b[wave]);
+            step(true, run + WAVES, s_b[wave], s_a[wave]);
+        }
+        step(run + WAVES < runs, run, s_a[wave], s_b[wave]);
+        if (run + WAVES < runs) step(false, run + WAVES, s_b[wave], s_a[wave]);
     }
     // sums through LDS: the wave's part of s_a is free, but loads into it may still be on their way
     __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);              // vmcnt(0)
@@ -525,6 +531,31 @@ __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const 
         const int n = n0 + b * 32 + col, tok = t0 + a * 32 + mfma32_row(i, half);
         if (n < m.n && tok < t) w4_store1<true>(y, int64_t(tok) * y_stride + n, v);
     }
+}
+
+// Sum over the 32 columns of a result tile: lane l of a half gets that of element l % 16.  Each step hands half of a lane's values to its partner
+// and takes the partner's share of the others: 45 operations, where summing up each value in all lanes takes 80 and 16 exchanges through LDS.
+__device__ __forceinline__ float sum_columns(f32x16 v) {
+    const int lane = threadIdx.x & 63;
+    float a[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) a[e] = v[e];
+    const bool b3 = lane & 8, b2 = lane & 4, b1 = lane & 2, b0 = lane & 1;
+#define LPMM_FOLD(BIT, HALF, CTRL) \
+    for (int e = 0; e < HALF; ++e) { \
+        const float keep = BIT ? a[e + HALF] : a[e], send = BIT ? a[e] : a[e + HALF]; \
+        a[e] = keep + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(send), CTRL, 0xF, 0xF, false)); \
+    }
+#pragma unroll
+    LPMM_FOLD(b3, 8, 0x140)                                    // with lane 15 - i of 16
+#pragma unroll
+    LPMM_FOLD(b2, 4, 0x141)                                    // with lane 7 - i of 8
+#pragma unroll
+    LPMM_FOLD(b1, 2, 0x4E)                                     // with lane i ^ 2
+#pragma unroll
+    LPMM_FOLD(b0, 1, 0xB1)                                     // with lane i ^ 1
+#undef LPMM_FOLD
+    return a[0] + __shfl_xor(a[0], 16);
 }
 
 // ---- gradient of the scales ---------------------------------------------------------------------------------------------------------
@@ -643,17 +674,10 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-        for (int b = 0; b < NT; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float v = sum[g][b][i];
-                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0xB1, 0xF, 0xF, false));
-                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x4E, 0xF, 0xF, false));
-                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x141, 0xF, 0xF, false));
-                v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x140, 0xF, 0xF, false));
-                v += __shfl_xor(v, 16);
-                if (col == 0) s_sum[wave / WN][g][nw + b * 32 + mfma32_row(i, half)] = v;
-            }
+        for (int b = 0; b < NT; ++b) {
+            const float v = sum_columns(sum[g][b]);
+            if (col < 16) s_sum[wave / WN][g][nw + b * 32 + mfma32_row(col, half)] = v;
+        }
     __syncthreads();
     for (int id = threadIdx.x; id < GROUPS * BN; id += THREADS) {
         const int g = id % GROUPS, n = id / GROUPS, at = run * GROUPS + g;
@@ -735,42 +759,41 @@ __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const
     stage_w.load(0, s_d0, wave);
     __syncthreads();
     const int shift = (col & 7) * 4;
-    bool in[KT];
+    uint32_t in[KT];                                           // mask: inputs beyond the row's end
     int place[KT];
 #pragma unroll
     for (int j = 0; j < KT; ++j) {
-        in[j] = k0 + kw + j * 32 + col < m.k;
+        in[j] = k0 + kw + j * 32 + col < m.k ? 0xFFFFFFFFu : 0u;
         place[j] = w4_place((kw + j * 32 + col) >> 3);
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < NT; ++i) {
+        f32x16 v[KT];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int row = nw + i * 32 + mfma32_row(e, half), n = n0 + row;
-            float v[KT];
+        for (int j = 0; j < KT; ++j)
 #pragma unroll
-            for (int j = 0; j < KT; ++j) {
+            for (int e = 0; e < 16; ++e) {
+                const int row = nw + i * 32 + mfma32_row(e, half);
                 const uint32_t word = reinterpret_cast<const uint32_t*>(s_d0 + lds_piece<2>(row, place[j] >> 2))[place[j] & 3];
                 const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word >> shift, 1.0f, 0);
-                v[j] = in[j] ? acc[i][j][e] * c.x : 0.0f;
+                v[j][e] = __uint_as_float(__float_as_uint(acc[i][j][e] * c.x) & in[j]);
             }
-            if constexpr (GROUP > 32) v[0] += v[1];
+        if constexpr (GROUP > 32) {
 #pragma unroll
-            for (int j = 0; j < (GROUP > 32 ? 1 : KT); ++j) {
-                float sum = v[j];
-                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0xB1, 0xF, 0xF, false));
-                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0x4E, 0xF, 0xF, false));
-                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0x141, 0xF, 0xF, false));
-                sum += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(sum), 0x140, 0xF, 0xF, false));
-                sum += __shfl_xor(sum, 16);
-                if (GROUP == 128) {
-                    if (col == 0) s_sum[wave >> 1][row] = sum;
-                } else {
-                    const int at = (k0 + kw + j * 32) / GROUP;
-                    if (col == 0 && n < m.n && at < m.groups) out[int64_t(blockIdx.y) * out_split + int64_t(n) * m.groups + at] = sum;
-                }
+            for (int e = 0; e < 16; ++e) v[0][e] += v[1][e];
+        }
+        const int row = nw + i * 32 + mfma32_row(col & 15, half), n = n0 + row;
+#pragma unroll
+        for (int j = 0; j < (GROUP > 32 ? 1 : KT); ++j) {
+            const float sum = sum_columns(v[j]);
+            if (GROUP == 128) {
+                if (col < 16) s_sum[wave >> 1][row] = sum;
+            } else {
+                const int at = (k0 + kw + j * 32) / GROUP;
+                if (col < 16 && n < m.n && at < m.groups) out[int64_t(blockIdx.y) * out_split + int64_t(n) * m.groups + at] = sum;
             }
         }
+    }
     if constexpr (GROUP == 128) {
         __syncthreads();
         const int n = n0 + int(threadIdx.x);
