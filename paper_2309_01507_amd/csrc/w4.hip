@@ -257,19 +257,25 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
     // 16-byte boundaries, whole runs, offsets within a tile below 2^31
+    constexpr int kFew = 16;                             // tokens
     const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22) && m.k < (1 << 22);
-    // Tiles of 64 x 64 with the runs split among a workgroup's waves while there are no more than two for each CU (4096 x 4096, us, with these and
-    // with tiles of 128 x 128: 64 tokens 14 and 32, 256 15 and 33, 512 27 and 36, 768 42 and 36)
-    if (t > 32 && direct && div_up(m.n, 64) * div_up(t, 64) <= 512) {
-        const int64_t n_tiles = div_up(m.n, 64), t_tiles = div_up(t, 64), blocks = div_up(n_tiles * t_tiles, 8) * 8;
-#define LPMM_SPLIT(G) hipLaunchKernelGGL((w4_linear_split_kernel<G, 2, 2>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, y, \
-                                         y_stride, int(n_tiles), int(t_tiles))
-        if (group == 32) LPMM_SPLIT(32); else if (group == 64) LPMM_SPLIT(64); else LPMM_SPLIT(128);
+    // The runs split among a workgroup's waves while tiles of 64 x 64 are no more than two for each CU; smaller tiles while they leave CUs idle
+    // (4096 x 4096, us, tiles of 128 x 128, 64 x 64, 64 rows x 32 tokens, 32 x 32: 64 tokens 32, 14, 8.8, 6.7; 100 33, 14, 9.2, 11;
+    // 256 33, 15, 17, 19; 512 36, 27, 33, 37; 768 36, 42)
+    const auto tiles_of = [&](int rows, int tokens) { return div_up(m.n, rows) * div_up(t, tokens); };
+    if (t > kFew && direct && tiles_of(64, 64) <= 512) {
+        const bool n32 = tiles_of(32, 32) <= 256, t32 = tiles_of(64, 32) <= 256;
+        const int64_t n_tiles = div_up(m.n, n32 ? 32 : 64), t_tiles = div_up(t, t32 ? 32 : 64), blocks = div_up(n_tiles * t_tiles, 8) * 8;
+#define LPMM_SPLIT(G, NT, TT) hipLaunchKernelGGL((w4_linear_split_kernel<G, NT, TT>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, \
+                                                 y, y_stride, int(n_tiles), int(t_tiles))
+#define LPMM_SPLIT_G(NT, TT) { if (group == 32) LPMM_SPLIT(32, NT, TT); else if (group == 64) LPMM_SPLIT(64, NT, TT); else LPMM_SPLIT(128, NT, TT); }
+        if (n32) LPMM_SPLIT_G(1, 1) else if (t32) LPMM_SPLIT_G(2, 1) else LPMM_SPLIT_G(2, 2)
+#undef LPMM_SPLIT_G
 #undef LPMM_SPLIT
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
-    if (t > 64 && direct) {
+    if (t > kFew && direct) {
         const int64_t n_tiles = div_up(m.n, 128), t_tiles = div_up(t, 128);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > kMaxBlocks) return LPMM_EINVAL;
@@ -281,7 +287,24 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         return LPMM_OK;
     }
     const bool bf16 = dtype == LPMM_BF16;
-    if (t > 64) {
+    // Elsewhere (us, fp32 with groups of 32: few rows' kernel, runs shared by waves with 32 and 64 rows of W, tiles of 128 x 64): 32 x 4096 x 4096 19, 26, 35;
+    // 64 x 4096 x 4096 37, 27, 36; 32 x 32000 x 4096 140, 78, 57; 100 x 4096 x 4096 -, 39, 37, 90; 512 x 4096 x 4096 -, 140, 106, 95; 77 x 50257 x 1024 -,
+    // 82, 68, 64
+    if (t > 32 ? t <= 64 || tiles_of(64, 32) <= 768 : t > kFew && tiles_of(64, 32) > 128) {
+        const bool n32 = tiles_of(32, 32) <= 256;
+        const int64_t n_tiles = div_up(m.n, n32 ? 32 : 64), t_tiles = div_up(t, 32), blocks = div_up(n_tiles * t_tiles, 8) * 8;
+        if (blocks > kMaxBlocks) return LPMM_EINVAL;
+#define LPMM_SHARE(B, G, NT) hipLaunchKernelGGL((w4_linear_share_kernel<B, G, NT>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, \
+                                                y, y_stride, int(n_tiles), int(t_tiles))
+#define LPMM_SHARE_G(B, NT) { if (group == 32) LPMM_SHARE(B, 32, NT); else if (group == 64) LPMM_SHARE(B, 64, NT); else LPMM_SHARE(B, 128, NT); }
+        if (bf16) { if (n32) LPMM_SHARE_G(true, 1) else LPMM_SHARE_G(true, 2) }
+        else { if (n32) LPMM_SHARE_G(false, 1) else LPMM_SHARE_G(false, 2) }
+#undef LPMM_SHARE_G
+#undef LPMM_SHARE
+        LPMM_HIP(hipGetLastError());
+        return LPMM_OK;
+    }
+    if (t > 32) {
         // bf16: two buffers; fp32, three times as large: one, and several workgroups a CU
         const int64_t n_tiles = div_up(m.n, bf16 ? 256 : 128), t_tiles = div_up(t, bf16 ? 128 : 64);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
@@ -297,23 +320,22 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
-    // At most 64 tokens: 16, 32 or 64 a workgroup; as many runs a wave as cover a row with 8 or 16 waves, up to what registers hold
+    // At most 32 tokens: 16 or 32 a workgroup; as many runs a wave as cover a row with 8 or 16 waves, up to what registers hold
     // (S waves a SIMD; E: the next tile's codes ahead of this one's products)
-    const int mt = t <= 16 ? 1 : t <= 32 || !bf16 ? 2 : 4, runs = m.words / 16;
-    const int64_t tiles = div_up(m.n, 16), groups_t = div_up(t, 16 * mt);
-#define LPMM_FEW(B, G, MT, W, A, S, E) hipLaunchKernelGGL((w4_linear_kernel<B, G, MT, W, A, S, E>), dim3(unsigned(std::min<int64_t>(tiles, 256 * 4 * S / W)), \
-                                                          unsigned(groups_t)), dim3(64 * W), 0, s, m, x, int(t), x_stride, y, y_stride)
+    const int mt = t <= 16 ? 1 : 2, runs = m.words / 16;
+    const int64_t tiles = div_up(m.n, 16);
+#define LPMM_FEW(B, G, MT, W, A, S, E) hipLaunchKernelGGL((w4_linear_kernel<B, G, MT, W, A, S, E>), dim3(unsigned(std::min<int64_t>(tiles, 256 * 4 * S / W))), \
+                                                          dim3(64 * W), 0, s, m, x, int(t), x_stride, y, y_stride)
 #define LPMM_FEW_G(B, MT, W, A, S, E) { if (group == 32) LPMM_FEW(B, 32, MT, W, A, S, E); else if (group == 64) LPMM_FEW(B, 64, MT, W, A, S, E); else LPMM_FEW(B, 128, MT, W, A, S, E); }
     if (bf16) {
         if (mt == 1) {
             if (runs <= 8) LPMM_FEW_G(true, 1, 8, 1, 4, true)
             else if (runs <= 16) LPMM_FEW_G(true, 1, 8, 2, 4, true)
             else LPMM_FEW_G(true, 1, 16, 2, 4, true)
-        } else if (mt == 2) {
-            if (runs <= 8) LPMM_FEW_G(true, 2, 8, 1, 4, true)
-            else LPMM_FEW_G(true, 2, 16, 1, 4, true)
+        } else if (runs <= 8) {
+            LPMM_FEW_G(true, 2, 8, 1, 4, true)
         } else {
-            LPMM_FEW_G(true, 4, 8, 1, 2, true)
+            LPMM_FEW_G(true, 2, 16, 1, 4, true)
         }
     } else if (mt == 1) {
         if (runs <= 8) LPMM_FEW_G(false, 1, 8, 1, 4, true)

@@ -273,7 +273,7 @@ __device__ __forceinline__ void w4_operand8(const void* p, int64_t i, int64_t en
 
 // ---- y = x W^T ---------------------------------------------------------------------------------------------------------------
 //
-// Few tokens (MT 16).  A workgroup takes tiles of 16 rows of W, one after the other; its waves share the runs of 128 in pieces of A next to each
+// At most 16 MT tokens.  A workgroup takes tiles of 16 rows of W, one after the other; its waves share the runs of 128 in pieces of A next to each
 // other and add up in LDS.  A lane's 16 bytes of codes are its operands of four 16x16x32 products: lane l holds row l % 16, and its word s
 // the elements 32 s + 8 (l / 16) .. + 7.  The operands of x stay in registers from tile to tile where the waves cover a row at once
 // (K <= 128 A WAVES); the next tile's codes are requested before this one's are used (EARLY: where registers
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(64 * WAVES, SIMD_WAVES) void w4_linear_kernel(W4Mat
     constexpr int TERMS = kW4Terms<BF16>, GROUPS = kW4Chunk / GROUP, SCALES = GROUPS * A;
     __shared__ f32x4 s_part[2][WAVES][MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-    const int tok0 = blockIdx.y * (MT * 16), tiles = (m.n + 15) >> 4, runs = m.words / 16;
+    const int tiles = (m.n + 15) >> 4, runs = m.words / 16;
     const int chunks = (runs + WAVES * A - 1) / (WAVES * A);
     uint4 q[A];
     float sc[SCALES];
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(64 * WAVES, SIMD_WAVES) void w4_linear_kernel(W4Mat
             for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int b = 0; b < MT; ++b) {
-                    const int at = ((chunk * WAVES + wave) * A + u) * kW4Chunk + s * 32 + quarter * 8, tok = tok0 + b * 16 + col;
+                    const int at = ((chunk * WAVES + wave) * A + u) * kW4Chunk + s * 32 + quarter * 8, tok = b * 16 + col;
 #pragma unroll
                     for (int j = 0; j < TERMS; ++j) a[u][s][b][j] = bf16x8{};
                     if (tok < t && at < m.k) w4_operand8<BF16>(x, int64_t(tok) * x_stride + at, int64_t(tok) * x_stride + m.k, a[u][s][b]);
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, SIMD_WAVES) void w4_linear_kernel(W4Mat
                 if (n < m.n) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int tok = tok0 + wave * 16 + quarter * 4 + i;
+                        const int tok = wave * 16 + quarter * 4 + i;
                         if (tok < t) w4_store1<BF16>(y, int64_t(tok) * y_stride + n, sum[i]);
                     }
                 }

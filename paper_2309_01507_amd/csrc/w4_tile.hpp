@@ -226,6 +226,108 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
         }
 }
 
+// The same for fewer tokens than fill the GPU with such tiles: 32 tokens by NT 32 rows of W per workgroup, whose 4 waves share the runs and join
+// their sums at the end.  Tokens and codes go from memory into the registers of the lanes that multiply them, a run ahead; nothing is staged.
+template <bool BF16, int GROUP, int NT>
+__global__ __launch_bounds__(256, 2) void w4_linear_share_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
+                                                              int n_tiles, int t_tiles) {
+    constexpr int TERMS = kW4Terms<BF16>, GROUPS = kW4Chunk / GROUP, WAVES = 4;
+    __shared__ float s_sum[WAVES][NT * 16 * 64];
+    int n_tile, t_tile;
+    if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
+    const int n0 = n_tile * NT * 32, t0 = t_tile * 32;
+    const int64_t row = int64_t(min(t0 + col, t - 1)) * x_stride;
+    const uint32_t* codes[NT];
+    const float* scales[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+        const int n = min(n0 + b * 32 + col, m.n - 1);
+        codes[b] = m.codes + int64_t(n) * m.words + half * 4;
+        scales[b] = m.scales + int64_t(n) * m.groups;
+    }
+    RawOctet<BF16> raw[8];
+    uint4 q[NT][2];
+    float sc[NT][GROUPS];
+    auto load = [&](int run) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int k = run * kW4Chunk + s * 16 + half * 8;
+            if (k < m.k) raw[s].load(x, row + k, row + m.k);
+            else raw[s].zero();
+        }
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            q[b][0] = *reinterpret_cast<const uint4*>(codes[b] + run * 16);
+            q[b][1] = *reinterpret_cast<const uint4*>(codes[b] + run * 16 + 8);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int at = run * GROUPS + g;
+                sc[b][g] = at < m.groups ? scales[b][at] : 0.0f;
+            }
+        }
+    };
+    f32x16 acc[NT] = {};
+    const int runs = m.words / 16;
+    if (wave < runs) load(wave);
+    for (int run = wave; run < runs; run += WAVES) {
+        RawOctet<BF16> now[8];
+        uint32_t w[NT][8];
+        float s_now[NT][GROUPS];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) now[s] = raw[s];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            // step s uses piece s % 2 (logical word 2 s + half), word s / 2
+            w[b][0] = q[b][0].x; w[b][1] = q[b][1].x; w[b][2] = q[b][0].y; w[b][3] = q[b][1].y;
+            w[b][4] = q[b][0].z; w[b][5] = q[b][1].z; w[b][6] = q[b][0].w; w[b][7] = q[b][1].w;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) s_now[b][g] = sc[b][g];
+        }
+        if (run + WAVES < runs) load(run + WAVES);
+        f32x16 part[NT];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            if (s * 16 % GROUP == 0) {
+#pragma unroll
+                for (int b = 0; b < NT; ++b) part[b] = f32x16{};
+            }
+            uint4 ax[TERMS];
+            now[s].terms(ax);
+#pragma unroll
+            for (int b = 0; b < NT; ++b) {
+                const bf16x8 bw = w4_codes_bf16(w[b][s]);
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) part[b] = mfma32(as_operand(ax[j]), bw, part[b]);
+            }
+            if ((s + 1) * 16 % GROUP == 0) {
+#pragma unroll
+                for (int b = 0; b < NT; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float sum = __builtin_fmaf(s_now[b][s * 16 / GROUP], part[b][i], acc[b][i]);
+                        if (GROUPS > 1) asm volatile("" : "+v"(sum));      // here: further down the sums of all groups would be held
+                        acc[b][i] = sum;
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < NT; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s_sum[wave][(b * 16 + i) * 64 + lane] = acc[b][i];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NT * 16 / WAVES; ++j) {
+        const int id = wave * (NT * 16 / WAVES) + j, i = id & 15, b = id >> 4;
+        float v = s_sum[0][id * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += s_sum[w][id * 64 + lane];
+        const int n = n0 + b * 32 + col, tok = t0 + mfma32_row(i, half);
+        if (n < m.n && tok < t) w4_store1<BF16>(y, int64_t(tok) * y_stride + n, v);
+    }
+}
+
 // ---- straight from memory into LDS -------------------------------------------------------------------------------------------------
 
 // Loads go through a buffer descriptor: the lane's part of an address is a 32-bit offset that stays, what moves is a scalar, and what lies

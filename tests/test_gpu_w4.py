@@ -152,6 +152,31 @@ def test_product_and_gradients(t, rows, cols, group, dtype):
     check_dscale(x.to(DEV), dy.to(DEV), w, values, "dscales")
 
 
+# Rows and tokens on both sides of what a launch takes small, middling and large tiles for, with rows of 1, 3, 5 and 9 runs of 128
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("t,rows,cols", [(17, 130, 384), (32, 70, 1152), (33, 4500, 640), (40, 9001, 128), (64, 9000, 384), (21, 33000, 128), (64, 33000, 384),
+                                         (100, 200, 1152), (300, 5001, 128), (700, 6000, 640)])
+def test_product_over_the_ranges_of_tiles(t, rows, cols, group, dtype, offset):
+    progress(f"w4 {t} x {rows} x {cols} group {group} {dtype} offset {offset}")
+    w, values, scales = weights(rows, cols, group, 7)
+    x = strided(activations(t, cols, dtype, 3), 8, offset)
+    check_linear(x, w, values, scales, dtype, "y")
+
+
+@pytest.mark.parametrize("group", GROUPS)
+@pytest.mark.parametrize("t,rows,cols", [(31, 300, 200), (65, 1000, 136), (400, 300, 4100), (1500, 1032, 640)])
+def test_gradient_of_the_scales_over_the_ranges_of_tiles(t, rows, cols, group):
+    progress(f"w4 dscale {t} x {rows} x {cols} group {group}")
+    w, values, _ = weights(rows, cols, group, 8)
+    for dtype, extra, offset in ((F32, 0, 0), (BF16, 8, 0), (BF16, 8, 1)):
+        extra += -cols % 8 if extra else 0
+        x = strided(activations(t, cols, dtype, 1), extra, offset)
+        dy = strided(activations(t, rows, dtype, 2, 1e-3), 8 + -rows % 8, offset)
+        check_dscale(x, dy, w, values, f"dscales {dtype} {offset}")
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("t,rows,cols,extra,offset", [(5, 48, 256, 8, 0), (5, 48, 256, 1, 0), (19, 70, 300, 3, 1), (140, 260, 384, 5, 3),
                                                       (140, 256, 384, 8, 0), (300, 520, 257, 7, 1), (1, 48, 256, 0, 1)])
