@@ -164,7 +164,9 @@ int dscale_splits(int64_t t, const W4Mat& m) {
     return splits_for(div_up(m.n, kDscaleRows) * (m.words / 16), div_up(t, kDscaleTokens), 768);
 }
 
-// The gradient of the input: large tiles of 256 tokens by 128 inputs, for few tokens small ones, the reduction split where that fills the GPU
+// The gradient of the input: tiles of 128 inputs by 256, 128 or 64 tokens, the largest that still fill the GPU, since W is converted once for a
+// tile (us: bf16 4096 x 11008 x 4096 off 16-byte boundaries 492, 562, 728; 1500 x 4096 x 4032 155, 118, 120; 512 x 4096 x 4096 68, 54, 63; 333 x 2304 x 768
+// 27, 20, 16; fp32 2048 x 4096 x 4096 -, 456, 509; 1000 x 4096 x 4096 -, 242, 258); the reduction is split where there are fewer
 struct DxPlan {
     bool direct;
     int bt, splits, n_per_split;
@@ -176,14 +178,14 @@ bool dx_aligned(const void* dy, int dtype, int64_t dy_stride, const W4Mat& m) {
 DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     DxPlan p{};
     p.direct = aligned_rows && t > 128;
-    p.bt = p.direct ? (div_up(t, 256) * div_up(m.k, kW4Chunk) >= 512 ? 256 : 128)
-         : !bf16 && div_up(t, 128) * div_up(m.k, kW4Chunk) >= 256 ? 128 : 64;
+    const int64_t k_tiles = div_up(m.k, kW4Chunk), tiles = div_up(t, 128) * k_tiles;
+    p.bt = bf16 && div_up(t, 256) * k_tiles >= 512 ? 256 : p.direct || tiles >= (bf16 ? 128 : 256) ? 128 : 64;
     const int64_t steps = div_up(m.n, kDxStep);
     // A step takes a workgroup about 0.9 us (fp32: 2), each further split the join 0.2 us and the time of writing and reading a part at 3 TB/s
     // (333 x 2304 x 768 bf16: 18 splits 21 us, 5 splits 15)
     const double step_us = bf16 ? 0.9 : 2.0, split_us = 0.2 + double(t) * m.k * 8 / 3e6;
     const int64_t worth = std::max<int64_t>(1, int64_t(std::sqrt(double(steps) * step_us / split_us)));
-    const int splits = splits_for(div_up(t, p.bt) * div_up(m.k, kW4Chunk), std::min(div_up(steps, 2), worth), 512);
+    const int splits = splits_for(div_up(t, p.bt) * k_tiles, std::min(div_up(steps, 2), worth), 512);
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
     p.splits = int(div_up(m.n, p.n_per_split));
     return p;
@@ -256,21 +258,24 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     m.codes = reinterpret_cast<const uint32_t*>(codes);
     m.scales = scales;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    // 16-byte boundaries, whole runs, offsets within a tile below 2^31
+    // 16-byte boundaries, whole octets, offsets within a tile below 2^31
     constexpr int kFew = 16;                             // tokens
-    const bool direct = dtype == LPMM_BF16 && m.k % kW4Chunk == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22) && m.k < (1 << 22);
+    const bool direct = dtype == LPMM_BF16 && m.k % 8 == 0 && aligned(x, 16) && x_stride % 8 == 0 && x_stride < (1 << 22) && m.k < (1 << 22);
     // The runs split among a workgroup's waves while tiles of 64 x 64 are no more than two for each CU; smaller tiles while they leave CUs idle
     // (4096 x 4096, us, tiles of 128 x 128, 64 x 64, 64 rows x 32 tokens, 32 x 32: 64 tokens 32, 14, 8.8, 6.7; 100 33, 14, 9.2, 11;
     // 256 33, 15, 17, 19; 512 36, 27, 33, 37; 768 36, 42)
+    const bool cut = m.k % kW4Chunk != 0;
     const auto tiles_of = [&](int rows, int tokens) { return div_up(m.n, rows) * div_up(t, tokens); };
     if (t > kFew && direct && tiles_of(64, 64) <= 512) {
         const bool n32 = tiles_of(32, 32) <= 256, t32 = tiles_of(64, 32) <= 256;
         const int64_t n_tiles = div_up(m.n, n32 ? 32 : 64), t_tiles = div_up(t, t32 ? 32 : 64), blocks = div_up(n_tiles * t_tiles, 8) * 8;
-#define LPMM_SPLIT(G, NT, TT) hipLaunchKernelGGL((w4_linear_split_kernel<G, NT, TT>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, \
+#define LPMM_SPLIT(G, NT, TT, C) hipLaunchKernelGGL((w4_linear_split_kernel<G, NT, TT, C>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, \
                                                  y, y_stride, int(n_tiles), int(t_tiles))
-#define LPMM_SPLIT_G(NT, TT) { if (group == 32) LPMM_SPLIT(32, NT, TT); else if (group == 64) LPMM_SPLIT(64, NT, TT); else LPMM_SPLIT(128, NT, TT); }
+#define LPMM_SPLIT_C(NT, TT, C) { if (group == 32) LPMM_SPLIT(32, NT, TT, C); else if (group == 64) LPMM_SPLIT(64, NT, TT, C); else LPMM_SPLIT(128, NT, TT, C); }
+#define LPMM_SPLIT_G(NT, TT) { if (cut) LPMM_SPLIT_C(NT, TT, true) else LPMM_SPLIT_C(NT, TT, false) }
         if (n32) LPMM_SPLIT_G(1, 1) else if (t32) LPMM_SPLIT_G(2, 1) else LPMM_SPLIT_G(2, 2)
 #undef LPMM_SPLIT_G
+#undef LPMM_SPLIT_C
 #undef LPMM_SPLIT
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
@@ -279,18 +284,20 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         const int64_t n_tiles = div_up(m.n, 128), t_tiles = div_up(t, 128);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > kMaxBlocks) return LPMM_EINVAL;
-#define LPMM_DIRECT(G) hipLaunchKernelGGL((w4_linear_direct_kernel<G, 2, 2, 2, 2>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, \
-                                          int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
-        if (group == 32) LPMM_DIRECT(32); else if (group == 64) LPMM_DIRECT(64); else LPMM_DIRECT(128);
+#define LPMM_DIRECT(G, C) hipLaunchKernelGGL((w4_linear_direct_kernel<G, 2, 2, 2, 2, C>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, \
+                                             int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
+#define LPMM_DIRECT_G(C) { if (group == 32) LPMM_DIRECT(32, C); else if (group == 64) LPMM_DIRECT(64, C); else LPMM_DIRECT(128, C); }
+        if (cut) LPMM_DIRECT_G(true) else LPMM_DIRECT_G(false)
+#undef LPMM_DIRECT_G
 #undef LPMM_DIRECT
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
     const bool bf16 = dtype == LPMM_BF16;
-    // Elsewhere (us, fp32 with groups of 32: few rows' kernel, runs shared by waves with 32 and 64 rows of W, tiles of 128 x 64): 32 x 4096 x 4096 19, 26, 35;
+    // Elsewhere (us, fp32 with groups of 32; the few tokens' kernel, runs shared by waves with 32 and 64 rows of W, tiles of 128 x 64): 32 x 4096 x 4096 19, 26, 35;
     // 64 x 4096 x 4096 37, 27, 36; 32 x 32000 x 4096 140, 78, 57; 100 x 4096 x 4096 -, 39, 37, 90; 512 x 4096 x 4096 -, 140, 106, 95; 77 x 50257 x 1024 -,
-    // 82, 68, 64
-    if (t > 32 ? t <= 64 || tiles_of(64, 32) <= 768 : t > kFew && tiles_of(64, 32) > 128) {
+    // 82, 68, 64.  bf16 off 16-byte boundaries, the last two: 256 x 4096 x 4096 59, 80; 300 x 4000 x 4032 78, 82; 512 x 4096 x 4096 105, 82)
+    if (t > 32 ? t <= 64 || tiles_of(64, 32) <= (bf16 ? 512 : 768) : t > kFew && tiles_of(64, 32) > 128) {
         const bool n32 = tiles_of(32, 32) <= 256;
         const int64_t n_tiles = div_up(m.n, n32 ? 32 : 64), t_tiles = div_up(t, 32), blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > kMaxBlocks) return LPMM_EINVAL;
@@ -305,16 +312,17 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         return LPMM_OK;
     }
     if (t > 32) {
-        // bf16: two buffers; fp32, three times as large: one, and several workgroups a CU
-        const int64_t n_tiles = div_up(m.n, bf16 ? 256 : 128), t_tiles = div_up(t, bf16 ? 128 : 64);
+        // 64 tokens by 256 rows of W with two buffers; fp32, whose terms take three times the room, by 128 with one; several workgroups a CU.
+        // (1000 x 4096 x 4096 bf16 off 16-byte boundaries: 54 us, with 128 tokens by 256 rows and 8 waves 88, with 128 by 128 114)
+        const int64_t n_tiles = div_up(m.n, bf16 ? 256 : 128), t_tiles = div_up(t, 64);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > kMaxBlocks) return LPMM_EINVAL;
-#define LPMM_TILE(B, G, WN, TT, BUF) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, WN, 2, 2, TT, BUF>), dim3(unsigned(blocks)), dim3(128 * WN), 0, s, m, x, \
+#define LPMM_TILE(B, G, WN, WT, TT, BUF) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, WN, WT, 2, TT, BUF>), dim3(unsigned(blocks)), dim3(64 * WT * WN), 0, s, m, x, \
                                                         int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
         if (bf16) {
-            if (group == 32) LPMM_TILE(true, 32, 4, 2, 2); else if (group == 64) LPMM_TILE(true, 64, 4, 2, 2); else LPMM_TILE(true, 128, 4, 2, 2);
+            if (group == 32) LPMM_TILE(true, 32, 4, 1, 2, 2); else if (group == 64) LPMM_TILE(true, 64, 4, 1, 2, 2); else LPMM_TILE(true, 128, 4, 1, 2, 2);
         } else {
-            if (group == 32) LPMM_TILE(false, 32, 2, 1, 1); else if (group == 64) LPMM_TILE(false, 64, 2, 1, 1); else LPMM_TILE(false, 128, 2, 1, 1);
+            if (group == 32) LPMM_TILE(false, 32, 2, 2, 1, 1); else if (group == 64) LPMM_TILE(false, 64, 2, 2, 1, 1); else LPMM_TILE(false, 128, 2, 2, 1, 1);
         }
 #undef LPMM_TILE
         LPMM_HIP(hipGetLastError());
@@ -385,6 +393,8 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
                                              int(k_tiles), p.n_per_split, parts, group_shift(group))
     if (p.direct && p.bt == 256) LPMM_DX_DIRECT(false, 4);          // as many tiles need no splits
     else if (p.direct) { if (parts) LPMM_DX_DIRECT(true, 2); else LPMM_DX_DIRECT(false, 2); }
+    else if (bf16 && p.bt == 256) LPMM_DX(true, 2, 4);
+    else if (bf16 && p.bt == 128) LPMM_DX(true, 2, 2);
     else if (bf16) LPMM_DX(true, 2, 1);
     else if (p.bt == 128) LPMM_DX(false, 4, 1);
     else LPMM_DX(false, 2, 1);

@@ -362,7 +362,7 @@ struct StageDirect {
     static constexpr int kPieces = ROWS << LOG, kOwn = kPieces / 64 / WAVES, kRowsAtOnce = 64 >> LOG;
     static_assert(kPieces % (64 * WAVES) == 0, "whole KiB per wave");
     Buffer buffer;
-    uint32_t off[kOwn];                                        // bytes
+    uint32_t off[kOwn], col[kOwn];                             // bytes
     // stride: bytes from one row to the next; rows: of the matrix from `first` on; those beyond arrive as 0
     // wave: of the WAVES
     __device__ __forceinline__ void setup(const void* first, int64_t stride, int64_t rows, int wave) {
@@ -372,7 +372,8 @@ struct StageDirect {
         for (int j = 0; j < kOwn; ++j) {
             const int r = (j * WAVES + wave) * kRowsAtOnce + (lane >> LOG);
             const int o = lane & ((1 << LOG) - 1);
-            off[j] = uint32_t(r) * uint32_t(stride) + ((TR ? lds_piece_tr(LOG, r, o) : lds_piece<LOG>(r, o)) - (r << LOG)) * 16;   // involutions
+            col[j] = ((TR ? lds_piece_tr(LOG, r, o) : lds_piece<LOG>(r, o)) - (r << LOG)) * 16;                                    // involutions
+            off[j] = uint32_t(r) * uint32_t(stride) + col[j];
         }
     }
     // at: bytes from a row's start
@@ -380,6 +381,12 @@ struct StageDirect {
 #pragma unroll
         for (int j = 0; j < kOwn; ++j)
             buffer.to_lds16(off[j], at, lds + (j * WAVES + wave) * 64);
+    }
+    // the same for rows of `end` bytes: octets beyond arrive as 0
+    __device__ __forceinline__ void load_cut(int at, int end, uint4* lds, int wave) const {
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j)
+            buffer.to_lds16(int(col[j]) < end - at ? off[j] : 0x80000000u, at, lds + (j * WAVES + wave) * 64);
     }
 };
 
@@ -411,7 +418,7 @@ __device__ __forceinline__ f32x16 opaque_zero() {
 // The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Tokens and codes are loaded straight into LDS, a run ahead;
 // a lane loads the scales of four groups at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at its
 // barrier.
-template <int GROUP, int WN, int WT, int NT, int TT>
+template <int GROUP, int WN, int WT, int NT, int TT, bool CUT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                         int64_t y_stride, int n_tiles, int t_tiles) {
     constexpr int BN = WN * NT * 32, BT = WT * TT * 32, GROUPS = kW4Chunk / GROUP, WAVES = WN * WT;
@@ -445,6 +452,10 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
             }
         }
     };
+    auto load_x = [&](int run, uint4* lds) {
+        if constexpr (CUT) stage_x.load_cut(run * (kW4Chunk * 2), m.k * 2, lds, wave);
+        else stage_x.load(run * (kW4Chunk * 2), lds, wave);
+    };
     f32x16 acc[TT][NT] = {};
     const f32x16 zero = opaque_zero();
     const int runs = m.words / 16;
@@ -454,7 +465,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
             for (int b = 0; b < NT; ++b) sc[b] = sc_next[b];
         }
         if (more) {
-            stage_x.load((run + 1) * (kW4Chunk * 2), next_x, wave);
+            load_x(run + 1, next_x);
             stage_w.load((run + 1) * (kW4Chunk / 2), next_w, wave);
             if ((run + 1) % QUAD == 0) load_scales((run + 1) * GROUPS);
         }
@@ -497,7 +508,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
         }
         __syncthreads();
     };
-    stage_x.load(0, s_x0, wave);
+    load_x(0, s_x0);
     stage_w.load(0, s_w0, wave);
     load_scales(0);
     __syncthreads();
@@ -523,7 +534,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
 
 // The same for fewer tokens than fill the GPU with such tiles: a tile of NT 32 rows of W and TT 32 tokens per workgroup, whose 4 waves share the
 // runs.  Each wave stages its own runs in its own part of LDS, one ahead, and waits for nobody until the sums are joined.
-template <int GROUP, int NT, int TT>
+template <int GROUP, int NT, int TT, bool CUT>
 __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
     constexpr int BN = NT * 32, BT = TT * 32, GROUPS = kW4Chunk / GROUP, WAVES = 4;
@@ -549,12 +560,13 @@ __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const 
     const f32x16 zero = opaque_zero();
     const int runs = m.words / 16;
     auto load = [&](int run, uint4* lds) {
-        stage_x.load(run * (kW4Chunk * 2), lds, 0);
+        if constexpr (CUT) stage_x.load_cut(run * (kW4Chunk * 2), m.k * 2, lds, 0);
+        else stage_x.load(run * (kW4Chunk * 2), lds, 0);
         stage_w.load(run * (kW4Chunk / 2), lds + StageX::kPieces, 0);
 #pragma unroll
         for (int b = 0; b < NT; ++b)
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][run * GROUPS + g];
+            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][CUT ? min(run * GROUPS + g, m.groups - 1) : run * GROUPS + g];    // beyond the last group all codes are 0
     };
     auto step = [&](bool more, int run, const uint4* now, uint4* next) {
         // No barrier here: this run's loads have landed and the last one's reads are done, before the next one's loads go out.  Nothing crosses.

@@ -165,6 +165,17 @@ def test_product_over_the_ranges_of_tiles(t, rows, cols, group, dtype, offset):
     check_linear(x, w, values, scales, dtype, "y")
 
 
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,rows,cols,group", [(129, 64, 130, 64), (1100, 96, 2050, 32), (2100, 70, 2000, 128), (8100, 32, 2040, 64), (60, 1500, 200, 128),
+                                               (300, 4000, 136, 64)])
+def test_gradient_of_the_input_over_the_ranges_of_tiles(t, rows, cols, group, dtype, offset):
+    progress(f"w4 dx {t} x {rows} x {cols} group {group} {dtype} offset {offset}")
+    w, values, scales = weights(rows, cols, group, 9)
+    dy = strided(activations(t, rows, dtype, 2), 8 + -rows % 8, offset)
+    check_dx(dy, w, values, scales, dtype, "dx")
+
+
 @pytest.mark.parametrize("group", GROUPS)
 @pytest.mark.parametrize("t,rows,cols", [(31, 300, 200), (65, 1000, 136), (400, 300, 4100), (1500, 1032, 640)])
 def test_gradient_of_the_scales_over_the_ranges_of_tiles(t, rows, cols, group):
