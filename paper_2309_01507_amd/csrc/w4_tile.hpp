@@ -118,7 +118,9 @@ struct Stage {
 //
 // A workgroup of WN x WT waves takes WN NT 32 rows of W and WT TT 32 tokens.  x goes through LDS in runs of 128; codes
 // go from memory into the registers of the waves that use them and are converted there.  Each group's products are summed from 0 and
-// join the total with one multiply-add by the scale.
+// join the total with one multiply-add by the scale.  For fp32 and for bf16 off 16-byte boundaries: x passes through registers, so that its rows may
+// start and end anywhere.  Bound by the matrix unit for fp32, whose products cost three each (77 x 50257 x 1024, groups of 32: 64 us, 124 TFLOP/s, 370 of
+// bf16; 4096 x 11008 x 4096, groups of 128: 1210 us, 305); by conversions and waits for bf16 (that: 480 us, 770 TFLOP/s).
 template <bool BF16, int GROUP, int WN, int WT, int NT, int TT, int BUFFERS>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                       int64_t y_stride, int n_tiles, int t_tiles) {
@@ -228,6 +230,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
 
 // The same for fewer tokens than fill the GPU with such tiles: 32 tokens by NT 32 rows of W per workgroup, whose 4 waves share the runs and join
 // their sums at the end.  Tokens and codes go from memory into the registers of the lanes that multiply them, a run ahead; nothing is staged.
+// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 128: fp32 30 us (tiles above: 77), bf16 22 (78).
 template <bool BF16, int GROUP, int NT>
 __global__ __launch_bounds__(256, 2) void w4_linear_share_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
@@ -415,9 +418,11 @@ __device__ __forceinline__ f32x16 opaque_zero() {
     return z;
 }
 
-// The same product for bf16 tokens on 16-byte boundaries and rows of whole runs.  Tokens and codes are loaded straight into LDS, a run ahead;
-// a lane loads the scales of four groups at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at its
-// barrier.
+// The same product for bf16 tokens on 16-byte boundaries (CUT: rows that end within a run).  Tokens and codes are loaded straight into LDS, a run
+// ahead; a lane loads the scales of four groups at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at
+// its barrier.  Bound by the matrix unit, beside which the conversion of the codes and the multiply-adds by the scales take issue slots:
+// 4096 x 11008 x 4096, groups of 128: 331 us, 1117 TFLOP/s (a library's bf16 product of that size, without the weights' expansion: 360 to
+// 429 us); groups of 64 375, of 32 443.  8 waves with one workgroup a CU and three buffers: 365 to 391; tokens through registers: 461.
 template <int GROUP, int WN, int WT, int NT, int TT, bool CUT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                         int64_t y_stride, int n_tiles, int t_tiles) {
@@ -533,7 +538,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
 }
 
 // The same for fewer tokens than fill the GPU with such tiles: a tile of NT 32 rows of W and TT 32 tokens per workgroup, whose 4 waves share the
-// runs.  Each wave stages its own runs in its own part of LDS, one ahead, and waits for nobody until the sums are joined.
+// runs.  Each wave stages its own runs in its own part of LDS, one ahead, and waits for nobody until the sums are joined.  Bound by the latency of
+// a wave's runs: 64 x 4096 x 4096, groups of 128: 6.2 us, 1.6 TB/s; 256 tokens 13.5 us, 635 TFLOP/s.
 template <int GROUP, int NT, int TT, bool CUT>
 __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
@@ -677,7 +683,9 @@ __device__ __forceinline__ float sum_columns(f32x16 v) {
 // dscales[n][g] = sum_t dy[t][n] P[t][n][g] with P the product's sum over the group before its scale: the same matrix products, and no
 // weight gradient of n x k is ever formed.  A workgroup takes WN NT 32 rows of W and a run of 128 and walks over the tokens
 // (those of split blockIdx.y); the run's codes stay converted in registers.  Here W is the A operand, so that a lane holds one token and
-// for it 4 consecutive rows of W at a time, as dy has them; the sum over the lanes' tokens waits until the end.
+// for it 4 consecutive rows of W at a time, as dy has them; the sum over the lanes' tokens waits until the end.  Bound by the matrix unit for
+// many tokens (fp32 4096 x 11008 x 4096, groups of 128: 1310 us, 281 TFLOP/s, 843 of bf16), by one tile's latency for few (fp32 333 x 2304 x 768,
+// groups of 64: 15.3 us with the join; 18.4 with every column summed up in all lanes).
 template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
                                                                       int64_t dy_stride, int n_tiles, int t_per_split, float* out,
@@ -806,7 +814,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
 // The same for bf16 on 16-byte boundaries, the other way round: dy^T x is summed over the tokens by the matrix unit alone, in tiles of 256 rows of
 // W by a run of 128 that are never written, and at the end multiplied by the codes and added up over the groups.  (With the product over the
 // inputs first, 4096 tokens and 11008 x 4096 took 603 us: a multiply-add a product and token, and dy's conversion.)  Both operands'
-// reduction runs down the rows of their arrays, hence the transposed reads.
+// reduction runs down the rows of their arrays, hence the transposed reads.  Bound by the matrix unit and the reads that feed it: 4096 x 11008 x 4096,
+// groups of 128: 322 us, 1146 TFLOP/s; 333 x 2304 x 768 10.4 us with the join, a third of it the end, where columns are summed up.
 template <int GROUP>
 __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
                                                                int64_t dy_stride, int n_tiles, int t_per_split, float* out,
@@ -930,7 +939,9 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 // unit in the last place per weight, as large as the one of the result) or as three bf16 terms for fp32, and goes to LDS as it stands in W, a
 // lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a
 // dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
-// would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.
+// would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
+// 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 510 us, 724), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
+// 64: 26.7 us).
 template <bool BF16, int WT, int TT>
 __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
                                                               int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
@@ -1044,7 +1055,9 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
 }
 
 // The same for bf16 tokens on 16-byte boundaries and rows of W in whole steps of 32: dy straight into LDS, value * scale as it stands in W, so that
-// a lane converts a word at a time; the transposition is the reads'.
+// a lane converts a word at a time; the transposition is the reads'.  Bound by the matrix unit and the reads that feed it: 4096 x 11008 x 4096 360 to
+// 425 us (with the clock that the card holds), 870 to 1030 TFLOP/s; without the fence behind the loads 10 % more, since they were then requested
+// at the step's end.
 template <bool PARTS, int TT>
 __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx, int64_t dx_stride,
                                                            int t_tiles, int k_tiles, int n_per_split, float* parts, int group_shift) {
