@@ -166,7 +166,7 @@ int dscale_splits(int64_t t, const W4Mat& m) {
 
 // The gradient of the input: tiles of 128 inputs by 256, 128 or 64 tokens, the largest that still fill the GPU, since W is converted once for a
 // tile (us: bf16 4096 x 11008 x 4096 off 16-byte boundaries 492, 562, 728; 1500 x 4096 x 4032 155, 118, 120; 512 x 4096 x 4096 68, 54, 63; 333 x 2304 x 768
-// 27, 20, 16; fp32 2048 x 4096 x 4096 -, 456, 509; 1000 x 4096 x 4096 -, 242, 258); the reduction is split where there are fewer
+// 27, 20, 16; fp32 2048 x 4096 x 4096 -, 456, 509; 512 x 4096 x 4096 -, 120, 135; 333 x 2304 x 2304 -, 42, 45); the reduction is split where there are fewer
 struct DxPlan {
     bool direct;
     int bt, splits, n_per_split;
@@ -179,13 +179,13 @@ DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     DxPlan p{};
     p.direct = aligned_rows && t > 128;
     const int64_t k_tiles = div_up(m.k, kW4Chunk), tiles = div_up(t, 128) * k_tiles;
-    p.bt = bf16 && div_up(t, 256) * k_tiles >= 512 ? 256 : p.direct || tiles >= (bf16 ? 128 : 256) ? 128 : 64;
+    p.bt = bf16 && div_up(t, 256) * k_tiles >= 512 ? 256 : p.direct || (bf16 ? tiles >= 128 : t > 64) ? 128 : 64;
     const int64_t steps = div_up(m.n, kDxStep);
     // A step takes a workgroup about 0.9 us (fp32: 2), each further split the join 0.2 us and the time of writing and reading a part at 3 TB/s
     // (333 x 2304 x 768 bf16: 18 splits 21 us, 5 splits 15)
     const double step_us = bf16 ? 0.9 : 2.0, split_us = 0.2 + double(t) * m.k * 8 / 3e6;
     const int64_t worth = std::max<int64_t>(1, int64_t(std::sqrt(double(steps) * step_us / split_us)));
-    const int splits = splits_for(div_up(t, p.bt) * k_tiles, std::min(div_up(steps, 2), worth), 512);
+    const int splits = splits_for(div_up(t, p.bt) * k_tiles, std::min(div_up(steps, 2), worth), bf16 || p.bt == 64 ? 512 : 256);     // one workgroup of 8 waves a CU
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
     p.splits = int(div_up(m.n, p.n_per_split));
     return p;
@@ -294,10 +294,11 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         return LPMM_OK;
     }
     const bool bf16 = dtype == LPMM_BF16;
-    // Elsewhere (us, fp32 with groups of 32; the few tokens' kernel, runs shared by waves with 32 and 64 rows of W, tiles of 128 x 64): 32 x 4096 x 4096 19, 26, 35;
-    // 64 x 4096 x 4096 37, 27, 36; 32 x 32000 x 4096 140, 78, 57; 100 x 4096 x 4096 -, 39, 37, 90; 512 x 4096 x 4096 -, 140, 106, 95; 77 x 50257 x 1024 -,
-    // 82, 68, 64.  bf16 off 16-byte boundaries, the last two: 256 x 4096 x 4096 59, 80; 300 x 4000 x 4032 78, 82; 512 x 4096 x 4096 105, 82)
-    if (t > 32 ? t <= 64 || tiles_of(64, 32) <= (bf16 ? 512 : 768) : t > kFew && tiles_of(64, 32) > 128) {
+    // Elsewhere (us, fp32 with groups of 32; the few tokens' kernel, runs shared by waves with 32 and 64 rows of W, tiles of 256 rows by 32 tokens): 32 x 4096 x 4096
+    // 19, 26, 35; 32 x 32000 x 4096 140, 78, 57; 64 x 4096 x 4096 37, 27, 36; 64 x 11008 x 4096 -, 61, 54, 82; 256 x 4096 x 4096 -, 75, 57, 83;
+    // 300 x 4000 x 4096 -, -, 99, 83; 64 x 50257 x 1024 -, -, 62, 38.  bf16 off 16-byte boundaries, the last two: 256 x 4096 x 4096 59, 80; 512 x 4096 x 4096 105, 82
+    const bool many = t > 32 || t > kFew && tiles_of(64, 32) > 128;
+    if (many && tiles_of(64, 32) <= 512) {
         const bool n32 = tiles_of(32, 32) <= 256;
         const int64_t n_tiles = div_up(m.n, n32 ? 32 : 64), t_tiles = div_up(t, 32), blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > kMaxBlocks) return LPMM_EINVAL;
@@ -311,18 +312,18 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
-    if (t > 32) {
-        // 64 tokens by 256 rows of W with two buffers; fp32, whose terms take three times the room, by 128 with one; several workgroups a CU.
-        // (1000 x 4096 x 4096 bf16 off 16-byte boundaries: 54 us, with 128 tokens by 256 rows and 8 waves 88, with 128 by 128 114)
-        const int64_t n_tiles = div_up(m.n, bf16 ? 256 : 128), t_tiles = div_up(t, 64);
+    if (many) {
+        // 256 rows of W by 64 tokens, fp32, whose terms take three times the room, by 32; 4 waves, two workgroups a CU.  (1000 x 4096 x 4096 bf16 off 16-byte
+        // boundaries, groups of 128: 54 us, with 8 waves and 128 tokens 88, with 128 by 128 114; fp32 105, 128 rows by 64 tokens 122, 256 by 64 and 8 waves 112)
+        const int64_t n_tiles = div_up(m.n, 256), t_tiles = div_up(t, bf16 ? 64 : 32);
         const int64_t blocks = div_up(n_tiles * t_tiles, 8) * 8;
         if (blocks > kMaxBlocks) return LPMM_EINVAL;
-#define LPMM_TILE(B, G, WN, WT, TT, BUF) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, WN, WT, 2, TT, BUF>), dim3(unsigned(blocks)), dim3(64 * WT * WN), 0, s, m, x, \
-                                                        int(t), x_stride, y, y_stride, int(n_tiles), int(t_tiles))
+#define LPMM_TILE(B, G, TT) hipLaunchKernelGGL((w4_linear_tile_kernel<B, G, 4, 1, 2, TT>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, y, \
+                                               y_stride, int(n_tiles), int(t_tiles))
         if (bf16) {
-            if (group == 32) LPMM_TILE(true, 32, 4, 1, 2, 2); else if (group == 64) LPMM_TILE(true, 64, 4, 1, 2, 2); else LPMM_TILE(true, 128, 4, 1, 2, 2);
+            if (group == 32) LPMM_TILE(true, 32, 2); else if (group == 64) LPMM_TILE(true, 64, 2); else LPMM_TILE(true, 128, 2);
         } else {
-            if (group == 32) LPMM_TILE(false, 32, 2, 2, 1, 1); else if (group == 64) LPMM_TILE(false, 64, 2, 2, 1, 1); else LPMM_TILE(false, 128, 2, 2, 1, 1);
+            if (group == 32) LPMM_TILE(false, 32, 1); else if (group == 64) LPMM_TILE(false, 64, 1); else LPMM_TILE(false, 128, 1);
         }
 #undef LPMM_TILE
         LPMM_HIP(hipGetLastError());

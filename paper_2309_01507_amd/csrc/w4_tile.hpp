@@ -119,14 +119,14 @@ struct Stage {
 // A workgroup of WN x WT waves takes WN NT 32 rows of W and WT TT 32 tokens.  x goes through LDS in runs of 128; codes
 // go from memory into the registers of the waves that use them and are converted there.  Each group's products are summed from 0 and
 // join the total with one multiply-add by the scale.  For fp32 and for bf16 off 16-byte boundaries: x passes through registers, so that its rows may
-// start and end anywhere.  Bound by the matrix unit for fp32, whose products cost three each (77 x 50257 x 1024, groups of 32: 64 us, 124 TFLOP/s, 370 of
-// bf16; 4096 x 11008 x 4096, groups of 128: 1210 us, 305); by conversions and waits for bf16 (that: 480 us, 770 TFLOP/s).
-template <bool BF16, int GROUP, int WN, int WT, int NT, int TT, int BUFFERS>
+// start and end anywhere.  Bound by the matrix unit, for fp32, whose products cost three each, and the taking apart beside it (77 x 50257 x 1024, groups
+// of 32: 50 us, 157 TFLOP/s, 470 of bf16; 4096 x 11008 x 4096, groups of 128: 1010 us, 366); by conversions and waits for bf16 (that: 480 us, 770 TFLOP/s).
+template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                       int64_t y_stride, int n_tiles, int t_tiles) {
     constexpr int TERMS = kW4Terms<BF16>, THREADS = 64 * WN * WT, BN = WN * NT * 32, BT = WT * TT * 32;
     typedef Stage<BF16, BT, 4, THREADS> StageX;
-    __shared__ uint4 s_x[BUFFERS][TERMS * StageX::kPieces];
+    __shared__ uint4 s_x[2][TERMS * StageX::kPieces];
     int n_tile, t_tile;
     if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
             stage.load(x, x_stride, t0, t, (run + 1) * kW4Chunk, m.k);
             load_w(run + 1);
         }
-        const uint4* lds = s_x[run & (BUFFERS - 1)];
+        const uint4* lds = s_x[run & 1];
         f32x16 part[TT][NT];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
@@ -211,8 +211,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
                         }
             }
         }
-        if (BUFFERS == 1) __syncthreads();                     // read before it is written
-        if (more) stage.store(s_x[(run + 1) & (BUFFERS - 1)]);
+        if (more) stage.store(s_x[(run + 1) & 1]);
         __syncthreads();
     }
 #pragma unroll
@@ -230,7 +229,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
 
 // The same for fewer tokens than fill the GPU with such tiles: 32 tokens by NT 32 rows of W per workgroup, whose 4 waves share the runs and join
 // their sums at the end.  Tokens and codes go from memory into the registers of the lanes that multiply them, a run ahead; nothing is staged.
-// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 128: fp32 30 us (tiles above: 77), bf16 22 (78).
+// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 128: fp32 30 to 33 us (tiles above: 56), bf16 22.
 template <bool BF16, int GROUP, int NT>
 __global__ __launch_bounds__(256, 2) void w4_linear_share_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
@@ -941,7 +940,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 // dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
 // would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
 // 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 510 us, 724), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
-// 64: 26.7 us).
+// 64: 26.7 us with the join).
 template <bool BF16, int WT, int TT>
 __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
                                                               int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
