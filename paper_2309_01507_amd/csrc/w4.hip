@@ -160,8 +160,10 @@ int splits_for(int64_t blocks, int64_t steps, int64_t want) {
 
 // The gradient of the scales: rows of W of a tile, tokens of a piece that splits are made of
 constexpr int kDscaleRows = 256, kDscaleTokens = 64;
-int dscale_splits(int64_t t, const W4Mat& m) {
-    return splits_for(div_up(m.n, kDscaleRows) * (m.words / 16), div_up(t, kDscaleTokens), 768);
+// What a CU holds of the kernel, once for each: two workgroups straight into LDS, one through registers (us, bf16 2000 x 2304 x 768 with 768, 512, 256
+// workgroups at most: 21.2, 16.5, 17.6, 4096 x 4096 x 1024 42, 38, 43; fp32 333 x 2304 x 768 15.1, 15.1, 12.8, 2000 x 2304 x 768 43, 37, 36)
+int dscale_splits(int64_t t, const W4Mat& m, bool direct) {
+    return splits_for(div_up(m.n, kDscaleRows) * (m.words / 16), div_up(t, kDscaleTokens), direct ? 512 : 256);
 }
 
 // The gradient of the input: tiles of 128 inputs by 256, 128 or 64 tokens, the largest that still fill the GPU, since W is converted once for a
@@ -414,7 +416,7 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
 size_t lpmm_w4_linear_dscale_workspace_bytes(int64_t t, const int64_t shape[2], int group) {
     W4Mat m{};
     if (check_w4(shape, group, &m) || t < 1 || t > kMaxTokens) return 0;
-    const int splits = dscale_splits(t, m);
+    const int splits = dscale_splits(t, m, true);            // no fewer than the others take
     return splits > 1 ? size_t(splits) * m.n * m.groups * 4 : 0;
 }
 
@@ -433,14 +435,14 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int64_t n_tiles = div_up(m.n, kDscaleRows), blocks = div_up(n_tiles * (m.words / 16), 8) * 8;
     if (blocks > kMaxBlocks) return LPMM_EINVAL;
-    int splits = dscale_splits(t, m);
+    const bool direct = dtype == LPMM_BF16 && aligned(x, 16) && aligned(dy, 16) && x_stride % 8 == 0 && dy_stride % 8 == 0 &&
+                        x_stride < (1 << 24) && dy_stride < (1 << 24) && m.k < (1 << 23);
+    int splits = dscale_splits(t, m, direct);
     const int per = int(div_up(div_up(t, kDscaleTokens), splits)) * kDscaleTokens;
     splits = std::max(1, int(div_up(t, std::max(per, 1))));
     const int64_t count = int64_t(m.n) * m.groups;
     float* out = splits > 1 ? static_cast<float*>(workspace) : dscales;
     const dim3 grid = dim3(unsigned(blocks), unsigned(splits));
-    const bool direct = dtype == LPMM_BF16 && aligned(x, 16) && aligned(dy, 16) && x_stride % 8 == 0 && dy_stride % 8 == 0 &&
-                        x_stride < (1 << 24) && dy_stride < (1 << 24) && m.k < (1 << 23);
     if (direct) {
 #define LPMM_DSCALE_DIRECT(G) hipLaunchKernelGGL(w4_dscale_direct_kernel<G>, grid, dim3(256), 0, s, m, x, dy, int(t), x_stride, dy_stride, int(n_tiles), \
                                                  per, out, count)
@@ -461,7 +463,7 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
 #undef LPMM_DSCALE
     LPMM_HIP(hipGetLastError());
     if (splits > 1) {
-        hipLaunchKernelGGL(w4_join_kernel, dim3(unsigned(div_up(count, 256))), dim3(256), 0, s, out, splits, count, count, dscales);
+        hipLaunchKernelGGL(w4_join_kernel, dim3(unsigned(div_up(count, 256))), dim3(256), 0, s, out, splits, count, dscales);
         LPMM_HIP(hipGetLastError());
     }
     return LPMM_OK;

@@ -684,7 +684,7 @@ __device__ __forceinline__ float sum_columns(f32x16 v) {
 // (those of split blockIdx.y); the run's codes stay converted in registers.  Here W is the A operand, so that a lane holds one token and
 // for it 4 consecutive rows of W at a time, as dy has them; the sum over the lanes' tokens waits until the end.  Bound by the matrix unit for
 // many tokens (fp32 4096 x 11008 x 4096, groups of 128: 1310 us, 281 TFLOP/s, 843 of bf16), by one tile's latency for few (fp32 333 x 2304 x 768,
-// groups of 64: 15.3 us with the join; 18.4 with every column summed up in all lanes).
+// groups of 64: 12.8 us with the join).
 template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
                                                                       int64_t dy_stride, int n_tiles, int t_per_split, float* out,
@@ -814,7 +814,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
 // W by a run of 128 that are never written, and at the end multiplied by the codes and added up over the groups.  (With the product over the
 // inputs first, 4096 tokens and 11008 x 4096 took 603 us: a multiply-add a product and token, and dy's conversion.)  Both operands'
 // reduction runs down the rows of their arrays, hence the transposed reads.  Bound by the matrix unit and the reads that feed it: 4096 x 11008 x 4096,
-// groups of 128: 322 us, 1146 TFLOP/s; 333 x 2304 x 768 10.4 us with the join, a third of it the end, where columns are summed up.
+// groups of 128: 322 us, 1146 TFLOP/s; 333 x 2304 x 768 10.0 us with the join, a third of it the end, where columns are summed up.
 template <int GROUP>
 __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
                                                                int64_t dy_stride, int n_tiles, int t_per_split, float* out,
@@ -923,13 +923,22 @@ __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const
     }
 }
 
-// Sum of `splits` arrays of `count` floats, `apart` from one to the next, in their order
-__global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int splits, int64_t apart, int64_t count, float* out) {
+// Sum of `splits` floats, `apart` from one to the next, in their order; 4 are on their way at a time
+__device__ __forceinline__ float sum_parts(const float* p, int splits, int64_t apart) {
+    float v = *p;
+    int s = 1;
+    for (; s + 4 <= splits; s += 4) {
+        const float a = p[s * apart], b = p[(s + 1) * apart], c = p[(s + 2) * apart], d = p[(s + 3) * apart];
+        v = v + a + b + c + d;
+    }
+    for (; s < splits; ++s) v += p[s * apart];
+    return v;
+}
+
+// The splits' parts added up.  Bound by latency (27648 sums of 6: 2 to 4 us).
+__global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int splits, int64_t count, float* out) {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= count) return;
-    float v = parts[i];
-    for (int s = 1; s < splits; ++s) v += parts[s * apart + i];
-    out[i] = v;
+    if (i < count) out[i] = sum_parts(parts + i, splits, count);
 }
 
 // ---- dx = dy W -------------------------------------------------------------------------------------------------------------------------
@@ -940,7 +949,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 // dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
 // would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
 // 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 510 us, 724), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
-// 64: 26.7 us with the join).
+// 64: 25.5 us with the join).
 template <bool BF16, int WT, int TT>
 __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
                                                               int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
@@ -1145,14 +1154,12 @@ __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const voi
         }
 }
 
-// Sum of the splits' parts (t x k each), in their order
+// The splits' parts (t x k each) added up
 template <bool BF16>
 __global__ __launch_bounds__(256) void w4_dx_join_kernel(const float* parts, int splits, int t, int k, void* dx, int64_t dx_stride) {
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, count = int64_t(t) * k;
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x, count = uint32_t(t) * uint32_t(k);     // below 2^25: larger ones are not split
     if (i >= count) return;
-    float v = parts[i];
-    for (int s = 1; s < splits; ++s) v += parts[s * count + i];
-    w4_store1<BF16>(dx, i / k * dx_stride + i % k, v);
+    w4_store1<BF16>(dx, int64_t(i / uint32_t(k)) * dx_stride + i % uint32_t(k), sum_parts(parts + i, splits, count));
 }
 
 }  // namespace lpmm
