@@ -303,12 +303,14 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     if (many && tiles_of(64, 32) <= 512) {
         const bool n32 = tiles_of(32, 32) <= 256;
         const int64_t n_tiles = div_up(m.n, n32 ? 32 : 64), t_tiles = div_up(t, 32), blocks = div_up(n_tiles * t_tiles, 8) * 8;
-        if (blocks > kMaxBlocks) return LPMM_EINVAL;
-#define LPMM_SHARE(B, G, NT) hipLaunchKernelGGL((w4_linear_share_kernel<B, G, NT>), dim3(unsigned(blocks)), dim3(256), 0, s, m, x, int(t), x_stride, \
+#define LPMM_SHARE(B, G, NT, W) hipLaunchKernelGGL((w4_linear_share_kernel<B, G, NT, W>), dim3(unsigned(blocks)), dim3(64 * W), 0, s, m, x, int(t), x_stride, \
                                                 y, y_stride, int(n_tiles), int(t_tiles))
-#define LPMM_SHARE_G(B, NT) { if (group == 32) LPMM_SHARE(B, 32, NT); else if (group == 64) LPMM_SHARE(B, 64, NT); else LPMM_SHARE(B, 128, NT); }
-        if (bf16) { if (n32) LPMM_SHARE_G(true, 1) else LPMM_SHARE_G(true, 2) }
-        else { if (n32) LPMM_SHARE_G(false, 1) else LPMM_SHARE_G(false, 2) }
+#define LPMM_SHARE_G(B, NT, W) { if (group == 32) LPMM_SHARE(B, 32, NT, W); else if (group == 64) LPMM_SHARE(B, 64, NT, W); else LPMM_SHARE(B, 128, NT, W); }
+        // 8 waves where CUs have one workgroup, 4 where they have two (fp32, groups of 32, 4 and 8: 64 x 4096 x 4096 26, 22; 100 x 4096 x 4096 36, 30;
+        // 256 x 4096 x 4096 56, 61; 32 x 32000 x 4096 58, 63)
+        const bool one = blocks <= 256;
+        if (bf16) { if (n32) LPMM_SHARE_G(true, 1, 8) else if (one) LPMM_SHARE_G(true, 2, 8) else LPMM_SHARE_G(true, 2, 4) }
+        else { if (n32) LPMM_SHARE_G(false, 1, 8) else if (one) LPMM_SHARE_G(false, 2, 8) else LPMM_SHARE_G(false, 2, 4) }
 #undef LPMM_SHARE_G
 #undef LPMM_SHARE
         LPMM_HIP(hipGetLastError());

@@ -227,13 +227,13 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
         }
 }
 
-// The same for fewer tokens than fill the GPU with such tiles: 32 tokens by NT 32 rows of W per workgroup, whose 4 waves share the runs and join
+// The same for fewer tokens than fill the GPU with such tiles: 32 tokens by NT 32 rows of W per workgroup, whose 4 or 8 waves share the runs and join
 // their sums at the end.  Tokens and codes go from memory into the registers of the lanes that multiply them, a run ahead; nothing is staged.
-// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 128: fp32 30 to 33 us (tiles above: 56), bf16 22.
-template <bool BF16, int GROUP, int NT>
-__global__ __launch_bounds__(256, 2) void w4_linear_share_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
+// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 64, fp32: 30 us (4 waves 37, tiles above 70).
+template <bool BF16, int GROUP, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void w4_linear_share_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
-    constexpr int TERMS = kW4Terms<BF16>, GROUPS = kW4Chunk / GROUP, WAVES = 4;
+    constexpr int TERMS = kW4Terms<BF16>, GROUPS = kW4Chunk / GROUP;
     __shared__ float s_sum[WAVES][NT * 16 * 64];
     int n_tile, t_tile;
     if (!tile_of(blockIdx.x, n_tiles, t_tiles, n_tile, t_tile)) return;
