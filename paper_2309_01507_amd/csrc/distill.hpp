@@ -261,7 +261,8 @@ __device__ __forceinline__ void distill_span_ml(const DistillArgs& a, int64_t ro
     }
 }
 
-// A workgroup takes a row: 4096 x 32000 bf16 45 us, 5.8 TB/s; 4096 x 50257, whose rows start off 16-byte boundaries, 91 us, 4.5 TB/s.
+// A workgroup takes a row: 4096 x 32000 bf16 45 us, 5.8 TB/s; 4096 x 50257, whose rows start off 16-byte boundaries, 91 us, 4.5 TB/s;
+// 61 x 32000 fp32, one row each for a quarter of the CUs, 8.0 us.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void distill_loss_kernel(const DistillArgs a) {
     const DistillSlots s_slots = distill_slots(a.slots);
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(THREADS) void distill_loss_kernel(const DistillArgs
 }
 
 // Few long rows: a workgroup takes `span` logits of a row and leaves its (m, l); a wave per row joins them.  Bound by the latency of two kernels:
-// 61 x 32000 fp32 8.6 us, 0.9 TB/s.
+// 16 x 131072 fp32 10.6 us, 0.8 TB/s.
 constexpr int kDistillThreads = 256;
 template <bool BF16>
 __global__ __launch_bounds__(kDistillThreads) void distill_part_kernel(const DistillArgs a, int span, float2* parts) {

@@ -120,7 +120,7 @@ struct Stage {
 // go from memory into the registers of the waves that use them and are converted there.  Each group's products are summed from 0 and
 // join the total with one multiply-add by the scale.  For fp32 and for bf16 off 16-byte boundaries: x passes through registers, so that its rows may
 // start and end anywhere.  Bound by the matrix unit, for fp32, whose products cost three each, and the taking apart beside it (77 x 50257 x 1024, groups
-// of 32: 50 us, 157 TFLOP/s, 470 of bf16; 4096 x 11008 x 4096, groups of 128: 1010 us, 366); by conversions and waits for bf16 (that: 480 us, 770 TFLOP/s).
+// of 32: 50 us, 157 TFLOP/s, 470 of bf16; 4096 x 11008 x 4096, groups of 128: 975 us, 379); by conversions and waits for bf16 (that: 480 us, 770 TFLOP/s).
 template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                       int64_t y_stride, int n_tiles, int t_tiles) {
@@ -948,7 +948,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 // lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a
 // dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
 // would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
-// 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 510 us, 724), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
+// 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 492 us, 750), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
 // 64: 25.5 us with the join).
 template <bool BF16, int WT, int TT>
 __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
