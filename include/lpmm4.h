@@ -496,7 +496,7 @@ int lpmm_w4_dequant(const uint8_t* codes, const float* scales, const int64_t sha
 int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const uint8_t* codes, const float* scales,
                    const int64_t shape[2], int group, void* y, int64_t y_stride, void* stream);
 
-/* dx[t][k] = sum_n dy[t][n] W[n][k]: its gradient with respect to x.  In bf16 value * scale is rounded to bf16 once.  workspace:
+/* dx[t][k] = sum_n dy[t][n] W[n][k]: its gradient with respect to x.  In bf16 value * scale is held as two bf16 numbers, to 2^-13 of it.  workspace:
  * device memory, 16-byte aligned, of the bytes that ..._workspace_bytes gives (0: none is needed, as for invalid arguments), contents
  * arbitrary before and after; calls that may overlap in time need one each.  The order of all sums is fixed: equal inputs
  * give equal bits. */

@@ -943,18 +943,35 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 
 // ---- dx = dy W -------------------------------------------------------------------------------------------------------------------------
 //
-// The reduction runs along W's rows, whose scales differ: value * scale is formed once per workgroup, as bf16 (one rounding of half a
-// unit in the last place per weight, as large as the one of the result) or as three bf16 terms for fp32, and goes to LDS as it stands in W, a
+// The reduction runs along W's rows, whose scales differ: value * scale is formed once per workgroup, as two bf16 terms for bf16 tokens (right to
+// 2^-13; a single one would round each weight as coarsely as the result) or as three for fp32, and goes to LDS as it stands in W, a
 // lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a
 // dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
 // would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
 // 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 492 us, 750), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
 // 64: 25.5 us with the join).
+
+// A scale as a + b: a has 6 significant bits, so that a code's value times a is exact in bf16, and value * b is rounded to bf16, 2^-13 of the weight.
+// b is taken 2^-20 of the scale too large, so that both have its sign and neither is 0: an infinite dy then meets no 0 and no infinity of the other sign.
+__device__ __forceinline__ void split_scale(float s, float& a, float& b) {
+    const bool finite = fabsf(s) < __builtin_inff();
+    a = finite ? __uint_as_float(__float_as_uint(s) & 0xFFFC0000u) : s;
+    b = finite ? __builtin_fmaf(s, 0x1p-20f, s - a) : __builtin_copysignf(1.0f, s);
+}
+// A word's weights as two terms
+__device__ __forceinline__ void w4_weights8(uint32_t word, float scale, uint4& a, uint4& b) {
+    float v[8], sa, sb;
+    w4_values8(word, v);
+    split_scale(scale, sa, sb);
+    a = make_uint4(pack_bf16(v[0] * sa, v[1] * sa), pack_bf16(v[2] * sa, v[3] * sa), pack_bf16(v[4] * sa, v[5] * sa), pack_bf16(v[6] * sa, v[7] * sa));
+    b = make_uint4(pack_bf16(v[0] * sb, v[1] * sb), pack_bf16(v[2] * sb, v[3] * sb), pack_bf16(v[4] * sb, v[5] * sb), pack_bf16(v[6] * sb, v[7] * sb));
+}
+
 template <bool BF16, int WT, int TT>
 __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx,
                                                               int64_t dx_stride, int t_tiles, int k_tiles, int n_per_split,
                                                               float* parts, int group_shift) {
-    constexpr int TERMS = kW4Terms<BF16>, DTERMS = BF16 ? 1 : 4, WK = 2, KT = 2, THREADS = 64 * WT * WK, BT = WT * TT * 32, STEP = 32;
+    constexpr int TERMS = BF16 ? 2 : 3, DTERMS = BF16 ? 1 : 4, WK = 2, KT = 2, THREADS = 64 * WT * WK, BT = WT * TT * 32, STEP = 32;
     constexpr int WPIECES = STEP << 4, OWN = WPIECES / THREADS, ROWS = STEP / OWN;            // of 128 inputs; a word makes a piece
     typedef Stage<BF16, BT, 2, THREADS> StageD;
     __shared__ uint4 s_d[2][DTERMS * StageD::kPieces];
@@ -998,20 +1015,19 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
         }
 #pragma unroll
         for (int j = 0; j < OWN; ++j) {
-            float v[8];
-            w4_values8(word[j], v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= sc[j];
-            uint32_t w[3][4];
+            const int to = lds_piece_tr(4, r + j * ROWS, d);
             if constexpr (BF16) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[0][e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                w4_weights8(word[j], sc[j], lds_w[to], lds_w[WPIECES + to]);
             } else {
-                split3_8(v, w);
-            }
+                float v[8];
+                w4_values8(word[j], v);
 #pragma unroll
-            for (int k = 0; k < TERMS; ++k)
-                lds_w[k * WPIECES + lds_piece_tr(4, r + j * ROWS, d)] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+                for (int e = 0; e < 8; ++e) v[e] *= sc[j];
+                uint32_t w[3][4];
+                split3_8(v, w);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) lds_w[k * WPIECES + to] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+            }
         }
     };
     f32x16 acc[TT][KT] = {};
@@ -1035,8 +1051,8 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
 #pragma unroll
                 for (int j = 0; j < DTERMS; ++j) {
                     const bf16x8 ad = as_operand(s_d[now][j * StageD::kPieces + lds_piece<2>(tw + a * 32 + col, 2 * s + half)]);
-                    // dy's terms 0, 1, 2 meet W's first 1, 2, 1 terms, the finite ones of term 0 its other two
-                    constexpr int from[4] = {0, 0, 0, 1}, to[4] = {1, 2, 1, 3};
+                    // fp32: dy's terms 0, 1, 2 meet W's first 1, 2, 1 terms, the finite ones of term 0 its other two
+                    constexpr int from[4] = {0, 0, 0, 1}, to[4] = {BF16 ? 2 : 1, 2, 1, 3};
 #pragma unroll
                     for (int b = 0; b < KT; ++b)
 #pragma unroll
@@ -1063,16 +1079,15 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
 }
 
 // The same for bf16 tokens on 16-byte boundaries and rows of W in whole steps of 32: dy straight into LDS, value * scale as it stands in W, so that
-// a lane converts a word at a time; the transposition is the reads'.  Bound by the matrix unit and the reads that feed it: 4096 x 11008 x 4096 360 to
-// 425 us (with the clock that the card holds), 870 to 1030 TFLOP/s; without the fence behind the loads 10 % more, since they were then requested
-// at the step's end.
+// a lane converts a word at a time; the transposition is the reads'.  Bound by the matrix unit, which takes two products for one: 4096 x 11008 x 4096
+// 583 us, 634 TFLOP/s, 1270 of bf16.  (With value * scale rounded to one bf16 number 362 us; the error against 64 bits was then 1.4 times that of rounding dx.)
 template <bool PARTS, int TT>
 __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx, int64_t dx_stride,
                                                            int t_tiles, int k_tiles, int n_per_split, float* parts, int group_shift) {
     constexpr int STEP = 32, KT = 2;                           // rows of W of a step; tiles of a wave: 32 TT tokens by 64 inputs
     typedef StageDirect<64 * TT, 2, 4> StageD;                 // tokens by 32 rows of W
     constexpr int WPIECES = STEP << 4;                         // of 128 inputs
-    __shared__ uint4 s_d0[StageD::kPieces], s_d1[StageD::kPieces], s_w0[WPIECES], s_w1[WPIECES];
+    __shared__ uint4 s_d0[StageD::kPieces], s_d1[StageD::kPieces], s_w0[2 * WPIECES], s_w1[2 * WPIECES];
     int t_tile, k_tile;
     if (!tile_of(blockIdx.x, t_tiles, k_tiles, t_tile, k_tile)) return;
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, half = lane >> 5;
@@ -1097,14 +1112,8 @@ __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const voi
     auto convert = [&](uint4* lds) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            float v[8];
-            w4_values8(word[j], v);
-            uint4 p;
-            p.x = pack_bf16(v[0] * sc[j], v[1] * sc[j]);
-            p.y = pack_bf16(v[2] * sc[j], v[3] * sc[j]);
-            p.z = pack_bf16(v[4] * sc[j], v[5] * sc[j]);
-            p.w = pack_bf16(v[6] * sc[j], v[7] * sc[j]);
-            lds[lds_piece_tr(4, r + 16 * j, d)] = p;
+            const int to = lds_piece_tr(4, r + 16 * j, d);
+            w4_weights8(word[j], sc[j], lds[to], lds[WPIECES + to]);
         }
     };
     f32x16 acc[TT][KT] = {};
@@ -1113,15 +1122,19 @@ __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const voi
         __builtin_amdgcn_sched_barrier(0);                     // requested here, not at the step's end
 #pragma unroll
         for (int s = 0; s < STEP / 16; ++s) {
-            bf16x8 a[TT], b[KT];
+            bf16x8 a[TT];
 #pragma unroll
             for (int i = 0; i < TT; ++i) a[i] = as_operand(now_d[lds_piece<2>(tw + i * 32 + col, 2 * s + half)]);
 #pragma unroll
-            for (int j = 0; j < KT; ++j) b[j] = operand_tr<4>(now_w, s * 16, kw + j * 32);
+            for (int term = 0; term < 2; ++term) {
+                bf16x8 b[KT];
 #pragma unroll
-            for (int i = 0; i < TT; ++i)
+                for (int j = 0; j < KT; ++j) b[j] = operand_tr<4>(now_w + term * WPIECES, s * 16, kw + j * 32);
 #pragma unroll
-                for (int j = 0; j < KT; ++j) acc[i][j] = mfma32(a[i], b[j], acc[i][j]);
+                for (int i = 0; i < TT; ++i)
+#pragma unroll
+                    for (int j = 0; j < KT; ++j) acc[i][j] = mfma32(a[i], b[j], acc[i][j]);
+            }
         }
         if (more) convert(next_w);
         __syncthreads();
