@@ -636,7 +636,10 @@ def _load_torch():
 
 
 def _w4_check(w: WeightsW4, what: str):
+    torch = _torch or _load_torch()
     codes, scales, rows, cols = w.codes, w.scales, w.rows, w.cols
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.float32:
+        raise ValueError(f"{what}: codes must be uint8 and scales float32, not {codes.dtype} and {scales.dtype}")
     if (codes.numel() != rows * ((cols + 127) // 128 * 64) or scales.shape != (rows, -(-cols // w.group)) or
             not codes.is_contiguous() or not scales.is_contiguous()):
         raise ValueError(f"{what}: codes or scales are not those of a {rows} x {cols} matrix with groups of {w.group}")

@@ -1,0 +1,24 @@
+"""What the 4-bit weights' and distillation's calls refuse before they touch a GPU, and what the layer does with a cast: no GPU needed."""
+import pytest
+import torch
+
+import paper_2309_01507_amd as lpmm
+
+ROWS, COLS, GROUP = 48, 160, 32
+
+
+def on_cpu(codes=torch.uint8, scales=torch.float32):
+    room = lpmm.lpmm_w4_sizes(ROWS, COLS, GROUP)
+    return lpmm.WeightsW4(ROWS, COLS, GROUP, torch.zeros(room[0], dtype=codes), torch.zeros(ROWS, room[1] // 4 // ROWS, dtype=scales))
+
+
+@pytest.mark.parametrize("codes,scales", [(torch.uint8, torch.bfloat16), (torch.uint8, torch.float16), (torch.uint8, torch.float64),
+                                          (torch.int8, torch.float32), (torch.int32, torch.float32)])
+def test_codes_and_scales_of_another_type(codes, scales):
+    """Scales of two bytes each would be read, and by the compressing call written, beyond their end."""
+    w = on_cpu(codes, scales)
+    x, dy = torch.zeros(3, COLS), torch.zeros(3, ROWS)
+    for call in (lambda: lpmm.lpmm_w4_linear(x, w), lambda: lpmm.lpmm_w4_linear_dx(dy, w), lambda: lpmm.lpmm_w4_linear_dscale(x, dy, w),
+                 lambda: lpmm.lpmm_w4_dequant(w), lambda: lpmm.lpmm_w4_quant(torch.zeros(ROWS, COLS), GROUP, w), lambda: lpmm.w4_linear(x, w)):
+        with pytest.raises(ValueError, match="codes must be uint8 and scales float32"):
+            call()
