@@ -50,8 +50,8 @@ def w4_linear(x: torch.Tensor, w: "_b.WeightsW4") -> torch.Tensor:
 
 
 class W4Linear(torch.nn.Module):
-    """A linear layer without bias whose weight is kept in 4 bits.  `scales` is a parameter (float32, out_features x groups), `codes` a
-    buffer; both are part of the state_dict."""
+    """A linear layer without bias whose weight is kept in 4 bits.  `scales` is a parameter (float32, out_features x groups, whatever the
+    module is cast to), `codes` a buffer; both are part of the state_dict."""
 
     def __init__(self, in_features: int, out_features: int, group: int = 128, device="cuda"):
         super().__init__()
@@ -67,6 +67,15 @@ class W4Linear(torch.nn.Module):
         layer = cls(weight.shape[1], weight.shape[0], group, weight.device)
         _b.lpmm_w4_quant(weight, group, _b.WeightsW4(weight.shape[0], weight.shape[1], group, layer.codes, layer.scales.data))
         return layer
+
+    def _apply(self, fn, recurse=True):
+        """Moves between devices are followed; casts (bfloat16(), to(torch.half), ...) leave codes, scales and their gradient as they are."""
+        def keep(t):
+            moved = fn(t)
+            if moved.dtype != t.dtype and (t is self.scales or t is self.scales.grad or t is self.codes):
+                moved = t.to(moved.device)
+            return moved
+        return super()._apply(keep, recurse)
 
     def weights(self) -> "_b.WeightsW4":
         return _b.WeightsW4(self.out_features, self.in_features, self.group, self.codes, self.scales)

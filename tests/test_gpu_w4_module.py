@@ -81,3 +81,17 @@ def test_recovery():
     print(f"[gpu-test] recovery {before:.5f} -> {after:.5f}, token by token off by {off:.1e}", flush=True)
     assert after < 0.9 * before
     assert off < 1e-4
+
+
+def test_a_cast_layer_computes_in_bf16():
+    """After model.to(torch.bfloat16) the layer takes bf16 inputs and its scales are the ones it had."""
+    torch.manual_seed(5)
+    layer = lpmm.W4Linear.from_weight(torch.randn(96, 200, device=DEV), 64)
+    full = ref.VALUES[ref.unpack(layer.codes, 96, 200)] * ref.spread(layer.scales.detach().cpu(), 64, 200)
+    model = torch.nn.Sequential(layer).to(torch.bfloat16)
+    x = torch.randn(7, 200, device=DEV).bfloat16().requires_grad_()
+    y = model(x)
+    y.backward(torch.ones_like(y))
+    want, mag = x.detach().cpu().double() @ full.t(), x.detach().cpu().double().abs() @ full.abs().t()
+    ref.assert_within(y.detach(), want, ref.bound(torch.bfloat16, want, mag, 204), "y")
+    assert layer.scales.grad.dtype == torch.float32 and x.grad.dtype == torch.bfloat16

@@ -22,3 +22,22 @@ def test_codes_and_scales_of_another_type(codes, scales):
                  lambda: lpmm.lpmm_w4_dequant(w), lambda: lpmm.lpmm_w4_quant(torch.zeros(ROWS, COLS), GROUP, w), lambda: lpmm.w4_linear(x, w)):
         with pytest.raises(ValueError, match="codes must be uint8 and scales float32"):
             call()
+
+
+@pytest.mark.parametrize("cast", [lambda m: m.bfloat16(), lambda m: m.half(), lambda m: m.double(), lambda m: m.to(torch.bfloat16),
+                                  lambda m: m.to("cpu", torch.float16), lambda m: m.type(torch.bfloat16), lambda m: m.float()])
+def test_a_cast_leaves_the_scales_as_they_are(cast):
+    layer = lpmm.W4Linear(COLS, ROWS, GROUP, device="cpu")
+    torch.nn.init.uniform_(layer.scales, 0.01, 0.02)
+    layer.codes.random_(0, 256)
+    scales, codes, parameter = layer.scales.detach().clone(), layer.codes.clone(), layer.scales
+    parameter.grad = torch.rand_like(scales)
+    grad = parameter.grad.clone()
+    model = torch.nn.Sequential(layer, torch.nn.Linear(ROWS, 4), torch.nn.LayerNorm(4))
+    cast(model)
+    assert layer.scales is parameter and parameter.requires_grad and torch.equal(parameter.detach(), scales)
+    assert parameter.dtype == parameter.grad.dtype == torch.float32 and torch.equal(parameter.grad, grad)
+    assert layer.codes.dtype == torch.uint8 and torch.equal(layer.codes, codes)
+    other = cast(torch.nn.Linear(2, 2))
+    assert model[1].weight.dtype == model[2].weight.dtype == other.weight.dtype, "the cast still holds for the rest of the model"
+    assert layer.to("meta").scales.device.type == "meta"
