@@ -811,6 +811,8 @@ def _workspace(workspace, need: int, like, stream, what: str):
             return like.new_empty(need, dtype=_torch.uint8)
     elif workspace.get_device() != like.get_device():
         raise ValueError(f"{what}: the workspace must be on the current GPU")
+    elif not workspace.is_contiguous():
+        raise ValueError(f"{what}: the workspace must be contiguous")
     return workspace
 
 

@@ -41,3 +41,13 @@ def test_a_cast_leaves_the_scales_as_they_are(cast):
     other = cast(torch.nn.Linear(2, 2))
     assert model[1].weight.dtype == model[2].weight.dtype == other.weight.dtype, "the cast still holds for the rest of the model"
     assert layer.to("meta").scales.device.type == "meta"
+
+
+@pytest.mark.parametrize("workspace", [torch.empty(1).expand(1 << 20), torch.empty(2, 64).t()])
+def test_a_workspace_with_gaps_or_repeats(workspace):
+    """An expanded tensor has fewer bytes than elements."""
+    from paper_2309_01507_amd import binding
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._workspace(workspace, 64, torch.empty(1), None, "call")
+    whole = torch.empty(64)
+    assert binding._workspace(whole, 64, torch.empty(1), None, "call") is whole
