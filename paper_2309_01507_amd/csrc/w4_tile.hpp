@@ -945,9 +945,9 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 //
 // The reduction runs along W's rows, whose scales differ: value * scale is formed once per workgroup, as two bf16 terms for bf16 tokens (right to
 // 2^-13; a single one would round each weight as coarsely as the result) or as three for fp32, and goes to LDS as it stands in W, a
-// lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there a
-// dy that is not finite meets W's first term only (a fourth array holds dy's first terms with 0 in its place), or infinity times a term of 0
-// would make NaN of infinity.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
+// lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there
+// infinity must not meet a term of 0 of a number that is not, which would make NaN of it.  A dy that is not finite meets W's first term only, and a fourth array,
+// dy's first terms with 2^-126 in its place, the other two; an infinite weight stands in W's third term, which meets that array only, and has 2^-126 in the first.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
 // 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 492 us, 750), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
 // 64: 25.5 us with the join).
 
@@ -965,6 +965,17 @@ __device__ __forceinline__ void w4_weights8(uint32_t word, float scale, uint4& a
     split_scale(scale, sa, sb);
     a = make_uint4(pack_bf16(v[0] * sa, v[1] * sa), pack_bf16(v[2] * sa, v[3] * sa), pack_bf16(v[4] * sa, v[5] * sa), pack_bf16(v[6] * sa, v[7] * sa));
     b = make_uint4(pack_bf16(v[0] * sb, v[1] * sb), pack_bf16(v[2] * sb, v[3] * sb), pack_bf16(v[4] * sb, v[5] * sb), pack_bf16(v[6] * sb, v[7] * sb));
+}
+// Three terms of 8 weights where some are infinite: those stand in the third term, and the first keeps their sign
+__device__ __forceinline__ void split3_infinite(const float v[8], uint32_t w[3][4]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (fabsf(v[e]) != __builtin_inff()) continue;
+        const int at = e / 2, shift = 16 * (e & 1);
+        const uint32_t others = ~(0xFFFFu << shift), sign = (__float_as_uint(v[e]) >> 31) << (15 + shift);
+        w[0][at] = (w[0][at] & others) | sign | 0x0080u << shift;
+        w[2][at] = (w[2][at] & others) | sign | 0x7F80u << shift;
+    }
 }
 
 template <bool BF16, int WT, int TT>
@@ -1007,8 +1018,8 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
                 uint32_t w[4] = {f[0].x, f[0].y, f[0].z, f[0].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
-                    if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+                    if ((w[e] & 0x7F80u) == 0x7F80u) w[e] = (w[e] & 0xFFFF8000u) | 0x0080u;
+                    if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] = (w[e] & 0x8000FFFFu) | 0x00800000u;
                 }
                 lds_d[3 * StageD::kPieces + lds_piece<2>(id >> 2, id & 3)] = make_uint4(w[0], w[1], w[2], w[3]);
             }
@@ -1025,6 +1036,7 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
                 for (int e = 0; e < 8; ++e) v[e] *= sc[j];
                 uint32_t w[3][4];
                 split3_8(v, w);
+                if (!(fabsf(sc[j]) < 0x1p125f)) split3_infinite(v, w);
 #pragma unroll
                 for (int k = 0; k < TERMS; ++k) lds_w[k * WPIECES + to] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
             }

@@ -69,3 +69,8 @@ def check_what_is_not_finite(t, dtype, offset):
 @pytest.mark.parametrize("t", [4, 150, 300])
 def test_infinite_weights_and_gradients_bf16(t, offset):
     check_what_is_not_finite(t, BF16, offset)
+
+
+@pytest.mark.parametrize("t", [4, 65, 300])
+def test_infinite_weights_and_gradients_fp32(t):
+    check_what_is_not_finite(t, F32, 0)
