@@ -571,7 +571,7 @@ __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const 
 #pragma unroll
         for (int b = 0; b < NT; ++b)
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][CUT ? min(run * GROUPS + g, m.groups - 1) : run * GROUPS + g];    // beyond the last group all codes are 0
+            for (int g = 0; g < GROUPS; ++g) sc[b][g] = scales[b][CUT ? min(run * GROUPS + g, m.groups - 1) : run * GROUPS + g];
     };
     auto step = [&](bool more, int run, const uint4* now, uint4* next) {
         // No barrier here: this run's loads have landed and the last one's reads are done, before the next one's loads go out.  Nothing crosses.
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const 
 #pragma unroll
         for (int b = 0; b < NT; ++b)
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) scale[b][g] = sc[b][g];
+            for (int g = 0; g < GROUPS; ++g) scale[b][g] = CUT && run * GROUPS + g >= m.groups ? 0.0f : sc[b][g];     // no group: the sum is 0, the scale another's
         if (more) load(run + WAVES, next);
         __builtin_amdgcn_sched_barrier(0);
         const uint4* now_w = now + StageX::kPieces;

@@ -74,3 +74,26 @@ def test_infinite_weights_and_gradients_bf16(t, offset):
 @pytest.mark.parametrize("t", [4, 65, 300])
 def test_infinite_weights_and_gradients_fp32(t):
     check_what_is_not_finite(t, F32, 0)
+
+
+# Each kind of tile: few tokens, runs split or shared among waves, large tiles; on 16-byte boundaries and off them
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("t,rows", [(3, 70), (20, 70), (40, 9000), (64, 9000), (300, 9000)])
+def test_infinite_scales_in_the_product(t, rows, group, dtype):
+    """A group's sum times its scale: an infinite scale, that of a short last group among them, gives infinity with the sum's sign."""
+    cols = 200
+    progress(f"w4 infinite scales {t} x {rows} x {cols} group {group} {dtype}")
+    w, values, scales = weights(rows, cols, group, 8)
+    last = scales.shape[1] - 1
+    scales[3, last], scales[66, last], scales[5, 0], scales[9, 1] = INF, -INF, INF, float("nan")
+    w = lpmm.WeightsW4(rows, cols, group, w.codes, scales.to(DEV))
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(t, cols, generator=g).to(dtype)
+    want = sum(scales[:, j].double()[None, :] * (x[:, j * group:(j + 1) * group].double() @ values[:, j * group:(j + 1) * group].t())
+               for j in range(last + 1))
+    for offset in (0, 1):
+        got = lpmm.lpmm_w4_linear(strided(x, 8, offset), w).cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        inf = torch.isinf(want)
+        assert torch.equal(torch.isinf(got), inf) and torch.equal(got[inf].double(), want[inf])
