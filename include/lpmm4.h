@@ -516,7 +516,8 @@ int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, i
  *
  * z: student's logits, t rows of v (z_dtype, z_stride).  top: float[t][slots], index: int64[t][slots], the teacher's largest logits
  * and where in the vocabulary they stand, both without gaps between rows; v is at most 2^30.  A slot counts if 0 <= index < v (fill short lists
- * with -1); 1 <= slots <= LPMM_DISTILL_MAX_SLOTS; an index may appear more than once.  tau: temperature, finite and > 0.
+ * with -1); 1 <= slots <= LPMM_DISTILL_MAX_SLOTS; an index may appear more than once.  tau: temperature, > 0, with log2(e) / tau and
+ * tau^2 finite in fp32.
  *   p    = softmax(top / tau) over a row's slots that count
  *   lse  = log sum_i exp(z_i / tau)
  *   loss = tau^2 sum_j p_j (log p_j - z[index_j] / tau + lse)            (terms with p_j = 0 are 0)

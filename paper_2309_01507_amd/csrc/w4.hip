@@ -56,7 +56,8 @@ int check_workspace(const void* p, size_t have, size_t need) {
 int check_distill(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
                   const int64_t* index, int slots, float tau, DistillArgs* a) {
     if (t > kMaxTokens || v < 1 || v > kMaxDim || slots < 1 || slots > LPMM_DISTILL_MAX_SLOTS) return LPMM_EINVAL;
-    if (!std::isfinite(tau) || !(tau > 0.0f) || !std::isfinite(1.0f / tau)) return LPMM_EINVAL;
+    // what the kernels multiply by: log2(e) / tau and tau^2
+    if (!(tau > 0.0f) || !std::isfinite(kLog2e / tau) || !std::isfinite(tau * tau)) return LPMM_EINVAL;
     LPMM_TRY(check_rows(z, z_dtype, t, v, z_stride));
     if (t > 0 && (check_floats(top) || !index || !aligned(index, 8))) return LPMM_EINVAL;
     a->z = z;

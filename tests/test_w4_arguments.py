@@ -51,3 +51,15 @@ def test_a_workspace_with_gaps_or_repeats(workspace):
         binding._workspace(workspace, 64, torch.empty(1), None, "call")
     whole = torch.empty(64)
     assert binding._workspace(whole, 64, torch.empty(1), None, "call") is whole
+
+
+@pytest.mark.parametrize("tau,fine", [(3.5e-39, False), (4.2e-39, False), (4.5e-39, True), (1e-3, True), (1.0, True), (1.8e19, True), (1.9e19, False),
+                                      (3.0e38, False), (float("inf"), False), (float("nan"), False), (0.0, False), (-1.0, False)])
+def test_temperatures_beyond_fp32(tau, fine):
+    """log2(e) / tau or tau^2 of infinity would meet a difference of 0.  No rows: nothing is launched."""
+    L = lpmm.lib()
+    want = 0 if fine else -1
+    args = [None, 0, 0, 100, 100, None, None, 6, tau]
+    assert L.lpmm_distill_loss(*args, None, None, None, 0, None) == want
+    assert L.lpmm_distill_grad(*args, None, None, None, 100, None) == want
+    assert L.lpmm_distill_loss_grad(*args, None, None, None, None, 100, None, 0, None) == want
