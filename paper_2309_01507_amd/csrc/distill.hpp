@@ -321,6 +321,37 @@ __device__ __forceinline__ void distill_zero(const DistillArgs& a, int64_t row0,
     for (int i = threadIdx.x * kPiece<BF16>; i < len; i += THREADS * kPiece<BF16>) piece_store<BF16, false>(a.dz, row0, i, len, zero);
 }
 
+// A row whose lse is so large that its rounding would be seen in exp(z / tau - lse), or takes the sum's logarithm with it as where all logits are the type's
+// lowest value: one workgroup sums the row up again and writes all of it.  dz may be z: what another workgroup writes is not read.
+constexpr float kLseLarge = 1024.0f;     // half a unit in the last place is 2^-14
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void distill_grad_row(const DistillArgs& a, int64_t row, const DistillSlots& s_slots, float g) {
+    __shared__ float s_m[THREADS / 64], s_l[THREADS / 64];
+    constexpr int VEC = kPiece<BF16>;
+    const int64_t z0 = row * a.z_stride, o0 = row * a.dz_stride;
+    float m, l;
+    if (threadIdx.x < 64) distill_teacher<BF16>(a, row, s_slots, m, l);
+    distill_span_ml<BF16, THREADS>(a, row, 0, a.v, s_m, s_l, m, l);        // behind its barrier everything has been read
+    m = s_m[0], l = s_l[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) join_ml(a.c, m, l, s_m[w], s_l[w]);
+    const float f = g / l;
+    for (int at = threadIdx.x * VEC; at < a.v; at += THREADS * VEC) {
+        float x[VEC];
+        piece_values<BF16>(piece_load<BF16>(a.z, z0, at, a.v), x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = f * exp2_fast((x[e] - m) * a.c);
+        piece_store<BF16, false>(a.dz, o0, at, a.v, x);
+    }
+    distill_repeats<THREADS>(a, s_slots);
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.slots; j += THREADS) {
+        const int at = s_slots.at[j];
+        if (at >= 0 && !s_slots.later[j])
+            w4_store1<BF16>(a.dz, o0 + at, g * (exp2_fast((s_slots.z[j] - m) * a.c) / l - distill_place_p(a, s_slots, j)));
+    }
+}
+
 // A workgroup takes kGradPieces pieces per thread of a row: 4096 x 32000 bf16 103 us, 5.1 TB/s; 4096 x 50257 159 us, 5.2 TB/s.
 constexpr int kGradPieces = 4;
 template <bool BF16, int THREADS> constexpr int kGradSpan = THREADS * kGradPieces * kPiece<BF16>;
@@ -331,9 +362,14 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillArgs
     const int64_t row = blockIdx.y;
     const int first = blockIdx.x * kGradSpan<BF16, THREADS>, last = min(first + kGradSpan<BF16, THREADS>, a.v);
     const int64_t z0 = row * a.z_stride, o0 = row * a.dz_stride;
+    const float grad = a.grad[row], g = grad * a.tau, lse = a.lse[row];
     const bool any = distill_any(a, row);
-    if (!any || a.grad[row] == 0.0f) {
+    if (!any || grad == 0.0f) {
         distill_zero<BF16, THREADS>(a, o0 + first, last - first);
+        return;
+    }
+    if (fabsf(lse) >= kLseLarge) {
+        if (blockIdx.x == 0) distill_grad_row<BF16, THREADS>(a, row, s_slots, g);
         return;
     }
     Vec16 r[kGradPieces];
@@ -344,7 +380,6 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillArgs
         float u_max, log_total;
         distill_teacher<BF16>(a, row, s_slots, u_max, log_total);
     }
-    const float g = a.grad[row] * a.tau, lse = a.lse[row];
     __syncthreads();                     // dz may be z: everything has been read (the slots' logits by the first wave)
 #pragma unroll
     for (int j = 0; j < kGradPieces; ++j) {
