@@ -104,7 +104,9 @@ class _Distill(torch.autograd.Function):
 
 def distill_loss(logits: torch.Tensor, top: torch.Tensor, index: torch.Tensor, tau: float = 1.0) -> torch.Tensor:
     """Loss of each token against a teacher's largest logits (lpmm_distill_loss): logits (..., vocabulary), top and index (..., slots),
-    index -1 in slots that do not count; the result has the leading dimensions."""
+    index -1 in slots that do not count; the result has the leading dimensions.  The teacher gets no gradient: detach its logits."""
+    if top.requires_grad and torch.is_grad_enabled():
+        raise ValueError("distill_loss: there is no gradient for the teacher's logits; detach them")
     lead = logits.shape[:-1]
     z = _flat(logits, logits.shape[-1])
     loss = _Distill.apply(z, top.reshape(-1, top.shape[-1]).contiguous(), index.reshape(-1, index.shape[-1]).contiguous(), float(tau))

@@ -63,3 +63,12 @@ def test_temperatures_beyond_fp32(tau, fine):
     assert L.lpmm_distill_loss(*args, None, None, None, 0, None) == want
     assert L.lpmm_distill_grad(*args, None, None, None, 100, None) == want
     assert L.lpmm_distill_loss_grad(*args, None, None, None, None, 100, None, 0, None) == want
+
+
+def test_a_teacher_that_wants_a_gradient():
+    z, top, index = torch.zeros(2, 10, requires_grad=True), torch.zeros(2, 3, requires_grad=True), torch.zeros(2, 3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="detach"):
+        lpmm.distill_loss(z, top, index)
+    for call in (lambda: lpmm.distill_loss(z, top.detach(), index), lambda: torch.no_grad()(lpmm.distill_loss)(z, top, index)):
+        with pytest.raises(ValueError, match="on the current GPU"):            # no GPU here: the next thing that is refused
+            call()
