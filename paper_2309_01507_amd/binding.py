@@ -720,6 +720,13 @@ def new_w4(rows: int, cols: int, group: int = 128, device="cuda") -> WeightsW4:
                      torch.empty(rows, sz[1] // (4 * rows), dtype=torch.float32, device=device))
 
 
+def _written(*tensors) -> None:
+    """Autograd learns that a kernel has written into the caller's tensors, and refuses a backward pass that saved them before."""
+    for t in tensors:
+        if not t.is_inference():
+            _torch.autograd.graph.increment_version(t)
+
+
 def lpmm_w4_quant(w, group: int = 128, out: Optional[WeightsW4] = None, stream=None) -> WeightsW4:
     """w: rows x cols, float32 or bfloat16.  Returns `out`, or new codes and scales."""
     if out is None:
@@ -736,6 +743,7 @@ def lpmm_w4_quant(w, group: int = 128, out: Optional[WeightsW4] = None, stream=N
     shape = _shape(out.rows, out.cols)
     _check(lib().lpmm_w4_quant(ptr, dtype, ld, ctypes.addressof(shape), group, out.codes.data_ptr(),
                                out.scales.data_ptr(), _stream(stream)), "lpmm_w4_quant")
+    _written(out.codes, out.scales)
     return out
 
 

@@ -26,15 +26,15 @@ class _Product(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, scales, w):
         flat = _flat(x.detach(), w.cols)
-        ctx.w, ctx.shape = w, x.shape
-        ctx.save_for_backward(flat if ctx.needs_input_grad[1] else None, scales)
+        ctx.rows, ctx.cols, ctx.group, ctx.shape = w.rows, w.cols, w.group, x.shape
+        ctx.save_for_backward(flat if ctx.needs_input_grad[1] else None, scales, w.codes)
         return _b.lpmm_w4_linear(flat, w).view(*x.shape[:-1], w.rows)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, scales = ctx.saved_tensors
-        w = _b.WeightsW4(ctx.w.rows, ctx.w.cols, ctx.w.group, ctx.w.codes, scales.detach())
+        x, scales, codes = ctx.saved_tensors
+        w = _b.WeightsW4(ctx.rows, ctx.cols, ctx.group, codes, scales.detach())
         dy = _flat(dy, w.rows)
         dx = _b.lpmm_w4_linear_dx(dy, w).view(ctx.shape) if ctx.needs_input_grad[0] else None
         dscales = _b.lpmm_w4_linear_dscale(x, dy, w) if ctx.needs_input_grad[1] else None

@@ -95,3 +95,25 @@ def test_a_cast_layer_computes_in_bf16():
     want, mag = x.detach().cpu().double() @ full.t(), x.detach().cpu().double().abs() @ full.abs().t()
     ref.assert_within(y.detach(), want, ref.bound(torch.bfloat16, want, mag, 204), "y")
     assert layer.scales.grad.dtype == torch.float32 and x.grad.dtype == torch.bfloat16
+
+
+@pytest.mark.parametrize("part", ["codes", "scales", "both"])
+def test_weights_quantized_anew_between_forward_and_backward(part):
+    """The gradient would be that of other weights than the product's."""
+    torch.manual_seed(6)
+    layer = lpmm.W4Linear.from_weight(torch.randn(40, 96, device=DEV), 32)
+    x = torch.randn(3, 96, device=DEV, requires_grad=True)
+    y = layer(x)
+    if part == "codes":
+        layer.codes.copy_(layer.codes.flip(0))
+    elif part == "scales":
+        with torch.no_grad():
+            layer.scales.mul_(2)
+    else:
+        lpmm.lpmm_w4_quant(torch.randn(40, 96, device=DEV), 32, layer.weights())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    layer(x).sum().backward()
+    assert x.grad is not None and layer.scales.grad is not None
+    with torch.inference_mode():
+        lpmm.lpmm_w4_quant(torch.randn(40, 96, device=DEV), 32, lpmm.new_w4(40, 96, 32))
