@@ -883,6 +883,8 @@ def lpmm_distill_grad(z, top, index, tau, lse, grad, dz=None, stream=None):
     _on_current("lpmm_distill_grad", z, top, index, lse, grad, dz)
     _check((_lib or lib()).lpmm_distill_grad(*args, _per_row(lse, t, "lse"), _per_row(grad, t, "grad"), dptr, dld,
                                              _stream(stream)), "lpmm_distill_grad")
+    if dptr == args[0]:
+        _written(dz)
     return dz
 
 
@@ -898,6 +900,8 @@ def lpmm_distill_loss_grad(z, top, index, tau, grad, loss=None, lse=None, dz=Non
     _on_current("lpmm_distill_loss_grad", z, top, index, grad, loss, lse, dz)
     _check(L.lpmm_distill_loss_grad(*args, _per_row(grad, t, "grad"), loss_ptr, lse_ptr, dptr, dld, _ptr(workspace),
                                     _room(workspace), _stream(stream)), "lpmm_distill_loss_grad")
+    if dptr == args[0]:
+        _written(dz)
     return loss, dz
 
 

@@ -117,3 +117,17 @@ def test_weights_quantized_anew_between_forward_and_backward(part):
     assert x.grad is not None and layer.scales.grad is not None
     with torch.inference_mode():
         lpmm.lpmm_w4_quant(torch.randn(40, 96, device=DEV), 32, lpmm.new_w4(40, 96, 32))
+
+
+def test_logits_overwritten_by_their_gradient_between_forward_and_backward():
+    """dz may be z; a backward pass that still needs the logits says so."""
+    z = torch.randn(4, 50, device=DEV, requires_grad=True)
+    logits = z * 1.0
+    top, index, grad = torch.randn(4, 3, device=DEV), torch.randint(0, 50, (4, 3), device=DEV), torch.ones(4, device=DEV)
+    for overwrite in (lambda: lpmm.lpmm_distill_loss_grad(logits.detach(), top, index, 1.0, grad, dz=logits.detach()),
+                      lambda: lpmm.lpmm_distill_grad(logits.detach(), top, index, 1.0, torch.zeros(4, device=DEV), grad, logits.detach())):
+        loss = lpmm.distill_loss(logits, top, index).sum()
+        overwrite()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward(retain_graph=True)
+    lpmm.distill_loss(logits, top, index).sum().backward()
