@@ -31,10 +31,6 @@ __device__ __forceinline__ int w4_place(int d) { return (d & 3) * 4 + (d >> 2); 
 
 // ---- elements ----------------------------------------------------------------------------------------------------------
 
-template <bool BF16> struct W4Elem;
-template <> struct W4Elem<true> { typedef uint16_t type; };
-template <> struct W4Elem<false> { typedef float type; };
-
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
 template <bool BF16>
 __device__ __forceinline__ float w4_load1(const void* p, int64_t i) {

@@ -341,18 +341,12 @@ struct Buffer {
         start = p;
         bytes = int(length < 0x7FFFFFFF ? length : 0x7FFFFFFF);
     }
-    // 16 (or 4) bytes a lane from lane offset `off` + `at` to lane * 16 (4) bytes behind `to`, which is the same in all lanes.  The
+    // 16 bytes a lane from lane offset `off` + `at` to lane * 16 bytes behind `to`, which is the same in all lanes.  The
     // descriptor's type exists in device code only.
     __device__ __forceinline__ void to_lds16(uint32_t off, int at, void* to) const {
 #ifdef __HIP_DEVICE_COMPILE__
         __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(start), 0, bytes, 0x00020000),
                                                  (__attribute__((address_space(3))) void*)(to), 16, off, at, 0, 0);
-#endif
-    }
-    __device__ __forceinline__ void to_lds4(uint32_t off, int at, void* to) const {
-#ifdef __HIP_DEVICE_COMPILE__
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(start), 0, bytes, 0x00020000),
-                                                 (__attribute__((address_space(3))) void*)(to), 4, off, at, 0, 0);
 #endif
     }
 };
