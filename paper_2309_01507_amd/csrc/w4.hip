@@ -135,22 +135,24 @@ int launch_grad(const DistillArgs& a, bool bf16, hipStream_t s) {
 bool launch_both(const DistillArgs& a, bool bf16, hipStream_t s) {
     const int64_t pieces = div_up(a.v, bf16 ? kPiece<true> : kPiece<false>);
     const dim3 rows(unsigned(a.t));
-#define LPMM_BOTH(N, I, W) if (pieces <= (N) * (I)) { \
-        if (bf16) hipLaunchKernelGGL((distill_both_kernel<true, N, I, W>), rows, dim3(N), distill_lds(a.slots), s, a); \
-        else hipLaunchKernelGGL((distill_both_kernel<false, N, I, W>), rows, dim3(N), distill_lds(a.slots), s, a); \
-        return true; }
+#define LPMM_BOTH_OF(B, N, I, W) { hipLaunchKernelGGL((distill_both_kernel<B, N, I, W>), rows, dim3(N), distill_lds(a.slots), s, a); return true; }
+#define LPMM_BOTH(N, I, W) if (pieces <= (N) * (I)) { if (bf16) LPMM_BOTH_OF(true, N, I, W) else LPMM_BOTH_OF(false, N, I, W) }
     LPMM_BOTH(64, 4, 8)
     LPMM_BOTH(64, 8, 4)
     LPMM_BOTH(256, 4, 8)
     LPMM_BOTH(256, 8, 4)
     LPMM_BOTH(256, 16, 3)
-    // 50257 bf16 logits: 4096 rows 205 us with 256 threads, 225 with 512; 300 rows, which do not fill the GPU, 22 and 19
-    if (a.t >= 1024) LPMM_BOTH(256, 25, 3)
+    // 25 pieces a thread, of which a few registers spill, pay for bf16 rows by the thousand (us with 256 and with 512 threads: 33000 logits, 2500 rows 67 and 64, 3500 rows 89
+    // and 85, 4096 106 and 116, 8000 203 and 219; 40000: 71 and 71, 103 and 115, 125 and 130, 233 and 245; 50257: 100 and 101, 160 and 176, 190 and 205, 364 and 396;
+    // 51200: 102 and 100, 141 and 139, 164 and 160, 317 and 303; 300 rows of 50257 22 and 19), for fp32 rows never (4096 rows of 17000, 20001, 25600: 113 and 107,
+    // 143 and 132, 168 and 154)
+    if (bf16 && a.t >= 3500 && pieces <= 256 * 25) LPMM_BOTH_OF(true, 256, 25, 3)
     LPMM_BOTH(512, 13, 4)
     LPMM_BOTH(512, 16, 4)
     LPMM_BOTH(1024, 13, 4)
     LPMM_BOTH(1024, 16, 4)
 #undef LPMM_BOTH
+#undef LPMM_BOTH_OF
     return false;
 }
 

@@ -49,3 +49,33 @@ def test_gradient_of_large_and_of_masked_rows(v, tau, dtype):
     ref.assert_within(lpmm.lpmm_distill_grad(zd, td, xd, tau, got_lse, gd), want, tol, "two calls")
     ref.assert_within(lpmm.lpmm_distill_loss_grad(zd, td, xd, tau, gd)[1], want, tol, "one call")
     ref.assert_within(lpmm.lpmm_distill_grad(zd, td, xd, tau, got_lse, gd, zd), want, tol, "in place")
+
+
+@pytest.mark.parametrize("t,v,dtype", [(3600, 33001, BF16), (3500, 51200, BF16), (3, 20001, F32), (1100, 25600, F32), (3, 60001, F32), (3600, 17000, F32), (5, 51201, BF16)])
+def test_rows_in_registers_of_every_shape(t, v, dtype):
+    """Loss and gradient at once, against 64 bits on the GPU; bounds as in the other tests."""
+    progress(f"distill at once {t} x {v} {dtype}")
+    g = torch.Generator(device=DEV).manual_seed(t)
+    slots, tau = 6, 1.5
+    z = (2.5 * torch.randn(t, v, generator=g, device=DEV)).to(dtype)
+    top, index = 4.0 + torch.randn(t, slots, generator=g, device=DEV), torch.randint(0, v, (t, slots), generator=g, device=DEV)
+    grad = torch.rand(t, generator=g, device=DEV)
+    loss, dz = lpmm.lpmm_distill_loss_grad(z, top, index, tau, grad)
+    u = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    for first in range(0, t, 512):
+        r = slice(first, min(first + 512, t))
+        x = z[r].double() / tau
+        log_q = torch.log_softmax(x, dim=1)
+        p = torch.softmax(top[r].double() / tau, dim=1)
+        at = log_q.gather(1, index[r])
+        want_loss = tau * tau * (p * (p.log() - at)).sum(dim=1)
+        size = (p * (at.abs() + 2 * top[r].double().abs() / tau + 16)).sum(dim=1)
+        q = log_q.exp()
+        target = torch.zeros_like(q).scatter_add_(1, index[r], p)
+        want = grad[r].double()[:, None] * tau * (q - target)
+        err = 2.0 ** -24 * (q * (64 + 4 * x.abs() + 4 * log_q.abs()) + target * (64 + 4 * top[r].double().abs().amax(dim=1, keepdim=True) / tau))
+        tol = u * want.abs() + (1 + u) * grad[r].double()[:, None] * tau * err + 1e-37
+        over = (dz[r].double() - want).abs() - tol
+        assert float(over.max()) <= 0, f"dz: {int((over > 0).sum())} too far off, worst by {float(over.max()):.3g}"
+        over = (loss[r].double() - want_loss).abs() - (tau * tau * 2.0 ** -24 * (8 * size + 80) + 2.0 ** -22 * want_loss.abs())
+        assert float(over.max()) <= 0, f"loss: worst by {float(over.max()):.3g}"
