@@ -170,8 +170,9 @@ int dscale_splits(int64_t t, const W4Mat& m, bool direct) {
 }
 
 // The gradient of the input: tiles of 128 inputs by 256, 128 or 64 tokens, the largest that still fill the GPU, since W is converted once for a
-// tile (us: bf16 4096 x 11008 x 4096 off 16-byte boundaries 492, 562, 728; 1500 x 4096 x 4032 155, 118, 120; 512 x 4096 x 4096 68, 54, 63; 333 x 2304 x 768
-// 27, 20, 16; fp32 2048 x 4096 x 4096 -, 456, 509; 512 x 4096 x 4096 -, 120, 135; 333 x 2304 x 2304 -, 42, 45); the reduction is split where there are fewer
+// tile (us with each: bf16 4096 x 11008 x 4096 609, 752, -; 1500 x 4096 x 4032 115, 115, -; 512 x 4096 x 4096 66, 54, -; off 16-byte boundaries 711, 885, 1041; 138,
+// 141, 155; 79, 62, 69; 333 x 2304 x 768 30, 21, 17; fp32 2048 x 4096 x 4096 -, 456, 508; 512 x 4096 x 4096 -, 123, 137; 333 x 2304 x 2304 -, 43, 47); the
+// reduction is split where there are fewer
 struct DxPlan {
     bool direct;
     int bt, splits, n_per_split;
@@ -186,9 +187,11 @@ DxPlan dx_plan(int64_t t, const W4Mat& m, bool bf16, bool aligned_rows) {
     const int64_t k_tiles = div_up(m.k, kW4Chunk), tiles = div_up(t, 128) * k_tiles;
     p.bt = bf16 && div_up(t, 256) * k_tiles >= 512 ? 256 : p.direct || (bf16 ? tiles >= 128 : t > 64) ? 128 : 64;
     const int64_t steps = div_up(m.n, kDxStep);
-    // A step takes a workgroup about 0.9 us (fp32: 2), each further split the join 0.2 us and the time of writing and reading a part at 3 TB/s
-    // (333 x 2304 x 768 bf16: 18 splits 21 us, 5 splits 15)
-    const double step_us = bf16 ? 0.9 : 2.0, split_us = 0.2 + double(t) * m.k * 8 / 3e6;
+    // A step takes a workgroup about 1.3 us (fp32: 3.2; 16 to 100 x 4096 x 4096 without splits: 64 steps, 83 to 88 and 190 to 222 us), each further split the join 0.2 us and
+    // the time of writing and reading a part at 3 TB/s.  What that takes and the best of all numbers of splits (us): 1 x 4096 x 4096 bf16 16: 13.2, 20: 12.5; fp32 16: 22,
+    // 20: 21.7; 16 x 2304 x 768 12: 10.4, 32: 9.5; 18: 12.8, 20: 12.8; 64 x 4096 x 4096 8: 22.5, 8: 22.4; 13: 34, 16: 31; 333 x 2304 x 768 6: 17.5, 10: 16.7; 9: 25, 9: 25;
+    // 512 x 4096 x 4096 3: 55, 4: 50; 2: 124, 2: 124; 1000 x 4096 x 1024 5: 35, 8: 32; 4: 68, 4: 68; 128 x 50272 x 1024 32: 54, 48: 52; 32: 103, 32: 103
+    const double step_us = bf16 ? 1.3 : 3.2, split_us = 0.2 + double(t) * m.k * 8 / 3e6;
     const int64_t worth = std::max<int64_t>(1, int64_t(std::sqrt(double(steps) * step_us / split_us)));
     const int splits = splits_for(div_up(t, p.bt) * k_tiles, std::min(div_up(steps, 2), worth), bf16 || p.bt == 64 ? 512 : 256);     // one workgroup of 8 waves a CU
     p.n_per_split = int(div_up(steps, splits)) * kDxStep;
