@@ -358,7 +358,11 @@ int lpmm_w4_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
         }
     } else if (mt == 1) {
         if (runs <= 8) LPMM_FEW_G(false, 1, 8, 1, 4, true)
-        else if (runs > 16 && tiles >= 1024) LPMM_FEW_G(false, 1, 8, 4, 2, false)      // 7 x 32000 x 4096, groups of 64: 53 us, with (16, 1, 4) 66
+        // x of a whole row in registers, some of which spill (238 in groups of 64, 16 in groups of 128), pays for many rows that 8 waves cover at once (us, with it and
+        // with (16, 1, 4); 7 x 32000 x 4096 groups of 64 55 and 67, of 128 34 and 66; 1 x 16384 x 4096 32 and 32, 22 and 31; 16 x 32000 x 4096 60 and 104, 37 and 104; longer
+        // rows 7 x 32000 x 8192 221 and 126, 187 and 126; groups of 32, with 594 spilled, 93 and 68 for 7 x 32000 x 4096)
+        else if (runs > 16 && runs <= 32 && tiles >= 1024 && group == 64) LPMM_FEW(false, 64, 1, 8, 4, 2, false);
+        else if (runs > 16 && runs <= 32 && tiles >= 1024 && group == 128) LPMM_FEW(false, 128, 1, 8, 4, 2, false);
         else LPMM_FEW_G(false, 1, 16, 1, 4, true)                                      // 1 x 4096 x 4096: 9 us, with (16, 2, 4) 17
     } else {
         LPMM_FEW_G(false, 2, 8, 1, 2, true)

@@ -277,8 +277,8 @@ __device__ __forceinline__ void w4_operand8(const void* p, int64_t i, int64_t en
 // the elements 32 s + 8 (l / 16) .. + 7.  The operands of x stay in registers from tile to tile where the waves cover a row at once
 // (K <= 128 A WAVES); the next tile's codes are requested before this one's are used (EARLY: where registers
 // hold them).  Bound by the latency of one round trip for few tiles (1 x 4096 x 4096 bf16, groups of 128: 4.9 us, 1.8 TB/s; 16 tokens 7.3),
-// by reading the codes for many (7 x 32000 x 4096, groups of 64: 18.2 us, 3.9 TB/s).  fp32 holds three terms of x, which leaves no registers to
-// read ahead: 53 us there.
+// by reading the codes for many (7 x 32000 x 4096, groups of 64: 18.2 us, 3.9 TB/s).  fp32 holds three terms of x: with a
+// row of them in registers nothing is read ahead and some spill, 55 us there (groups of 128 34), with one run a wave x is read again for each tile, 67.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));      // 16 and 8 bytes at the alignment of a float
 typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 
