@@ -506,7 +506,8 @@ int lpmm_w4_linear_dx(const void* dy, int dtype, int64_t t, int64_t dy_stride, c
                       size_t workspace_bytes, void* stream);
 
 /* dscales[n][j] = sum_t dy[t][n] sum_{k in group j} x[t][k] value[code[n][k]]: its gradient with respect to the scales,
- * float[n][ceil(k/group)], written, not added to.  x and dy share a type.  Workspace and order as above. */
+ * float[n][ceil(k/group)], written, not added to.  x and dy share a type.  Which of the two sums comes first depends on sizes and alignment:
+ * of an infinite dy the result is infinite or NaN.  Workspace and order as above. */
 size_t lpmm_w4_linear_dscale_workspace_bytes(int64_t t, const int64_t shape[2], int group);
 int lpmm_w4_linear_dscale(const void* x, const void* dy, int dtype, int64_t t, int64_t x_stride, int64_t dy_stride,
                           const uint8_t* codes, const int64_t shape[2], int group, float* dscales, void* workspace,

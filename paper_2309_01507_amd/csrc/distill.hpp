@@ -261,8 +261,8 @@ __device__ __forceinline__ void distill_span_ml(const DistillArgs& a, int64_t ro
     }
 }
 
-// A workgroup takes a row: 4096 x 32000 bf16 45 us, 5.8 TB/s; 4096 x 50257, whose rows start off 16-byte boundaries, 91 us, 4.5 TB/s;
-// 61 x 32000 fp32, one row each for a quarter of the CUs, 8.0 us.
+// A workgroup takes a row: 4096 x 32000 bf16 45 us, 5.8 TB/s; 4096 x 50257, whose rows start off 16-byte boundaries, 89 us, 4.6 TB/s;
+// 61 x 32000 fp32, one row each for a quarter of the CUs, 8.0 to 8.4 us.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void distill_loss_kernel(const DistillArgs a) {
     const DistillSlots s_slots = distill_slots(a.slots);
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(THREADS) void distill_loss_kernel(const DistillArgs
 }
 
 // Few long rows: a workgroup takes `span` logits of a row and leaves its (m, l); a wave per row joins them.  Bound by the latency of two kernels:
-// 16 x 131072 fp32 10.6 us, 0.8 TB/s.
+// 16 x 131072 fp32 11.8 us, 0.7 TB/s.
 constexpr int kDistillThreads = 256;
 template <bool BF16>
 __global__ __launch_bounds__(kDistillThreads) void distill_part_kernel(const DistillArgs a, int span, float2* parts) {
@@ -352,7 +352,8 @@ __device__ __forceinline__ void distill_grad_row(const DistillArgs& a, int64_t r
     }
 }
 
-// A workgroup takes kGradPieces pieces per thread of a row: 4096 x 32000 bf16 103 us, 5.1 TB/s; 4096 x 50257 159 us, 5.2 TB/s.
+// A workgroup takes kGradPieces pieces per thread of a row: 4096 x 32000 bf16, 20 slots, 90 us, 5.8 TB/s; 4096 x 50257, 64 slots, 158 us,
+// 5.2 TB/s.
 constexpr int kGradPieces = 4;
 template <bool BF16, int THREADS> constexpr int kGradSpan = THREADS * kGradPieces * kPiece<BF16>;
 template <bool BF16, int THREADS>
@@ -403,9 +404,10 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(const DistillArgs
 
 // ---- both ----------------------------------------------------------------------------------------------------------------------------
 
-// A workgroup takes a row and holds it in registers, ITEMS pieces a thread: one read, one write.  Bound by memory: 4096 x 32000 fp32 189 us,
-// 5.6 TB/s, bf16 110 us, 4.8 TB/s; 4096 x 50257 bf16 196 to 205 us, 4.0 to 4.2 TB/s (50256: 176; loss, then gradient: 250).  dz goes past the caches but for the
-// shortest rows (NT; 4096 x 57344 bf16 186 us, 198 through them; 65536 x 2000 bf16 200 and 183, fp32 334 and 302).
+// A workgroup takes a row and holds it in registers, ITEMS pieces a thread: one read, one write.  Bound by memory: 4096 x 32000 fp32, 20 slots, 183 us,
+// 5.7 TB/s, bf16 105 us, 5.0 TB/s; 4096 x 50257 bf16, 64 slots, 196 to 200 us, 4.1 TB/s (50256: 177; loss, then gradient: 248).  dz goes past the caches but for the
+// shortest rows (NT; us past them and through them, 64 slots: 4096 x 57344 bf16 185 and 196, 65536 x 2000 bf16 200 and 179, fp32 330 and 303; 8 slots: 174 and 189,
+// 107 and 115, 204 and 210).  The largest shapes spill a few registers: 4 with 25 pieces a thread, 3 to 8 with 16 in 1024 threads.
 template <bool BF16, int THREADS, int ITEMS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void distill_both_kernel(const DistillArgs a) {
     constexpr bool NT = THREADS > 64 || (BF16 && ITEMS > 4);

@@ -3,7 +3,7 @@
 //
 // E2M1 codes are exact in bf16 and gfx950 converts two of them with one instruction, so a product of bf16 inputs with codes
 // goes through the matrix instructions without any rounding; the group's scale is applied to the group's fp32 sum.  fp32
-// inputs are taken apart into three bf16 numbers that add up to them exactly, so the same instructions serve them at a third of the rate.
+// inputs are taken apart into three bf16 numbers that add up to them, so the same instructions serve them at a third of the rate.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -92,7 +92,8 @@ __device__ __forceinline__ float w4_threshold(float m, float s) {
 }
 
 // A lane takes the 8 elements of one word, 16 lanes a run of 128: the group's maximum is a butterfly over 4 to 16 of them and w is read once.  Bound
-// by memory: 32000 x 4096 fp32, groups of 128: 117 us, 5.1 TB/s; 1024 x 50257 bf16, groups of 32: 40 us, 3.3 TB/s (rows off 16-byte boundaries, and
+// by memory: 32000 x 4096 fp32, groups of 128: 117 us, 5.1 TB/s (call after call from a graph; between other kernels, in front of a profiler, 143); 1024 x 50257
+// bf16, groups of 32: 39 us, 3.5 TB/s (rows off 16-byte boundaries, and
 // the eight exact comparisons of an element).
 template <bool BF16, int GROUP>
 __global__ __launch_bounds__(256) void w4_quant_kernel(const void* w, int64_t w_stride, int n, int k, int runs, int groups,
@@ -144,7 +145,8 @@ __device__ __forceinline__ void w4_values8(uint32_t word, float out[8]) {
     v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 3); out[6] = v.x; out[7] = v.y;
 }
 
-// A lane writes the 8 values of one word.  Bound by memory: 32000 x 4096 fp32 115 us, 5.2 TB/s; 1024 x 50257 bf16 22 us, 6.2 TB/s.
+// A lane writes the 8 values of one word.  Bound by memory: 32000 x 4096 fp32 115 us, 5.2 TB/s (between other kernels 127);
+// 1024 x 50257 bf16 22 us, 6.2 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void w4_dequant_kernel(W4Mat m, int runs, int group_shift, void* w, int64_t w_stride) {
     const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);
@@ -187,7 +189,7 @@ __device__ __forceinline__ bf16x8 w4_codes_bf16(uint32_t word) {
     return u.v;
 }
 
-// Floats as three bf16 numbers each with that sum, exactly: the value rounded to 8 bits of significand, what is left (at most 16 bits)
+// Floats as three bf16 numbers each with that sum, exactly from 2^-110 on (below, within the least bf16 number): the value rounded to 8 bits of significand, what is left (at most 16 bits)
 // rounded to 8, and what is left then.  Two at a time, packed.
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const bf16x2 p = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
@@ -276,9 +278,11 @@ __device__ __forceinline__ void w4_operand8(const void* p, int64_t i, int64_t en
 // other and add up in LDS.  A lane's 16 bytes of codes are its operands of four 16x16x32 products: lane l holds row l % 16, and its word s
 // the elements 32 s + 8 (l / 16) .. + 7.  The operands of x stay in registers from tile to tile where the waves cover a row at once
 // (K <= 128 A WAVES); the next tile's codes are requested before this one's are used (EARLY: where registers
-// hold them).  Bound by the latency of one round trip for few tiles (1 x 4096 x 4096 bf16, groups of 128: 4.9 us, 1.8 TB/s; 16 tokens 7.3),
-// by reading the codes for many (7 x 32000 x 4096, groups of 64: 18.2 us, 3.9 TB/s).  fp32 holds three terms of x: with a
-// row of them in registers nothing is read ahead and some spill, 55 us there (groups of 128 34), with one run a wave x is read again for each tile, 67.
+// hold them).  Bound by the latency of one round trip for few tiles (1 x 4096 x 4096 bf16, groups of 128: 4.9 us, 1.8 TB/s; 16 tokens 7.3; beyond what
+// the registers hold of a row x is read again for each chunk: 7 x 4096 x 11008 10.9 us), by reading the codes for many (7 x 32000 x 4096, groups of 64: 18 to 19 us,
+// 3.9 TB/s).  fp32 holds three terms of x: with a
+// row of them in registers nothing is read ahead and some spill, 53 us there (groups of 128 33), with one run a wave x is read again for each tile, 67.  (bf16 in groups of
+// 32 with two runs a wave spills 6.)
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));      // 16 and 8 bytes at the alignment of a float
 typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 

@@ -120,7 +120,8 @@ struct Stage {
 // go from memory into the registers of the waves that use them and are converted there.  Each group's products are summed from 0 and
 // join the total with one multiply-add by the scale.  For fp32 and for bf16 off 16-byte boundaries: x passes through registers, so that its rows may
 // start and end anywhere.  Bound by the matrix unit, for fp32, whose products cost three each, and the taking apart beside it (77 x 50257 x 1024, groups
-// of 32: 50 us, 157 TFLOP/s, 470 of bf16; 4096 x 11008 x 4096, groups of 128: 975 us, 379); by conversions and waits for bf16 (that: 480 us, 770 TFLOP/s).
+// of 32: 51 to 54 us, 150 TFLOP/s, 450 of bf16; 4096 x 11008 x 4096, groups of 128: 945 to 990 us, 380); by conversions and waits for bf16 (that: 469 us, 790 TFLOP/s; groups
+// of 64 spill 4 registers).
 template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                       int64_t y_stride, int n_tiles, int t_tiles) {
@@ -229,7 +230,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_tile_kernel(W4Mat m
 
 // The same for fewer tokens than fill the GPU with such tiles: 32 tokens by NT 32 rows of W per workgroup, whose 4 or 8 waves share the runs and join
 // their sums at the end.  Tokens and codes go from memory into the registers of the lanes that multiply them, a run ahead; nothing is staged.
-// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 64, fp32: 30 us (4 waves 37, tiles above 70).
+// Bound by latency and the taking apart of fp32 (each workgroup repeats it): 100 x 4096 x 4096, groups of 64, fp32: 31 us (4 waves 37, tiles above 70); with
+// 64 rows of W 5 to 11 registers spill.
 template <bool BF16, int GROUP, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void w4_linear_share_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
@@ -415,7 +417,7 @@ __device__ __forceinline__ f32x16 opaque_zero() {
 // ahead; a lane loads the scales of four groups at a time.  Two workgroups of 4 waves share a CU, so that one computes while the other waits at
 // its barrier.  Bound by the matrix unit, beside which the conversion of the codes and the multiply-adds by the scales take issue slots:
 // 4096 x 11008 x 4096, groups of 128: 331 us, 1117 TFLOP/s (a library's bf16 product of that size, without the weights' expansion: 360 to
-// 429 us); groups of 64 375, of 32 443.  8 waves with one workgroup a CU and three buffers: 365 to 391; tokens through registers: 461.
+// 429 us); groups of 64 359, of 32 424.  8 waves with one workgroup a CU and three buffers: 365 to 391; tokens through registers: 461.
 template <int GROUP, int WN, int WT, int NT, int TT, bool CUT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y,
                                                                         int64_t y_stride, int n_tiles, int t_tiles) {
@@ -532,7 +534,8 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_linear_direct_kernel(W4Mat
 
 // The same for fewer tokens than fill the GPU with such tiles: a tile of NT 32 rows of W and TT 32 tokens per workgroup, whose 4 waves share the
 // runs.  Each wave stages its own runs in its own part of LDS, one ahead, and waits for nobody until the sums are joined.  Bound by the latency of
-// a wave's runs: 64 x 4096 x 4096, groups of 128: 6.2 us, 1.6 TB/s; 256 tokens 13.5 us, 635 TFLOP/s.
+// a wave's runs: 64 x 4096 x 4096, groups of 128: 6.1 us, 1.6 TB/s; 256 tokens 13.6 us, 630 TFLOP/s, with one
+// wave a SIMD, beside whose conversions and waits nothing runs.
 template <int GROUP, int NT, int TT, bool CUT>
 __global__ __launch_bounds__(256, 1) void w4_linear_split_kernel(W4Mat m, const void* x, int t, int64_t x_stride, void* y, int64_t y_stride,
                                                               int n_tiles, int t_tiles) {
@@ -676,9 +679,9 @@ __device__ __forceinline__ float sum_columns(f32x16 v) {
 // dscales[n][g] = sum_t dy[t][n] P[t][n][g] with P the product's sum over the group before its scale: the same matrix products, and no
 // weight gradient of n x k is ever formed.  A workgroup takes WN NT 32 rows of W and a run of 128 and walks over the tokens
 // (those of split blockIdx.y); the run's codes stay converted in registers.  Here W is the A operand, so that a lane holds one token and
-// for it 4 consecutive rows of W at a time, as dy has them; the sum over the lanes' tokens waits until the end.  Bound by the matrix unit for
-// many tokens (fp32 4096 x 11008 x 4096, groups of 128: 1310 us, 281 TFLOP/s, 843 of bf16), by one tile's latency for few (fp32 333 x 2304 x 768,
-// groups of 64: 12.8 us with the join).
+// for it 4 consecutive rows of W at a time, as dy has them; the sum over the lanes' tokens waits until the end.  Bound by LDS for
+// many tokens, which delivers one fragment of x for each matrix instruction (fp32 4096 x 11008 x 4096, groups of 128: 1310 us, 281 TFLOP/s, 843 of bf16; bf16
+// off 16-byte boundaries 758 us, groups of 64 with 2 registers spilled), by one tile's latency for few (fp32 333 x 2304 x 768, groups of 64: 12.5 us with the join).
 template <bool BF16, int GROUP, int WN, int WT, int NT, int TT>
 __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
                                                                       int64_t dy_stride, int n_tiles, int t_per_split, float* out,
@@ -808,7 +811,7 @@ __global__ __launch_bounds__(64 * WN * WT, 2) void w4_dscale_tile_kernel(W4Mat m
 // W by a run of 128 that are never written, and at the end multiplied by the codes and added up over the groups.  (With the product over the
 // inputs first, 4096 tokens and 11008 x 4096 took 603 us: a multiply-add a product and token, and dy's conversion.)  Both operands'
 // reduction runs down the rows of their arrays, hence the transposed reads.  Bound by the matrix unit and the reads that feed it: 4096 x 11008 x 4096,
-// groups of 128: 322 us, 1146 TFLOP/s; 333 x 2304 x 768 10.0 us with the join, a third of it the end, where columns are summed up.
+// groups of 128: 319 us, 1160 TFLOP/s; 333 x 2304 x 768 10.0 us with the join, a third of it the end, where columns are summed up.
 template <int GROUP>
 __global__ __launch_bounds__(256, 2) void w4_dscale_direct_kernel(W4Mat m, const void* x, const void* dy, int t, int64_t x_stride,
                                                                int64_t dy_stride, int n_tiles, int t_per_split, float* out,
@@ -942,8 +945,8 @@ __global__ __launch_bounds__(256) void w4_join_kernel(const float* parts, int sp
 // lane a word at a time; the transposition is the reads'.  fp32 takes the six products of terms that reach 2^-24 of the largest; there
 // infinity must not meet a term of 0 of a number that is not, which would make NaN of it.  A dy that is not finite meets W's first term only, and a fourth array,
 // dy's first terms with 2^-126 in its place, the other two; an infinite weight stands in W's third term, which meets that array only, and has 2^-126 in the first.  dy goes through registers, so that rows may start and end anywhere.  Bound by the matrix unit for many tokens (fp32
-// 4096 x 11008 x 4096: 2340 us, 158 TFLOP/s, 946 of bf16; bf16 492 us, 750), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
-// 64: 25.5 us with the join).
+// 4096 x 11008 x 4096: 2425 us, 152 TFLOP/s, 914 of bf16; bf16 705 us, 524, 1050 of bf16), by the steps' latency for few (fp32 333 x 2304 x 768, groups of
+// 64: 25 us with the join).
 
 // A scale as a + b: a has 6 significant bits, so that a code's value times a is exact in bf16, and value * b is rounded to bf16, 2^-13 of the weight.
 // b is taken 2^-20 of the scale too large, so that both have its sign and neither is 0: an infinite dy then meets no 0 and no infinity of the other sign.
@@ -1086,7 +1089,7 @@ __global__ __launch_bounds__(128 * WT, 2) void w4_dx_tile_kernel(W4Mat m, const 
 
 // The same for bf16 tokens on 16-byte boundaries and rows of W in whole steps of 32: dy straight into LDS, value * scale as it stands in W, so that
 // a lane converts a word at a time; the transposition is the reads'.  Bound by the matrix unit, which takes two products for one: 4096 x 11008 x 4096
-// 583 us, 634 TFLOP/s, 1270 of bf16.  (With value * scale rounded to one bf16 number 362 us; the error against 64 bits was then 1.4 times that of rounding dx.)
+// 573 to 610 us, 605 to 645 TFLOP/s, twice that of bf16.  (With value * scale rounded to one bf16 number 362 us; the error against 64 bits was then 1.4 times that of rounding dx.)
 template <bool PARTS, int TT>
 __global__ __launch_bounds__(256, 2) void w4_dx_direct_kernel(W4Mat m, const void* dy, int t, int64_t dy_stride, void* dx, int64_t dx_stride,
                                                            int t_tiles, int k_tiles, int n_per_split, float* parts, int group_shift) {
