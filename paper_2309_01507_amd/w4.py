@@ -108,6 +108,8 @@ def distill_loss(logits: torch.Tensor, top: torch.Tensor, index: torch.Tensor, t
     if top.requires_grad and torch.is_grad_enabled():
         raise ValueError("distill_loss: there is no gradient for the teacher's logits; detach them")
     lead = logits.shape[:-1]
+    if top.shape[:-1] != lead or index.shape != top.shape:
+        raise ValueError(f"distill_loss: top and index must be {tuple(lead)} x slots, like the logits")
     z = _flat(logits, logits.shape[-1])
     loss = _Distill.apply(z, top.reshape(-1, top.shape[-1]).contiguous(), index.reshape(-1, index.shape[-1]).contiguous(), float(tau))
     return loss.view(lead)

@@ -72,3 +72,12 @@ def test_a_teacher_that_wants_a_gradient():
     for call in (lambda: lpmm.distill_loss(z, top.detach(), index), lambda: torch.no_grad()(lpmm.distill_loss)(z, top, index)):
         with pytest.raises(ValueError, match="on the current GPU"):            # no GPU here: the next thing that is refused
             call()
+
+
+@pytest.mark.parametrize("shape", [(3, 2, 4), (6, 4), (2, 2, 4), (4,)])
+def test_a_teacher_of_another_shape(shape):
+    """As many rows in another order would be paired with the wrong tokens."""
+    z, top, index = torch.zeros(2, 3, 10), torch.zeros(2, 3, 4), torch.zeros(2, 3, 4, dtype=torch.int64)
+    for a, b in ((torch.zeros(shape), torch.zeros(shape, dtype=torch.int64)), (torch.zeros(shape), index), (top, torch.zeros(shape, dtype=torch.int64))):
+        with pytest.raises(ValueError, match="like the logits"):
+            lpmm.distill_loss(z, a, b)
