@@ -541,6 +541,71 @@ int lpmm_distill_loss_grad(const void* z, int z_dtype, int64_t t, int64_t v, int
                            const int64_t* index, int slots, float tau, const float* grad, float* loss, float* lse,
                            void* dz, int64_t dz_stride, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- tokens drawn from logits --------------------------------------------------------------------------------------------
+ *
+ * For each row of z (t rows of v logits; z_dtype, z_stride; v at most 2^30) one token, drawn with the row's number u from [0, 1):
+ *   weight  w_i = exp((z_i - max z) / temperature)
+ *   order   falling z, equal ones by rising index
+ *   top_k   the first top_k in that order are kept (0: all)
+ *   top_p   of these each one whose predecessors' weights add up to less than top_p of the sum over all of these (1 and more: all)
+ *   min_p   and of these those with w_i >= min_p (0: all).  The first in the order is kept always.
+ *   token   the lowest index at which the running sum, by rising index, of the kept weights exceeds u times their sum
+ *   logprob log(w_token / that sum), float[t]
+ * temperature 0: the first in the order, logprob 0.  Weights and sums are held in 64 bits.  Each option is one value for all rows or, where the pointer is not null,
+ * an array on the device with one for each row.  Values for all rows are refused where they are NaN, or temperature or top_k negative;
+ * a row's own are taken as they come: a temperature that is not above 0 as 0, top_k below 1 and a top_p of NaN as all, a min_p of NaN as 0.
+ * -infinity is never drawn; where the largest logit is +infinity, only those that are it are.  A row with a NaN, or with nothing
+ * above -infinity, gets token -1 and logprob NaN.  A u below 0 (or NaN) is taken as 0, one of 1 or more draws the last that is kept.  tokens: int64[t]. */
+typedef struct lpmm_sample_options {
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    const float* temperatures;
+    const int32_t* top_ks;
+    const float* top_ps;
+    const float* min_ps;
+} lpmm_sample_options;
+int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* u, const lpmm_sample_options* options,
+                int64_t* tokens, float* logprob, void* stream);
+
+/* ---- the norm of all gradients, and clipping -------------------------------------------------------------------------------
+ *
+ * A plan lists the gradients (LPMM_F32 or LPMM_BF16, numel >= 0 elements next to each other, their elements' alignment) and where
+ * their scaled values go: out == grad scales in place, another buffer of the same type leaves grad as it is, null for a plan that is only
+ * measured.  What is written may overlap nothing else of the plan: a tensor that is listed twice is refused, unless it is only read. */
+typedef struct lpmm_grad_desc {
+    const void* grad;
+    void* out;
+    int64_t numel;
+    int32_t dtype;
+    int32_t reserved;       /* 0 */
+} lpmm_grad_desc;
+
+/* Filled by lpmm_grad_plan_build; the caller keeps it, and copies it as it likes. */
+typedef struct lpmm_grad_plan {
+    void* device;
+    int64_t tensors, chunks;
+    int32_t log_bytes, writes;
+} lpmm_grad_plan;
+
+/* Bytes of device memory for a plan (0 for an invalid list; only numel and dtype are read), and the plan itself: `device`, 256-byte aligned, is the caller's
+ * and has to live, untouched, as long as the plan is used.  The plan refers to the tensors by address.  Building waits for
+ * the stream, so it cannot be captured (LPMM_EINVAL); the calls below can. */
+size_t lpmm_grad_plan_bytes(const lpmm_grad_desc* descs, int64_t n);
+int lpmm_grad_plan_build(const lpmm_grad_desc* descs, int64_t n, void* device, size_t bytes, void* stream, lpmm_grad_plan* plan);
+
+/* norm[0] = sqrt of the sum of all squares (LPMM_GRAD_NORM_L2), or the largest magnitude (LPMM_GRAD_NORM_MAX); 0 for a plan without elements.  Summed in
+ * 64 bits in a fixed order: equal inputs give equal bits.  One NaN makes it NaN.  A plan holds the workspace of this call: two
+ * calls on the same plan must not overlap in time. */
+#define LPMM_GRAD_NORM_L2  0
+#define LPMM_GRAD_NORM_MAX 1
+int lpmm_grad_norm(const lpmm_grad_plan* plan, int kind, float* norm, void* stream);
+
+/* out = grad * min(1, limit / (norm[0] + 1e-6)), the factor rounded to fp32, the product to the gradient's type.  A factor of 1 writes nothing in
+ * place.  norm: device memory.  limit >= 0, infinity included, which is factor 1; a NaN norm makes all gradients NaN, an infinite one makes finite gradients 0. */
+int lpmm_grad_clip(const lpmm_grad_plan* plan, const float* norm, float limit, void* stream);
+/* Both, one after the other. */
+int lpmm_grad_norm_clip(const lpmm_grad_plan* plan, int kind, float limit, float* norm, void* stream);
+
 /* Per-kernel timing for benchmarks, with HIP events recorded on each call's own stream.
  * lpmm_profile_begin(max_calls): from now on every lpmm_adamw4_step / _step_bf16g call in this process
  * records an event before the first pass, between the two and after the second, and every

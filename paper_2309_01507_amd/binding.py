@@ -20,7 +20,7 @@ _LIB = os.path.join(_HERE, "lpmm4.so")
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-SOURCES = ("lpmm4.hip", "w4.hip")
+SOURCES = ("lpmm4.hip", "w4.hip", "sample.hip", "grads.hip")
 
 GRAD_F32, GRAD_BF16 = 0, 1
 
@@ -141,6 +141,13 @@ def lib() -> ctypes.CDLL:
         L.lpmm_distill_loss.argtypes = distill_args + [_VP, _VP, _VP, ctypes.c_size_t, _VP]
         L.lpmm_distill_grad.argtypes = distill_args + [_VP, _VP, _VP, _I64, _VP]
         L.lpmm_distill_loss_grad.argtypes = distill_args + [_VP] * 4 + [_I64, _VP, ctypes.c_size_t, _VP]
+        L.lpmm_sample.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP]
+        L.lpmm_grad_plan_bytes.argtypes = [_VP, _I64]
+        L.lpmm_grad_plan_bytes.restype = ctypes.c_size_t
+        L.lpmm_grad_plan_build.argtypes = [_VP, _I64, _VP, ctypes.c_size_t, _VP, _VP]
+        L.lpmm_grad_norm.argtypes = [_VP, ctypes.c_int, _VP, _VP]
+        L.lpmm_grad_clip.argtypes = [_VP, _VP, _F, _VP]
+        L.lpmm_grad_norm_clip.argtypes = [_VP, ctypes.c_int, _F, _VP, _VP]
         L.lpmm_profile_begin.argtypes = [_I64]
         L.lpmm_profile_end.argtypes = [_VP, _VP]
         _lib = L
@@ -903,6 +910,134 @@ def lpmm_distill_loss_grad(z, top, index, tau, grad, loss=None, lse=None, dz=Non
     if dptr == args[0]:
         _written(dz)
     return loss, dz
+
+
+# ---- tokens drawn from logits --------------------------------------------------------------------------------
+
+class SampleOptions(ctypes.Structure):
+    """Mirror of lpmm_sample_options."""
+    _fields_ = [("temperature", _F), ("top_p", _F), ("min_p", _F), ("top_k", ctypes.c_int32), ("temperatures", _VP), ("top_ks", _VP),
+                ("top_ps", _VP), ("min_ps", _VP)]
+
+
+def _option(o: SampleOptions, name: str, x, dtype, t: int, on: list) -> None:
+    if isinstance(x, _torch.Tensor):
+        if x.dtype is not dtype or x.shape != (t,) or not x.is_contiguous():
+            raise ValueError(f"lpmm_sample: {name} must be a number, or {dtype}, contiguous, one per row")
+        setattr(o, name + "s", x.data_ptr())
+        on.append(x)
+    else:
+        setattr(o, name, x if name != "top_k" else min(max(int(x), -1), 0x7FFFFFFF))
+
+
+def lpmm_sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprob=None, stream=None):
+    """(tokens, logprob): a token for each row of the logits z, drawn with the row's number u from [0, 1) (float32).  Each option is a number,
+    or a tensor with one for each row (float32; top_k int32)."""
+    torch = _torch or _load_torch()
+    if z.dim() != 2:
+        raise ValueError("lpmm_sample: logits must be rows x vocabulary")
+    t, v = z.shape
+    ptr, dtype, _, ld = _rows(z, v, "logits")
+    o, on = SampleOptions(), [z, u]
+    _option(o, "temperature", temperature, torch.float32, t, on)
+    _option(o, "top_k", top_k, torch.int32, t, on)
+    _option(o, "top_p", top_p, torch.float32, t, on)
+    _option(o, "min_p", min_p, torch.float32, t, on)
+    uptr = _per_row(u, t, "u")
+    if tokens is None:
+        tokens = _new(None, (t,), torch.int64, z.device, stream, "tokens")
+    elif tokens.dtype is not torch.int64 or tokens.shape != (t,) or not tokens.is_contiguous():
+        raise ValueError("tokens must be int64, contiguous, one per row")
+    logprob, lptr = _row_out(logprob, u, t, stream, "logprob")
+    _on_current("lpmm_sample", *on, tokens, logprob)
+    _check((_lib or lib()).lpmm_sample(ptr, dtype, t, v, ld, uptr, ctypes.addressof(o), tokens.data_ptr(), lptr, _stream(stream)), "lpmm_sample")
+    return tokens, logprob
+
+
+# ---- the norm of all gradients, and clipping -------------------------------------------------------------------
+
+GRAD_NORM_L2, GRAD_NORM_MAX = 0, 1
+
+
+class GradDesc(ctypes.Structure):
+    """Mirror of lpmm_grad_desc."""
+    _fields_ = [("grad", _VP), ("out", _VP), ("numel", _I64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class GradPlanHost(ctypes.Structure):
+    """Mirror of lpmm_grad_plan."""
+    _fields_ = [("device", _VP), ("tensors", _I64), ("chunks", _I64), ("log_bytes", ctypes.c_int32), ("writes", ctypes.c_int32)]
+
+
+@dataclass
+class GradPlan:
+    """Gradients that are measured and scaled together; refers to them (and holds them) by address.  Two calls on one plan must not overlap."""
+    grads: "object"
+    outs: "object"
+    memory: "object"
+    host: GradPlanHost
+
+
+def new_grad_plan(grads, outs=None, stream=None) -> GradPlan:
+    """Gradients (float32 or bfloat16, contiguous, on the current GPU) as one vector; `outs`: where lpmm_grad_clip writes, in place by default."""
+    torch = _torch or _load_torch()
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if len(outs) != len(grads):
+        raise ValueError("new_grad_plan: one output for each gradient")
+    here = torch._C._cuda_getDevice() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+    descs = (GradDesc * max(1, len(grads)))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        for x, name in ((g, "gradients"), (o, "outputs")):
+            if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_contiguous():
+                raise ValueError(f"new_grad_plan: {name} must be contiguous, float32 or bfloat16")
+            if x.get_device() != here or here < 0:
+                raise ValueError(f"new_grad_plan: {name} must be on the current GPU")
+        if o.dtype != g.dtype or o.numel() != g.numel():
+            raise ValueError("new_grad_plan: an output has the type and size of its gradient")
+        descs[i] = GradDesc(g.data_ptr(), o.data_ptr(), g.numel(), BF16 if g.dtype is torch.bfloat16 else F32, 0)
+    L = lib()
+    need = L.lpmm_grad_plan_bytes(ctypes.addressof(descs), len(grads))
+    if need == 0:
+        raise LpmmError("lpmm_grad_plan_bytes: invalid tensor list")
+    memory = torch.empty(need, dtype=torch.uint8, device=f"cuda:{here}")
+    host = GradPlanHost()
+    _check(L.lpmm_grad_plan_build(ctypes.addressof(descs), len(grads), memory.data_ptr(), need, _stream(stream), ctypes.addressof(host)),
+           "lpmm_grad_plan_build")
+    return GradPlan(grads, outs, memory, host)
+
+
+def _grad_norm_out(plan: GradPlan, norm, stream, what: str):
+    norm = _new(norm, (1,), _torch.float32, plan.memory.device, stream, "norm")
+    _on_current(what, plan.memory, norm)
+    return norm
+
+
+def lpmm_grad_norm(plan: GradPlan, kind: int = GRAD_NORM_L2, norm=None, stream=None):
+    """The norm of all gradients as one vector: a tensor of one float32."""
+    norm = _grad_norm_out(plan, norm, stream, "lpmm_grad_norm")
+    _check((_lib or lib()).lpmm_grad_norm(ctypes.addressof(plan.host), int(kind), norm.data_ptr(), _stream(stream)), "lpmm_grad_norm")
+    return norm
+
+
+def _written_all(tensors) -> None:
+    _torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
+def lpmm_grad_clip(plan: GradPlan, norm, limit: float, stream=None) -> None:
+    """Scales the gradients by min(1, limit / (norm + 1e-6)) into the plan's outputs."""
+    norm = _grad_norm_out(plan, norm, stream, "lpmm_grad_clip")
+    _check((_lib or lib()).lpmm_grad_clip(ctypes.addressof(plan.host), norm.data_ptr(), limit, _stream(stream)), "lpmm_grad_clip")
+    _written_all(plan.outs)
+
+
+def lpmm_grad_norm_clip(plan: GradPlan, limit: float, kind: int = GRAD_NORM_L2, norm=None, stream=None):
+    """Both; returns the norm from before."""
+    norm = _grad_norm_out(plan, norm, stream, "lpmm_grad_norm_clip")
+    _check((_lib or lib()).lpmm_grad_norm_clip(ctypes.addressof(plan.host), int(kind), limit, norm.data_ptr(), _stream(stream)),
+           "lpmm_grad_norm_clip")
+    _written_all(plan.outs)
+    return norm
 
 
 # ---- many tensors in one call ------------------------------------------------------------------------

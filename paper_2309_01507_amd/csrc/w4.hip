@@ -14,13 +14,9 @@ namespace {
 
 using namespace lpmm;
 
-constexpr int64_t kMaxDim = int64_t(1) << 30;
-// A launch has fewer than 2^32 threads
-constexpr int64_t kMaxTokens = (int64_t(1) << 24) - 1, kMaxWeights = int64_t(1) << 34, kMaxBlocks = (int64_t(1) << 23) - 1;
+constexpr int64_t kMaxWeights = int64_t(1) << 34;
 
-int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int group_shift(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
-int elem_size(int dtype) { return dtype == LPMM_BF16 ? 2 : 4; }
 
 int check_w4(const int64_t* shape, int group, W4Mat* m) {
     if (!shape || (group != 32 && group != 64 && group != 128)) return LPMM_EINVAL;
@@ -33,25 +29,6 @@ int check_w4(const int64_t* shape, int group, W4Mat* m) {
     m->groups = int(div_up(shape[1], group));
     return LPMM_OK;
 }
-
-// `rows` rows of `len` elements, `stride` apart
-int check_rows(const void* p, int dtype, int64_t rows, int64_t len, int64_t stride) {
-    if (dtype != LPMM_F32 && dtype != LPMM_BF16) return LPMM_EINVAL;
-    if (rows < 0 || rows > kMaxDim || stride < len || stride > (int64_t(1) << 40)) return LPMM_EINVAL;
-    if (rows > 0 && (!p || !aligned(p, elem_size(dtype)))) return LPMM_EINVAL;
-    return LPMM_OK;
-}
-
-int check_codes(const uint8_t* codes) { return codes && aligned(codes, 16) ? LPMM_OK : LPMM_EINVAL; }
-int check_floats(const float* p) { return p && aligned(p, 4) ? LPMM_OK : LPMM_EINVAL; }
-
-int check_workspace(const void* p, size_t have, size_t need) {
-    if (need == 0) return LPMM_OK;
-    if (!p || !aligned(p, 16)) return LPMM_EINVAL;
-    return have < need ? LPMM_EWORKSPACE : LPMM_OK;
-}
-
-#define LPMM_TRY(call) do { const int rc_ = (call); if (rc_) return rc_; } while (0)
 
 int check_distill(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* top,
                   const int64_t* index, int slots, float tau, DistillArgs* a) {

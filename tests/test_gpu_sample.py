@@ -1,0 +1,173 @@
+"""Tokens drawn from logits on the GPU against a plain 64-bit form: every token, and its log-probability."""
+import pytest
+import torch
+
+import paper_2309_01507_amd as lpmm
+import sample_util as ref
+from conftest import progress
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+
+
+def logits(t, v, dtype, seed, spread=2.5):
+    g = torch.Generator().manual_seed(seed)
+    return (spread * torch.randn(t, v, generator=g)).to(dtype), torch.rand(t, generator=g)
+
+
+def run(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, what="", on_gpu=None):
+    on = lambda o: o.to(DEV) if torch.is_tensor(o) else o
+    zd = z.to(DEV) if on_gpu is None else on_gpu
+    tokens, logprob = lpmm.lpmm_sample(zd, u.to(DEV), on(temperature), on(top_k), on(top_p), on(min_p))
+    ref.check(z, u, temperature, top_k, top_p, min_p, tokens, logprob, what)
+    return tokens, logprob
+
+
+OPTIONS = [{}, {"top_k": 7}, {"top_p": 0.8}, {"min_p": 0.05}, {"temperature": 0.5, "top_k": 40, "top_p": 0.9, "min_p": 0.01},
+           {"temperature": 1.7, "top_p": 0.999}, {"top_k": 1}, {"top_p": 0.0}, {"min_p": 1.0}, {"min_p": 2.0}, {"temperature": 0.0, "top_k": 3}]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [1, 2, 63, 64, 65, 255, 257, 1000, 1024, 1025, 4099])
+def test_sizes_and_options(v, dtype):
+    for n, options in enumerate(OPTIONS):
+        z, u = logits(9, v, dtype, 100 * v + n)
+        run(z, u, what=f"{v} {options}", **options)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,v", [(3, 32000), (2, 50257), (2, 131073), (1, 300001)])
+def test_large_vocabularies(t, v, dtype):
+    for n, options in enumerate(OPTIONS[:6] + [{"top_k": 2000, "top_p": 0.99}, {"temperature": 4.0, "top_k": v - 1, "top_p": 0.5}]):
+        progress(f"sample {t} x {v} {options}")
+        z, u = logits(t, v, dtype, v + n)
+        z[:, v - v // 50:] = -INF
+        run(z, u, what=f"{v} {options}", **options)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [100, 3000, 50257])
+def test_equal_logits(v, dtype):
+    """Few values: borders fall among equal logits, which the index orders; more of them than a list holds."""
+    for n, values in enumerate((1, 2, 5)):
+        g = torch.Generator().manual_seed(v + n)
+        z = torch.randint(0, values, (6, v), generator=g).to(dtype) - 3
+        u = torch.rand(6, generator=g)
+        # numbers of equal weights that a rounded share does not hit: kept ones are counted without a doubt
+        for options in ({}, {"top_k": v // 3}, {"top_p": 0.37}, {"top_k": v // 2 + 1, "top_p": 0.71}, {"min_p": 0.3, "top_p": 0.55}):
+            run(z, u, what=f"{values} values {options}", **options)
+
+
+def test_each_row_its_own():
+    t, v = 200, 2111
+    z, u = logits(t, v, F32, 5)
+    g = torch.Generator().manual_seed(6)
+    heat = 0.2 + 2 * torch.rand(t, generator=g)
+    heat[::7] = 0.0
+    k = torch.randint(0, 60, (t,), generator=g, dtype=torch.int32)
+    k[::5] = v + 3
+    p, least = torch.rand(t, generator=g), 0.2 * torch.rand(t, generator=g)
+    p[::4], least[::3] = 1.0, 0.0
+    run(z, u, heat, k, p, least, what="each")
+    # values that a call for all rows refuses
+    heat[1], heat[2], heat[3], heat[4] = -1.0, NAN, INF, 1e-30
+    k[5], k[6], p[8], p[9], p[10], least[11], least[12] = -4, -2 ** 31, NAN, -3.0, INF, NAN, -1.0
+    tokens, logprob = lpmm.lpmm_sample(z.to(DEV), u.to(DEV), heat.to(DEV), k.to(DEV), p.to(DEV), least.to(DEV))
+    heat[1] = heat[2] = 0.0
+    heat[3] = 1e30                                            # all weights 1, to 30 digits
+    k[5] = k[6] = 0
+    p[8], p[9], least[11], least[12] = 1.0, 0.0, 0.0, 0.0
+    ref.check(z, u, heat, k, p, least, tokens, logprob, "odd values")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_masked_and_unusual_rows(dtype):
+    v = 1500
+    low = torch.finfo(dtype).min
+    z, u = logits(12, v, dtype, 8)
+    z[0] = -INF
+    z[1] = low
+    z[2, 5:] = -INF
+    z[3, :-1] = -INF
+    z[4, 700] = NAN
+    z[5, 3] = z[5, 900] = INF
+    z[6, 3], z[6, 9] = INF, -INF
+    z[7] = INF
+    z[8, ::2] = low
+    z[9] = -INF
+    z[9, 44] = NAN
+    z[10, 0], z[10, 1] = torch.finfo(dtype).max, low
+    z[11] = 0.0
+    z[11, ::3] = -0.0
+    for options in ({}, {"top_k": 4}, {"top_p": 0.6}, {"top_k": 900, "top_p": 0.95}, {"min_p": 0.5}, {"temperature": 0.0}, {"temperature": 0.01, "top_p": 0.9}):
+        run(z, u, what=f"{options}", **options)
+
+
+def test_numbers_at_the_ends():
+    """u of 0, just below 1, 1, negative, NaN: the first kept, the last kept."""
+    v = 333
+    z, _ = logits(7, v, F32, 9)
+    z[:] = z[0]
+    z[:, 0] = z[:, -1] = -INF
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, -1.0, NAN, INF, -INF])
+    for options in ({}, {"top_k": 11}):
+        tokens, _ = lpmm.lpmm_sample(z.to(DEV), u.to(DEV), **options)
+        kept = torch.topk(z[0], options.get("top_k", v - 2)).indices
+        first, last = int(kept.min()), int(kept.max())
+        assert tokens.tolist() == [first, last, last, first, first, last, first]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_anywhere(dtype):
+    """Rows apart, off every boundary, and beyond 2^31 elements"""
+    z, u = logits(5, 777, dtype, 10)
+    for gap, off in ((1, 1), (3, 5), (0, 3)):
+        room = torch.full((5 * (777 + gap) + off,), NAN, dtype=dtype, device=DEV)
+        view = room[off:].view(5, 777 + gap)[:, :777]
+        view.copy_(z)
+        run(z, u, top_p=0.9, what=f"{gap} {off}", on_gpu=view)
+    far = torch.empty(2 ** 31 + 1000, dtype=dtype, device=DEV)
+    view = far.as_strided((2, 777), (2 ** 31 + 64, 1))
+    view.copy_(z[:2])
+    run(z[:2], u[:2], top_k=30, what="far", on_gpu=view)
+
+
+def test_no_rows_and_given_outputs():
+    z = torch.zeros(0, 100, device=DEV)
+    tokens, logprob = lpmm.lpmm_sample(z, torch.zeros(0, device=DEV))
+    assert tokens.shape == logprob.shape == (0,) and tokens.dtype == torch.int64
+    z, u = logits(4, 900, F32, 11)
+    z, u = z.to(DEV), u.to(DEV)
+    want = lpmm.lpmm_sample(z, u, top_p=0.9)
+    room, lp = torch.full((6,), 77, device=DEV), torch.full((6,), 7.0, device=DEV)
+    got = lpmm.lpmm_sample(z, u, top_p=0.9, tokens=room[1:5], logprob=lp[1:5])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert room[[0, 5]].tolist() == [77, 77] and lp[[0, 5]].tolist() == [7.0, 7.0]
+
+
+def test_on_a_stream_and_captured():
+    """The same bits on another stream and from a captured graph, replayed with other logits and numbers in between"""
+    t, v = 20, 9001
+    z, u = logits(t, v, BF16, 12)
+    z, u = z.to(DEV), u.to(DEV)
+    sets = [(z.clone(), u.clone()), (z.flip(0).contiguous(), u.flip(0).contiguous()), (z * 0.5, 1 - u)]
+    options = dict(temperature=0.9, top_k=500, top_p=0.95, min_p=0.001)
+    want = [lpmm.lpmm_sample(a, b, **options) for a, b in sets]
+    tokens, logprob = torch.empty(t, dtype=torch.int64, device=DEV), torch.empty(t, device=DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    lpmm.lpmm_sample(z, u, **options, tokens=tokens, logprob=logprob, stream=s)
+    s.synchronize()
+    assert torch.equal(tokens, want[0][0]) and torch.equal(logprob, want[0][1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lpmm.lpmm_sample(z, u, **options, tokens=tokens, logprob=logprob)
+    for n in (0, 1, 2, 1, 0):
+        z.copy_(sets[n][0])
+        u.copy_(sets[n][1])
+        graph.replay()
+        assert torch.equal(tokens, want[n][0]) and torch.equal(logprob, want[n][1])
+        torch.randn(1000, device=DEV).sum().item()
