@@ -541,6 +541,46 @@ int lpmm_distill_loss_grad(const void* z, int z_dtype, int64_t t, int64_t v, int
                            const int64_t* index, int slots, float tau, const float* grad, float* loss, float* lse,
                            void* dz, int64_t dz_stride, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- matrices in 8-bit floating point with a power of two for each block of 128 -----------------------------------------
+ *
+ * A matrix of `rows` x `cols` in blocks of 1 x 128 (tile 1: activations, gradients) or 128 x 128 (tile 128: weights) elements, the last ones cut off
+ * by its edges.  An element is code * 2^(scale - 127).
+ *   scale   one byte per block: the least power of two that brings the block's largest finite magnitude to at most 448, at least 2^-127 (a block of zeros)
+ *   code    E4M3 (1 sign, 4 exponent, 3 fraction bits; up to 448, no infinities): the element divided by the power, which is exact, rounded to the
+ *           nearest, ties to even.  Infinities and NaN have the code of NaN.
+ *   codes   rows of cols rounded up to a multiple of 128 bytes, the rest of a row 0 (the products rely on that); 16-byte aligned
+ *   scales  ceil(rows / tile) rows of ceil(cols / 128) bytes rounded up to a multiple of 4, the rest 0; 4-byte aligned
+ * cols is at most 2^22, rows at most 2^30, with 2^33 codes at most.  Tensors of rows, workspaces and streams as for the 4-bit weights above. */
+typedef struct lpmm_f8 {
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t rows, cols;
+    int32_t tile;           /* 1 or 128 */
+    int32_t reserved;       /* 0 */
+} lpmm_f8;
+
+/* Bytes of {codes, scales}. */
+int lpmm_f8_sizes(int64_t rows, int64_t cols, int tile, size_t sizes[2]);
+
+/* x, out->rows x out->cols of dtype, into 8 bits; and x together with its transpose from one reading: out_t is cols x rows of the same tile, its blocks of 1 x 128
+ * lie along the rows of x (rows >= 1, at most 128 * 65535, as for tile 128). */
+int lpmm_f8_quant(const void* x, int dtype, int64_t stride, const lpmm_f8* out, void* stream);
+int lpmm_f8_quant_both(const void* x, int dtype, int64_t stride, const lpmm_f8* out, const lpmm_f8* out_t, void* stream);
+
+/* The values, which bf16 holds exactly too (below 2^-133, and beyond its largest number, as near as it can). */
+int lpmm_f8_dequant(const lpmm_f8* f, void* out, int dtype, int64_t stride, void* stream);
+
+/* c[i][j] = sum_k a[i][k] b[j][k], a->rows x b->rows; any tiles.  LPMM_F32: summed in fp32.  LPMM_BF16: by the matrix instructions on 8 bits, which cut
+ * off what lies some 2^-13 below the largest of 64 or 128 products, then in fp32, and rounded.  The order of all sums is fixed. */
+size_t lpmm_f8_matmul_workspace_bytes(int64_t a_rows, int64_t b_rows, int64_t cols);
+int lpmm_f8_matmul(const lpmm_f8* a, const lpmm_f8* b, void* c, int dtype, int64_t stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* y = x W^T, a linear layer for t tokens, one or many: x is brought to 8 bits (tile 1) within the call, y has its type.  The same bits as
+ * lpmm_f8_quant and lpmm_f8_matmul are not promised: sums may be taken in another order. */
+size_t lpmm_f8_linear_workspace_bytes(int64_t t, int64_t n, int64_t k);
+int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const lpmm_f8* w, void* y, int64_t y_stride, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
 /* ---- tokens drawn from logits --------------------------------------------------------------------------------------------
  *
  * For each row of z (t rows of v logits; z_dtype, z_stride; v at most 2^30) one token, drawn with the row's number u from [0, 1):

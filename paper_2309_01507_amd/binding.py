@@ -20,7 +20,7 @@ _LIB = os.path.join(_HERE, "lpmm4.so")
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-SOURCES = ("lpmm4.hip", "w4.hip", "sample.hip", "grads.hip")
+SOURCES = ("lpmm4.hip", "w4.hip", "f8.hip", "sample.hip", "grads.hip")
 
 GRAD_F32, GRAD_BF16 = 0, 1
 
@@ -141,6 +141,16 @@ def lib() -> ctypes.CDLL:
         L.lpmm_distill_loss.argtypes = distill_args + [_VP, _VP, _VP, ctypes.c_size_t, _VP]
         L.lpmm_distill_grad.argtypes = distill_args + [_VP, _VP, _VP, _I64, _VP]
         L.lpmm_distill_loss_grad.argtypes = distill_args + [_VP] * 4 + [_I64, _VP, ctypes.c_size_t, _VP]
+        L.lpmm_f8_sizes.argtypes = [_I64, _I64, ctypes.c_int, _VP]
+        L.lpmm_f8_quant.argtypes = [_VP, ctypes.c_int, _I64, _VP, _VP]
+        L.lpmm_f8_quant_both.argtypes = [_VP, ctypes.c_int, _I64, _VP, _VP, _VP]
+        L.lpmm_f8_dequant.argtypes = [_VP, _VP, ctypes.c_int, _I64, _VP]
+        L.lpmm_f8_matmul_workspace_bytes.argtypes = [_I64] * 3
+        L.lpmm_f8_matmul_workspace_bytes.restype = ctypes.c_size_t
+        L.lpmm_f8_matmul.argtypes = [_VP, _VP, _VP, ctypes.c_int, _I64, _VP, ctypes.c_size_t, _VP]
+        L.lpmm_f8_linear_workspace_bytes.argtypes = [_I64] * 3
+        L.lpmm_f8_linear_workspace_bytes.restype = ctypes.c_size_t
+        L.lpmm_f8_linear.argtypes = [_VP, ctypes.c_int, _I64, _I64, _VP, _VP, _I64, _VP, ctypes.c_size_t, _VP]
         L.lpmm_sample.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP]
         L.lpmm_grad_plan_bytes.argtypes = [_VP, _I64]
         L.lpmm_grad_plan_bytes.restype = ctypes.c_size_t
@@ -910,6 +920,135 @@ def lpmm_distill_loss_grad(z, top, index, tau, grad, loss=None, lse=None, dz=Non
     if dptr == args[0]:
         _written(dz)
     return loss, dz
+
+
+# ---- matrices in 8 bits with a power of two for each block of 128 ---------------------------------------------
+
+class _F8(ctypes.Structure):
+    """Mirror of lpmm_f8."""
+    _fields_ = [("codes", _VP), ("scales", _VP), ("rows", _I64), ("cols", _I64), ("tile", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+@dataclass
+class MatF8:
+    """A rows x cols matrix in 8 bits (lpmm4.h): E4M3 codes and a power of two for each block of tile x 128 elements, uint8 both.
+    codes.view(torch.float8_e4m3fn) are the codes as torch has them."""
+    rows: int
+    cols: int
+    tile: int
+    codes: "object"
+    scales: "object"
+
+
+def _f8_check(m: MatF8, what: str) -> _F8:
+    torch = _torch or _load_torch()
+    codes, scales, rows, cols, tile = m.codes, m.scales, m.rows, m.cols, m.tile
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
+        raise ValueError(f"{what}: codes and scales must be uint8, not {codes.dtype} and {scales.dtype}")
+    blocks = (cols + 127) // 128
+    if (tile not in (1, 128) or codes.numel() != rows * blocks * 128 or scales.numel() != -(-rows // tile) * ((blocks + 3) // 4 * 4) or
+            not codes.is_contiguous() or not scales.is_contiguous()):
+        raise ValueError(f"{what}: codes or scales are not those of a {rows} x {cols} matrix with blocks of {tile} x 128")
+    return _F8(codes.data_ptr(), scales.data_ptr(), rows, cols, tile, 0)
+
+
+def lpmm_f8_sizes(rows: int, cols: int, tile: int = 1):
+    """Bytes of the codes and of the scales."""
+    sizes = (ctypes.c_size_t * 2)()
+    _check(lib().lpmm_f8_sizes(int(rows), int(cols), int(tile), ctypes.addressof(sizes)), "lpmm_f8_sizes")
+    return [int(s) for s in sizes]
+
+
+def new_f8(rows: int, cols: int, tile: int = 1, device="cuda") -> MatF8:
+    """Allocate (torch) room for a matrix in 8 bits; lpmm_f8_quant fills it."""
+    import torch
+    sz = lpmm_f8_sizes(rows, cols, tile)
+    return MatF8(rows, cols, tile, torch.empty(rows, -(-cols // 128) * 128, dtype=torch.uint8, device=device),
+                 torch.empty(sz[1], dtype=torch.uint8, device=device).view(-(-rows // tile), -1) if sz[1] else
+                 torch.empty(0, 4, dtype=torch.uint8, device=device))
+
+
+def _f8_out(out, rows: int, cols: int, tile: int, like, stream, what: str) -> MatF8:
+    if out is None:
+        if stream is not None:
+            raise ValueError(f"{what}: a call on a stream of its own needs its outputs given")
+        return new_f8(rows, cols, tile, like.device)
+    if (out.rows, out.cols, out.tile) != (rows, cols, tile):
+        raise ValueError(f"{what}: the output has another shape or tile")
+    return out
+
+
+def lpmm_f8_quant(x, tile: int = 1, out: Optional[MatF8] = None, stream=None) -> MatF8:
+    """x (float32 or bfloat16) in 8 bits, in blocks of 1 x 128 or 128 x 128.  Returns `out`, or new codes and scales."""
+    if x.dim() != 2:
+        raise ValueError("lpmm_f8_quant: x must be a matrix")
+    rows, cols = x.shape
+    ptr, dtype, _, ld = _rows(x, cols, "x")
+    out = _f8_out(out, rows, cols, tile, x, stream, "lpmm_f8_quant")
+    f = _f8_check(out, "out")
+    _on_current("lpmm_f8_quant", x, out.codes, out.scales)
+    _check((_lib or lib()).lpmm_f8_quant(ptr, dtype, ld, ctypes.addressof(f), _stream(stream)), "lpmm_f8_quant")
+    _written(out.codes, out.scales)
+    return out
+
+
+def lpmm_f8_quant_both(x, tile: int = 1, out: Optional[MatF8] = None, out_t: Optional[MatF8] = None, stream=None):
+    """(x, x transposed) in 8 bits, from one reading; blocks of 1 x 128 lie along the rows of each."""
+    if x.dim() != 2:
+        raise ValueError("lpmm_f8_quant_both: x must be a matrix")
+    rows, cols = x.shape
+    ptr, dtype, _, ld = _rows(x, cols, "x")
+    out = _f8_out(out, rows, cols, tile, x, stream, "lpmm_f8_quant_both")
+    out_t = _f8_out(out_t, cols, rows, tile, x, stream, "lpmm_f8_quant_both")
+    f, ft = _f8_check(out, "out"), _f8_check(out_t, "out_t")
+    _on_current("lpmm_f8_quant_both", x, out.codes, out.scales, out_t.codes, out_t.scales)
+    _check((_lib or lib()).lpmm_f8_quant_both(ptr, dtype, ld, ctypes.addressof(f), ctypes.addressof(ft), _stream(stream)), "lpmm_f8_quant_both")
+    _written(out.codes, out.scales, out_t.codes, out_t.scales)
+    return out, out_t
+
+
+def lpmm_f8_dequant(m: MatF8, dtype=None, out=None, stream=None):
+    """The values as a rows x cols matrix, float32 or bfloat16 (`dtype`, or that of `out`; float32 by default)."""
+    torch = _torch or _load_torch()
+    f = _f8_check(m, "lpmm_f8_dequant")
+    if dtype is None:
+        dtype = torch.float32 if out is None else out.dtype
+    out = _new(out, (m.rows, m.cols), dtype, m.codes.device, stream, "out")
+    ptr, dt, _, ld = _rows(out, m.cols, "out")
+    _on_current("lpmm_f8_dequant", m.codes, m.scales, out)
+    _check((_lib or lib()).lpmm_f8_dequant(ctypes.addressof(f), ptr, dt, ld, _stream(stream)), "lpmm_f8_dequant")
+    return out
+
+
+def lpmm_f8_matmul(a: MatF8, b: MatF8, dtype=None, out=None, workspace=None, stream=None):
+    """a b^T, a.rows x b.rows, float32 or bfloat16 (`dtype`, or that of `out`; bfloat16 by default); any tiles."""
+    torch = _torch or _load_torch()
+    fa, fb = _f8_check(a, "lpmm_f8_matmul"), _f8_check(b, "lpmm_f8_matmul")
+    if a.cols != b.cols:
+        raise ValueError(f"lpmm_f8_matmul: rows of {a.cols} and of {b.cols} elements")
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    out = _new(out, (a.rows, b.rows), dtype, a.codes.device, stream, "out")
+    ptr, dt, _, ld = _rows(out, b.rows, "out")
+    L = _lib or lib()
+    workspace = _workspace(workspace, L.lpmm_f8_matmul_workspace_bytes(a.rows, b.rows, a.cols), a.codes, stream, "lpmm_f8_matmul")
+    _on_current("lpmm_f8_matmul", a.codes, a.scales, b.codes, b.scales, out)
+    _check(L.lpmm_f8_matmul(ctypes.addressof(fa), ctypes.addressof(fb), ptr, dt, ld, _ptr(workspace), _room(workspace), _stream(stream)),
+           "lpmm_f8_matmul")
+    return out
+
+
+def lpmm_f8_linear(x, w: MatF8, y=None, workspace=None, stream=None):
+    """y = x W^T: x is tokens x cols (float32 or bfloat16) and is brought to 8 bits within the call, y tokens x rows of the same type."""
+    f = _f8_check(w, "lpmm_f8_linear")
+    ptr, dtype, t, ld = _rows(x, w.cols, "x")
+    y, yptr, yld = _matrix_out(y, x, t, w.rows, stream, "y")
+    L = _lib or lib()
+    workspace = _workspace(workspace, L.lpmm_f8_linear_workspace_bytes(t, w.rows, w.cols), x, stream, "lpmm_f8_linear")
+    _on_current("lpmm_f8_linear", x, w.codes, w.scales, y)
+    _check(L.lpmm_f8_linear(ptr, dtype, t, ld, ctypes.addressof(f), yptr, yld, _ptr(workspace), _room(workspace), _stream(stream)),
+           "lpmm_f8_linear")
+    return y
 
 
 # ---- tokens drawn from logits --------------------------------------------------------------------------------

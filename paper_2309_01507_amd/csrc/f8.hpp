@@ -1,0 +1,241 @@
+// Matrices in 8-bit floating point with a power of two for each block of 128: bringing them there and back, for the rows of a matrix,
+// for its transpose, or both from one reading (format and formulas: include/lpmm4.h).
+//
+// The power is found from the bits of the block's largest element, and multiplying by it is exact, so the rounding to E4M3 by the
+// hardware's conversion is the only one.
+#pragma once
+
+#include "rows.hpp"
+
+namespace lpmm {
+
+constexpr int kF8Block = 128;
+
+struct F8Mat {
+    const uint8_t* codes;
+    const uint8_t* scales;
+    int rows;
+    int bytes;                           // of a row of codes: columns rounded up to whole blocks
+    int scale_bytes;                     // of a row of scales
+    int shift;                           // log2 of the rows of a block: 0 or 7
+};
+
+// ---- scales ------------------------------------------------------------------------------------------------------------------------
+
+// A magnitude's bits for the block's maximum: what is not finite does not count
+__device__ __forceinline__ uint32_t f8_magnitude(float x) {
+    const uint32_t a = __float_as_uint(x) & 0x7FFFFFFFu;
+    return a < 0x7F800000u ? a : 0u;
+}
+// exponent + 127 of the least power of two that brings `top` to at most 448 = 1.75 * 2^8
+__device__ __forceinline__ uint32_t f8_scale(uint32_t top) {
+    const int e = int((top + 0x1FFFFFu) >> 23) - 8;
+    return e > 0 ? uint32_t(e) : 0u;
+}
+__device__ __forceinline__ float f8_inverse(uint32_t scale) { return __uint_as_float((254u - scale) << 23); }
+__device__ __forceinline__ float f8_power(uint32_t scale) { return __uint_as_float(scale ? scale << 23 : 0x00400000u); }
+
+// Codes of 4 values times `inverse`.  Infinities, for which there is no code, become NaN.
+__device__ __forceinline__ uint32_t f8_codes4(float a, float b, float c, float d, float inverse) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
+    return uint32_t(w);
+}
+
+__device__ __forceinline__ uint32_t umax32(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// Maximum over groups of 16 lanes
+__device__ __forceinline__ uint32_t umax16(uint32_t x) {
+    x = umax32(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0xB1, 0xF, 0xF, false)));      // lane ^ 1
+    x = umax32(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x4E, 0xF, 0xF, false)));      // lane ^ 2
+    x = umax32(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x141, 0xF, 0xF, false)));     // mirrored among 8
+    x = umax32(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x140, 0xF, 0xF, false)));     // and 16
+    return x;
+}
+
+// ---- to 8 bits ---------------------------------------------------------------------------------------------------------------------
+
+// Blocks of 1 x 128: 16 lanes a block, 8 elements each.
+template <bool BF16>
+__global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t stride, int rows, int cols, int blocks, uint8_t* codes, uint8_t* scales,
+                                                       int scale_bytes) {
+    const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);          // block, counted over all rows
+    const int row = int(unit / uint32_t(blocks)), block = int(unit % uint32_t(blocks)), d = threadIdx.x & 15;
+    if (row >= rows) return;                                              // 16 lanes at a time
+    const int at = block * kF8Block + d * 8;
+    float v[8];
+    w4_load8<BF16>(x, int64_t(row) * stride + at, int64_t(row) * stride + cols, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = umax32(top, f8_magnitude(v[e]));
+    const uint32_t scale = f8_scale(umax16(top));
+    const float inverse = f8_inverse(scale);
+    uint2 w;
+    w.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
+    w.y = f8_codes4(v[4], v[5], v[6], v[7], inverse);
+    *reinterpret_cast<uint2*>(codes + int64_t(unit) * kF8Block + d * 8) = w;
+    if (d == 0) scales[int64_t(row) * scale_bytes + block] = uint8_t(scale);
+    else if (block == blocks - 1 && blocks - 1 + d < scale_bytes) scales[int64_t(row) * scale_bytes + blocks - 1 + d] = 0;
+}
+
+// A tile of 128 x 128 a workgroup, for 128 x 128 blocks and for a matrix together with its transpose.  A thread takes 8 rows by 8
+// columns: the maxima of rows, columns or all go over lanes and LDS, the transposed codes through LDS, 8 rows a piece.
+// TILE: rows of a block, 1 or 128.  codes or codes_t may be null.
+template <bool BF16, int TILE>
+__global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64_t stride, int rows, int cols, uint8_t* codes, uint8_t* scales,
+                                                            int code_bytes, int scale_bytes, uint8_t* codes_t, uint8_t* scales_t, int code_bytes_t,
+                                                            int scale_bytes_t) {
+    __shared__ uint32_t s_top[4][kF8Block];
+    __shared__ uint2 s_codes[kF8Block * 16];                              // [column][8 rows a piece]
+    const int p = threadIdx.x & 15, g = threadIdx.x >> 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int block_c = blockIdx.x, block_r = blockIdx.y, r0 = block_r * kF8Block + g * 8, c0 = block_c * kF8Block + p * 8;
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (r0 + i < rows) {
+            w4_load8<BF16>(x, int64_t(r0 + i) * stride + c0, int64_t(r0 + i) * stride + cols, v[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+        }
+    }
+    uint32_t row_scale[8], col_scale[8];
+    if constexpr (TILE == 1) {
+        uint32_t col_top[8] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t a = f8_magnitude(v[i][e]);
+                top = umax32(top, a);
+                col_top[e] = umax32(col_top[e], a);
+            }
+            row_scale[i] = f8_scale(umax16(top));
+        }
+        if (codes_t) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                col_top[e] = umax32(col_top[e], __shfl_xor(col_top[e], 16, 64));
+                col_top[e] = umax32(col_top[e], __shfl_xor(col_top[e], 32, 64));
+            }
+            if (lane < 16) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s_top[wave][p * 8 + e] = col_top[e];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) top = umax32(top, s_top[w][p * 8 + e]);
+                col_scale[e] = f8_scale(top);
+            }
+        }
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = umax32(top, f8_magnitude(v[i][e]));
+        top = umax16(top);
+        top = umax32(top, __shfl_xor(top, 16, 64));
+        top = umax32(top, __shfl_xor(top, 32, 64));
+        if (lane == 0) s_top[0][wave] = top;
+        __syncthreads();
+        top = umax32(umax32(s_top[0][0], s_top[0][1]), umax32(s_top[0][2], s_top[0][3]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row_scale[i] = col_scale[i] = f8_scale(top);
+    }
+    if (codes) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (r0 + i >= rows) break;
+            const float inverse = f8_inverse(row_scale[i]);
+            uint2 w;
+            w.x = f8_codes4(v[i][0], v[i][1], v[i][2], v[i][3], inverse);
+            w.y = f8_codes4(v[i][4], v[i][5], v[i][6], v[i][7], inverse);
+            *reinterpret_cast<uint2*>(codes + int64_t(r0 + i) * code_bytes + c0) = w;
+            if (TILE == 1 && p == 0) scales[int64_t(r0 + i) * scale_bytes + block_c] = uint8_t(row_scale[i]);
+            if (TILE == 1 && p > 0 && block_c == int(gridDim.x) - 1 && block_c + p < scale_bytes) scales[int64_t(r0 + i) * scale_bytes + block_c + p] = 0;
+        }
+        if (TILE > 1 && g == 0) {
+            if (p == 0) scales[int64_t(block_r) * scale_bytes + block_c] = uint8_t(row_scale[0]);
+            else if (block_c == int(gridDim.x) - 1 && block_c + p < scale_bytes) scales[int64_t(block_r) * scale_bytes + block_c + p] = 0;
+        }
+    }
+    if (codes_t) {
+        // piece g of column c at g ^ (c / 8): the 16 lanes of a store hit all banks
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float inverse = f8_inverse(col_scale[e]);
+            uint2 w;
+            w.x = f8_codes4(v[0][e], v[1][e], v[2][e], v[3][e], inverse);
+            w.y = f8_codes4(v[4][e], v[5][e], v[6][e], v[7][e], inverse);
+            s_codes[(p * 8 + e) * 16 + (g ^ p)] = w;
+        }
+        if (TILE == 1 && g == 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (c0 + e >= cols) break;
+                uint8_t* to = scales_t + int64_t(c0 + e) * scale_bytes_t;
+                to[block_r] = uint8_t(col_scale[e]);
+                if (block_r == int(gridDim.y) - 1)
+                    for (int b = block_r + 1; b < scale_bytes_t; ++b) to[b] = 0;
+            }
+        }
+        if (TILE > 1 && g == 0) {
+            if (p == 0) scales_t[int64_t(block_c) * scale_bytes_t + block_r] = uint8_t(col_scale[0]);
+            else if (block_r == int(gridDim.y) - 1 && block_r + p < scale_bytes_t) scales_t[int64_t(block_c) * scale_bytes_t + block_r + p] = 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int id = threadIdx.x + j * 256, c = id >> 3, q = id & 7;          // 16 rows of a column
+            if (block_c * kF8Block + c >= cols) continue;
+            const uint2 a = s_codes[c * 16 + ((2 * q) ^ (c >> 3))], b = s_codes[c * 16 + ((2 * q + 1) ^ (c >> 3))];
+            *reinterpret_cast<uint4*>(codes_t + int64_t(block_c * kF8Block + c) * code_bytes_t + block_r * kF8Block + q * 16) = make_uint4(a.x, a.y, b.x, b.y);
+        }
+    }
+}
+
+// ---- and back ----------------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void f8_values4(uint32_t w, float power, float out[4]) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), true);
+    out[0] = lo.x * power; out[1] = lo.y * power; out[2] = hi.x * power; out[3] = hi.y * power;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void f8_dequant_kernel(F8Mat m, int cols, int blocks, void* out, int64_t stride) {
+    const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);
+    const int row = int(unit / uint32_t(blocks)), block = int(unit % uint32_t(blocks)), d = threadIdx.x & 15;
+    const int at = block * kF8Block + d * 8;
+    if (row >= m.rows || at >= cols) return;
+    const uint2 w = *reinterpret_cast<const uint2*>(m.codes + int64_t(unit) * kF8Block + d * 8);
+    const float power = f8_power(m.scales[int64_t(row >> m.shift) * m.scale_bytes + block]);
+    float v[8];
+    f8_values4(w.x, power, v);
+    f8_values4(w.y, power, v + 4);
+    const int64_t base = int64_t(row) * stride + at;
+    if (at + 8 <= cols) {
+        if constexpr (BF16) {
+            Vec16 u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u.v[e] = uint32_t(to_bf16(v[2 * e])) | uint32_t(to_bf16(v[2 * e + 1])) << 16;
+            *reinterpret_cast<Vec16*>(static_cast<uint16_t*>(out) + base) = u;
+        } else {
+            Vec16f a, b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { a.v[e] = v[e]; b.v[e] = v[4 + e]; }
+            *reinterpret_cast<Vec16f*>(static_cast<float*>(out) + base) = a;
+            *reinterpret_cast<Vec16f*>(static_cast<float*>(out) + base + 4) = b;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (at + e < cols) w4_store1<BF16>(out, base + e, v[e]);
+    }
+}
+
+}  // namespace lpmm

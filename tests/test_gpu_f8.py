@@ -1,0 +1,322 @@
+"""Matrices in 8 bits with a power of two for each block of 128, and their products, on the GPU against plain 64-bit forms."""
+import pytest
+import torch
+
+import f8_util as ref
+import paper_2309_01507_amd as lpmm
+from conftest import progress
+from f8_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+
+
+def matrix(rows, cols, dtype, seed, spread=1.5):
+    """Rows and columns of different size"""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g) * (spread * torch.randn(rows, 1, generator=g)).exp()
+    return (x * (spread * torch.randn(1, cols, generator=g)).exp()).to(dtype)
+
+
+def check_quant(x, tile, on_gpu=None, what=""):
+    xd = x.to(DEV) if on_gpu is None else on_gpu
+    want, scales = ref.quantize(x, tile)
+    want_t, scales_t = ref.quantize(x.t(), tile)
+    q = lpmm.lpmm_f8_quant(xd, tile)
+    p, pt = lpmm.lpmm_f8_quant_both(xd, tile)
+    for m, v, s in ((q, want, scales), (p, want, scales), (pt, want_t, scales_t)):
+        got, got_scales = ref.unpack(m)
+        assert torch.equal(got_scales, s) and ref.same(got, v), f"{what} {tuple(x.shape)} tile {tile}"
+        for dtype in (F32, BF16):
+            back = lpmm.lpmm_f8_dequant(m, dtype).cpu().double()
+            assert ref.same(back, v), f"{what}: back to {dtype}"
+    return q
+
+
+SHAPES = [(1, 1), (1, 128), (3, 127), (2, 129), (128, 128), (127, 130), (129, 257), (300, 77), (16, 1000), (1000, 16), (260, 520)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_there_and_back(rows, cols, tile, dtype):
+    check_quant(matrix(rows, cols, dtype, rows + cols), tile)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_every_code_and_border(dtype, tile):
+    """Each code, each point half way between two (which bf16 holds), and their neighbours; for several powers, and largest elements at the power's border"""
+    codes = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    points = torch.cat([codes, (codes[1:] + codes[:-1]) / 2])
+    fine = torch.cat([points, points * (1 + 2.0 ** -7), points * (1 - 2.0 ** -8), torch.tensor([2.0 ** -11, 2.0 ** -10, 1.5 * 2.0 ** -10, 449.0, 463.0])])
+    fine = torch.cat([fine, -fine]).to(dtype).float()
+    for e in (-60, -3, 0, 1, 40):
+        for top in (448.0, 450.0, 224.0, 226.0):
+            x = torch.zeros(-(-fine.numel() // 100), 127)
+            kept = torch.where(fine.abs() <= top, fine, torch.zeros_like(fine))
+            for r in range(x.shape[0]):
+                part = kept[r * 100:(r + 1) * 100]
+                x[r, :part.numel()] = part
+            x[:, 126] = top
+            check_quant((x * 2.0 ** e).to(dtype), tile, what=f"2^{e}, {top}")
+
+
+@pytest.mark.parametrize("tile", [1, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_unusual_values(dtype, tile):
+    """Zeros, infinities, NaN, the type's largest and least numbers"""
+    x = matrix(9, 300, dtype, 4, 0.3)
+    x[0] = 0.0
+    x[1, 5], x[1, 6] = INF, -INF
+    x[2, 200] = NAN
+    x[3, :128] = INF
+    x[4, :128] = NAN
+    x[5] *= 1e-30
+    x[6, ::3] = -0.0
+    check_quant(x, tile)
+    big, small = torch.finfo(dtype).max, torch.finfo(dtype).tiny
+    x = torch.zeros(6, 200, dtype=dtype)
+    x[0, 3], x[0, 4] = big / 2, big / 300
+    x[1, 3], x[1, 4] = small, small * 200
+    x[2, :3] = torch.tensor([small / 8, small / 16, -small / 4]).to(dtype)          # below the normal numbers
+    for r in range(6):                                                              # one kind a block
+        check_quant(x[r:r + 1].clone(), tile)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_anywhere(dtype):
+    x = matrix(70, 333, dtype, 5)
+    for gap, off in ((1, 1), (3, 5), (4, 0)):
+        room = torch.full((70 * (333 + gap) + off,), NAN, dtype=dtype, device=DEV)
+        view = room[off:off + 70 * (333 + gap)].view(70, 333 + gap)[:, :333]
+        view.copy_(x)
+        for tile in (1, 128):
+            q = check_quant(x, tile, view, f"{gap} {off}")
+        out = torch.full_like(room, 77.0)
+        to = out[off:off + 70 * (333 + gap)].view(70, 333 + gap)[:, :333]
+        lpmm.lpmm_f8_dequant(q, out=to)
+        assert torch.equal(to, lpmm.lpmm_f8_dequant(q, dtype))
+        to.fill_(77.0)
+        assert bool((out == 77.0).all()), "around the rows"
+
+
+def product_of(m, n, k, dtype, tiles, seed, what=""):
+    x, w = matrix(m, k, F32, seed, 0.7), matrix(n, k, F32, seed + 1, 0.7)
+    a, b = lpmm.lpmm_f8_quant(x.to(DEV), tiles[0]), lpmm.lpmm_f8_quant(w.to(DEV), tiles[1])
+    c = lpmm.lpmm_f8_matmul(a, b, dtype)
+    ref.check_product(c, ref.unpack(a)[0], ref.unpack(b)[0], f"{m} x {n} x {k} {what}")
+    return c
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tiles", [(1, 128), (1, 1), (128, 1), (128, 128)])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (5, 3, 100), (33, 65, 129), (128, 128, 128), (130, 257, 384), (64, 300, 1000), (257, 129, 2050)])
+def test_products(m, n, k, tiles, dtype):
+    product_of(m, n, k, dtype, tiles, m + n + k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(1000, 700, 640), (17, 5000, 300), (2, 2, 40000), (600, 2000, 1100), (5000, 33, 257)])
+def test_larger_products(m, n, k, dtype):
+    product_of(m, n, k, dtype, (1, 128), m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [1, 2, 7, 16, 17, 31, 64, 100, 200])
+def test_linear(t, dtype):
+    for n, k in ((1, 1), (15, 127), (100, 200), (333, 1000), (77, 4100)):
+        x, w = matrix(t, k, dtype, t + n + k, 0.7), matrix(n, k, F32, t + n + k + 1, 0.7)
+        q = lpmm.lpmm_f8_quant(w.to(DEV), 128)
+        y = lpmm.lpmm_f8_linear(x.to(DEV), q)
+        assert y.dtype == dtype
+        ref.check_product(y, ref.quantize(x, 1)[0], ref.unpack(q)[0], f"{t} x {n} x {k}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [3, 40])
+def test_linear_rows_anywhere(t, dtype):
+    """x and y with gaps and off their boundaries; what lies around y stays; weights in blocks of 1 x 128 too"""
+    n, k = 130, 515
+    x, w = matrix(t, k, dtype, 1, 0.7), matrix(n, k, F32, 2, 0.7)
+    for tile in (128, 1):
+        q = lpmm.lpmm_f8_quant(w.to(DEV), tile)
+        want = lpmm.lpmm_f8_linear(x.to(DEV), q)
+        ref.check_product(want, ref.quantize(x, 1)[0], ref.unpack(q)[0], f"tile {tile}")
+        xs = torch.full((t, k + 3), NAN, dtype=dtype, device=DEV)[:, 1:1 + k]
+        xs.copy_(x)
+        room = torch.full((t, n + 5), 77.0, dtype=dtype, device=DEV)
+        y = lpmm.lpmm_f8_linear(xs, q, room[:, 3:3 + n])
+        assert torch.equal(y, want) and bool((room[:, :3] == 77.0).all()) and bool((room[:, 3 + n:] == 77.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_what_is_not_finite_is_carried_through(dtype):
+    for t in (2, 40):
+        x, w = matrix(t, 300, dtype, 8, 0.5), matrix(150, 300, F32, 9, 0.5)
+        x[1, 7] = NAN
+        w[3, 299] = INF
+        x[0] = 0.0
+        q = lpmm.lpmm_f8_quant(w.to(DEV), 128)
+        y = lpmm.lpmm_f8_linear(x.to(DEV), q).cpu()
+        assert bool(y[1].isnan().all()) and bool(y[:, 3].isnan().all())
+        ref.check_product(y, ref.quantize(x, 1)[0], ref.unpack(q)[0], f"{t}")
+
+
+def test_blocks_far_apart_in_size():
+    """Neighbouring blocks' powers 2^60 apart: each is applied to its own block."""
+    g = torch.Generator().manual_seed(3)
+    x, w = torch.randn(50, 512, generator=g), torch.randn(140, 512, generator=g)
+    for j, e in enumerate((-30, 0, 30, -5)):
+        x[:, j * 128:(j + 1) * 128] *= 2.0 ** e
+        w[:, j * 128:(j + 1) * 128] *= 2.0 ** -e * (1 + j)
+    for dtype in (F32, BF16):
+        for t in (5, 50):
+            q = lpmm.lpmm_f8_quant(w.to(DEV), 128)
+            y = lpmm.lpmm_f8_linear(x[:t].to(dtype).to(DEV), q)
+            ref.check_product(y, ref.quantize(x[:t].to(dtype), 1)[0], ref.unpack(q)[0], f"{t} {dtype}")
+
+
+def test_empty():
+    q = lpmm.lpmm_f8_quant(torch.randn(20, 130, device=DEV), 128)
+    assert lpmm.lpmm_f8_linear(torch.empty(0, 130, device=DEV), q).shape == (0, 20)
+    none = lpmm.lpmm_f8_quant(torch.empty(0, 130, device=DEV))
+    assert lpmm.lpmm_f8_matmul(none, q).shape == (0, 20) and lpmm.lpmm_f8_matmul(q, none).shape == (20, 0)
+    assert lpmm.lpmm_f8_dequant(none).shape == (0, 130)
+    with pytest.raises(lpmm.LpmmError):
+        lpmm.lpmm_f8_quant_both(torch.empty(0, 130, device=DEV))
+
+
+def test_beyond_32_bits():
+    """More than 2^31 codes, and results: the last rows"""
+    n, k = 600_011, 4096
+    progress("weights of 2.4e9 codes")
+    q = lpmm.new_f8(n, k, 128)
+    q.codes.zero_()
+    q.scales.fill_(127)
+    last = matrix(130, k, F32, 3, 0.3)
+    part = lpmm.lpmm_f8_quant(last.to(DEV), 1)
+    q.codes[n - 130:] = part.codes
+    w = ref.unpack(lpmm.MatF8(130, k, 1, part.codes, torch.full_like(part.scales, 127)))[0]
+    for t, dtype in ((2, BF16), (2, F32), (40, BF16)):
+        x = matrix(t, k, dtype, 4, 0.3)
+        y = lpmm.lpmm_f8_linear(x.to(DEV), q)
+        assert bool((y[:, :n - 130] == 0).all())
+        ref.check_product(y[:, n - 130:], ref.quantize(x, 1)[0], w, f"{t}")
+    progress("back to 2.4e9 values")
+    back = lpmm.lpmm_f8_dequant(q, BF16)
+    assert torch.equal(back[n - 130:].cpu().double(), w) and not bool(back[:n - 130].any())
+    again = lpmm.lpmm_f8_quant(back, 128)
+    assert torch.equal(lpmm.lpmm_f8_dequant(again, BF16)[n - 2:], lpmm.lpmm_f8_dequant(lpmm.lpmm_f8_quant(back[(n - 1) // 128 * 128:], 128), BF16)[-2:])
+
+
+@pytest.mark.parametrize("t", [4, 100])
+def test_on_a_stream_and_captured(t):
+    """The same bits on another stream and from a captured graph, replayed with other inputs in between"""
+    n, k = 200, 1000
+    x, q = matrix(t, k, BF16, 1).to(DEV), lpmm.lpmm_f8_quant(matrix(n, k, F32, 2).to(DEV), 128)
+    sets = [x.clone(), (x * 2).flip(0).contiguous(), x.flip(1).contiguous()]
+    want = [lpmm.lpmm_f8_linear(v, q) for v in sets]
+    y = torch.empty(t, n, dtype=BF16, device=DEV)
+    room = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    lpmm.lpmm_f8_linear(x, q, y, room, stream=s)
+    s.synchronize()
+    assert torch.equal(y, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lpmm.lpmm_f8_linear(x, q, y)
+        p, pt = lpmm.lpmm_f8_quant_both(x)
+        c = lpmm.lpmm_f8_matmul(pt, pt, F32)
+    for i in (0, 1, 2, 1, 0):
+        x.copy_(sets[i])
+        graph.replay()
+        assert torch.equal(y, want[i])
+        eager = lpmm.lpmm_f8_quant_both(sets[i])
+        assert torch.equal(p.codes, eager[0].codes) and torch.equal(pt.scales, eager[1].scales)
+        assert torch.equal(c, lpmm.lpmm_f8_matmul(eager[1], eager[1], F32))
+        torch.randn(1000, device=DEV).sum().item()
+
+
+def test_refusals():
+    q = lpmm.lpmm_f8_quant(torch.randn(20, 130, device=DEV), 128)
+    x = torch.randn(30, 130, device=DEV)
+    need = lpmm.lib().lpmm_f8_linear_workspace_bytes(30, 20, 130)
+    assert need > 0
+    with pytest.raises(lpmm.LpmmError, match="workspace"):
+        lpmm.lpmm_f8_linear(x, q, workspace=torch.empty(need - 1, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError):
+        lpmm.lpmm_f8_linear(x.cpu(), q)
+    with pytest.raises(ValueError):
+        lpmm.lpmm_f8_linear(x, q, y=torch.empty(30, 20, device=DEV, dtype=BF16))
+    with pytest.raises(ValueError):
+        lpmm.lpmm_f8_matmul(q, lpmm.lpmm_f8_quant(x[:, :128]))
+
+
+# ---- the layer -------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,w_dtype", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("t", [1, 9, 150])
+def test_layer_and_gradients(t, dtype, w_dtype):
+    """y, dx and dW against their formulas, each from its own 8-bit operands"""
+    n, k = 140, 270
+    x, w, dy = matrix(t, k, dtype, 1, 0.6), matrix(n, k, w_dtype, 2, 0.6), matrix(t, n, dtype, 3, 0.6)
+    layer = lpmm.F8Linear.from_weight(w.to(DEV))
+    xd = x.to(DEV).requires_grad_()
+    y = layer(xd)
+    dx, dw = torch.autograd.grad(y, (xd, layer.weight), dy.to(DEV))
+    assert y.dtype == dx.dtype == dtype and dw.dtype == w_dtype
+    val = lambda m, tile=1: ref.quantize(m, tile)[0]
+    qw = val(w, 128)
+    ref.check_product(y, val(x), qw, "y")
+    ref.check_product(dx, val(dy), qw.t().contiguous(), "dx")
+    ref.check_product(dw, val(dy.t()), val(x.t()), "dW")
+    # one of the two alone gives the same values
+    dx1, = torch.autograd.grad(lpmm.f8_linear(xd, layer.weight.detach()), xd, dy.to(DEV))
+    dw1, = torch.autograd.grad(layer(x.to(DEV)), layer.weight, dy.to(DEV))
+    ref.check_product(dx1, val(dy), qw.t().contiguous(), "dx alone")
+    assert torch.equal(dw1, dw)
+
+
+def test_gradients_against_differences():
+    """Whole numbers up to 15 with a 15 in every block are 8-bit values as they are, both ways round: the layer is linear among them, and a
+    difference is the gradient's."""
+    g = torch.Generator().manual_seed(6)
+    t, n, k = 20, 30, 200
+    whole = lambda r, c: torch.randint(-7, 8, (r, c), generator=g).float()
+    x, w, dy = whole(t, k), whole(n, k), whole(t, n)
+    x[0], x[:, 0], x[:, 128], w[0, 0], w[0, 128], dy[0], dy[:, 0] = 15, 15, 15, 15, 15, 15, 15
+    xd, wd, dyd = x.to(DEV).requires_grad_(), w.to(DEV).requires_grad_(), dy.to(DEV)
+    loss = lambda a, b: (lpmm.f8_linear(a, b).double() * dyd.double()).sum()
+    dx, dw = torch.autograd.grad(loss(xd, wd), (xd, wd))
+    for _ in range(5):
+        sx, sw = whole(t, k).to(DEV).clamp(-1, 1), whole(n, k).to(DEV).clamp(-1, 1)
+        sx[0], sx[:, 0], sx[:, 128], sw[0, 0], sw[0, 128] = 0, 0, 0, 0, 0
+        assert float(loss(xd + sx, wd) - loss(xd, wd)) == float((dx.double() * sx.double()).sum())
+        assert float(loss(xd, wd + sw) - loss(xd, wd)) == float((dw.double() * sw.double()).sum())
+
+
+def test_layer_shapes_and_states():
+    torch.manual_seed(0)
+    layer = lpmm.F8Linear(100, 33)
+    other = lpmm.F8Linear(100, 33)
+    other.load_state_dict(layer.state_dict())
+    x = torch.randn(2, 3, 100, device=DEV, requires_grad=True)
+    y = layer(x)
+    assert y.shape == (2, 3, 33) and torch.equal(y, other(x))
+    y.sum().backward()                                       # a gradient that arrives expanded
+    first, first_x = layer.weight.grad.clone(), x.grad.clone()
+    layer.weight.grad = x.grad = None
+    (layer(x).permute(2, 0, 1) * torch.ones(33, 2, 3, device=DEV)).sum().backward()        # and one that arrives transposed
+    assert torch.equal(layer.weight.grad, first) and torch.equal(x.grad, first_x)
+    empty = torch.empty(0, 100, device=DEV, requires_grad=True)
+    layer.weight.grad = None
+    layer(empty).sum().backward()
+    assert empty.grad.shape == (0, 100) and not bool(layer.weight.grad.any())
+    one = layer(torch.randn(100, device=DEV))
+    assert one.shape == (33,)
+    with pytest.raises(ValueError):
+        layer(torch.randn(5, 99, device=DEV))
