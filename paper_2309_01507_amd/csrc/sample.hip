@@ -40,8 +40,15 @@ extern "C" int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int
     a.logprob = logprob;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 rows{unsigned(t)};
-    if (z_dtype == LPMM_BF16) hipLaunchKernelGGL((sample_kernel<true, 256>), rows, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((sample_kernel<false, 256>), rows, dim3(256), 0, s, a);
+    // Threads of a row: as many as speed up its passes, as few as leave room for other rows (us with 256, 512, 1024: 1 x 1000 12.8, 13.1, 15.4; 1 x 4000 15.4, 13.9, 16.4;
+    // 1 x 16000 32, 25, 25; 256 x 32000 66, 46, 42; 300 x 32000 80, 63, 72; 768 x 32000 97, 83, 110; 2048 x 32000 215, 211, 294; 2000 x 16000 105, 111, 185;
+    // 2000 x 4000 43, 54, 111)
+#define LPMM_SAMPLE(T) { if (z_dtype == LPMM_BF16) hipLaunchKernelGGL((sample_kernel<true, T>), rows, dim3(T), 0, s, a); \
+                         else hipLaunchKernelGGL((sample_kernel<false, T>), rows, dim3(T), 0, s, a); }
+    if (v <= 2048 || (t > 1024 && v <= 16384)) LPMM_SAMPLE(256)
+    else if (t > 256 || v <= 16384) LPMM_SAMPLE(512)
+    else LPMM_SAMPLE(1024)
+#undef LPMM_SAMPLE
     LPMM_HIP(hipGetLastError());
     return LPMM_OK;
 }
