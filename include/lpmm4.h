@@ -549,7 +549,8 @@ int lpmm_distill_loss_grad(const void* z, int z_dtype, int64_t t, int64_t v, int
  *   code    E4M3 (1 sign, 4 exponent, 3 fraction bits; up to 448, no infinities): the element divided by the power, which is exact, rounded to the
  *           nearest, ties to even.  Infinities and NaN have the code of NaN.
  *   codes   rows of cols rounded up to a multiple of 128 bytes, the rest of a row 0 (the products rely on that); 16-byte aligned
- *   scales  ceil(rows / tile) rows of ceil(cols / 128) bytes rounded up to a multiple of 4, the rest 0; 4-byte aligned
+ *   scales  tile 128: ceil(rows / 128) rows of ceil(cols / 128) bytes rounded up to a multiple of 4; tile 1, whose products read neighbouring rows'
+ *           scales together: ceil(cols / 128) rows of `rows` bytes rounded up to a multiple of 4.  The rest of a row is 0; 4-byte aligned.
  * cols is at most 2^22, rows at most 2^30, with 2^33 codes at most.  Tensors of rows, workspaces and streams as for the 4-bit weights above. */
 typedef struct lpmm_f8 {
     uint8_t* codes;

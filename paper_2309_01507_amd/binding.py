@@ -940,13 +940,19 @@ class MatF8:
     scales: "object"
 
 
+def _f8_scales(rows: int, cols: int, tile: int):
+    """(rows, bytes of a row) of the scales: blocks of one row stand below each other, those of 128 rows side by side"""
+    blocks = (cols + 127) // 128
+    return (blocks, (rows + 3) // 4 * 4) if tile == 1 else ((rows + 127) // 128, (blocks + 3) // 4 * 4)
+
+
 def _f8_check(m: MatF8, what: str) -> _F8:
     torch = _torch or _load_torch()
     codes, scales, rows, cols, tile = m.codes, m.scales, m.rows, m.cols, m.tile
     if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
         raise ValueError(f"{what}: codes and scales must be uint8, not {codes.dtype} and {scales.dtype}")
-    blocks = (cols + 127) // 128
-    if (tile not in (1, 128) or codes.numel() != rows * blocks * 128 or scales.numel() != -(-rows // tile) * ((blocks + 3) // 4 * 4) or
+    down, across = _f8_scales(rows, cols, tile)
+    if (tile not in (1, 128) or codes.numel() != rows * ((cols + 127) // 128 * 128) or scales.numel() != down * across or
             not codes.is_contiguous() or not scales.is_contiguous()):
         raise ValueError(f"{what}: codes or scales are not those of a {rows} x {cols} matrix with blocks of {tile} x 128")
     return _F8(codes.data_ptr(), scales.data_ptr(), rows, cols, tile, 0)
@@ -962,10 +968,9 @@ def lpmm_f8_sizes(rows: int, cols: int, tile: int = 1):
 def new_f8(rows: int, cols: int, tile: int = 1, device="cuda") -> MatF8:
     """Allocate (torch) room for a matrix in 8 bits; lpmm_f8_quant fills it."""
     import torch
-    sz = lpmm_f8_sizes(rows, cols, tile)
+    lpmm_f8_sizes(rows, cols, tile)                     # refuses what the library does not take
     return MatF8(rows, cols, tile, torch.empty(rows, -(-cols // 128) * 128, dtype=torch.uint8, device=device),
-                 torch.empty(sz[1], dtype=torch.uint8, device=device).view(-(-rows // tile), -1) if sz[1] else
-                 torch.empty(0, 4, dtype=torch.uint8, device=device))
+                 torch.empty(_f8_scales(rows, cols, tile), dtype=torch.uint8, device=device))
 
 
 def _f8_out(out, rows: int, cols: int, tile: int, like, stream, what: str) -> MatF8:

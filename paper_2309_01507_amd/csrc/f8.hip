@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "host_util.hpp"
 #include "f8_tile.hpp"
@@ -15,14 +16,16 @@ using namespace lpmm;
 constexpr int64_t kMaxF8Row = int64_t(1) << 22, kMaxF8Codes = int64_t(1) << 33;
 
 int64_t code_bytes(int64_t cols) { return div_up(cols, kF8Block) * kF8Block; }
-int64_t scale_bytes(int64_t cols) { return div_up(div_up(cols, kF8Block), 4) * 4; }
+int64_t scale_bytes(int64_t rows, int64_t cols, int tile) { return div_up(tile == 1 ? rows : div_up(cols, kF8Block), 4) * 4; }
+
+int64_t scale_rows(const F8Mat& m) { return m.shift == 0 ? m.bytes / kF8Block : div_up(m.rows, kF8Block); }
 
 int check_f8(int64_t rows, int64_t cols, int tile, F8Mat* m) {
     if ((tile != 1 && tile != 128) || rows < 0 || cols < 1 || rows > kMaxDim || cols > kMaxF8Row) return LPMM_EINVAL;
     if (rows > kMaxF8Codes / code_bytes(cols)) return LPMM_EINVAL;
     m->rows = int(rows);
     m->bytes = int(code_bytes(cols));
-    m->scale_bytes = int(scale_bytes(cols));
+    m->scale_bytes = int(scale_bytes(rows, cols, tile));
     m->shift = tile == 1 ? 0 : 7;
     return LPMM_OK;
 }
@@ -38,7 +41,7 @@ int check_f8(const lpmm_f8* f, F8Mat* m) {
 
 int launch_quant(const void* x, int dtype, int64_t stride, const F8Mat& m, int64_t cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
     const int blocks = m.bytes / kF8Block;
-    const int64_t groups = div_up(int64_t(m.rows) * blocks, 16);
+    const int64_t groups = div_up(m.rows, 4) * div_up(blocks, 4);
     if (groups > kMaxBlocks) return LPMM_EINVAL;
     const dim3 grid{unsigned(groups)};
     if (dtype == LPMM_BF16)
@@ -69,41 +72,64 @@ int check_out(const lpmm_f8* f, int64_t rows, int64_t cols, int tile, F8Mat* m) 
     return f->rows == rows && f->cols == cols && f->tile == tile ? LPMM_OK : LPMM_EINVAL;
 }
 
-// Parts of the reduction: as many as fill the GPU once
+// Tiles of 256 x 256 (8 waves, one workgroup a CU), 128 x 128, 64 x 128 or 64 x 64 (4 waves, two to four workgroups a CU), and the parts of the reduction.
+// us of each, b's rows x columns with a's rows: bf16 4096 x 4096: 64 -, 15.3, 12.4, 11.5; 333 27, 23, 16.5, 15.7; 1024 42, 29, 26, 31; 4096 63, 70, -, -;
+// 11008 x 4096: 333 41, 30, 33, 40; 1024 53, 58, 64, 74; 2000 103, 94, -, -; 4096 166, 188, -, -; 50257 x 1024: 64 20, 15, 13.4, 14.5; 128 21, 16, 19.5, 19; 512 37, 46, 43, 51;
+// fp32 4096 x 4096: 512 40, 32, 28, 29; 4096 110, 121, -, -; 11008 x 4096: 512 69, 56, 51, 61; 1024 99, 95, 96, 107; 50257 x 1024: 128 33, 23, 26, 25
+enum class Tile { k256, k128, k64x128, k64 };
 struct ProductPlan {
+    Tile tile;
     int splits, per;
 };
-ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks) {
-    const int64_t tiles = div_up(m, 128) * div_up(n, 128);
-    const int64_t want = std::max<int64_t>(1, std::min(blocks / 2, 512 / std::max<int64_t>(1, tiles)));
-    ProductPlan p{};
-    p.per = int(div_up(blocks, want));
-    p.splits = int(div_up(blocks, p.per));
+ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool fast) {
+    const auto tiles = [&](int64_t rows, int64_t cols) { return div_up(m, rows) * div_up(n, cols); };
+    // What a round of workgroups costs, the large tiles' as 10: those run alone on a CU, of 128 x 128 two
+    const int64_t large = div_up(tiles(256, 256), 256) * 10, middle = div_up(tiles(128, 128), 512) * (fast ? 6 : 5);
+    ProductPlan p{Tile::k64, 1, int(blocks)};
+    if (tiles(256, 256) >= 160 && large <= middle) p.tile = Tile::k256;
+    else if (tiles(128, 128) >= 250 && (fast || m <= 128)) p.tile = Tile::k128;       // fp32 leaves the matrix unit waiting in smaller tiles no longer
+    else if (tiles(64, 128) >= 280) p.tile = Tile::k64x128;
+    const int64_t small = tiles(64, 64);
+    // A block takes a tile of 64 x 64 some 0.28 us (fp32 0.45), the join 2.5 us and 0.2 more for each part: parts pay where most CUs have nothing to do (us without and
+    // with 4: 16 x 4096 x 4096 12, 9.6; 128 x 4096 x 4096 13.0, 13.9; 300 x 300 x 16000 with 8 17.6)
+    const double whole = double(blocks) * (fast ? 0.28 : 0.45);
+    if (p.tile == Tile::k64 && small <= 96 && whole >= 6.0) {
+        const int64_t want = std::min<int64_t>(512 / small, int64_t(std::sqrt(whole / 0.2)));
+        p.per = int(div_up(blocks, std::max<int64_t>(1, want)));
+        p.splits = int(div_up(blocks, p.per));
+    }
     return p;
 }
 size_t product_bytes(int64_t m, int64_t n, const ProductPlan& p) { return p.splits > 1 ? size_t(p.splits) * size_t(m) * size_t(n) * 4 : 0; }
 
 int launch_product(const F8Mat& a, const F8Mat& b, void* c, int dtype, int64_t stride, void* workspace, hipStream_t s) {
     if (a.rows == 0 || b.rows == 0) return LPMM_OK;
-    const ProductPlan p = product_plan(a.rows, b.rows, a.bytes / kF8Block);
-    const int64_t m_tiles = div_up(a.rows, 128), n_tiles = div_up(b.rows, 128), blocks = div_up(m_tiles * n_tiles, 8) * 8;
+    const bool fast = dtype == LPMM_BF16;
+    const ProductPlan p = product_plan(a.rows, b.rows, a.bytes / kF8Block, fast);
+    const int64_t bm = p.tile == Tile::k256 ? 256 : p.tile == Tile::k128 ? 128 : 64, bn = p.tile == Tile::k256 ? 256 : p.tile == Tile::k64 ? 64 : 128;
+    const int64_t m_tiles = div_up(a.rows, bm), n_tiles = div_up(b.rows, bn), blocks = div_up(m_tiles * n_tiles, 8) * 8;
     if (blocks > kMaxBlocks) return LPMM_EINVAL;
     float* parts = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
     const dim3 grid(unsigned(blocks), unsigned(p.splits));
-    if (dtype == LPMM_BF16) hipLaunchKernelGGL((f8_tile_kernel<true, true, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, b, c, stride, int(m_tiles), int(n_tiles), p.per, parts);
-    else hipLaunchKernelGGL((f8_tile_kernel<false, false, 2, 2, 2, 2>), grid, dim3(256), 0, s, a, b, c, stride, int(m_tiles), int(n_tiles), p.per, parts);
+#define LPMM_TILE(WM, WN, MT, NT) { \
+        if (fast) hipLaunchKernelGGL((f8_tile_kernel<true, WM, WN, MT, NT>), grid, dim3(64 * WM * WN), 0, s, a, b, c, stride, int(m_tiles), int(n_tiles), p.per, parts); \
+        else hipLaunchKernelGGL((f8_tile_kernel<false, WM, WN, MT, NT>), grid, dim3(64 * WM * WN), 0, s, a, b, c, stride, int(m_tiles), int(n_tiles), p.per, parts); }
+    if (p.tile == Tile::k256) LPMM_TILE(4, 2, 2, 4)
+    else if (p.tile == Tile::k128) LPMM_TILE(2, 2, 2, 2)
+    else if (p.tile == Tile::k64x128) LPMM_TILE(2, 2, 1, 2)
+    else LPMM_TILE(2, 2, 1, 1)
+#undef LPMM_TILE
     LPMM_HIP(hipGetLastError());
     if (parts) {
-        const int64_t groups = div_up(int64_t(a.rows) * b.rows, 256);
-        if (groups > kMaxBlocks) return LPMM_EINVAL;
-        if (dtype == LPMM_BF16) hipLaunchKernelGGL(f8_join_kernel<true>, dim3(unsigned(groups)), dim3(256), 0, s, parts, p.splits, a.rows, b.rows, c, stride);
-        else hipLaunchKernelGGL(f8_join_kernel<false>, dim3(unsigned(groups)), dim3(256), 0, s, parts, p.splits, a.rows, b.rows, c, stride);
+        const dim3 groups{unsigned(div_up(int64_t(a.rows) * b.rows, 256))};        // at most 96 tiles of 64 x 64
+        if (fast) hipLaunchKernelGGL(f8_join_kernel<true>, groups, dim3(256), 0, s, parts, p.splits, a.rows, b.rows, c, stride);
+        else hipLaunchKernelGGL(f8_join_kernel<false>, groups, dim3(256), 0, s, parts, p.splits, a.rows, b.rows, c, stride);
         LPMM_HIP(hipGetLastError());
     }
     return LPMM_OK;
 }
 
-constexpr int kF8Few = 16;               // tokens that a wave's operand holds
+bool few(int64_t t, int64_t bytes) { return t <= kF8FewTokens && t * bytes <= kF8FewBytes; }
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
@@ -116,7 +142,7 @@ int lpmm_f8_sizes(int64_t rows, int64_t cols, int tile, size_t sizes[2]) {
     if (!sizes) return LPMM_EINVAL;
     LPMM_TRY(check_f8(rows, cols, tile, &m));
     sizes[0] = size_t(m.rows) * m.bytes;
-    sizes[1] = size_t(div_up(rows, tile)) * m.scale_bytes;
+    sizes[1] = size_t(scale_rows(m)) * m.scale_bytes;
     return LPMM_OK;
 }
 
@@ -158,7 +184,8 @@ int lpmm_f8_dequant(const lpmm_f8* f, void* out, int dtype, int64_t stride, void
 size_t lpmm_f8_matmul_workspace_bytes(int64_t a_rows, int64_t b_rows, int64_t cols) {
     F8Mat a{}, b{};
     if (check_f8(a_rows, cols, 1, &a) || check_f8(b_rows, cols, 1, &b) || a_rows < 1 || b_rows < 1) return 0;
-    return product_bytes(a_rows, b_rows, product_plan(a_rows, b_rows, a.bytes / kF8Block));
+    const int64_t blocks = a.bytes / kF8Block;
+    return std::max(product_bytes(a_rows, b_rows, product_plan(a_rows, b_rows, blocks, false)), product_bytes(a_rows, b_rows, product_plan(a_rows, b_rows, blocks, true)));
 }
 
 int lpmm_f8_matmul(const lpmm_f8* a, const lpmm_f8* b, void* c, int dtype, int64_t stride, void* workspace, size_t workspace_bytes, void* stream) {
@@ -173,8 +200,8 @@ int lpmm_f8_matmul(const lpmm_f8* a, const lpmm_f8* b, void* c, int dtype, int64
 
 size_t lpmm_f8_linear_workspace_bytes(int64_t t, int64_t n, int64_t k) {
     F8Mat x{}, w{};
-    if (t <= kF8Few || t > kMaxTokens || check_f8(t, k, 1, &x) || check_f8(n, k, 128, &w) || n < 1) return 0;
-    return up16(size_t(t) * x.bytes) + up16(size_t(t) * x.scale_bytes) + lpmm_f8_matmul_workspace_bytes(t, n, k);
+    if (t < 1 || t > kMaxTokens || check_f8(t, k, 1, &x) || check_f8(n, k, 128, &w) || n < 1 || few(t, x.bytes)) return 0;
+    return up16(size_t(t) * x.bytes) + up16(size_t(scale_rows(x)) * x.scale_bytes) + lpmm_f8_matmul_workspace_bytes(t, n, k);
 }
 
 int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const lpmm_f8* w, void* y, int64_t y_stride, void* workspace,
@@ -186,10 +213,16 @@ int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     LPMM_TRY(check_rows(y, dtype, w->rows ? t : 0, w->rows, y_stride));
     if (t == 0 || mw.rows == 0) return LPMM_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (t <= kF8Few) {
-        const dim3 grid{unsigned(div_up(mw.rows, 16))};
-        if (dtype == LPMM_BF16) hipLaunchKernelGGL((f8_few_kernel<true, 1, 8>), grid, dim3(512), 0, s, mw, x, int(t), int(w->cols), x_stride, y, y_stride);
-        else hipLaunchKernelGGL((f8_few_kernel<false, 1, 8>), grid, dim3(512), 0, s, mw, x, int(t), int(w->cols), x_stride, y, y_stride);
+    if (few(t, mw.bytes)) {
+        const size_t lds = up16(size_t(t) * (mw.bytes + mw.bytes / kF8Block));
+        // 16 waves share the blocks of 16 rows; where rows abound, two those of 32 (us, 1 token, each: 4096 x 4096 5.3, 18; 11008 x 4096 10.3, 18; 32000 x 4096 23, 22;
+        // 50257 x 1024 11.5, 11.2).  Two workgroups a CU while x leaves room for them (16 tokens 11008 x 4096 one 17.4, two 24)
+        const int64_t most = lds <= 32768 ? 512 : 256;
+#define LPMM_FEW(B, K, N, T) hipLaunchKernelGGL((f8_few_kernel<B, K, N, T, 2>), dim3(unsigned(std::min<int64_t>(most, div_up(mw.rows, 16 * T * N)))), dim3(64 * K * N), lds, \
+                                                s, mw, x, int(t), int(w->cols), x_stride, y, y_stride)
+        if (mw.rows >= 16384) { if (dtype == LPMM_BF16) LPMM_FEW(true, 2, 4, 2); else LPMM_FEW(false, 2, 4, 2); }
+        else { if (dtype == LPMM_BF16) LPMM_FEW(true, 16, 1, 1); else LPMM_FEW(false, 16, 1, 1); }
+#undef LPMM_FEW
         LPMM_HIP(hipGetLastError());
         return LPMM_OK;
     }
@@ -200,7 +233,7 @@ int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     mx.codes = codes;
     mx.scales = scales;
     LPMM_TRY(launch_quant(x, dtype, x_stride, mx, w->cols, codes, scales, s));
-    return launch_product(mx, mw, y, dtype, y_stride, scales + up16(size_t(t) * mx.scale_bytes), s);
+    return launch_product(mx, mw, y, dtype, y_stride, scales + up16(size_t(scale_rows(mx)) * mx.scale_bytes), s);
 }
 
 }  // extern "C"

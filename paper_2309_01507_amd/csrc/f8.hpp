@@ -16,8 +16,13 @@ struct F8Mat {
     const uint8_t* scales;
     int rows;
     int bytes;                           // of a row of codes: columns rounded up to whole blocks
-    int scale_bytes;                     // of a row of scales
     int shift;                           // log2 of the rows of a block: 0 or 7
+    // Scales of blocks of one row stand next to those of the rows below, so that a wave's operand finds its own in one line; those of blocks of 128
+    // rows next to those of the blocks to the right.
+    int scale_bytes;                     // of a row of scales
+    __host__ __device__ __forceinline__ int64_t scale_at(int row, int block) const {
+        return shift == 0 ? int64_t(block) * scale_bytes + row : int64_t(row >> shift) * scale_bytes + block;
+    }
 };
 
 // ---- scales ------------------------------------------------------------------------------------------------------------------------
@@ -55,13 +60,18 @@ __device__ __forceinline__ uint32_t umax16(uint32_t x) {
 
 // ---- to 8 bits ---------------------------------------------------------------------------------------------------------------------
 
-// Blocks of 1 x 128: 16 lanes a block, 8 elements each.
+// Blocks of 1 x 128: 16 lanes a block, 8 elements each; a wave takes four blocks of a row, a workgroup of four rows.  rows_up: rows rounded up to a
+// multiple of 4, so that the rest of a row of scales is written too.
 template <bool BF16>
 __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t stride, int rows, int cols, int blocks, uint8_t* codes, uint8_t* scales,
-                                                       int scale_bytes) {
-    const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);          // block, counted over all rows
-    const int row = int(unit / uint32_t(blocks)), block = int(unit % uint32_t(blocks)), d = threadIdx.x & 15;
-    if (row >= rows) return;                                              // 16 lanes at a time
+                                                       int rows_up) {
+    const int across = (blocks + 3) >> 2, group = int(blockIdx.x / uint32_t(across)), d = threadIdx.x & 15;
+    const int row = group * 4 + (threadIdx.x >> 6), block = int(blockIdx.x % uint32_t(across)) * 4 + (threadIdx.x >> 4 & 3);
+    if (block >= blocks) return;                                          // 16 lanes at a time
+    if (row >= rows) {
+        if (d == 0) scales[int64_t(block) * rows_up + row] = 0;
+        return;
+    }
     const int at = block * kF8Block + d * 8;
     float v[8];
     w4_load8<BF16>(x, int64_t(row) * stride + at, int64_t(row) * stride + cols, v);
@@ -73,9 +83,8 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t st
     uint2 w;
     w.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
     w.y = f8_codes4(v[4], v[5], v[6], v[7], inverse);
-    *reinterpret_cast<uint2*>(codes + int64_t(unit) * kF8Block + d * 8) = w;
-    if (d == 0) scales[int64_t(row) * scale_bytes + block] = uint8_t(scale);
-    else if (block == blocks - 1 && blocks - 1 + d < scale_bytes) scales[int64_t(row) * scale_bytes + blocks - 1 + d] = 0;
+    *reinterpret_cast<uint2*>(codes + (int64_t(row) * blocks + block) * kF8Block + d * 8) = w;
+    if (d == 0) scales[int64_t(block) * rows_up + row] = uint8_t(scale);
 }
 
 // A tile of 128 x 128 a workgroup, for 128 x 128 blocks and for a matrix together with its transpose.  A thread takes 8 rows by 8
@@ -156,8 +165,12 @@ __global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64
             w.x = f8_codes4(v[i][0], v[i][1], v[i][2], v[i][3], inverse);
             w.y = f8_codes4(v[i][4], v[i][5], v[i][6], v[i][7], inverse);
             *reinterpret_cast<uint2*>(codes + int64_t(r0 + i) * code_bytes + c0) = w;
-            if (TILE == 1 && p == 0) scales[int64_t(r0 + i) * scale_bytes + block_c] = uint8_t(row_scale[i]);
-            if (TILE == 1 && p > 0 && block_c == int(gridDim.x) - 1 && block_c + p < scale_bytes) scales[int64_t(r0 + i) * scale_bytes + block_c + p] = 0;
+            if (TILE == 1 && p == 0) scales[int64_t(block_c) * scale_bytes + r0 + i] = uint8_t(row_scale[i]);
+        }
+        if (TILE == 1 && p == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r0 + i >= rows && r0 + i < scale_bytes) scales[int64_t(block_c) * scale_bytes + r0 + i] = 0;
         }
         if (TILE > 1 && g == 0) {
             if (p == 0) scales[int64_t(block_r) * scale_bytes + block_c] = uint8_t(row_scale[0]);
@@ -176,13 +189,8 @@ __global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64
         }
         if (TILE == 1 && g == 0) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (c0 + e >= cols) break;
-                uint8_t* to = scales_t + int64_t(c0 + e) * scale_bytes_t;
-                to[block_r] = uint8_t(col_scale[e]);
-                if (block_r == int(gridDim.y) - 1)
-                    for (int b = block_r + 1; b < scale_bytes_t; ++b) to[b] = 0;
-            }
+            for (int e = 0; e < 8; ++e)
+                if (c0 + e < scale_bytes_t) scales_t[int64_t(block_r) * scale_bytes_t + c0 + e] = uint8_t(c0 + e < cols ? col_scale[e] : 0u);
         }
         if (TILE > 1 && g == 0) {
             if (p == 0) scales_t[int64_t(block_c) * scale_bytes_t + block_r] = uint8_t(col_scale[0]);
@@ -213,7 +221,7 @@ __global__ __launch_bounds__(256) void f8_dequant_kernel(F8Mat m, int cols, int 
     const int at = block * kF8Block + d * 8;
     if (row >= m.rows || at >= cols) return;
     const uint2 w = *reinterpret_cast<const uint2*>(m.codes + int64_t(unit) * kF8Block + d * 8);
-    const float power = f8_power(m.scales[int64_t(row >> m.shift) * m.scale_bytes + block]);
+    const float power = f8_power(m.scales[m.scale_at(row, block)]);
     float v[8];
     f8_values4(w.x, power, v);
     f8_values4(w.y, power, v + 4);

@@ -17,9 +17,12 @@ namespace lpmm {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ f32x16 mfma_f8(uint4 a0, uint4 a1, uint4 b0, uint4 b1, f32x16 c, int scale_a, int scale_b) {
-    const i32x8 a = {int(a0.x), int(a0.y), int(a0.z), int(a0.w), int(a1.x), int(a1.y), int(a1.z), int(a1.w)};
-    const i32x8 b = {int(b0.x), int(b0.y), int(b0.z), int(b0.w), int(b1.x), int(b1.y), int(b1.z), int(b1.w)};
+// 32 codes, of two pieces
+__device__ __forceinline__ i32x8 f8_operand(uint4 lo, uint4 hi) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    return __builtin_shufflevector(__builtin_bit_cast(i32x4, lo), __builtin_bit_cast(i32x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ f32x16 mfma_f8(i32x8 a, i32x8 b, f32x16 c, int scale_a, int scale_b) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
 }
 
@@ -41,20 +44,27 @@ struct StageF8 {
     static constexpr int kPieces = ROWS * 8, kOwn = kPieces / 64 / WAVES;
     static_assert(kPieces % (64 * WAVES) == 0 && ROWS % (32 * EACH) == 0, "whole KiB per wave");
     Buffer buffer;
-    uint32_t off[kOwn];
+    uint32_t off, step;                                        // of the first piece, and from one of the wave's pieces to the next
     static __device__ __forceinline__ int of(int r) { return r / (32 * EACH) * (32 * EACH) + (r % 32) * EACH + r / 32 % EACH; }
     __device__ __forceinline__ void setup(const F8Mat& m, int first, int wave) {
-        const int lane = threadIdx.x & 63, rows = min(m.rows - first, ROWS);
+        const int lane = threadIdx.x & 63, rows = min(m.rows - first, ROWS), r = wave * 8 + (lane >> 3), o = lane & 7;
         buffer.set(m.codes + int64_t(first) * m.bytes, int64_t(rows) * m.bytes);
-#pragma unroll
-        for (int j = 0; j < kOwn; ++j) {
-            const int r = (j * WAVES + wave) * 8 + (lane >> 3), o = lane & 7;
-            off[j] = uint32_t(of(r)) * uint32_t(m.bytes) + uint32_t(lds_piece<3>(r, o) - r * 8) * 16;
-        }
+        off = uint32_t(of(r)) * uint32_t(m.bytes) + uint32_t(lds_piece<3>(r, o) - r * 8) * 16;
+        step = uint32_t(m.bytes);
     }
     __device__ __forceinline__ void load(int at, uint4* lds, int wave) const {
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) buffer.to_lds16(off[j], at, lds + (j * WAVES + wave) * 64);
+        for (int j = 0; j < kOwn; ++j) {
+            // rows j * WAVES * 8 further on; the swizzle repeats every 16 rows
+            static_assert(WAVES % 4 == 0, "whole parts of 32 rows");
+            const int r = j * WAVES * 8;
+            buffer.to_lds16(off + uint32_t(of_step(r, wave)) * step, at, lds + (j * WAVES + wave) * 64);
+        }
+    }
+    // of(r + w) - of(w) for the wave's first row w, r a multiple of 32
+    static __device__ __forceinline__ int of_step(int r, int wave) {
+        const int w = wave * 8;
+        return of(r + w) - of(w);
     }
 };
 
@@ -82,7 +92,7 @@ __device__ __forceinline__ void f8_store(void* out, int64_t at, int left, const 
 
 // A workgroup of WM x WN waves takes WM MT 32 rows of a and WN NT 32 rows of b; blocks of 128 go through LDS, one ahead.  FAST: results of 16
 // bits.  blockIdx.y: which of the reduction's parts of `per` blocks; their sums go to parts[y][row][column] as fp32 where there are several.
-template <bool FAST, bool BF16, int WM, int WN, int MT, int NT>
+template <bool FAST, int WM, int WN, int MT, int NT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8Mat a, F8Mat b, void* c, int64_t stride, int m_tiles, int n_tiles, int per, float* parts) {
     constexpr int BM = WM * MT * 32, BN = WN * NT * 32, WAVES = WM * WN;
     typedef StageF8<BM, WAVES, 1> StageA;
@@ -97,66 +107,88 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8Mat a, F8Mat
     StageB stage_b;
     stage_a.setup(a, m0, wave);
     stage_b.setup(b, n0, wave);
-    const uint8_t* scale_a[MT];
-    const uint8_t* scale_b[NT];
+    uint32_t scale_a[MT], scale_b[NT];                               // where their rows' scales begin: arrays of less than 2^29 bytes
 #pragma unroll
-    for (int i = 0; i < MT; ++i) scale_a[i] = a.scales + int64_t(min(m0 + mw + i * 32 + col, a.rows - 1) >> a.shift) * a.scale_bytes;
+    for (int i = 0; i < MT; ++i) scale_a[i] = uint32_t(a.scale_at(min(m0 + mw + i * 32 + col, a.rows - 1), 0));
 #pragma unroll
-    for (int j = 0; j < NT; ++j) scale_b[j] = b.scales + int64_t(min(n0 + nw + col * NT + j, b.rows - 1) >> b.shift) * b.scale_bytes;
+    for (int j = 0; j < NT; ++j) scale_b[j] = uint32_t(b.scale_at(min(n0 + nw + col * NT + j, b.rows - 1), 0));
     const int blocks = a.bytes / kF8Block, first = blockIdx.y * per, last = min(blocks, first + per);
     f32x16 acc[MT][NT] = {};
-    uint32_t sa[MT], sb[NT], sa_next[MT], sb_next[NT];
+    uint32_t sa[MT], sb[NT], sa_next[MT], sb_next[NT];              // this block's scales, and the next one's
     auto load_scales = [&](int block) {
+        const uint8_t* in_a = a.scales + a.scale_at(0, min(block, blocks - 1));
+        const uint8_t* in_b = b.scales + b.scale_at(0, min(block, blocks - 1));
 #pragma unroll
-        for (int i = 0; i < MT; ++i) sa_next[i] = scale_a[i][block];
+        for (int i = 0; i < MT; ++i) sa_next[i] = in_a[scale_a[i]];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) sb_next[j] = scale_b[j][block];
+        for (int j = 0; j < NT; ++j) sb_next[j] = in_b[scale_b[j]];
     };
-    auto step = [&](bool more, int block, const uint4* now_a, const uint4* now_b, uint4* next_a, uint4* next_b) {
+    auto take_scales = [&]() {
 #pragma unroll
         for (int i = 0; i < MT; ++i) sa[i] = sa_next[i];
 #pragma unroll
         for (int j = 0; j < NT; ++j) sb[j] = sb_next[j];
-        if (more) {
-            stage_a.load((block + 1) * kF8Block, next_a, wave);
-            stage_b.load((block + 1) * kF8Block, next_b, wave);
-            load_scales(block + 1);
-        }
-        if constexpr (FAST) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                uint4 vb[NT][2];
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) vb[j][q] = now_b[lds_piece<3>(nw + j * 32 + col, s * 4 + q * 2 + half)];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const uint4 v0 = now_a[lds_piece<3>(mw + i * 32 + col, s * 4 + half)], v1 = now_a[lds_piece<3>(mw + i * 32 + col, s * 4 + 2 + half)];
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma_f8(v0, v1, vb[j][0], vb[j][1], acc[i][j], int(sa[i]), int(sb[j]));
-                }
-            }
-        } else {
-            float pa[MT], pb[NT];
+    };
+    // operands of half a block
+    auto read_a = [&](int s, int i, const uint4* lds) {
+        return f8_operand(lds[lds_piece<3>(mw + col, s * 4 + half) + i * 256], lds[lds_piece<3>(mw + col, s * 4 + 2 + half) + i * 256]);
+    };
+    auto read_b = [&](int s, int j, const uint4* lds) {
+        return f8_operand(lds[lds_piece<3>(nw + col, s * 4 + half) + j * 256], lds[lds_piece<3>(nw + col, s * 4 + 2 + half) + j * 256]);
+    };
+    auto load = [&](int block, uint4* to_a, uint4* to_b) {
+        stage_a.load(block * kF8Block, to_a, wave);
+        stage_b.load(block * kF8Block, to_b, wave);
+    };
+    // This wave's loads have arrived and its reads have ended, and so have all others'
+    auto meet = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __syncthreads();
+    };
+    load(first, s_a0, s_b0);
+    load_scales(first);
+    auto step = [&](bool more, int block, const uint4* now_a, const uint4* now_b, uint4* next_a, uint4* next_b) {
+        take_scales();
+        load_scales(block + 1);
+        if (more) load(block + 1, next_a, next_b);
+        float pa[MT], pb[NT];
+        if constexpr (!FAST) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) pa[i] = f8_power(sa[i]);
 #pragma unroll
             for (int j = 0; j < NT; ++j) pb[j] = f8_power(sb[j]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                uint4 vb[NT];
+        for (int s = 0; s < 2; ++s) {
+            i32x8 va[MT], vb[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) vb[j] = read_b(s, j, now_b);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) va[i] = read_a(s, i, now_a);
+            if constexpr (FAST) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = mfma_f8(va[i], vb[j], acc[i][j], int(sa[i]), int(sb[j]));
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
+                __builtin_amdgcn_sched_barrier(0);
+                continue;
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
                 bf16x8 xb[NT][2];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    vb[j] = now_b[lds_piece<3>(nw + j * 32 + col, 2 * s + half)];
-                    xb[j][0] = f8_bf16(vb[j].x, vb[j].y, pb[j]);
-                    xb[j][1] = f8_bf16(vb[j].z, vb[j].w, pb[j]);
+                    xb[j][0] = f8_bf16(vb[j][4 * q], vb[j][4 * q + 1], pb[j]);
+                    xb[j][1] = f8_bf16(vb[j][4 * q + 2], vb[j][4 * q + 3], pb[j]);
                 }
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const uint4 v = now_a[lds_piece<3>(mw + i * 32 + col, 2 * s + half)];
-                    const bf16x8 x0 = f8_bf16(v.x, v.y, pa[i]), x1 = f8_bf16(v.z, v.w, pa[i]);
+                    const bf16x8 x0 = f8_bf16(va[i][4 * q], va[i][4 * q + 1], pa[i]), x1 = f8_bf16(va[i][4 * q + 2], va[i][4 * q + 3], pa[i]);
 #pragma unroll
                     for (int j = 0; j < NT; ++j) {
                         acc[i][j] = mfma32(x0, xb[j][0], acc[i][j]);
@@ -165,20 +197,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8Mat a, F8Mat
                 }
             }
         }
-        __syncthreads();
+        meet();
     };
-    if (first < last) {
-        stage_a.load(first * kF8Block, s_a0, wave);
-        stage_b.load(first * kF8Block, s_b0, wave);
-        load_scales(first);
-    }
-    __syncthreads();
+    meet();
     int block = first;
     for (; block + 2 < last; block += 2) {
         step(true, block, s_a0, s_b0, s_a1, s_b1);
         step(true, block + 1, s_a1, s_b1, s_a0, s_b0);
     }
-    if (block < last) step(block + 1 < last, block, s_a0, s_b0, s_a1, s_b1);
+    step(block + 1 < last, block, s_a0, s_b0, s_a1, s_b1);
     if (block + 1 < last) step(false, block + 1, s_a1, s_b1, s_a0, s_b0);
     const int n = n0 + nw + col * NT;
 #pragma unroll
@@ -191,7 +218,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_tile_kernel(F8Mat a, F8Mat
             for (int j = 0; j < NT; ++j) v[j] = acc[i][j][e];
             if (m < a.rows) {
                 if (parts) f8_store<false, NT>(parts, (int64_t(blockIdx.y) * a.rows + m) * b.rows + n, b.rows - n, v);
-                else f8_store<BF16, NT>(c, int64_t(m) * stride + n, b.rows - n, v);
+                else f8_store<FAST, NT>(c, int64_t(m) * stride + n, b.rows - n, v);
             }
         }
 }
@@ -210,86 +237,111 @@ __global__ __launch_bounds__(256) void f8_join_kernel(const float* parts, int co
 //
 // Operand layout of v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds, of row (A) or column (B) l % 16, 32 bytes of the quarter l / 16 of the
 // reduction's 128; of the result column l % 16, rows 4 (l / 16) + i for i = 0..3.
-__device__ __forceinline__ f32x4 mfma16_f8(const uint32_t a[8], const uint32_t b[8], f32x4 c, int scale_a, int scale_b) {
-    const i32x8 va = {int(a[0]), int(a[1]), int(a[2]), int(a[3]), int(a[4]), int(a[5]), int(a[6]), int(a[7])};
-    const i32x8 vb = {int(b[0]), int(b[1]), int(b[2]), int(b[3]), int(b[4]), int(b[5]), int(b[6]), int(b[7])};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, c, 0, 0, 0, scale_a, 0, scale_b);
-}
+constexpr int kF8FewTokens = 16, kF8FewBytes = 65536;          // codes of x that LDS holds beside a second workgroup
 
-// y = x W^T for at most 16 tokens: a workgroup takes NT 16 rows of W, its waves every WAVES-th block.  x comes as it is and is brought to 8 bits in the
-// registers that are the operand: a block of a token lies in 4 lanes.  FAST goes with BF16.
-template <bool BF16, int NT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void f8_few_kernel(F8Mat w, const void* x, int t, int k, int64_t x_stride, void* y, int64_t y_stride) {
-    __shared__ float s_sum[WAVES][NT * 4 * 64];
-    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 15, quarter = lane >> 4;
-    const int n0 = blockIdx.x * NT * 16, blocks = w.bytes / kF8Block;
-    const uint8_t* codes[NT];
-    const uint8_t* scales[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int n = min(n0 + j * 16 + col, w.rows - 1);
-        codes[j] = w.codes + int64_t(n) * w.bytes + quarter * 32;
-        scales[j] = w.scales + int64_t(n >> w.shift) * w.scale_bytes;
-    }
-    const int64_t row = int64_t(col) * x_stride;
-    uint4 q[NT][2];
-    uint32_t sc[NT];
-    float v[32];
-    auto load = [&](int block) {
+// y = x W^T for at most 16 tokens whose codes fit into LDS.  WK x WN waves: 16 NT rows of W each, every WK-th block; a workgroup goes on to other rows
+// as long as there are any.  Codes of W come from memory into the registers that are the operand, AHEAD blocks in front of their use; the first
+// are on their way while the workgroup brings x to 8 bits.  The waves' sums of a row meet in LDS.
+template <bool BF16, int WK, int WN, int NT, int AHEAD>
+__global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const void* x, int t, int k, int64_t x_stride, void* y, int64_t y_stride) {
+    constexpr int THREADS = 64 * WK * WN, ROWS = WN * NT * 16, PART = NT * 4 * 64;
+    extern __shared__ uint4 s_x[];                                        // codes of x: [block][token], swizzled; then a scale for each
+    __shared__ float s_sum[2][WK * WN * PART];
+    const int blocks = w.bytes / kF8Block, lane = threadIdx.x & 63, wave = wave_number(), wk = wave % WK, wn = wave / WK;
+    const int col = lane & 15, quarter = lane >> 4, tiles = (w.rows + ROWS - 1) / ROWS;
+    uint8_t* s_scale = reinterpret_cast<uint8_t*>(s_x + blocks * t * 8);
+    uint4 q[AHEAD][NT][2];
+    uint32_t sw[AHEAD][NT];
+    // the wave's steps: blocks wk, wk + WK, ... of one tile, then of the next
+    int to_tile = blockIdx.x, to_block = wk;
+    auto load = [&](int slot) {
+        if (to_tile >= tiles) return;
+        const uint8_t* in = w.scales + w.scale_at(0, to_block);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            q[j][0] = *reinterpret_cast<const uint4*>(codes[j] + int64_t(block) * kF8Block);
-            q[j][1] = *reinterpret_cast<const uint4*>(codes[j] + int64_t(block) * kF8Block + 16);
-            sc[j] = scales[j][block];
+            const int n = min(to_tile * ROWS + (wn * NT + j) * 16 + col, w.rows - 1);
+            const uint8_t* at = w.codes + int64_t(n) * w.bytes + to_block * kF8Block + quarter * 32;
+            q[slot][j][0] = *reinterpret_cast<const uint4*>(at);
+            q[slot][j][1] = *reinterpret_cast<const uint4*>(at + 16);
+            sw[slot][j] = in[w.scale_at(n, 0)];
         }
-        const int at = block * kF8Block + quarter * 32;
-#pragma unroll
-        for (int o = 0; o < 4; ++o) {
-            if (col < t && at + o * 8 < k) {
-                w4_load8<BF16>(x, row + at + o * 8, row + k, v + o * 8);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[o * 8 + e] = 0.0f;
-            }
+        to_block += WK;
+        if (to_block >= blocks) {
+            to_block = wk;
+            to_tile += gridDim.x;
         }
     };
-    f32x4 acc[NT] = {};
-    for (int block = wave; block < blocks; block += WAVES) {
-        load(block);
+    if (wk < blocks) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(i);
+    }
+    for (int unit = threadIdx.x >> 4; unit < t * blocks; unit += THREADS / 16) {       // 16 lanes a block of a token
+        const int block = unit / t, token = unit - block * t, d = threadIdx.x & 15, at = block * kF8Block + d * 8;
+        const int64_t row = int64_t(token) * x_stride;
+        float v[8];
+        w4_load8<BF16>(x, row + at, row + k, v);
         uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) top = umax32(top, f8_magnitude(v[e]));
-        top = umax32(top, __shfl_xor(top, 16, 64));
-        top = umax32(top, __shfl_xor(top, 32, 64));
-        const uint32_t scale = f8_scale(top);
+        for (int e = 0; e < 8; ++e) top = umax32(top, f8_magnitude(v[e]));
+        const uint32_t scale = f8_scale(umax16(top));
         const float inverse = f8_inverse(scale);
-        uint32_t xa[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) xa[e] = f8_codes4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], inverse);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const uint32_t wb[8] = {q[j][0].x, q[j][0].y, q[j][0].z, q[j][0].w, q[j][1].x, q[j][1].y, q[j][1].z, q[j][1].w};
-            if constexpr (BF16) {
-                acc[j] = mfma16_f8(xa, wb, acc[j], int(scale), int(sc[j]));
-            } else {
-                const float px = f8_power(scale), pw = f8_power(sc[j]);
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_bf16(xa[2 * s], xa[2 * s + 1], px), f8_bf16(wb[2 * s], wb[2 * s + 1], pw), acc[j], 0, 0, 0);
-            }
-        }
+        uint2 c;
+        c.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
+        c.y = f8_codes4(v[4], v[5], v[6], v[7], inverse);
+        reinterpret_cast<uint2*>(s_x + block * t * 8)[lds_piece<3>(token, d >> 1) * 2 + (d & 1)] = c;
+        if (d == 0) s_scale[unit] = uint8_t(scale);
     }
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s_sum[wave][(j * 4 + i) * 64 + lane] = acc[j][i];
     __syncthreads();
-    for (int id = threadIdx.x; id < NT * 256; id += 64 * WAVES) {
-        float sum = s_sum[0][id];
+    int parity = 0;
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, parity ^= 1) {
+        f32x4 acc[NT] = {};
+        for (int block = wk; block < blocks; block += WK) {
+            uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
+            uint32_t sx = 127;
+            if (col < t) {
+                const uint4* from = s_x + block * t * 8;
+                x0 = from[lds_piece<3>(col, quarter * 2)];
+                x1 = from[lds_piece<3>(col, quarter * 2 + 1)];
+                sx = s_scale[block * t + col];
+            }
 #pragma unroll
-        for (int o = 1; o < WAVES; ++o) sum += s_sum[o][id];
-        const int j = id >> 8, i = id >> 6 & 3, n = n0 + j * 16 + (id & 15), tok = 4 * (id >> 4 & 3) + i;
-        if (n < w.rows && tok < t) w4_store1<BF16>(y, int64_t(tok) * y_stride + n, sum);
+            for (int j = 0; j < NT; ++j) {
+                if constexpr (BF16) {
+                    acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_operand(x0, x1), f8_operand(q[0][j][0], q[0][j][1]), acc[j], 0, 0, 0, int(sx), 0,
+                                                                              int(sw[0][j]));
+                } else {
+                    const float px = f8_power(sx), pw = f8_power(sw[0][j]);
+                    const uint4 w0 = q[0][j][0], w1 = q[0][j][1];
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_bf16(x0.x, x0.y, px), f8_bf16(w0.x, w0.y, pw), acc[j], 0, 0, 0);
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_bf16(x0.z, x0.w, px), f8_bf16(w0.z, w0.w, pw), acc[j], 0, 0, 0);
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_bf16(x1.x, x1.y, px), f8_bf16(w1.x, w1.y, pw), acc[j], 0, 0, 0);
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_bf16(x1.z, x1.w, px), f8_bf16(w1.z, w1.w, pw), acc[j], 0, 0, 0);
+                }
+            }
+            // the queue moves up by one
+#pragma unroll
+            for (int i = 0; i + 1 < AHEAD; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    q[i][j][0] = q[i + 1][j][0];
+                    q[i][j][1] = q[i + 1][j][1];
+                    sw[i][j] = sw[i + 1][j];
+                }
+            load(AHEAD - 1);
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s_sum[parity][wave * PART + (j * 4 + i) * 64 + lane] = acc[j][i];
+        __syncthreads();                                                  // the other half of s_sum is free by the next one
+        for (int id = threadIdx.x; id < WN * PART; id += THREADS) {
+            const int part = id / PART, e = id % PART;
+            float sum = 0.0f;
+#pragma unroll
+            for (int o = 0; o < WK; ++o) sum += s_sum[parity][(part * WK + o) * PART + e];
+            const int n = tile * ROWS + (part * NT + e / 256) * 16 + (e & 15), tok = 4 * (e >> 4 & 3) + (e >> 6 & 3);
+            if (n < w.rows && tok < t) w4_store1<BF16>(y, int64_t(tok) * y_stride + n, sum);
+        }
     }
 }
 

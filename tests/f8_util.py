@@ -45,8 +45,13 @@ def unpack(m):
     assert codes.shape == (m.rows, -(-m.cols // 128) * 128)
     assert bool((codes[:, m.cols:] == 0).all()), "the rest of a row is 0"
     blocks = -(-m.cols // 128)
-    assert scales.shape == (-(-m.rows // m.tile), -(-blocks // 4) * 4)
-    assert bool((scales[:, blocks:] == 0).all()), "the rest of a row of scales is 0"
+    if m.tile == 1:
+        assert scales.shape == (blocks, -(-m.rows // 4) * 4)
+        assert bool((scales[:, m.rows:] == 0).all()), "the rest of a row of scales is 0"
+        scales = scales[:, :m.rows].t()
+    else:
+        assert scales.shape == (-(-m.rows // 128), -(-blocks // 4) * 4)
+        assert bool((scales[:, blocks:] == 0).all()), "the rest of a row of scales is 0"
     power, part = codes >> 3 & 15, (codes & 7).double()
     v = torch.where(power > 0, (8 + part) * 2.0 ** (power.double() - 10), part * 2.0 ** -9)
     v[(codes & 127) == 127] = math.nan

@@ -199,7 +199,9 @@ def test_beyond_32_bits():
     last = matrix(130, k, F32, 3, 0.3)
     part = lpmm.lpmm_f8_quant(last.to(DEV), 1)
     q.codes[n - 130:] = part.codes
-    w = ref.unpack(lpmm.MatF8(130, k, 1, part.codes, torch.full_like(part.scales, 127)))[0]
+    ones = torch.zeros_like(part.scales)
+    ones[:, :130] = 127
+    w = ref.unpack(lpmm.MatF8(130, k, 1, part.codes, ones))[0]
     for t, dtype in ((2, BF16), (2, F32), (40, BF16)):
         x = matrix(t, k, dtype, 4, 0.3)
         y = lpmm.lpmm_f8_linear(x.to(DEV), q)
