@@ -582,6 +582,20 @@ size_t lpmm_f8_linear_workspace_bytes(int64_t t, int64_t n, int64_t k);
 int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const lpmm_f8* w, void* y, int64_t y_stride, void* workspace,
                    size_t workspace_bytes, void* stream);
 
+/* A layer's training step with 8-bit operands, two calls: y = Q(x) Q(W)^T, then dx = Q(dy) Q(W) and dW = Q(dy^T) Q(x^T)^T, where Q(x), Q(dy) and their transposes are in
+ * blocks of 1 x 128 along the sum and Q(W) in blocks of 128 x 128.  x, y, dy, dx: dtype; W, dW: w_dtype; dx and dW are written, not added to.  grads: which of
+ * the gradients the second call will want (the same value for both calls; the other's pointers are not looked at).  kept: what the first call leaves for the second,
+ * 16-byte aligned, of the bytes that ..._kept_bytes gives, untouched in between; the second call may be repeated.  workspace as above, one size for
+ * both calls.  1 <= t, n, k <= 2^22. */
+#define LPMM_F8_DX 1
+#define LPMM_F8_DW 2
+size_t lpmm_f8_train_kept_bytes(int64_t t, int64_t n, int64_t k, int grads);
+size_t lpmm_f8_train_workspace_bytes(int64_t t, int64_t n, int64_t k);
+int lpmm_f8_train_forward(const void* x, int dtype, int64_t t, int64_t x_stride, const void* w, int w_dtype, int64_t n, int64_t k, int64_t w_stride, int grads,
+                          void* y, int64_t y_stride, void* kept, size_t kept_bytes, void* workspace, size_t workspace_bytes, void* stream);
+int lpmm_f8_train_backward(const void* dy, int dtype, int64_t t, int64_t dy_stride, int64_t n, int64_t k, int grads, const void* kept, size_t kept_bytes, void* dx,
+                           int64_t dx_stride, void* dw, int w_dtype, int64_t dw_stride, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- tokens drawn from logits --------------------------------------------------------------------------------------------
  *
  * For each row of z (t rows of v logits; z_dtype, z_stride; v at most 2^30) one token, drawn with the row's number u from [0, 1):

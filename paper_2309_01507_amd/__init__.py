@@ -23,6 +23,7 @@ from .binding import (  # noqa: F401
     WeightsW4, new_w4, lpmm_w4_sizes, lpmm_w4_quant, lpmm_w4_dequant, lpmm_w4_linear, lpmm_w4_linear_dx,
     lpmm_w4_linear_dscale, lpmm_distill_loss, lpmm_distill_grad, lpmm_distill_loss_grad, DISTILL_MAX_SLOTS, F32, BF16,
     MatF8, new_f8, lpmm_f8_sizes, lpmm_f8_quant, lpmm_f8_quant_both, lpmm_f8_dequant, lpmm_f8_matmul, lpmm_f8_linear,
+    lpmm_f8_train_forward, lpmm_f8_train_backward, F8_DX, F8_DW,
     lpmm_sample, GradPlan, new_grad_plan, lpmm_grad_norm, lpmm_grad_clip, lpmm_grad_norm_clip, GRAD_NORM_L2, GRAD_NORM_MAX,
 )
 from .optim import AdamW4bit, SGDM4bit  # noqa: F401,E402

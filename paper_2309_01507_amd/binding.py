@@ -151,6 +151,14 @@ def lib() -> ctypes.CDLL:
         L.lpmm_f8_linear_workspace_bytes.argtypes = [_I64] * 3
         L.lpmm_f8_linear_workspace_bytes.restype = ctypes.c_size_t
         L.lpmm_f8_linear.argtypes = [_VP, ctypes.c_int, _I64, _I64, _VP, _VP, _I64, _VP, ctypes.c_size_t, _VP]
+        L.lpmm_f8_train_kept_bytes.argtypes = [_I64] * 3 + [ctypes.c_int]
+        L.lpmm_f8_train_kept_bytes.restype = ctypes.c_size_t
+        L.lpmm_f8_train_workspace_bytes.argtypes = [_I64] * 3
+        L.lpmm_f8_train_workspace_bytes.restype = ctypes.c_size_t
+        L.lpmm_f8_train_forward.argtypes = [_VP, ctypes.c_int, _I64, _I64, _VP, ctypes.c_int, _I64, _I64, _I64, ctypes.c_int, _VP, _I64, _VP, ctypes.c_size_t,
+                                            _VP, ctypes.c_size_t, _VP]
+        L.lpmm_f8_train_backward.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _I64, ctypes.c_int, _VP, ctypes.c_size_t, _VP, _I64, _VP, ctypes.c_int, _I64,
+                                             _VP, ctypes.c_size_t, _VP]
         L.lpmm_sample.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP]
         L.lpmm_grad_plan_bytes.argtypes = [_VP, _I64]
         L.lpmm_grad_plan_bytes.restype = ctypes.c_size_t
@@ -1054,6 +1062,55 @@ def lpmm_f8_linear(x, w: MatF8, y=None, workspace=None, stream=None):
     _check(L.lpmm_f8_linear(ptr, dtype, t, ld, ctypes.addressof(f), yptr, yld, _ptr(workspace), _room(workspace), _stream(stream)),
            "lpmm_f8_linear")
     return y
+
+
+F8_DX, F8_DW = 1, 2
+
+
+def lpmm_f8_train_forward(x, w, grads: int = F8_DX | F8_DW, y=None, kept=None, workspace=None, stream=None):
+    """(y, kept): y = Q(x) Q(W)^T for x tokens x cols and W rows x cols (float32 or bfloat16 each), y of x's type; `kept` is what lpmm_f8_train_backward
+    needs for the gradients that `grads` names (None for none)."""
+    torch = _torch or _load_torch()
+    if w.dim() != 2:
+        raise ValueError("lpmm_f8_train_forward: w must be a matrix")
+    n, k = w.shape
+    wp, w_dtype, _, wld = _rows(w, k, "w")
+    xp, dtype, t, xld = _rows(x, k, "x")
+    L = _lib or lib()
+    room, need = L.lpmm_f8_train_kept_bytes(t, n, k, grads), L.lpmm_f8_train_workspace_bytes(t, n, k)
+    y, yp, yld = _matrix_out(y, x, t, n, stream, "y")
+    kept = _workspace(kept, room, x, stream, "lpmm_f8_train_forward")
+    workspace = _workspace(workspace, need, x, stream, "lpmm_f8_train_forward")
+    _on_current("lpmm_f8_train_forward", x, w, y)
+    _check(L.lpmm_f8_train_forward(xp, dtype, t, xld, wp, w_dtype, n, k, wld, grads, yp, yld, _ptr(kept), _room(kept), _ptr(workspace), _room(workspace),
+                                   _stream(stream)), "lpmm_f8_train_forward")
+    return y, kept
+
+
+def lpmm_f8_train_backward(dy, kept, cols: int, w_dtype=None, grads: int = F8_DX | F8_DW, dx=None, dw=None, workspace=None, stream=None):
+    """(dx, dW) of lpmm_f8_train_forward with the same `grads`, None where it names them not; dW has w_dtype (float32 by default)."""
+    torch = _torch or _load_torch()
+    if dy.dim() != 2:
+        raise ValueError("lpmm_f8_train_backward: dy must be a matrix")
+    t, n = dy.shape
+    ptr, dtype, _, ld = _rows(dy, n, "dy")
+    xp = wp = None
+    xld = wld = cols
+    if grads & F8_DX:
+        dx, xp, xld = _matrix_out(dx, dy, t, cols, stream, "dx")
+        _on_current("lpmm_f8_train_backward", dy, dx)
+    if grads & F8_DW:
+        dw = _new(dw, (n, cols), w_dtype or torch.float32, dy.device, stream, "dw")
+        wp, _, _, wld = _rows(dw, cols, "dw")
+        _on_current("lpmm_f8_train_backward", dy, dw)
+    L = _lib or lib()
+    workspace = _workspace(workspace, L.lpmm_f8_train_workspace_bytes(t, n, cols), dy, stream, "lpmm_f8_train_backward")
+    if kept is not None and (kept.get_device() != dy.get_device() or not kept.is_contiguous()):
+        raise ValueError("lpmm_f8_train_backward: kept must be on the current GPU and contiguous")
+    _on_current("lpmm_f8_train_backward", dy)
+    _check(L.lpmm_f8_train_backward(ptr, dtype, t, ld, n, cols, grads, _ptr(kept), _room(kept), xp, xld, wp, BF16 if grads & F8_DW and dw.dtype is torch.bfloat16 else F32,
+                                    wld, _ptr(workspace), _room(workspace), _stream(stream)), "lpmm_f8_train_backward")
+    return dx if grads & F8_DX else None, dw if grads & F8_DW else None
 
 
 # ---- tokens drawn from logits --------------------------------------------------------------------------------

@@ -133,6 +133,40 @@ bool few(int64_t t, int64_t bytes) { return t <= kF8FewTokens && t * bytes <= kF
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
+// A matrix laid out in a caller's memory from `at` on, which moves behind it
+F8Mat carve(char*& at, int64_t rows, int64_t cols, int tile) {
+    F8Mat m{};
+    check_f8(rows, cols, tile, &m);                              // the caller has checked them
+    m.codes = reinterpret_cast<uint8_t*>(at);
+    at += up16(size_t(m.rows) * m.bytes);
+    m.scales = reinterpret_cast<uint8_t*>(at);
+    at += up16(size_t(scale_rows(m)) * m.scale_bytes);
+    return m;
+}
+size_t carved(int64_t rows, int64_t cols, int tile) {
+    char* at = nullptr;
+    carve(at, rows, cols, tile);
+    return size_t(at - static_cast<char*>(nullptr));
+}
+
+int check_train(int64_t t, int64_t n, int64_t k, int grads) {
+    F8Mat m{};
+    if (t < 1 || t > kMaxTokens || t > kMaxF8Row || n < 1 || n > kMaxF8Row || grads < 0 || grads > 3) return LPMM_EINVAL;
+    LPMM_TRY(check_f8(t, k, 1, &m));
+    LPMM_TRY(check_f8(k, t, 1, &m));
+    LPMM_TRY(check_f8(t, n, 1, &m));
+    LPMM_TRY(check_f8(n, t, 1, &m));
+    LPMM_TRY(check_f8(k, n, 128, &m));
+    return check_f8(n, k, 128, &m);
+}
+
+uint8_t* writable(const uint8_t* p) { return const_cast<uint8_t*>(p); }
+
+int quant_into(const void* x, int dtype, int64_t stride, int64_t rows, int64_t cols, int tile, const F8Mat& m, const F8Mat& mt, hipStream_t s) {
+    if (tile == 1 && !mt.codes) return launch_quant(x, dtype, stride, m, cols, writable(m.codes), writable(m.scales), s);
+    return launch_quant_tile(x, dtype, stride, rows, cols, tile, m, mt, writable(m.codes), writable(m.scales), writable(mt.codes), writable(mt.scales), s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -234,6 +268,57 @@ int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     mx.scales = scales;
     LPMM_TRY(launch_quant(x, dtype, x_stride, mx, w->cols, codes, scales, s));
     return launch_product(mx, mw, y, dtype, y_stride, scales + up16(size_t(scale_rows(mx)) * mx.scale_bytes), s);
+}
+
+size_t lpmm_f8_train_kept_bytes(int64_t t, int64_t n, int64_t k, int grads) {
+    if (check_train(t, n, k, grads)) return 0;
+    return (grads & LPMM_F8_DX ? carved(k, n, 128) : 0) + (grads & LPMM_F8_DW ? carved(k, t, 1) : 0);
+}
+
+size_t lpmm_f8_train_workspace_bytes(int64_t t, int64_t n, int64_t k) {
+    if (check_train(t, n, k, 0)) return 0;
+    const size_t forward = carved(t, k, 1) + carved(n, k, 128) + lpmm_f8_matmul_workspace_bytes(t, n, k);
+    const size_t backward = carved(t, n, 1) + carved(n, t, 1) + std::max(lpmm_f8_matmul_workspace_bytes(t, k, n), lpmm_f8_matmul_workspace_bytes(n, k, t));
+    return std::max(forward, backward);
+}
+
+int lpmm_f8_train_forward(const void* x, int dtype, int64_t t, int64_t x_stride, const void* w, int w_dtype, int64_t n, int64_t k, int64_t w_stride, int grads,
+                          void* y, int64_t y_stride, void* kept, size_t kept_bytes, void* workspace, size_t workspace_bytes, void* stream) {
+    LPMM_TRY(check_train(t, n, k, grads));
+    LPMM_TRY(check_rows(x, dtype, t, k, x_stride));
+    LPMM_TRY(check_rows(w, w_dtype, n, k, w_stride));
+    LPMM_TRY(check_rows(y, dtype, t, n, y_stride));
+    LPMM_TRY(check_workspace(kept, kept_bytes, lpmm_f8_train_kept_bytes(t, n, k, grads)));
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_f8_train_workspace_bytes(t, n, k)));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* at = static_cast<char*>(workspace);
+    const F8Mat qx = carve(at, t, k, 1), qw = carve(at, n, k, 128);
+    char* keep = static_cast<char*>(kept);
+    const F8Mat qwt = grads & LPMM_F8_DX ? carve(keep, k, n, 128) : F8Mat{}, qxt = grads & LPMM_F8_DW ? carve(keep, k, t, 1) : F8Mat{};
+    LPMM_TRY(quant_into(w, w_dtype, w_stride, n, k, 128, qw, qwt, s));
+    LPMM_TRY(quant_into(x, dtype, x_stride, t, k, 1, qx, qxt, s));
+    return launch_product(qx, qw, y, dtype, y_stride, at, s);
+}
+
+int lpmm_f8_train_backward(const void* dy, int dtype, int64_t t, int64_t dy_stride, int64_t n, int64_t k, int grads, const void* kept, size_t kept_bytes, void* dx,
+                           int64_t dx_stride, void* dw, int w_dtype, int64_t dw_stride, void* workspace, size_t workspace_bytes, void* stream) {
+    LPMM_TRY(check_train(t, n, k, grads));
+    const bool want_x = grads & LPMM_F8_DX, want_w = grads & LPMM_F8_DW;
+    LPMM_TRY(check_rows(dy, dtype, t, n, dy_stride));
+    if (want_x) LPMM_TRY(check_rows(dx, dtype, t, k, dx_stride));
+    if (want_w) LPMM_TRY(check_rows(dw, w_dtype, n, k, dw_stride));
+    LPMM_TRY(check_workspace(kept, kept_bytes, lpmm_f8_train_kept_bytes(t, n, k, grads)));
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_f8_train_workspace_bytes(t, n, k)));
+    if (!want_x && !want_w) return LPMM_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* at = static_cast<char*>(workspace);
+    const F8Mat q = carve(at, t, n, 1), qt = want_w ? carve(at, n, t, 1) : F8Mat{};
+    char* keep = static_cast<char*>(const_cast<void*>(kept));
+    const F8Mat qwt = want_x ? carve(keep, k, n, 128) : F8Mat{}, qxt = want_w ? carve(keep, k, t, 1) : F8Mat{};
+    LPMM_TRY(quant_into(dy, dtype, dy_stride, t, n, 1, q, qt, s));
+    if (want_x) LPMM_TRY(launch_product(q, qwt, dx, dtype, dx_stride, at, s));
+    if (want_w) LPMM_TRY(launch_product(qt, qxt, dw, w_dtype, dw_stride, at, s));
+    return LPMM_OK;
 }
 
 }  // extern "C"

@@ -22,39 +22,29 @@ from .w4 import _flat
 class _Product(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight):
-        flat = _flat(x.detach(), weight.shape[1])
-        w = weight.detach()
-        t = flat.shape[0]
         need_x, need_w = ctx.needs_input_grad
-        qw, qwt = _b.lpmm_f8_quant_both(w, 128) if need_x else (_b.lpmm_f8_quant(w, 128), None)
-        qxt = None
-        if need_w and t:
-            qx, qxt = _b.lpmm_f8_quant_both(flat, 1)
-            y = _b.lpmm_f8_matmul(qx, qw, flat.dtype)
+        n, k = weight.shape
+        flat = _flat(x.detach(), k)
+        ctx.grads, ctx.shape, ctx.w_shape, ctx.w_dtype = need_x * _b.F8_DX | need_w * _b.F8_DW, x.shape, weight.shape, weight.dtype
+        if flat.shape[0] == 0:
+            kept, y = None, flat.new_empty(0, n)
+        elif ctx.grads:
+            y, kept = _b.lpmm_f8_train_forward(flat, _flat(weight.detach(), k), ctx.grads)
         else:
-            y = _b.lpmm_f8_linear(flat, qw)
-        ctx.t, ctx.shape, ctx.w_shape, ctx.w_dtype = t, x.shape, weight.shape, weight.dtype
-        ctx.save_for_backward(*((qwt.codes, qwt.scales) if qwt else (None, None)), *((qxt.codes, qxt.scales) if qxt else (None, None)))
-        return y.view(*x.shape[:-1], weight.shape[0])
+            kept, y = None, _b.lpmm_f8_linear(flat, _b.lpmm_f8_quant(_flat(weight.detach(), k), 128))
+        ctx.save_for_backward(kept)
+        return y.view(*x.shape[:-1], n)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        w_codes, w_scales, x_codes, x_scales = ctx.saved_tensors
-        (n, k), t = ctx.w_shape, ctx.t
+        kept, = ctx.saved_tensors
+        n, k = ctx.w_shape
         dy = _flat(dy, n)
-        dx = dw = None
-        need_x, need_w = ctx.needs_input_grad
-        if t == 0:
-            return (dy.new_zeros(ctx.shape) if need_x else None, dy.new_zeros(n, k, dtype=ctx.w_dtype) if need_w else None)
-        if need_w:
-            q, qt = _b.lpmm_f8_quant_both(dy, 1)
-            dw = _b.lpmm_f8_matmul(qt, _b.MatF8(k, t, 1, x_codes, x_scales), ctx.w_dtype)
-            if need_x:
-                dx = _b.lpmm_f8_matmul(q, _b.MatF8(k, n, 128, w_codes, w_scales), dy.dtype)
-        elif need_x:
-            dx = _b.lpmm_f8_linear(dy, _b.MatF8(k, n, 128, w_codes, w_scales))
-        return dx.view(ctx.shape) if need_x else None, dw
+        if dy.shape[0] == 0:
+            return (dy.new_empty(ctx.shape) if ctx.grads & _b.F8_DX else None, dy.new_zeros(n, k, dtype=ctx.w_dtype) if ctx.grads & _b.F8_DW else None)
+        dx, dw = _b.lpmm_f8_train_backward(dy, kept, k, ctx.w_dtype, ctx.grads)
+        return None if dx is None else dx.view(ctx.shape), dw
 
 
 def f8_linear(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
