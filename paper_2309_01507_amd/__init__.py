@@ -26,6 +26,7 @@ from .binding import (  # noqa: F401
     lpmm_f8_train_forward, lpmm_f8_train_backward, F8_DX, F8_DW,
     lpmm_sample, GradPlan, new_grad_plan, lpmm_grad_norm, lpmm_grad_clip, lpmm_grad_norm_clip, GRAD_NORM_L2, GRAD_NORM_MAX,
 )
-from .optim import AdamW4bit, SGDM4bit  # noqa: F401,E402
+from .optim import AdamW4bit, SGDM4bit, clip_grad_norm  # noqa: F401,E402
 from .w4 import W4Linear, w4_linear, distill_loss  # noqa: F401,E402
 from .f8 import F8Linear, f8_linear  # noqa: F401,E402
+from .sampling import sample  # noqa: F401,E402

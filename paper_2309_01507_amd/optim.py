@@ -4,6 +4,9 @@ call lpmm_adamw4_step_multi / lpmm_sgdm4_step_multi.  Orchestration only -- ever
     opt = AdamW4bit(model.parameters(), lr=1e-3, weight_decay=0.01)
     loss.backward(); opt.step(); opt.zero_grad()
 
+With max_norm given, step() first scales the gradients in place so that their norm, as one vector, is at most that;
+clip_grad_norm does it apart from a step, for an optimizer's parameters or any others.
+
 Parameters must be fp32, contiguous and on one GPU; gradients fp32 or bf16 (one type per optimizer).  A plan
 refers to parameter and gradient buffers by address, so it is rebuilt whenever one of them has moved (keep
 gradients in place with zero_grad(set_to_none=False) to avoid that).
@@ -17,12 +20,33 @@ from . import binding as _b
 QUANT_MIN_NUMEL = 4096          # App. C.1: tensors of at most 4096 elements keep fp32 states
 
 
+def _norm_kind(norm_type) -> int:
+    if norm_type in (2, 2.0):
+        return _b.GRAD_NORM_L2
+    if norm_type in (float("inf"), "inf"):
+        return _b.GRAD_NORM_MAX
+    raise ValueError("norm_type must be 2 or inf")
+
+
+def clip_grad_norm(parameters, max_norm: float, norm_type=2.0) -> torch.Tensor:
+    """Scales the parameters' gradients in place so that their norm, as one vector, is at most max_norm: by
+    max_norm / (norm + 1e-6) where that is below 1.  Returns the norm from before, a tensor of one float32; parameters without a gradient
+    do not count.  Gradients must be contiguous, float32 or bfloat16, on the current GPU.  Each call uploads a list of them and waits for it: a training loop
+    that keeps its gradients in place has an optimizer's clip_grad_norm, or a plan (new_grad_plan)."""
+    kind = _norm_kind(norm_type)
+    parameters = [parameters] if torch.is_tensor(parameters) else list(parameters)
+    plan = _b.new_grad_plan([p.grad for p in parameters if p.grad is not None])
+    return _b.lpmm_grad_norm_clip(plan, max_norm, kind)
+
+
 def _default_no_decay(p: torch.Tensor) -> bool:
     return p.ndim <= 1              # biases and normalization weights
 
 
 class _PlanOptimizer:
-    def __init__(self, params, no_decay):
+    def __init__(self, params, no_decay, max_norm=None):
+        if max_norm is not None and not max_norm >= 0:
+            raise ValueError("max_norm must be at least 0")
         self.params = [p for p in params if p.requires_grad]
         if not self.params:
             raise ValueError("no parameters")
@@ -33,7 +57,9 @@ class _PlanOptimizer:
         self.device = dev
         self.no_decay = no_decay if callable(no_decay) else (lambda p, flag=bool(no_decay): flag and p.ndim <= 1)
         self.t = 0
+        self.max_norm = max_norm
         self._plan = None
+        self._grad_plan = None
         self._key = None
         self._states = None
 
@@ -52,6 +78,7 @@ class _PlanOptimizer:
         key = tuple((p.data_ptr(), g.data_ptr()) for p, g in zip(self.params, grads)) + (grads[0].dtype,)
         if key == self._key:
             return
+        self._grad_plan = None
         with torch.cuda.device(self.device):
             _b.ensure_init(4096)            # lookup tables; a plan carries its own workspace
             if self._states is None:
@@ -65,8 +92,21 @@ class _PlanOptimizer:
         self._key = key
 
     @torch.no_grad()
+    def clip_grad_norm(self, max_norm: float, norm_type=2.0) -> torch.Tensor:
+        """Scales the gradients in place (see the function of this name) and returns their norm from before, a tensor of one float32.  The list of gradients
+        stays on the device as long as they keep their addresses."""
+        kind = _norm_kind(norm_type)
+        self._ensure_plan()
+        with torch.cuda.device(self.device):
+            if self._grad_plan is None:
+                self._grad_plan = _b.new_grad_plan([p.grad for p in self.params])
+            return _b.lpmm_grad_norm_clip(self._grad_plan, max_norm, kind)
+
+    @torch.no_grad()
     def step(self):
         self._ensure_plan()
+        if self.max_norm is not None:
+            self.clip_grad_norm(self.max_norm)
         self.t += 1
         if torch._C._cuda_getDevice() == self.device.index:
             self._step(self._plan)
@@ -140,8 +180,8 @@ class AdamW4bit(_PlanOptimizer):
     states, larger 1-dimensional ones block-wise 4-bit states."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, second_moment="rank1",
-                 no_decay=_default_no_decay, capturable=False):
-        super().__init__(params, no_decay)
+                 no_decay=_default_no_decay, capturable=False, max_norm=None):
+        super().__init__(params, no_decay, max_norm)
         if second_moment not in ("rank1", "factor", "b128"):
             raise ValueError("second_moment must be rank1, factor or b128")
         self.lr, self.betas, self.eps, self.weight_decay, self.second_moment = lr, betas, eps, weight_decay, second_moment
@@ -188,8 +228,8 @@ class AdamW4bit(_PlanOptimizer):
 class SGDM4bit(_PlanOptimizer):
     """SGD with momentum, momentum in 4 bits (fp32 for tensors of at most 4096 elements); no weight decay."""
 
-    def __init__(self, params, lr=1e-2, momentum=0.9):
-        super().__init__(params, no_decay=False)
+    def __init__(self, params, lr=1e-2, momentum=0.9, max_norm=None):
+        super().__init__(params, no_decay=False, max_norm=max_norm)
         self.lr, self.momentum = lr, momentum
 
     def _new_state(self, p):

@@ -99,3 +99,15 @@ def test_lists_of_other_tensors():
                 lambda: lpmm.new_grad_plan([g], []), lambda: lpmm.new_grad_plan([g], [torch.zeros(5)])):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_modules_refuse():
+    z = torch.zeros(2, 3, 10)
+    for bad in (lambda: lpmm.sample(z, u=torch.zeros(3, 2)), lambda: lpmm.sample(z, temperature=torch.zeros(6)), lambda: lpmm.sample(z, top_k=torch.zeros(2, 3)),
+                lambda: lpmm.sample(z), lambda: lpmm.clip_grad_norm([], 1.0, norm_type=1), lambda: lpmm.clip_grad_norm(torch.nn.Parameter(z), 1.0, 3.0)):
+        with pytest.raises(ValueError):
+            bad()
+    p = torch.nn.Parameter(z)
+    p.grad = torch.ones_like(z)
+    with pytest.raises(ValueError, match="GPU"):
+        lpmm.clip_grad_norm([p], 1.0)
