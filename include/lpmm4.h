@@ -610,7 +610,8 @@ int lpmm_f8_train_backward(const void* dy, int dtype, int64_t t, int64_t dy_stri
  * an array on the device with one for each row.  Values for all rows are refused where they are NaN, or temperature or top_k negative;
  * a row's own are taken as they come: a temperature that is not above 0 as 0, top_k below 1 and a top_p of NaN as all, a min_p of NaN as 0.
  * -infinity is never drawn; where the largest logit is +infinity, only those that are it are.  A row with a NaN, or with nothing
- * above -infinity, gets token -1 and logprob NaN.  A u below 0 (or NaN) is taken as 0, one of 1 or more draws the last that is kept.  tokens: int64[t]. */
+ * above -infinity, gets token -1 and logprob NaN.  A u below 0 (or NaN) is taken as 0, one of 1 or more draws the last that is kept.  tokens: int64[t].
+ * workspace as for the 4-bit weights above. */
 typedef struct lpmm_sample_options {
     float temperature, top_p, min_p;
     int32_t top_k;
@@ -619,8 +620,9 @@ typedef struct lpmm_sample_options {
     const float* top_ps;
     const float* min_ps;
 } lpmm_sample_options;
+size_t lpmm_sample_workspace_bytes(int64_t t, int64_t v);
 int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* u, const lpmm_sample_options* options,
-                int64_t* tokens, float* logprob, void* stream);
+                int64_t* tokens, float* logprob, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- the norm of all gradients, and clipping -------------------------------------------------------------------------------
  *

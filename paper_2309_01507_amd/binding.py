@@ -159,7 +159,9 @@ def lib() -> ctypes.CDLL:
                                             _VP, ctypes.c_size_t, _VP]
         L.lpmm_f8_train_backward.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _I64, ctypes.c_int, _VP, ctypes.c_size_t, _VP, _I64, _VP, ctypes.c_int, _I64,
                                              _VP, ctypes.c_size_t, _VP]
-        L.lpmm_sample.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP]
+        L.lpmm_sample_workspace_bytes.argtypes = [_I64, _I64]
+        L.lpmm_sample_workspace_bytes.restype = ctypes.c_size_t
+        L.lpmm_sample.argtypes = [_VP, ctypes.c_int, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]
         L.lpmm_grad_plan_bytes.argtypes = [_VP, _I64]
         L.lpmm_grad_plan_bytes.restype = ctypes.c_size_t
         L.lpmm_grad_plan_build.argtypes = [_VP, _I64, _VP, ctypes.c_size_t, _VP, _VP]
@@ -1131,7 +1133,7 @@ def _option(o: SampleOptions, name: str, x, dtype, t: int, on: list) -> None:
         setattr(o, name, x if name != "top_k" else min(max(int(x), -1), 0x7FFFFFFF))
 
 
-def lpmm_sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprob=None, stream=None):
+def lpmm_sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprob=None, workspace=None, stream=None):
     """(tokens, logprob): a token for each row of the logits z, drawn with the row's number u from [0, 1) (float32).  Each option is a number,
     or a tensor with one for each row (float32; top_k int32)."""
     torch = _torch or _load_torch()
@@ -1150,8 +1152,11 @@ def lpmm_sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
     elif tokens.dtype is not torch.int64 or tokens.shape != (t,) or not tokens.is_contiguous():
         raise ValueError("tokens must be int64, contiguous, one per row")
     logprob, lptr = _row_out(logprob, u, t, stream, "logprob")
+    L = _lib or lib()
+    workspace = _workspace(workspace, L.lpmm_sample_workspace_bytes(t, v), z, stream, "lpmm_sample")
     _on_current("lpmm_sample", *on, tokens, logprob)
-    _check((_lib or lib()).lpmm_sample(ptr, dtype, t, v, ld, uptr, ctypes.addressof(o), tokens.data_ptr(), lptr, _stream(stream)), "lpmm_sample")
+    _check(L.lpmm_sample(ptr, dtype, t, v, ld, uptr, ctypes.addressof(o), tokens.data_ptr(), lptr, _ptr(workspace), _room(workspace), _stream(stream)),
+           "lpmm_sample")
     return tokens, logprob
 
 

@@ -8,10 +8,29 @@
 #include "host_util.hpp"
 #include "sample.hpp"
 
+namespace {
+
 using namespace lpmm;
 
-extern "C" int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* u, const lpmm_sample_options* options,
-                           int64_t* tokens, float* logprob, void* stream) {
+// Workgroups of a row; 1: one does it all.  Sharing costs two launches and the handing over, and takes from the four readings of a row.  One workgroup against several,
+// us, fp32 with top_p 0.95: 1 x 8000 19 and 24, 1 x 16000 27 and 26, 1 x 32000 36 and 27, 1 x 131072 110 and 34; 16 x 16000 28 and 27, 16 x 50257 51 and 35;
+// 64 x 16000 28 and 32, 64 x 32000 39 and 39, 64 x 50257 52 and 46; 128 x 50257 57 and 62 (there the workgroups of a row each wait for a CU).  512 for all rows
+// together: with 256 16 to 64 rows take up to a fourth longer, with 1024 64 x 32000 takes 45.
+int sample_shares(int64_t t, int64_t v) {
+    if (t < 1 || t > 64 || v < 16384 + 256 * t || v > int64_t(kSampleBins) * 256) return 1;
+    return int(std::min<int64_t>(std::min<int64_t>(kSampleShares, 512 / t), div_up(v, 2048)));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lpmm_sample_workspace_bytes(int64_t t, int64_t v) {
+    return t < 1 || t > kMaxTokens || v < 1 || v > kMaxDim || sample_shares(t, v) == 1 ? 0 : size_t(t) * sizeof(SampleWork);
+}
+
+int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stride, const float* u, const lpmm_sample_options* options,
+                int64_t* tokens, float* logprob, void* workspace, size_t workspace_bytes, void* stream) {
     if (!options || t > kMaxTokens || v < 1 || v > kMaxDim) return LPMM_EINVAL;
     LPMM_TRY(check_rows(z, z_dtype, t, v, z_stride));
     const lpmm_sample_options& o = *options;
@@ -39,6 +58,21 @@ extern "C" int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int
     a.tokens = tokens;
     a.logprob = logprob;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    LPMM_TRY(check_workspace(workspace, workspace_bytes, lpmm_sample_workspace_bytes(t, v)));
+    const int shares = sample_shares(t, v);
+    if (shares > 1) {
+        const int64_t lines = div_up(v, z_dtype == LPMM_BF16 ? 512 : 256);
+        const int per = int(div_up(lines, shares));
+        const dim3 grid(unsigned(div_up(lines, per)), unsigned(t)), threads(kSampleShareThreads);
+        SampleWork* work = static_cast<SampleWork*>(workspace);
+#define LPMM_SHARE(K) { if (z_dtype == LPMM_BF16) hipLaunchKernelGGL(K<true>, grid, threads, 0, s, a, work, per); \
+                        else hipLaunchKernelGGL(K<false>, grid, threads, 0, s, a, work, per); LPMM_HIP(hipGetLastError()); }
+        LPMM_SHARE(sample_largest_kernel)
+        LPMM_SHARE(sample_bins_kernel)
+        LPMM_SHARE(sample_finish_kernel)
+#undef LPMM_SHARE
+        return LPMM_OK;
+    }
     const dim3 rows{unsigned(t)};
     // Threads of a row: as many as speed up its passes, as few as leave room for other rows (us with 256, 512, 1024: 1 x 1000 12.8, 13.1, 15.4; 1 x 4000 15.4, 13.9, 16.4;
     // 1 x 16000 32, 25, 25; 256 x 32000 66, 46, 42; 300 x 32000 80, 63, 72; 768 x 32000 97, 83, 110; 2048 x 32000 215, 211, 294; 2000 x 16000 105, 111, 185;
@@ -52,3 +86,5 @@ extern "C" int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int
     LPMM_HIP(hipGetLastError());
     return LPMM_OK;
 }
+
+}  // extern "C"

@@ -157,8 +157,10 @@ struct SampleRow {
 
     // f(first index, logits of a piece) for this thread's part of the row, by rising index
     template <typename F>
-    __device__ __forceinline__ void pieces(F&& f) {
-        for (int64_t first = int64_t(threadIdx.x) * E; first < v; first += THREADS * E) {
+    __device__ __forceinline__ void pieces(F&& f) { pieces(0, v, f); }
+    template <typename F>
+    __device__ __forceinline__ void pieces(int from, int to, F&& f) {
+        for (int64_t first = from + int64_t(threadIdx.x) * E; first < to; first += THREADS * E) {
             float x[E];
             elements(piece(int(first)), x);
             f(int(first), x);
@@ -280,8 +282,31 @@ struct SampleRow {
         return i;
     }
 
-    // Sorts the list by falling key, then rising index.
+    // Sorts the list by falling key, then rising index: short ones by counting for each what is in front of it, shared by groups of threads (s.bin is overwritten)
     __device__ __forceinline__ void sort(int count) {
+        if (count <= kSampleFew) {
+            constexpr int PARTS = THREADS / kSampleFew;
+            const int i = threadIdx.x % kSampleFew, part = threadIdx.x / kSampleFew;
+            auto both = [&](int j) { return u64(s.key[j]) << 32 | ~uint32_t(s.index[j]); };
+            const u64 mine = i < count ? both(i) : 0;
+            if (part == 0) s.bin[i] = 0;
+            __syncthreads();
+            if (i < count) {
+                u64 front = 0;
+                for (int j = part; j < count; j += PARTS) front += both(j) > mine;
+                if (front) atomicAdd(&s.bin[i], front);
+            }
+            __syncthreads();
+            if (part == 0 && i < count) s.bin[kSampleFew + s.bin[i]] = mine;
+            __syncthreads();
+            if (part == 0 && i < count) {
+                const u64 x = s.bin[kSampleFew + i];
+                s.key[i] = uint32_t(x >> 32);
+                s.index[i] = int(~uint32_t(x));
+            }
+            __syncthreads();
+            return;
+        }
         int size = 64;
         while (size < count) size *= 2;
         for (int j = count + threadIdx.x; j < size; j += THREADS) {      // behind all: nothing has a lower key and a higher index
@@ -414,7 +439,12 @@ struct SampleRow {
             each([&](int i, float x) { enlist(inside(i, x) && int((high - sample_key(x)) >> shift) == bin, i, x); });
             __syncthreads();
         }
-        const int count = s.count;
+        return end_of_list<WEIGHTS>(s.count, ahead, target);
+    }
+
+    // Where, in the order of the list's logits, the running sum from `ahead` on reaches `target`
+    template <bool WEIGHTS>
+    __device__ __forceinline__ SampleEnd end_of_list(const int count, const u64 ahead, const u64 target) {
         if (count <= kSampleFew) {
             // each logit's predecessors' weights, the comparisons shared by groups of threads
             constexpr int PARTS = THREADS / kSampleFew;
@@ -445,6 +475,7 @@ struct SampleRow {
         for (int j = threadIdx.x; j < count; j += THREADS) s.bin[j] = WEIGHTS ? weight(of_key(s.key[j])) : 1;
         __syncthreads();
         int at;
+        u64 before, want;
         crossing<false>(count, [&](u64) { return target - ahead; }, at, before, want);
         const SampleEnd found{of_key(s.key[at]), s.index[at]};
         __syncthreads();
@@ -452,12 +483,12 @@ struct SampleRow {
     }
     static __device__ __forceinline__ float of_key(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-    // Largest logit with its lowest index, smallest finite one; false if there is a NaN or nothing above -infinity
-    __device__ __forceinline__ bool extremes(int& where, float& least) {
+    // Largest logit with its lowest index, smallest finite one of logits from .. to; false if there is a NaN or nothing above -infinity
+    __device__ __forceinline__ bool extremes(int from, int to, int& where, float& least) {
         float best = -__builtin_inff(), low = __builtin_inff();
         int at = 0x7FFFFFFF;
         bool bad = false;
-        pieces([&](int first, const float x[E]) {
+        pieces(from, to, [&](int first, const float x[E]) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 bad |= x[e] != x[e];
@@ -494,54 +525,77 @@ struct SampleRow {
         return !s.bad && best > -__builtin_inff();
     }
 
+    struct Options {
+        float heat, p, share, u;
+        int k;                               // 0: all
+    };
+    __device__ __forceinline__ Options options(int row) const {
+        Options o{a.temperatures ? a.temperatures[row] : a.temperature, a.top_ps ? a.top_ps[row] : a.top_p, a.min_ps ? a.min_ps[row] : a.min_p, a.u[row],
+                  a.top_ks ? a.top_ks[row] : a.top_k};
+        if (!(o.k > 0 && o.k < v)) o.k = 0;
+        return o;
+    }
+    // top is known
+    __device__ __forceinline__ void measure(const Options& o) {
+        c = fmax(1.4426950408889634 / double(o.heat), 1e-300);           // above 0: infinitely far stays so
+        zero = top == __builtin_inff() ? 1.7976931348623157e308 : double(top);
+    }
+    static __device__ __forceinline__ float reach(float top, float least) { return fmaxf(fminf(top - least, 0x1p100f), 0x1p-100f); }
+    static __device__ __forceinline__ float reach(float top, float least, float heat) { return fmaxf(fminf(reach(top, least), 28.0f * heat), 0x1p-100f); }
+    static __device__ __forceinline__ u64 part_of(float p, u64 all) {
+        const double want = ceil(double(p) * double(all));
+        return want >= 1.0 ? min(u64(want), all) : u64(1);
+    }
+    static __device__ __forceinline__ u64 place_of(float u, u64 all) {
+        const double at = double(u) * double(all);
+        return !(at >= 0.0) ? u64(1) : at < double(all) ? min(u64(at) + 1, all) : all;          // NaN: the first
+    }
+    // The least logit that min_p leaves, for 0 < share < 1
+    __device__ __forceinline__ float least_kept(const Options& o) const {
+        const double border = double(top) + double(o.heat) * log(double(o.share));
+        const float x = float(border);
+        return double(x) < border ? next(x) : x;
+    }
+    __device__ __forceinline__ void say(int row, int token, float logprob) const {
+        a.tokens[row] = token;
+        a.logprob[row] = logprob;
+    }
+    __device__ __forceinline__ void say_drawn(int row, const Options& o, int token, u64 all) const {
+        const float x = z(token);
+        const double one = __longlong_as_double(int64_t(1023 + a.bits) << 52);
+        say(row, token, float((x == top ? 0.0 : (double(x) - double(top)) / double(o.heat)) - log(double(all) / one)));
+    }
+
     __device__ __forceinline__ void draw(int row) {
-        const float heat = a.temperatures ? a.temperatures[row] : a.temperature, p = a.top_ps ? a.top_ps[row] : a.top_p;
-        const float share = a.min_ps ? a.min_ps[row] : a.min_p, u = a.u[row];
-        const int k = a.top_ks ? a.top_ks[row] : a.top_k;
+        const Options o = options(row);
         int first;
         float least;
-        if (!extremes(first, least)) {
-            if (threadIdx.x == 0) { a.tokens[row] = -1; a.logprob[row] = __builtin_nanf(""); }
+        if (!extremes(0, v, first, least)) {
+            if (threadIdx.x == 0) say(row, -1, __builtin_nanf(""));
             return;
         }
-        if (!(heat > 0.0f)) {
-            if (threadIdx.x == 0) { a.tokens[row] = first; a.logprob[row] = 0.0f; }
+        if (!(o.heat > 0.0f)) {
+            if (threadIdx.x == 0) say(row, first, 0.0f);
             return;
         }
-        c = fmax(1.4426950408889634 / double(heat), 1e-300);             // above 0: infinitely far stays so
-        zero = top == __builtin_inff() ? 1.7976931348623157e308 : double(top);
+        measure(o);
         SampleEnd end{-__builtin_inff(), 0x7FFFFFFF};
-        const float span = fmaxf(fminf(top - least, 0x1p100f), 0x1p-100f);
-        const bool some = k > 0 && k < v;
-        if (some) end = last_of<false, true>(end, span, [&](u64 all) { return min(u64(k), all); });
-        if (p < 1.0f) {
-            const float width = fmaxf(fminf(span, 28.0f * heat), 0x1p-100f);
-            auto share_of = [&](u64 all) {
-                const double want = ceil(double(p) * double(all));
-                return want >= 1.0 ? min(u64(want), all) : u64(1);
-            };
-            end = some ? last_of<true, false>(end, width, share_of) : last_of<true, true>(end, width, share_of);
+        if (o.k) end = last_of<false, true>(end, reach(top, least), [&](u64 all) { return min(u64(o.k), all); });
+        if (o.p < 1.0f) {
+            const float width = reach(top, least, o.heat);
+            auto target = [&](u64 all) { return part_of(o.p, all); };
+            end = o.k ? last_of<true, false>(end, width, target) : last_of<true, true>(end, width, target);
         }
-        if (share >= 1.0f) {
-            const SampleEnd e = share > 1.0f ? SampleEnd{top, first} : SampleEnd{top, 0x7FFFFFFF};
+        if (o.share >= 1.0f) {
+            const SampleEnd e = o.share > 1.0f ? SampleEnd{top, first} : SampleEnd{top, 0x7FFFFFFF};
             if (end.keeps(e.z, e.index)) end = e;
-        } else if (share > 0.0f) {
-            const double border = double(top) + double(heat) * log(double(share));
-            float x = float(border);
-            if (double(x) < border) x = next(x);
+        } else if (o.share > 0.0f) {
+            const float x = least_kept(o);
             if (x > end.z) end = SampleEnd{x, 0x7FFFFFFF};
         }
         u64 all;
-        const int i = index_of([&](int at, const float x[E], u64 w[E]) { return weights<false>(end, at, x, w); }, [&](u64 sum) {
-            const double at = double(u) * double(sum);
-            return !(at >= 0.0) ? u64(1) : at < double(sum) ? min(u64(at) + 1, sum) : sum;          // NaN: the first
-        }, all);
-        if (threadIdx.x == 0) {
-            const float x = z(i);
-            const double one = __longlong_as_double(int64_t(1023 + a.bits) << 52);
-            a.tokens[row] = i;
-            a.logprob[row] = float((x == top ? 0.0 : (double(x) - double(top)) / double(heat)) - log(double(all) / one));
-        }
+        const int i = index_of([&](int at, const float x[E], u64 w[E]) { return weights<false>(end, at, x, w); }, [&](u64 sum) { return place_of(o.u, sum); }, all);
+        if (threadIdx.x == 0) say_drawn(row, o, i, all);
     }
 
     static __device__ __forceinline__ float next(float x) {              // the next float up
@@ -552,13 +606,288 @@ struct SampleRow {
 };
 
 // Bound by arithmetic: a logit takes two weights (some 25 instructions in 64 bits each), two bins and an atomic, read four times from L2; with few rows, whose
-// workgroups have a CU each, by the waits between its steps (some 12 us).  2048 x 32000 bf16, top_p 0.98: 211 us, 620 GB/s (512 threads; without top_p 105); 1 x 32000
-// fp32 35 us; 61 x 50257 bf16 with all options 54.  A row kept in LDS was 5 percent faster with one row a CU, and 1.4 times slower with many; in registers it spilled.
+// workgroups have a CU each, by the waits between its steps (some 12 us).  2048 x 32000 bf16, top_p 0.98: 211 us, 620 GB/s (512 threads; without top_p 105).
+// A row kept in LDS was 5 percent faster with one row a CU, and 1.4 times slower with many; in registers it spilled.
 template <bool BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a) {
     __shared__ typename SampleRow<BF16, THREADS>::Shared s;
     SampleRow<BF16, THREADS> row{a, s, int64_t(blockIdx.x) * a.z_stride, a.v, 0.0f, 0.0, 0.0};
     row.draw(blockIdx.x);
+}
+
+// ---- few rows: several workgroups a row -------------------------------------------------------------------------------------------
+//
+// Three launches: the largest logit; the bins, from which the last workgroup of a row to finish finds the one in question; the sums of the lines
+// above it and the list of its logits, from which the last one draws.  With top_k the list is of all logits down to the bin.  Lists that are too long, and min_p of 1
+// and more, are left to the last workgroup as a whole.
+
+constexpr int kSampleShares = 32, kSampleShareThreads = 256;
+
+struct SampleWork {                      // of a row
+    u64 bin[kSampleBins];
+    u64 line[kSampleBins];               // sums of 64 pieces
+    uint32_t key[kSampleList];
+    int index[kSampleList];
+    float top[kSampleShares], low[kSampleShares];       // of each workgroup's part
+    int at[kSampleShares], bad[kSampleShares];
+    u64 before, target;                  // of the bin in question
+    int found;                           // that bin
+    int count;                           // of the list
+    uint32_t tickets[2];                 // workgroups that are done
+};
+
+// What other workgroups have written goes past the L2 of an XCD
+template <typename T>
+__device__ __forceinline__ T far_load(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T>
+__device__ __forceinline__ void far_store(T* p, T v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+template <bool BF16>
+struct SampleShare : SampleRow<BF16, kSampleShareThreads> {
+    typedef SampleRow<BF16, kSampleShareThreads> Row;
+    typedef typename Row::Options Options;
+    using Row::E;
+    using Row::a;
+    using Row::s;
+    using Row::v;
+    using Row::top;
+    static constexpr int T = kSampleShareThreads, LINE = 64 * E;
+    SampleWork& w;
+    int row, part, parts, from, to;      // from: a multiple of LINE
+
+    __device__ __forceinline__ SampleShare(const SampleArgs& args, typename Row::Shared& shared, SampleWork* work, int per)
+        : Row{args, shared, int64_t(blockIdx.y) * args.z_stride, args.v, 0.0f, 0.0, 0.0}, w(work[blockIdx.y]), row(blockIdx.y), part(blockIdx.x), parts(gridDim.x),
+          from(int(blockIdx.x) * per * LINE), to(min(args.v, from + per * LINE)) {}
+
+    __device__ __forceinline__ void largest() {
+        for (int j = part * T + threadIdx.x; j < kSampleBins; j += parts * T) w.bin[j] = 0;
+        int at;
+        float low;
+        Row::extremes(from, to, at, low);
+        if (threadIdx.x == 0) {
+            w.top[part] = top;
+            w.at[part] = at;
+            w.low[part] = low;
+            w.bad[part] = s.bad;
+            if (part == 0) w.count = w.tickets[0] = w.tickets[1] = 0;
+        }
+    }
+    // of the whole row; false: nothing is left to do, workgroup 0 has said so
+    __device__ __forceinline__ bool known(const Options& o, int& first, float& least) {
+        const int g = min(int(threadIdx.x & (kSampleShares - 1)), parts - 1);
+        float best = w.top[g], low = w.low[g];
+        int at = w.at[g], bad = w.bad[g];
+#pragma unroll
+        for (int m = 1; m < kSampleShares; m *= 2) {
+            const float x = __shfl_xor(best, m, 64);
+            const int i = __shfl_xor(at, m, 64);
+            if (x > best || (x == best && i < at)) { best = x; at = i; }
+            low = fminf(low, __shfl_xor(low, m, 64));
+            bad |= __shfl_xor(bad, m, 64);
+        }
+        least = low;
+        top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(best)));
+        first = at;
+        if (bad || top == -__builtin_inff() || !(o.heat > 0.0f)) {
+            if (part == 0 && threadIdx.x == 0) {
+                if (bad || top == -__builtin_inff()) Row::say(row, -1, __builtin_nanf(""));
+                else Row::say(row, first, 0.0f);
+            }
+            return false;
+        }
+        Row::measure(o);
+        return true;
+    }
+    // True in the row's last workgroup, which then sees what the others have written past the L2 caches: every wave waits until its own writes have arrived there.  (A fence
+    // would write back and discard whole caches, once for each wave: 61 x 50257 92 us.)
+    __device__ __forceinline__ bool last_one(int which) {
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __syncthreads();
+        if (threadIdx.x == 0) s.found = __hip_atomic_fetch_add(&w.tickets[which], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == uint32_t(parts - 1);
+        __syncthreads();
+        const bool last = s.found;
+        __syncthreads();
+        return last;
+    }
+    __device__ __forceinline__ float width(const Options& o, float least) const {
+        return o.k ? Row::reach(top, least) : Row::reach(top, least, o.heat);
+    }
+    __device__ __forceinline__ int coarse(float x, float per) const { return int(fminf((top - x) * per, float(kSampleBins - 1))); }
+
+    __device__ __forceinline__ void bins() {
+        const Options o = Row::options(row);
+        int first;
+        float least;
+        if (!known(o, first, least) || (!o.k && !(o.p < 1.0f))) return;
+        const float per = kSampleBins / width(o, least);
+        Row::bins_clear();
+        Row::pieces(from, to, [&](int at, const float x[E]) {
+            // what lies behind the row's end is behind all of top_k's
+#pragma unroll
+            for (int e = 0; e < E; ++e) atomicAdd(&s.bin[coarse(x[e], per)], o.k ? u64(1) : Row::weight(x[e]));
+        });
+        __syncthreads();
+        for (int j = threadIdx.x; j < kSampleBins; j += T)
+            if (s.bin[j]) __hip_atomic_fetch_add(&w.bin[j], s.bin[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (!last_one(0)) return;
+        for (int j = threadIdx.x; j < kSampleBins; j += T) s.bin[j] = far_load(&w.bin[j]);
+        __syncthreads();
+        int bin;
+        u64 before, target;
+        Row::template crossing<true>(kSampleBins, [&](u64 all) { return o.k ? min(u64(o.k), all) : Row::part_of(o.p, all); }, bin, before, target);
+        if (threadIdx.x == 0) {
+            w.found = bin;
+            w.before = before;
+            w.target = target;
+        }
+    }
+
+    __device__ __forceinline__ void finish(u64* s_line) {
+        const Options o = Row::options(row);
+        int first;
+        float least;
+        if (!known(o, first, least)) return;
+        const bool some = o.k || o.p < 1.0f;
+        const float per = kSampleBins / width(o, least), low = o.share > 0.0f && o.share < 1.0f ? Row::least_kept(o) : -__builtin_inff();
+        const int bin = some ? w.found : kSampleBins, lane = threadIdx.x & 63;
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        // a wave a line: the sums of what is above the bin
+        const int l0 = from / LINE + (threadIdx.x >> 6);
+        uint4 next = l0 * LINE + lane * E < to ? Row::piece(l0 * LINE + lane * E) : make_uint4(0, 0, 0, 0);
+        for (int l = l0; l * LINE < to; l += T / 64) {
+            const int at = l * LINE + lane * E, behind = at + T / 64 * LINE;
+            const uint4 now = next;
+            if (behind < to) next = Row::piece(behind);
+            u64 sum = 0;
+            if (at < v) {
+                float x[E];
+                Row::elements(now, x);
+                bool above[E], any = false;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int b = coarse(x[e], per);
+                    above[e] = b < bin && x[e] >= low;
+                    any |= above[e];
+                    if (some) Row::enlist(o.k ? b <= bin && at + e < v : b == bin, at + e, x[e]);
+                }
+                if (!o.k && __any(any)) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const u64 y = Row::weight(x[e]);
+                        sum += above[e] ? y : 0;
+                    }
+                }
+            }
+            sum = wave_sum(sum);
+            if (lane == 0) far_store(&w.line[l], sum);
+        }
+        if (some) {
+            // this workgroup's list behind the others'
+            __syncthreads();
+            const int mine = s.count;
+            if (threadIdx.x == 0 && mine) s.found = __hip_atomic_fetch_add(&w.count, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            const int behind = mine ? s.found : 0;
+            for (int j = threadIdx.x; j < min(mine, kSampleList) && behind + j < kSampleList; j += T) {
+                far_store(&w.key[behind + j], s.key[j]);
+                far_store(&w.index[behind + j], s.index[j]);
+            }
+        }
+        if (!last_one(1)) return;
+        const int count = far_load(&w.count), lines = (v + LINE - 1) / LINE;
+        if (count > kSampleList || o.share >= 1.0f) {
+            Row::draw(row);
+            return;
+        }
+        for (int j = threadIdx.x; j < count; j += T) {
+            s.key[j] = far_load(&w.key[j]);
+            s.index[j] = far_load(&w.index[j]);
+        }
+        __syncthreads();
+        u64 all;
+        if (o.k) {
+            Row::sort(count);
+            int n = min(o.k, count);
+            for (int j = threadIdx.x; j < n; j += T) s.bin[j] = Row::weight(Row::of_key(s.key[j]));
+            __syncthreads();
+            if (o.p < 1.0f) {
+                int at;
+                u64 before, target;
+                Row::template crossing<false>(n, [&](u64 sum) { return Row::part_of(o.p, sum); }, at, before, target);
+                n = at + 1;
+            }
+            // the first of the list stays, and of the others what min_p leaves, by index: behind these what it does not
+            __syncthreads();
+            for (int j = threadIdx.x; j < n; j += T) s.key[j] = j == 0 || Row::of_key(s.key[j]) >= low ? ~uint32_t(s.index[j]) : 0u;
+            __syncthreads();
+            Row::sort(n);
+            for (int j = threadIdx.x; j < n; j += T) s.bin[j] = s.key[j] ? Row::weight(Row::z(s.index[j])) : 0;
+            __syncthreads();
+            int at;
+            u64 before, target;
+            all = Row::template crossing<false>(n, [&](u64 sum) { return Row::place_of(o.u, sum); }, at, before, target);
+            if (threadIdx.x == 0) Row::say_drawn(row, o, s.index[at], all);
+            return;
+        }
+        SampleEnd end{-__builtin_inff(), 0x7FFFFFFF};
+        if (some) end = Row::template end_of_list<true>(count, w.before, w.target);
+        for (int j = threadIdx.x; j < lines; j += T) s_line[j] = far_load(&w.line[j]);
+        __syncthreads();
+        if (some) {
+            // end_of_list may have sorted s.key and s.index, together
+            for (int j = threadIdx.x; j < count; j += T) {
+                const float x = Row::of_key(s.key[j]);
+                if (end.keeps(x, s.index[j]) && x >= low) atomicAdd(&s_line[s.index[j] / LINE], Row::weight(x));
+            }
+            __syncthreads();
+        }
+        if (low > end.z) end = SampleEnd{low, 0x7FFFFFFF};
+        for (int j = threadIdx.x; j < lines; j += T) s.bin[j] = s_line[j];
+        __syncthreads();
+        int line;
+        u64 before, target;
+        all = Row::template crossing<false>(lines, [&](u64 sum) { return Row::place_of(o.u, sum); }, line, before, target);
+        if (threadIdx.x < 64) {
+            const int at = line * LINE + lane * E;
+            u64 y[E], sum = 0;
+            if (at < v) {
+                float x[E];
+                Row::elements(Row::piece(at), x);
+                if (Row::template weights<false>(end, at, x, y)) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sum += y[e];
+                }
+            }
+            u64 ahead = before + wave_scan(sum) - sum;
+            if (ahead < target && ahead + sum >= target) {
+                int found = at;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    ahead += y[e];
+                    if (ahead < target) found = at + e + 1;
+                }
+                Row::say_drawn(row, o, found, all);
+            }
+        }
+    }
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kSampleShareThreads) void sample_largest_kernel(const SampleArgs a, SampleWork* work, int per) {
+    __shared__ typename SampleShare<BF16>::Row::Shared s;
+    SampleShare<BF16>(a, s, work, per).largest();
+}
+template <bool BF16>
+__global__ __launch_bounds__(kSampleShareThreads) void sample_bins_kernel(const SampleArgs a, SampleWork* work, int per) {
+    __shared__ typename SampleShare<BF16>::Row::Shared s;
+    SampleShare<BF16>(a, s, work, per).bins();
+}
+template <bool BF16>
+__global__ __launch_bounds__(kSampleShareThreads) void sample_finish_kernel(const SampleArgs a, SampleWork* work, int per) {
+    __shared__ typename SampleShare<BF16>::Row::Shared s;
+    __shared__ u64 s_line[kSampleBins];
+    SampleShare<BF16>(a, s, work, per).finish(s_line);
 }
 
 }  // namespace lpmm

@@ -148,18 +148,19 @@ def test_no_rows_and_given_outputs():
     assert room[[0, 5]].tolist() == [77, 77] and lp[[0, 5]].tolist() == [7.0, 7.0]
 
 
-def test_on_a_stream_and_captured():
-    """The same bits on another stream and from a captured graph, replayed with other logits and numbers in between"""
-    t, v = 20, 9001
+@pytest.mark.parametrize("t,v", [(20, 9001), (20, 22001)])
+def test_on_a_stream_and_captured(t, v):
+    """The same bits on another stream and from a captured graph, replayed with other logits and numbers in between; a row's one workgroup, and several"""
     z, u = logits(t, v, BF16, 12)
     z, u = z.to(DEV), u.to(DEV)
     sets = [(z.clone(), u.clone()), (z.flip(0).contiguous(), u.flip(0).contiguous()), (z * 0.5, 1 - u)]
     options = dict(temperature=0.9, top_k=500, top_p=0.95, min_p=0.001)
     want = [lpmm.lpmm_sample(a, b, **options) for a, b in sets]
     tokens, logprob = torch.empty(t, dtype=torch.int64, device=DEV), torch.empty(t, device=DEV)
+    room = torch.empty(lpmm.lib().lpmm_sample_workspace_bytes(t, v), dtype=torch.uint8, device=DEV)
     torch.cuda.synchronize()
     s = torch.cuda.Stream()
-    lpmm.lpmm_sample(z, u, **options, tokens=tokens, logprob=logprob, stream=s)
+    lpmm.lpmm_sample(z, u, **options, tokens=tokens, logprob=logprob, workspace=room, stream=s)
     s.synchronize()
     assert torch.equal(tokens, want[0][0]) and torch.equal(logprob, want[0][1])
     graph = torch.cuda.CUDAGraph()
@@ -171,3 +172,59 @@ def test_on_a_stream_and_captured():
         graph.replay()
         assert torch.equal(tokens, want[n][0]) and torch.equal(logprob, want[n][1])
         torch.randn(1000, device=DEV).sum().item()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,v", [(1, 16639), (1, 16640), (3, 20001), (5, 17665), (17, 24013), (64, 32768), (65, 33024), (1, 524288), (1, 524289)])
+def test_few_rows(t, v, dtype):
+    """Rows shared by several workgroups, and sizes next to where that begins and ends; the list's way and the lines' way"""
+    for n, options in enumerate(OPTIONS + [{"top_k": 900, "top_p": 0.9}, {"top_k": 1500}, {"temperature": 3.0, "top_p": 0.6, "min_p": 0.1}]):
+        if t > 60 and n % 3:
+            continue
+        z, u = logits(t, v, dtype, 7 * v + t + n)
+        run(z, u, what=f"{t} x {v} {options}", **options)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_few_rows_of_equal_and_unusual_logits(dtype):
+    v = 20000
+    low = torch.finfo(dtype).min
+    for n, options in enumerate(({}, {"top_k": 4}, {"top_k": 3000}, {"top_p": 0.6}, {"top_k": 700, "top_p": 0.95, "min_p": 0.001}, {"min_p": 0.5, "top_p": 0.7}, {"min_p": 1.0},
+                                 {"min_p": 1.5, "top_p": 0.3}, {"temperature": 0.0}, {"temperature": 0.01, "top_p": 0.9})):
+        z, u = logits(12, v, dtype, 60 + n)
+        z[0] = -INF
+        z[1] = low
+        z[2, 5:] = -INF
+        z[3, :-1] = -INF
+        z[4, 17000] = NAN
+        z[5, 3] = z[5, 19900] = INF
+        z[6, 3], z[6, 9] = INF, -INF
+        z[7] = INF
+        z[8, ::2] = low
+        z[9] = (z[9] * 2).round()
+        z[10] = 0.25
+        z[11] = z[11].round()
+        run(z, u, what=f"{options}", **options)
+
+
+def test_workspaces():
+    """A call on a stream of its own is given one; two calls at once have one each; one that is too small, off its boundary or missing is refused"""
+    z, u = logits(2, 19000, F32, 70)
+    z, u = z.to(DEV), u.to(DEV)
+    need = lpmm.lib().lpmm_sample_workspace_bytes(2, 19000)
+    assert need > 0 and lpmm.lib().lpmm_sample_workspace_bytes(65, 50000) == lpmm.lib().lpmm_sample_workspace_bytes(2, 16895) == 0
+    want = lpmm.lpmm_sample(z, u, top_p=0.9)
+    room = [torch.randint(0, 256, (need,), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    out = [(torch.empty(2, dtype=torch.int64, device=DEV), torch.empty(2, device=DEV)) for _ in range(2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, r, o in zip(streams, room, out):
+            lpmm.lpmm_sample(z, u, top_p=0.9, tokens=o[0], logprob=o[1], workspace=r, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[0], want[0]) and torch.equal(o[1], want[1]) for o in out)
+    for bad in (room[0][:-1], room[0][1:]):
+        with pytest.raises(lpmm.LpmmError):
+            lpmm.lpmm_sample(z, u, workspace=bad)
+    with pytest.raises(ValueError):
+        lpmm.lpmm_sample(z, u, tokens=out[0][0], logprob=out[0][1], stream=streams[0])

@@ -30,16 +30,16 @@ def test_options_for_all_rows(name, value, fine):
     """No rows: nothing is launched."""
     o = B.SampleOptions(1.0, 1.0, 0.0, 0)
     setattr(o, name, value)
-    assert lpmm.lib().lpmm_sample(None, 0, 0, 100, 100, None, ctypes.addressof(o), None, None, None) == (0 if fine else -1)
+    assert lpmm.lib().lpmm_sample(None, 0, 0, 100, 100, None, ctypes.addressof(o), None, None, None, 0, None) == (0 if fine else -1)
 
 
 def test_sampling_sizes():
     o = B.SampleOptions(1.0, 1.0, 0.0, 0)
-    call = lambda t, v, ld, dtype=0: lpmm.lib().lpmm_sample(None, dtype, t, v, ld, None, ctypes.addressof(o), None, None, None)
+    call = lambda t, v, ld, dtype=0: lpmm.lib().lpmm_sample(None, dtype, t, v, ld, None, ctypes.addressof(o), None, None, None, 0, None)
     assert call(0, 1, 1) == 0 and call(0, 2 ** 30, 2 ** 30, 1) == 0
     assert call(-1, 1, 1) == call(0, 0, 1) == call(0, 2 ** 30 + 1, 2 ** 31) == call(0, 10, 9) == call(0, 10, 10, 2) == call(2 ** 24, 1, 1) == -1
     assert call(1, 10, 10) == -1, "null pointers"
-    assert lpmm.lib().lpmm_sample(None, 0, 0, 1, 1, None, None, None, None, None) == -1
+    assert lpmm.lib().lpmm_sample(None, 0, 0, 1, 1, None, None, None, None, None, 0, None) == -1
     o.temperatures = 2
     assert call(0, 1, 1) == -1, "an array off its boundary"
 
