@@ -74,9 +74,9 @@ int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stri
         return LPMM_OK;
     }
     const dim3 rows{unsigned(t)};
-    // Threads of a row: as many as speed up its passes, as few as leave room for other rows (us with 256, 512, 1024: 1 x 1000 12.8, 13.1, 15.4; 1 x 4000 15.4, 13.9, 16.4;
-    // 1 x 16000 32, 25, 25; 256 x 32000 66, 46, 42; 300 x 32000 80, 63, 72; 768 x 32000 97, 83, 110; 2048 x 32000 215, 211, 294; 2000 x 16000 105, 111, 185;
-    // 2000 x 4000 43, 54, 111)
+    // Threads of a row: as many as speed up its passes, as few as leave room for other rows (us with 256, 512, 1024, bf16 with top_p: 1 x 1000 13.5, 14.2, 17.2;
+    // 1 x 16000 26, 22, 22; 256 x 32000 48, 38, 38, with top_k too 72, 50, 45; 256 x 131072 168, 110, 95; 300 x 32000 54, 45, 48; 768 x 32000 69, 66, 77;
+    // 2048 x 32000 150, 147, 184; 2000 x 16000 82, 88, 124; 2000 x 4000 38, 49, 85)
 #define LPMM_SAMPLE(T) { if (z_dtype == LPMM_BF16) hipLaunchKernelGGL((sample_kernel<true, T>), rows, dim3(T), 0, s, a); \
                          else hipLaunchKernelGGL((sample_kernel<false, T>), rows, dim3(T), 0, s, a); }
     if (v <= 2048 || (t > 1024 && v <= 16384)) LPMM_SAMPLE(256)

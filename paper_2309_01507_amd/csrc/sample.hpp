@@ -14,7 +14,7 @@ namespace lpmm {
 
 typedef unsigned long long u64;
 
-constexpr int kSampleBins = 2048, kSampleList = 1024, kSampleFew = 128;
+constexpr int kSampleBins = 2048, kSampleList = 1024, kSampleFew = 128, kSampleLines = kSampleBins / 2;
 
 struct SampleArgs {
     const void* z;
@@ -72,10 +72,10 @@ __device__ __forceinline__ double fma_by(double a, double b, double c) {
     return r;
 }
 
-// 2^bits times 2^y for y <= 0 to a whole number, to some 2^-47 of 1: y = n + f with |f| <= 1/2, the series of 2^f up to the 11th power (what is
-// left is below 7e-15), and the sum with 2^52 rounds to a whole number in its low bits.
-__device__ __forceinline__ u64 sample_weight(double y, int bits) {
-    y = fmin(fmax(y, -100.0), 0.0);
+// 2^bits times 2^y for y <= 0, -infinity included, to a whole number, to some 2^-47 of 1: y = n + f with |f| <= 1/2, the series of 2^f up to the 11th power (what is
+// left is below 7e-15), and the sum with 2^52, which is returned, rounds to a whole number in its low bits.
+__device__ __forceinline__ double sample_rounded(double y, int bits) {
+    y = fmax(y, -100.0);
     const double shifted = y + 0x1.8p52, f = y - (shifted - 0x1.8p52);
     const int n = int(uint32_t(u64(__double_as_longlong(shifted))));
     double p = fma_by(f, 7.0549116208011209e-09, 1.0178086009239699e-07);       // ln(2)^k / k!
@@ -89,12 +89,13 @@ __device__ __forceinline__ u64 sample_weight(double y, int bits) {
     p = fma_by(p, f, 6.9314718055994529e-01);
     p = __builtin_fma(p, f, 1.0);
     const double power = __hiloint2double((1023 + bits + n) << 20, 0);
-    return u64(__double_as_longlong(fma_by(p, power, 0x1p52))) & 0xFFFFFFFFFFFFFull;
+    return fma_by(p, power, 0x1p52);
 }
+__device__ __forceinline__ u64 sample_low_bits(double rounded) { return u64(__double_as_longlong(rounded)) & 0xFFFFFFFFFFFFFull; }
 
 template <bool BF16, int THREADS>
 struct SampleRow {
-    static constexpr int E = BF16 ? 8 : 4, kWaves = THREADS / 64;
+    static constexpr int E = BF16 ? 8 : 4, kWaves = THREADS / 64, LINE = 64 * E;      // a line: what a wave takes at once
     struct Shared {
         u64 bin[kSampleBins];            // also the sums of the row's pieces, and the sorted list's weights
         uint32_t key[kSampleList];
@@ -175,7 +176,8 @@ struct SampleRow {
         });
     }
 
-    __device__ __forceinline__ u64 weight(float x) const { return sample_weight((double(x) - zero) * c, a.bits); }
+    __device__ __forceinline__ double rounded(float x) const { return sample_rounded((double(x) - zero) * c, a.bits); }                   // of a finite x, or -infinity
+    __device__ __forceinline__ u64 weight(float x) const { return sample_low_bits(sample_rounded(fmin((double(x) - zero) * c, 0.0), a.bits)); }
 
     // Sum over the workgroup, and what the threads before this one have (s.wave is free again after the caller's next barrier)
     __device__ __forceinline__ u64 scan(u64 x, u64& before) {
@@ -192,25 +194,26 @@ struct SampleRow {
         return all;
     }
 
-    // The first of s.bin[0 .. count) at which the running sum reaches target_of(the whole sum), which is from 1 to that sum; the sum in front of it.
+    // The first of bin[0 .. count) at which the running sum reaches target_of(the whole sum), which is from 1 to that sum; the sum in front of it.
     // ALL: count is kSampleBins.
     template <bool ALL, typename Target>
-    __device__ __forceinline__ u64 crossing(int count, Target&& target_of, int& at, u64& before, u64& target) {
+    __device__ __forceinline__ u64 crossing(int count, Target&& target_of, int& at, u64& before, u64& target, const u64* bins = nullptr) {
+        const u64* bin = bins ? bins : s.bin;
         constexpr int EACH = kSampleBins / THREADS;
         const int each = ALL ? EACH : (count + THREADS - 1) / THREADS, first = threadIdx.x * each;
         u64 sum = 0;
         if constexpr (ALL) {
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) sum += s.bin[first + j];
+            for (int j = 0; j < EACH; ++j) sum += bin[first + j];
         } else {
-            for (int j = first; j < min(first + each, count); ++j) sum += s.bin[j];
+            for (int j = first; j < min(first + each, count); ++j) sum += bin[j];
         }
         u64 ahead;
         const u64 all = scan(sum, ahead);
         target = target_of(all);
         if (ahead < target && ahead + sum >= target) {
             int j = first;
-            while (ahead + s.bin[j] < target) ahead += s.bin[j++];
+            while (ahead + bin[j] < target) ahead += bin[j++];
             s.found = j;
             s.found_before = ahead;
         }
@@ -225,26 +228,11 @@ struct SampleRow {
     // all of them are 0.
     template <typename Weight, typename Target>
     __device__ __forceinline__ int index_of(Weight&& weights_of, Target&& target_of, u64& all) {
-        constexpr int LINE = 64 * E;
         const int lines = (v + LINE - 1) / LINE, per = (lines + kSampleBins - 1) / kSampleBins, entries = (lines + per - 1) / per;
         const int lane = threadIdx.x & 63;
-        auto line_sum = [&](int l) {
-            u64 sum = 0;
-            const int first = l * LINE + lane * E;
-            if (first < v) {
-                float x[E];
-                elements(piece(first), x);
-                u64 w[E];
-                if (weights_of(first, x, w)) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) sum += w[e];
-                }
-            }
-            return sum;
-        };
         for (int p = threadIdx.x >> 6; p < entries; p += kWaves) {
             u64 sum = 0;
-            for (int l = p * per; l < min(lines, (p + 1) * per); ++l) sum += line_sum(l);
+            for (int l = p * per; l < min(lines, (p + 1) * per); ++l) sum += line_sum(l, weights_of);
             sum = wave_sum(sum);
             if (lane == 0) s.bin[p] = sum;
         }
@@ -252,13 +240,34 @@ struct SampleRow {
         int entry;
         u64 before, target;
         all = crossing<false>(entries, target_of, entry, before, target);
+        return index_in(entry * per, min(lines, (entry + 1) * per), before, target, weights_of);
+    }
+    // this lane's part of a line
+    template <typename Weight>
+    __device__ __forceinline__ u64 line_sum(int l, Weight&& weights_of) {
+        u64 sum = 0;
+        const int first = l * LINE + int(threadIdx.x & 63) * E;
+        if (first < v) {
+            float x[E];
+            elements(piece(first), x);
+            u64 w[E];
+            if (weights_of(first, x, w)) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum += w[e];
+            }
+        }
+        return sum;
+    }
+    // The index at which the running sum, `before` in front of line l0, reaches `target`, which is within the lines to l1
+    template <typename Weight>
+    __device__ __forceinline__ int index_in(int l0, int l1, u64 before, u64 target, Weight&& weights_of) {
         if (threadIdx.x < 64) {
-            for (int l = entry * per; l < min(lines, (entry + 1) * per); ++l) {
-                const u64 sum = line_sum(l), with = wave_scan(sum), line = last_lane(with);
+            for (int l = l0; l < l1; ++l) {
+                const u64 sum = line_sum(l, weights_of), with = wave_scan(sum), line = last_lane(with);
                 if (before + line >= target) {
                     u64 ahead = before + with - sum;
                     if (ahead < target && ahead + sum >= target) {
-                        const int first = l * LINE + lane * E;
+                        const int first = l * LINE + int(threadIdx.x) * E;
                         int found = first;
                         float x[E];
                         elements(piece(first), x);
@@ -282,18 +291,18 @@ struct SampleRow {
         return i;
     }
 
+    __device__ __forceinline__ u64 place(int j) const { return u64(s.key[j]) << 32 | ~uint32_t(s.index[j]); }      // larger: further in front
     // Sorts the list by falling key, then rising index: short ones by counting for each what is in front of it, shared by groups of threads (s.bin is overwritten)
     __device__ __forceinline__ void sort(int count) {
         if (count <= kSampleFew) {
             constexpr int PARTS = THREADS / kSampleFew;
             const int i = threadIdx.x % kSampleFew, part = threadIdx.x / kSampleFew;
-            auto both = [&](int j) { return u64(s.key[j]) << 32 | ~uint32_t(s.index[j]); };
-            const u64 mine = i < count ? both(i) : 0;
+            const u64 mine = i < count ? place(i) : 0;
             if (part == 0) s.bin[i] = 0;
             __syncthreads();
             if (i < count) {
                 u64 front = 0;
-                for (int j = part; j < count; j += PARTS) front += both(j) > mine;
+                for (int j = part; j < count; j += PARTS) front += place(j) > mine;
                 if (front) atomicAdd(&s.bin[i], front);
             }
             __syncthreads();
@@ -449,22 +458,22 @@ struct SampleRow {
             // each logit's predecessors' weights, the comparisons shared by groups of threads
             constexpr int PARTS = THREADS / kSampleFew;
             const int i = threadIdx.x % kSampleFew, part = threadIdx.x / kSampleFew;
-            if (part == 0 && i < count) s.bin[i] = 0;
+            u64* const weight_of = s.bin + kSampleFew;
+            if (part == 0 && i < count) {
+                s.bin[i] = 0;
+                weight_of[i] = WEIGHTS ? weight(of_key(s.key[i])) : 1;
+            }
             __syncthreads();
-            const uint32_t key = i < count ? s.key[i] : 0u;
-            const int index = i < count ? s.index[i] : 0;
+            const u64 mine = i < count ? place(i) : 0;
             if (i < count) {
                 u64 sum = 0;
-                for (int j = part; j < count; j += PARTS) {
-                    const uint32_t other = s.key[j];
-                    if (other > key || (other == key && s.index[j] < index)) sum += WEIGHTS ? weight(of_key(other)) : 1;
-                }
+                for (int j = part; j < count; j += PARTS) sum += place(j) > mine ? weight_of[j] : 0;
                 if (sum) atomicAdd(&s.bin[i], sum);
             }
             __syncthreads();
             if (part == 0 && i < count) {
                 const u64 front = ahead + s.bin[i];
-                if (front < target && front + (WEIGHTS ? weight(of_key(key)) : 1) >= target) s.found = i;
+                if (front < target && front + weight_of[i] >= target) s.found = i;
             }
             __syncthreads();
             const SampleEnd found{of_key(s.key[s.found]), s.index[s.found]};
@@ -483,25 +492,40 @@ struct SampleRow {
     }
     static __device__ __forceinline__ float of_key(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-    // Largest logit with its lowest index, smallest finite one of logits from .. to; false if there is a NaN or nothing above -infinity
+    // Largest logit, with its lowest index if WHERE, and the smallest, with top_k the smallest finite one, of logits from .. to; false if there is a NaN or nothing
+    // above -infinity
+    template <bool WHERE>
     __device__ __forceinline__ bool extremes(int from, int to, int& where, float& least) {
         float best = -__builtin_inff(), low = __builtin_inff();
         int at = 0x7FFFFFFF;
         bool bad = false;
         pieces(from, to, [&](int first, const float x[E]) {
+            if constexpr (WHERE) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                bad |= x[e] != x[e];
-                const bool more = x[e] > best;
-                best = more ? x[e] : best;
-                at = more ? first + e : at;
-                low = fminf(low, x[e] == -__builtin_inff() ? low : x[e]);
+                for (int e = 0; e < E; ++e) {
+                    bad |= x[e] != x[e];
+                    const bool more = x[e] > best;
+                    best = more ? x[e] : best;
+                    at = more ? first + e : at;
+                    low = fminf(low, x[e] == -__builtin_inff() ? low : x[e]);
+                }
+            } else {
+                // a NaN stays
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    best = __builtin_elementwise_maximum(best, x[e]);
+                    low = __builtin_elementwise_minimum(low, x[e]);
+                }
             }
         });
+        if constexpr (!WHERE) {
+            bad = best != best;
+            if (bad) best = low = 0.0f;
+        }
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
             const float x = __shfl_xor(best, m, 64);
-            const int i = __shfl_xor(at, m, 64);
+            const int i = WHERE ? __shfl_xor(at, m, 64) : 0;
             if (x > best || (x == best && i < at)) { best = x; at = i; }
             low = fminf(low, __shfl_xor(low, m, 64));
         }
@@ -566,11 +590,128 @@ struct SampleRow {
         say(row, token, float((x == top ? 0.0 : (double(x) - double(top)) / double(o.heat)) - log(double(all) / one)));
     }
 
+    // Without top_k, and with min_p below 1: the border of the share p is first looked for in 32 bits, which leaves a range of logits, and one pass in 64 bits
+    // gives the whole sum, the sums of what is above that range by lines, and the range's logits as a list.  False: the border is not in the range, or there
+    // are too many logits in it.
+    __device__ __forceinline__ bool draw_once(int row, const Options& o, float least) {
+        const bool some = o.p < 1.0f;
+        const float low = o.share > 0.0f ? least_kept(o) : -__builtin_inff();
+        float sure = low, from = __builtin_inff();                       // kept: what is not below sure (if the border is in the range); the range: from there down to `from`
+        if (some) {
+            const float per = kSampleBins / reach(top, least, o.heat), slope = -float(c);
+            bins_clear();
+            pieces([&](int, const float x[E]) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float below = top - x[e];
+                    atomicAdd(&s.bin[int(fminf(below * per, float(kSampleBins - 1)))], u64(uint32_t(__builtin_amdgcn_exp2f(__builtin_fmaf(below, slope, 31.0f)))));
+                }
+            });
+            __syncthreads();
+            int bin;
+            u64 before, lowest, highest = 0;
+            crossing<true>(kSampleBins, [&](u64 all) {
+                // these sums are off by some 2^-20 of the whole
+                const u64 want = part_of(o.p, all), slack = (all >> 18) + 1;
+                highest = min(want + slack, all);
+                return want > slack ? want - slack : u64(1);
+            }, bin, before, lowest);
+            int last = bin;
+            for (u64 sum = before + s.bin[bin]; sum < highest && last < kSampleBins - 1; sum += s.bin[last]) ++last;
+            // a little more than these bins: a logit of theirs is in the range however the bin's number was rounded
+            const float up = top - float(bin) / per * (1.0f - 0x1p-20f);
+            if (up >= low) {
+                sure = next(up);
+                from = last == kSampleBins - 1 ? -__builtin_inff() : top - float(last + 1) / per * (1.0f + 0x1p-20f);
+            }
+            __syncthreads();
+        }
+        u64* const line = s.bin + kSampleLines;                          // the bins in front are the list's
+        const int lines = (v + LINE - 1) / LINE, per = max(lines > 2 * kWaves ? 2 : 1, (lines + kSampleLines - 1) / kSampleLines), entries = (lines + per - 1) / per;
+        const int lane = threadIdx.x & 63;
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        u64 all = 0, above = 0;
+        for (int p = threadIdx.x >> 6; p < entries; p += kWaves) {
+            u64 sum = 0;
+            for (int l = p * per; l < min(lines, (p + 1) * per); ++l) {
+                const int at = l * LINE + lane * E;
+                float x[E];
+                elements(piece(at), x);
+                if (!some) {
+                    bool any = false;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) any |= x[e] >= sure;
+                    if (!__any(any)) continue;
+                    double upper = 0x1p52;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) upper = __builtin_fma(rounded(x[e]) - 0x1p52, x[e] >= sure ? 1.0 : 0.0, upper);
+                    sum += sample_low_bits(upper);
+                    continue;
+                }
+                double every = 0x1p52, upper = 0x1p52;                   // with E weights below 2^53, and exact
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const bool in = x[e] >= sure;
+                    const double w = rounded(x[e]) - 0x1p52;
+                    every += w;
+                    upper = __builtin_fma(w, in ? 1.0 : 0.0, upper);
+                    enlist(!in && x[e] >= from, at + e, x[e]);
+                }
+                all += sample_low_bits(every);
+                sum += sample_low_bits(upper);
+            }
+            above += sum;
+            sum = wave_sum(sum);
+            if (lane == 0) line[p] = sum;
+        }
+        SampleEnd end{low, 0x7FFFFFFF};
+        if (some) {
+            u64 ahead;
+            all = scan(all, ahead);
+            __syncthreads();
+            above = scan(above, ahead);
+            const u64 target = part_of(o.p, all);
+            const int count = s.count;
+            if (above >= target) {
+                __syncthreads();
+                return false;
+            }
+            if (from < __builtin_inff()) {
+                if (count > kSampleList) {
+                    __syncthreads();
+                    return false;
+                }
+                u64 sum = 0;
+                for (int j = threadIdx.x; j < count; j += THREADS) sum += weight(of_key(s.key[j]));
+                __syncthreads();
+                sum = scan(sum, ahead);
+                __syncthreads();
+                if (above + sum < target) return false;
+                end = end_of_list<true>(count, above, target);
+                for (int j = threadIdx.x; j < count; j += THREADS) {     // the list may have been sorted
+                    const float x = of_key(s.key[j]);
+                    if (end.keeps(x, s.index[j]) && x >= low) atomicAdd(&line[s.index[j] / (LINE * per)], weight(x));
+                }
+                if (low > end.z) end = SampleEnd{low, 0x7FFFFFFF};
+            }
+        }
+        __syncthreads();
+        int entry;
+        u64 before, target;
+        all = crossing<false>(entries, [&](u64 sum) { return place_of(o.u, sum); }, entry, before, target, line);
+        const int i = index_in(entry * per, min(lines, (entry + 1) * per), before, target, [&](int at, const float x[E], u64 w[E]) { return weights<false>(end, at, x, w); });
+        if (threadIdx.x == 0) say_drawn(row, o, i, all);
+        return true;
+    }
+
     __device__ __forceinline__ void draw(int row) {
         const Options o = options(row);
         int first;
         float least;
-        if (!extremes(0, v, first, least)) {
+        // the index is for the least of probabilities from 1 up and the temperature 0; top_k needs the smallest finite logit
+        const bool simple = !o.k && !(o.share >= 1.0f) && o.heat > 0.0f;
+        if (!(simple ? extremes<false>(0, v, first, least) : extremes<true>(0, v, first, least))) {
             if (threadIdx.x == 0) say(row, -1, __builtin_nanf(""));
             return;
         }
@@ -579,6 +720,7 @@ struct SampleRow {
             return;
         }
         measure(o);
+        if (simple && top < __builtin_inff() && draw_once(row, o, least)) return;
         SampleEnd end{-__builtin_inff(), 0x7FFFFFFF};
         if (o.k) end = last_of<false, true>(end, reach(top, least), [&](u64 all) { return min(u64(o.k), all); });
         if (o.p < 1.0f) {
@@ -605,11 +747,13 @@ struct SampleRow {
     }
 };
 
-// Bound by arithmetic: a logit takes two weights (some 25 instructions in 64 bits each), two bins and an atomic, read four times from L2; with few rows, whose
-// workgroups have a CU each, by the waits between its steps (some 12 us).  2048 x 32000 bf16, top_p 0.98: 211 us, 620 GB/s (512 threads; without top_p 105).
-// A row kept in LDS was 5 percent faster with one row a CU, and 1.4 times slower with many; in registers it spilled.
+// Bound by the vector units: of 62 instructions for a logit the weight in 64 bits is 25, the sums and comparisons beside it 8, the search in 32 bits 12 and the largest 3
+// (the rest is by row), 91 percent of the time; the row is read three times, mostly from behind L2.  2048 x 32000 bf16, top_p 0.98: 149 us, 880 GB/s of logits (with two
+// passes in 64 bits, one for the bins of the border and one for the sums, 211); without top_p 93; with top_k 128.  1 x 16000 22 us, by the waits between the steps.  A row
+// kept in LDS was 5 percent faster with one row a CU, and 1.4 times slower with many; in registers it spilled.  512 threads are held to 64 registers, so that four workgroups
+// run on a CU (151 us without).
 template <bool BF16, int THREADS>
-__global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a) {
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 : 1) void sample_kernel(const SampleArgs a) {
     __shared__ typename SampleRow<BF16, THREADS>::Shared s;
     SampleRow<BF16, THREADS> row{a, s, int64_t(blockIdx.x) * a.z_stride, a.v, 0.0f, 0.0, 0.0};
     row.draw(blockIdx.x);
@@ -617,7 +761,8 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a) {
 
 // ---- few rows: several workgroups a row -------------------------------------------------------------------------------------------
 //
-// Three launches: the largest logit; the bins, from which the last workgroup of a row to finish finds the one in question; the sums of the lines
+// Three launches, with the whole row read in each (1 x 32000 fp32 22 us, 1 x 131072 bf16 32, 61 x 50257 bf16 with all options 37: bound by the waits of the last workgroups, of
+// 61 rows 16 us for the bins and 16 for the end): the largest logit; the bins, from which the last workgroup of a row to finish finds the one in question; the sums of the lines
 // above it and the list of its logits, from which the last one draws.  With top_k the list is of all logits down to the bin.  Lists that are too long, and min_p of 1
 // and more, are left to the last workgroup as a whole.
 
@@ -647,11 +792,12 @@ struct SampleShare : SampleRow<BF16, kSampleShareThreads> {
     typedef SampleRow<BF16, kSampleShareThreads> Row;
     typedef typename Row::Options Options;
     using Row::E;
+    using Row::LINE;
     using Row::a;
     using Row::s;
     using Row::v;
     using Row::top;
-    static constexpr int T = kSampleShareThreads, LINE = 64 * E;
+    static constexpr int T = kSampleShareThreads;
     SampleWork& w;
     int row, part, parts, from, to;      // from: a multiple of LINE
 
@@ -663,7 +809,7 @@ struct SampleShare : SampleRow<BF16, kSampleShareThreads> {
         for (int j = part * T + threadIdx.x; j < kSampleBins; j += parts * T) w.bin[j] = 0;
         int at;
         float low;
-        Row::extremes(from, to, at, low);
+        Row::template extremes<true>(from, to, at, low);
         if (threadIdx.x == 0) {
             w.top[part] = top;
             w.at[part] = at;

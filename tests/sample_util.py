@@ -41,16 +41,21 @@ def draw(z, u, temperature, top_k, top_p, min_p):
     return token, d - math.log(sums[-1]), near, float(w.sum())
 
 
-def check(z, u, temperature, top_k, top_p, min_p, tokens, logprob, what):
+def check(z, u, temperature, top_k, top_p, min_p, tokens, logprob, what, unsure=0):
     """Weights, the largest of them 1, are whole numbers of 2^-46 and their sums exact: a border can move by v 2^-47, and by v 2^-53 of the sum for the
-    64-bit sums here; a draw nearer to one than 4 times that may fall on the other side (none of the seeds does).  The logarithm is rounded to fp32 once."""
+    64-bit sums here; a draw nearer to one than 4 times that may fall on the other side: `unsure` rows at most,
+    which are passed over (none, unless a test says so).  The logarithm is rounded to fp32 once."""
     t, v = z.shape
     of = lambda o, r: float(o[r]) if torch.is_tensor(o) else float(np.float32(o))
     tokens, logprob = tokens.cpu(), logprob.cpu().double()
     for r in range(t):
         k = int(top_k[r]) if torch.is_tensor(top_k) else top_k
         token, lp, near, size = draw(z[r], of(u, r), of(temperature, r), k, of(top_p, r), of(min_p, r))
-        assert near > v * (2.0 ** -45 + size * 2.0 ** -51), f"{what}, row {r}: another seed is needed"
+        equal = bool(((z[r] == z[r].max()) | (z[r] == -math.inf)).all())          # weights of 1 and 0: nothing is rounded, and no border moves
+        if not (equal or near > v * (2.0 ** -45 + size * 2.0 ** -51)):
+            assert unsure > 0, f"{what}, row {r}: another seed is needed"
+            unsure -= 1
+            continue
         assert int(tokens[r]) == token, f"{what}, row {r}: token {int(tokens[r])}, not {token}"
         if math.isnan(lp):
             assert math.isnan(float(logprob[r])), f"{what}, row {r}"

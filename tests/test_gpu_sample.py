@@ -18,11 +18,11 @@ def logits(t, v, dtype, seed, spread=2.5):
     return (spread * torch.randn(t, v, generator=g)).to(dtype), torch.rand(t, generator=g)
 
 
-def run(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, what="", on_gpu=None):
+def run(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, what="", on_gpu=None, unsure=0):
     on = lambda o: o.to(DEV) if torch.is_tensor(o) else o
     zd = z.to(DEV) if on_gpu is None else on_gpu
     tokens, logprob = lpmm.lpmm_sample(zd, u.to(DEV), on(temperature), on(top_k), on(top_p), on(min_p))
-    ref.check(z, u, temperature, top_k, top_p, min_p, tokens, logprob, what)
+    ref.check(z, u, temperature, top_k, top_p, min_p, tokens, logprob, what, unsure)
     return tokens, logprob
 
 
@@ -228,3 +228,19 @@ def test_workspaces():
             lpmm.lpmm_sample(z, u, workspace=bad)
     with pytest.raises(ValueError):
         lpmm.lpmm_sample(z, u, tokens=out[0][0], logprob=out[0][1], stream=streams[0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [130, 2500, 9000, 21000])
+def test_borders_of_shares(v, dtype):
+    """The share's border next to the least probability's, in the first and the last range of logits, among equal ones, and logits that sit on the ranges' own borders.  Shares of
+    1 - 2^-20 and more end among weights that are near 2^-46: of 70 rows up to four end too near to one to say which."""
+    for n, spread in enumerate((0.001, 0.3, 3.0, 40.0)):
+        z, u = logits(70, v, dtype, v + n, spread)
+        z[20:40] = (z[20:40] * (512 / 7)).round() * (7 / 512)            # 28 / 2048: the width of a range at temperature 1
+        z[40:60] = (z[40:60] * 2).round() / 2
+        z[60:, ::3] = -INF
+        p = torch.tensor([0.0, 1e-30, 0.01, 0.5, 0.9, 0.999, 1 - 2**-20, 1 - 2**-24, 0.7, 0.95]).repeat(7)
+        least = torch.tensor([0.0, 0.0, 0.001, 0.1, 0.5, 0.9, 0.999]).repeat_interleave(10)
+        run(z, u, 1.0, 0, p, least, what=f"{v} {spread}", unsure=4)
+        run(z, u, torch.linspace(0.05, 4, 70), 0, p, least[torch.arange(70) * 7 % 70], what=f"{v} {spread}, temperatures", unsure=4)
