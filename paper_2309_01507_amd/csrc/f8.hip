@@ -52,13 +52,12 @@ int launch_quant(const void* x, int dtype, int64_t stride, const F8Mat& m, int64
     return LPMM_OK;
 }
 
-// Tiles down the rows go in launches of at most 2^15
 int launch_quant_tile(const void* x, int dtype, int64_t stride, int64_t rows, int64_t cols, int tile, const F8Mat& m, const F8Mat& mt, uint8_t* codes,
                       uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, hipStream_t s) {
-    const int64_t across = div_up(cols, kF8Block), down = div_up(rows, kF8Block);
-    if (down > 65535) return LPMM_EINVAL;
-    const dim3 grid{unsigned(across), unsigned(down)};
-#define LPMM_F8_TILE(B, T) hipLaunchKernelGGL((f8_quant_tile_kernel<B, T>), grid, dim3(256), 0, s, x, stride, int(rows), int(cols), codes, scales, m.bytes, \
+    const int64_t across = div_up(cols, kF8Block), tiles = across * div_up(rows, kF8Block);
+    if (tiles > kMaxBlocks) return LPMM_EINVAL;
+    const dim3 grid{unsigned(tiles)};
+#define LPMM_F8_TILE(B, T) hipLaunchKernelGGL((f8_quant_tile_kernel<B, T>), grid, dim3(256), 0, s, x, stride, int(rows), int(cols), int(across), codes, scales, m.bytes, \
                                               m.scale_bytes, codes_t, scales_t, mt.bytes, mt.scale_bytes)
     if (dtype == LPMM_BF16) { if (tile == 1) LPMM_F8_TILE(true, 1); else LPMM_F8_TILE(true, 128); }
     else { if (tile == 1) LPMM_F8_TILE(false, 1); else LPMM_F8_TILE(false, 128); }
@@ -87,7 +86,7 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool fast) {
     const int64_t large = div_up(tiles(256, 256), 256) * 10, middle = div_up(tiles(128, 128), 512) * (fast ? 6 : 5);
     ProductPlan p{Tile::k64, 1, int(blocks)};
     if (tiles(256, 256) >= 160 && large <= middle) p.tile = Tile::k256;
-    else if (tiles(128, 128) >= 250 && (fast || m <= 128)) p.tile = Tile::k128;       // fp32 leaves the matrix unit waiting in smaller tiles no longer
+    else if (tiles(128, 128) >= 250 && (fast || m <= 128)) p.tile = Tile::k128;       // fp32 gains by these, with few rows alone
     else if (tiles(64, 128) >= 280) p.tile = Tile::k64x128;
     const int64_t small = tiles(64, 64);
     // A block takes a tile of 64 x 64 some 0.28 us (fp32 0.45), the join 2.5 us and 0.2 more for each part: parts pay where most CUs have nothing to do (us without and

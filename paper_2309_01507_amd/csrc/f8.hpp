@@ -91,13 +91,13 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t st
 // columns: the maxima of rows, columns or all go over lanes and LDS, the transposed codes through LDS, 8 rows a piece.
 // TILE: rows of a block, 1 or 128.  codes or codes_t may be null.
 template <bool BF16, int TILE>
-__global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64_t stride, int rows, int cols, uint8_t* codes, uint8_t* scales,
+__global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64_t stride, int rows, int cols, int across, uint8_t* codes, uint8_t* scales,
                                                             int code_bytes, int scale_bytes, uint8_t* codes_t, uint8_t* scales_t, int code_bytes_t,
                                                             int scale_bytes_t) {
     __shared__ uint32_t s_top[4][kF8Block];
     __shared__ uint2 s_codes[kF8Block * 16];                              // [column][8 rows a piece]
     const int p = threadIdx.x & 15, g = threadIdx.x >> 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int block_c = blockIdx.x, block_r = blockIdx.y, r0 = block_r * kF8Block + g * 8, c0 = block_c * kF8Block + p * 8;
+    const int block_r = int(blockIdx.x) / across, block_c = int(blockIdx.x) - block_r * across, r0 = block_r * kF8Block + g * 8, c0 = block_c * kF8Block + p * 8;
     float v[8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64
         }
         if (TILE > 1 && g == 0) {
             if (p == 0) scales[int64_t(block_r) * scale_bytes + block_c] = uint8_t(row_scale[0]);
-            else if (block_c == int(gridDim.x) - 1 && block_c + p < scale_bytes) scales[int64_t(block_r) * scale_bytes + block_c + p] = 0;
+            else if (block_c == across - 1 && block_c + p < scale_bytes) scales[int64_t(block_r) * scale_bytes + block_c + p] = 0;
         }
     }
     if (codes_t) {
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64
         }
         if (TILE > 1 && g == 0) {
             if (p == 0) scales_t[int64_t(block_c) * scale_bytes_t + block_r] = uint8_t(col_scale[0]);
-            else if (block_r == int(gridDim.y) - 1 && block_r + p < scale_bytes_t) scales_t[int64_t(block_c) * scale_bytes_t + block_r + p] = 0;
+            else if ((block_r + 1) * kF8Block >= rows && block_r + p < scale_bytes_t) scales_t[int64_t(block_c) * scale_bytes_t + block_r + p] = 0;
         }
         __syncthreads();
 #pragma unroll

@@ -9,7 +9,8 @@ Orchestration only -- every number is computed by lpmm4.so.
     dW = Q(dy^T) Q(x^T)^T     blocks of 1 x 128 along the tokens
 
 Rounding to 8 bits passes gradients through as they are.  Inputs are float32 or bfloat16, (..., in_features); gradients of gradients are
-not defined.  Weights that stay as they are can be kept in 8 bits alone: lpmm_f8_quant(weight, 128) once, then lpmm_f8_linear.
+not defined.  A step that is captured into a graph calls lpmm_f8_train_forward and lpmm_f8_train_backward themselves: autograd runs the sum into a leaf's .grad on the
+stream that first used the leaf.  Weights that stay as they are can be kept in 8 bits alone: lpmm_f8_quant(weight, 128) once, then lpmm_f8_linear.
 """
 from __future__ import annotations
 
@@ -51,6 +52,8 @@ def f8_linear(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
     """y = x W^T by 8-bit products, with gradients for x (..., in_features) and weight (out_features, in_features); float32 or bfloat16 each."""
     if weight.dim() != 2 or x.shape[-1:] != weight.shape[1:]:
         raise ValueError(f"f8_linear: {tuple(x.shape)} and a weight of {tuple(weight.shape)}")
+    if not torch.is_grad_enabled():
+        x, weight = x.detach(), weight.detach()              # nothing is laid out for gradients
     return _Product.apply(x, weight)
 
 

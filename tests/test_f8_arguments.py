@@ -71,6 +71,33 @@ def test_library_refuses():
     assert L.lpmm_f8_linear_workspace_bytes(0, 5, 130) == L.lpmm_f8_linear_workspace_bytes(100, 0, 130) == L.lpmm_f8_matmul_workspace_bytes(5, 5, 0) == 0
 
 
+def test_library_refuses_training_calls():
+    L = lpmm.lib()
+    t, n, k = 20, 30, 140
+    kept, need = L.lpmm_f8_train_kept_bytes(t, n, k, 3), L.lpmm_f8_train_workspace_bytes(t, n, k)
+    assert L.lpmm_f8_train_kept_bytes(t, n, k, 0) == 0 and 0 < L.lpmm_f8_train_kept_bytes(t, n, k, 1) < kept and 0 < L.lpmm_f8_train_kept_bytes(t, n, k, 2) < kept
+    assert kept >= 256 * 30 + 140 * 128 and need > 0
+    P = 4096
+
+    def forward(x=P, dtype=0, t=t, xs=k, w=P, wd=0, n=n, k=k, ws=k, grads=3, y=P, ys=n, keep=P, keep_bytes=kept, room=P, room_bytes=need):
+        return L.lpmm_f8_train_forward(x, dtype, t, xs, w, wd, n, k, ws, grads, y, ys, keep, keep_bytes, room, room_bytes, None)
+
+    def backward(dy=P, dtype=0, t=t, ds=n, n=n, k=k, grads=3, keep=P, keep_bytes=kept, dx=P, xs=k, dw=P, wd=0, ws=k, room=P, room_bytes=need):
+        return L.lpmm_f8_train_backward(dy, dtype, t, ds, n, k, grads, keep, keep_bytes, dx, xs, dw, wd, ws, room, room_bytes, None)
+
+    big = 2 ** 22 + 1
+    for bad in (dict(t=0), dict(n=0), dict(k=0), dict(t=big), dict(n=big, ys=big), dict(k=big, xs=big, ws=big), dict(grads=4), dict(grads=-1), dict(t=2 ** 22, k=2 ** 22, xs=2 ** 22, ws=2 ** 22),
+                dict(x=None), dict(w=None), dict(y=None), dict(x=P + 2), dict(w=P + 1), dict(dtype=2), dict(wd=3), dict(xs=k - 1), dict(ws=k - 1), dict(ys=n - 1),
+                dict(keep=None), dict(keep=P + 8), dict(room=None), dict(room=P + 8)):
+        assert forward(**bad) == -1, bad
+    for bad in (dict(t=0), dict(n=0), dict(k=0), dict(t=big), dict(grads=4), dict(dy=None), dict(dy=P + 2), dict(dtype=2), dict(ds=n - 1), dict(dx=None), dict(xs=k - 1), dict(dw=None),
+                dict(wd=2), dict(ws=k - 1), dict(keep=None), dict(keep=P + 8), dict(room=None), dict(room=P + 8)):
+        assert backward(**bad) == -1, bad
+    assert forward(keep_bytes=kept - 1) == forward(room_bytes=need - 1) == backward(keep_bytes=kept - 1) == backward(room_bytes=need - 1) == -4
+    assert backward(grads=0, dx=None, dw=None) == 0, "nothing is wanted"
+    assert L.lpmm_f8_train_kept_bytes(0, n, k, 3) == L.lpmm_f8_train_kept_bytes(t, n, k, 4) == L.lpmm_f8_train_workspace_bytes(t, 0, k) == 0
+
+
 def test_a_cast_of_the_layer():
     layer = lpmm.F8Linear(100, 30, device="cpu")
     assert layer.weight.dtype == torch.float32 and layer.bfloat16().weight.dtype == torch.bfloat16

@@ -125,6 +125,31 @@ def test_larger_products(m, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(4100, 2600, 300), (2053, 2100, 515), (100, 32001, 260), (300, 9000, 130)])
+def test_tiles_of_every_size(m, n, k, dtype):
+    """256 x 256, 128 x 128 and 64 x 128, with edges in both directions"""
+    product_of(m, n, k, dtype, (1, 128), m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,n,k", [(1, 16384, 130), (3, 16400, 260), (16, 20001, 515), (2, 70000, 40)])
+def test_few_tokens_and_many_rows(t, n, k, dtype):
+    x, w = matrix(t, k, dtype, t, 0.7), matrix(n, k, F32, n, 0.7)
+    q = lpmm.lpmm_f8_quant(w.to(DEV), 128)
+    ref.check_product(lpmm.lpmm_f8_linear(x.to(DEV), q), ref.quantize(x, 1)[0], ref.unpack(q)[0], f"{t} x {n} x {k}")
+
+
+def test_many_blocks_down():
+    """More than 65535 blocks below each other"""
+    rows = 128 * 65536 + 5
+    x = torch.ones(rows, 3, dtype=BF16, device=DEV)
+    x[-5:] = 3 * 2.0 ** 20
+    q = lpmm.lpmm_f8_quant(x, 128)
+    assert torch.equal(lpmm.lpmm_f8_dequant(q, BF16), x)
+    assert bool((q.scales[:-1, 0] == q.scales[0, 0]).all()) and int(q.scales[-1, 0]) == ref.scale_of(x[-5:].double().cpu())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("t", [1, 2, 7, 16, 17, 31, 64, 100, 200])
 def test_linear(t, dtype):
     for n, k in ((1, 1), (15, 127), (100, 200), (333, 1000), (77, 4100)):
@@ -281,6 +306,100 @@ def test_layer_and_gradients(t, dtype, w_dtype):
     dw1, = torch.autograd.grad(layer(x.to(DEV)), layer.weight, dy.to(DEV))
     ref.check_product(dx1, val(dy), qw.t().contiguous(), "dx alone")
     assert torch.equal(dw1, dw)
+
+
+@pytest.mark.parametrize("dtype,w_dtype", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)])
+@pytest.mark.parametrize("t,n,k", [(1, 1, 1), (130, 257, 100), (20, 40, 515)])
+def test_training_calls(t, n, k, dtype, w_dtype):
+    """Tensors with gaps and off their boundaries, each choice of gradients, and the second call repeated"""
+    x, w, dy = matrix(t, k, dtype, 1, 0.6), matrix(n, k, w_dtype, 2, 0.6), matrix(t, n, dtype, 3, 0.6)
+    rooms = []
+
+    def apart(rows, cols, dtype, value=None):
+        room = torch.full((rows, cols + 5), 77.0, dtype=dtype, device=DEV)
+        rooms.append((room, cols))
+        if value is not None:
+            room[:, 1:1 + cols] = value.to(DEV)
+        return room[:, 1:1 + cols]
+
+    val = lambda m, tile=1: ref.quantize(m, tile)[0]
+    qw = val(w, 128)
+    xs, ws, dys = apart(t, k, dtype, x), apart(n, k, w_dtype, w), apart(t, n, dtype, dy)
+    first = None
+    for grads in (lpmm.F8_DX | lpmm.F8_DW, lpmm.F8_DX, lpmm.F8_DW):
+        y, kept = lpmm.lpmm_f8_train_forward(xs, ws, grads, apart(t, n, dtype))
+        ref.check_product(y, val(x), qw, "y")
+        copy = kept.clone()
+        dx, dw = lpmm.lpmm_f8_train_backward(dys, kept, k, w_dtype, grads, apart(t, k, dtype) if grads & lpmm.F8_DX else None, apart(n, k, w_dtype) if grads & lpmm.F8_DW else None)
+        again = lpmm.lpmm_f8_train_backward(dys, kept, k, w_dtype, grads)
+        assert torch.equal(kept, copy)
+        if grads & lpmm.F8_DX:
+            ref.check_product(dx, val(dy), qw.t().contiguous(), "dx")
+            assert torch.equal(dx, again[0])
+        else:
+            assert dx is again[0] is None
+        if grads & lpmm.F8_DW:
+            ref.check_product(dw, val(dy.t()), val(x.t()), "dW")
+            assert torch.equal(dw, again[1]) and dw.dtype == w_dtype
+        else:
+            assert dw is again[1] is None
+        first = first or (y, dx, dw)
+        assert torch.equal(y, first[0]) and (dx is None or torch.equal(dx, first[1])) and (dw is None or torch.equal(dw, first[2]))
+    y, kept = lpmm.lpmm_f8_train_forward(xs, ws, 0)
+    assert kept is None and torch.equal(y, first[0]) and lpmm.lpmm_f8_train_backward(dys, kept, k, grads=0) == (None, None)
+    for room, cols in rooms:
+        assert bool((room[:, 0] == 77).all()) and bool((room[:, 1 + cols:] == 77).all()), "around the rows"
+
+
+def test_training_calls_captured():
+    """On another stream with its own memory, and captured and replayed with other values between"""
+    t, n, k = 70, 130, 200
+    sets = [(matrix(t, k, BF16, s).to(DEV), matrix(n, k, F32, s + 9).to(DEV), matrix(t, n, BF16, s + 5).to(DEV)) for s in (1, 2, 3)]
+
+    def step(x, w, dy, stream=None, y=None, kept=None, dx=None, dw=None, room=None):
+        y, kept = lpmm.lpmm_f8_train_forward(x, w, y=y, kept=kept, workspace=room, stream=stream)
+        return (y, *lpmm.lpmm_f8_train_backward(dy, kept, k, dx=dx, dw=dw, workspace=room, stream=stream))
+
+    want = [step(*s) for s in sets]
+    L = lpmm.lib()
+    kept = torch.empty(L.lpmm_f8_train_kept_bytes(t, n, k, 3), dtype=torch.uint8, device=DEV)
+    room = torch.empty(L.lpmm_f8_train_workspace_bytes(t, n, k), dtype=torch.uint8, device=DEV)
+    outs = [torch.empty_like(o) for o in want[0]]
+    x, w, dy = (v.clone() for v in sets[0])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    step(x, w, dy, s, outs[0], kept, outs[1], outs[2], room)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want[0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, w, dy)
+    for i in (0, 1, 2, 1, 0):
+        for to, v in zip((x, w, dy), sets[i]):
+            to.copy_(v)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[i]))
+        torch.randn(1000, device=DEV).sum().item()
+    with pytest.raises(ValueError):
+        lpmm.lpmm_f8_train_forward(x, w, stream=s)               # memory of the current stream for another
+    with pytest.raises(lpmm.LpmmError):
+        lpmm.lpmm_f8_train_forward(x, w, kept=kept[:-1])
+    with pytest.raises(lpmm.LpmmError):
+        lpmm.lpmm_f8_train_backward(dy, kept, k, workspace=room[8:])
+    with pytest.raises(ValueError):
+        lpmm.lpmm_f8_train_backward(dy, kept.cpu(), k)
+
+
+def test_layer_without_gradients():
+    """No gradients wanted: nothing is kept, and the product is as close"""
+    layer = lpmm.F8Linear(300, 70)
+    x = matrix(50, 300, BF16, 1).to(DEV).requires_grad_()
+    val = ref.quantize(x.detach().cpu(), 1)[0], ref.quantize(layer.weight.detach().cpu(), 128)[0]
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            y = layer(x)
+        assert y.grad_fn is None and not y.requires_grad
+        ref.check_product(y, *val, str(mode))
 
 
 def test_gradients_against_differences():
