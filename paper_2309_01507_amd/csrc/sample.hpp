@@ -598,7 +598,7 @@ struct SampleRow {
         const float low = o.share > 0.0f ? least_kept(o) : -__builtin_inff();
         float sure = low, from = __builtin_inff();                       // kept: what is not below sure (if the border is in the range); the range: from there down to `from`
         if (some) {
-            const float per = kSampleBins / reach(top, least, o.heat), slope = -float(c);
+            const float per = kSampleBins / reach(top, least, o.heat), slope = -fminf(float(c), 0x1.FFFFFEp127f);      // finite: the largest's weight is 1
             bins_clear();
             pieces([&](int, const float x[E]) {
 #pragma unroll

@@ -244,3 +244,18 @@ def test_borders_of_shares(v, dtype):
         least = torch.tensor([0.0, 0.0, 0.001, 0.1, 0.5, 0.9, 0.999]).repeat_interleave(10)
         run(z, u, 1.0, 0, p, least, what=f"{v} {spread}", unsure=4)
         run(z, u, torch.linspace(0.05, 4, 70), 0, p, least[torch.arange(70) * 7 % 70], what=f"{v} {spread}, temperatures", unsure=4)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,v", [(6, 3000), (6, 20000)])
+def test_extreme_temperatures(t, v, dtype):
+    """Where 1 / temperature, differences or their products leave fp32's range; logits at its ends"""
+    for n, heat in enumerate((2.0**-149, 2.0**-126, 1e-30, 1e30, 3e38, INF)):
+        z, u = logits(t, v, dtype, 500 + n)
+        z[1] = z[1] * 1e-38
+        z[2] = torch.where(z[2] > 0, z[2] * 1e37, z[2])
+        z[3, 5], z[3, 9] = torch.finfo(dtype).max, torch.finfo(dtype).min
+        z[4, ::2] = -INF
+        z[5, 7] = z[5, 70] = INF
+        for options in ({}, {"top_p": 0.7}, {"top_p": 0.9, "min_p": 0.3}, {"top_k": 50, "top_p": 0.9}):
+            run(z, u, temperature=heat, what=f"{heat} {options}", **options)
