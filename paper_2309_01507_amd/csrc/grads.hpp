@@ -33,46 +33,55 @@ struct GradPlan {
     int32_t log_bytes;                   // of a chunk
 };
 
-// The 16-byte pieces of a chunk, counted from the boundary at or before the tensor's start
+// The 16-byte pieces of a chunk, counted from the boundary at or before the tensor's start: those from `in0` to `in1` lie within the tensor, and there may be one in front
+// of them and one behind that lie there in part.
 struct GradSpan {
     const char* base;                    // that boundary
-    int64_t piece0, piece1;
+    int64_t piece0, in0, in1, piece1;
     int64_t lead;                        // elements between the boundary and the tensor's start
 };
 template <bool BF16>
 __device__ __forceinline__ GradSpan grad_span(const GradTensor& t, int number, int log_bytes) {
-    constexpr int E = BF16 ? 2 : 4;
+    constexpr int N = BF16 ? 8 : 4, E = BF16 ? 2 : 4;
     GradSpan s;
     const uintptr_t at = reinterpret_cast<uintptr_t>(t.grad);
     s.base = reinterpret_cast<const char*>(at & ~uintptr_t(15));
     s.lead = int64_t(at & 15) / E;
-    const int64_t pieces = ((s.lead + t.numel) * E + 15) >> 4;
+    const int64_t end = s.lead + t.numel;
     s.piece0 = int64_t(number) << (log_bytes - 4);
-    s.piece1 = min(pieces, s.piece0 + (int64_t(1) << (log_bytes - 4)));
+    s.piece1 = min((end + N - 1) / N, s.piece0 + (int64_t(1) << (log_bytes - 4)));
+    s.in1 = min(end / N, s.piece1);
+    s.in0 = s.piece0 + (s.piece0 == 0 && s.lead > 0);
+    if (s.in1 < s.in0) s.in0 = s.in1 = min(s.in0, s.piece1);             // a piece or two, none of them within
     return s;
 }
 
-// Floats of a 16-byte piece; `i0`: the tensor's element that its first one is (negative in front of the tensor).  What lies outside is
-// 0 and not read.
+// whole(piece, its 16 bytes), kGradAhead pieces of a thread on their way at once; edge(piece) for those that are not within
+constexpr int kGradAhead = 4;
+template <typename Whole, typename Edge>
+__device__ __forceinline__ void grad_pieces(const GradSpan& s, Whole&& whole, Edge&& edge) {
+    for (int64_t p = s.in0 + threadIdx.x; p < s.in1; p += kGradAhead * kGradThreads) {
+        uint4 q[kGradAhead];
+#pragma unroll
+        for (int j = 0; j < kGradAhead; ++j) q[j] = *reinterpret_cast<const uint4*>(s.base + (min(p + j * kGradThreads, s.in1 - 1) << 4));
+#pragma unroll
+        for (int j = 0; j < kGradAhead; ++j)
+            if (p + j * kGradThreads < s.in1) whole(p + j * kGradThreads, q[j]);
+    }
+    if (threadIdx.x == 0 && s.piece0 < s.in0) edge(s.piece0);
+    if (threadIdx.x == 64 && s.in1 < s.piece1) edge(s.in1);
+}
 template <bool BF16>
-__device__ __forceinline__ void grad_piece(const char* base, int64_t piece, int64_t i0, int64_t numel, float x[8]) {
-    constexpr int N = BF16 ? 8 : 4;
-    const char* at = base + (piece << 4);
-    if (i0 >= 0 && i0 + N <= numel) {
-        const uint4 q = *reinterpret_cast<const uint4*>(at);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+__device__ __forceinline__ void grad_floats(const uint4& q, float x[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (BF16) {
-                x[2 * e] = __uint_as_float(w[e] << 16);
-                x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-            } else {
-                x[e] = __uint_as_float(w[e]);
-            }
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (BF16) {
+            x[2 * e] = __uint_as_float(w[e] << 16);
+            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        } else {
+            x[e] = __uint_as_float(w[e]);
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = i0 + e >= 0 && i0 + e < numel ? w4_load1<BF16>(at, e) : 0.0f;
     }
 }
 
@@ -90,12 +99,16 @@ template <bool BF16, bool MOST>
 __device__ __forceinline__ void grad_chunk(const GradTensor& t, int number, int log_bytes, double& sum, uint32_t& most) {
     constexpr int N = BF16 ? 8 : 4;
     const GradSpan s = grad_span<BF16>(t, number, log_bytes);
-    for (int64_t p = s.piece0 + threadIdx.x; p < s.piece1; p += kGradThreads) {
+    grad_pieces(s, [&](int64_t, const uint4& q) {
         float x[8];
-        grad_piece<BF16>(s.base, p, p * N - s.lead, t.numel, x);
+        grad_floats<BF16>(q, x);
 #pragma unroll
         for (int e = 0; e < N; ++e) grad_take<MOST>(sum, most, x[e]);
-    }
+    }, [&](int64_t p) {
+        const int64_t i0 = p * N - s.lead;
+        for (int e = 0; e < N; ++e)
+            if (i0 + e >= 0 && i0 + e < t.numel) grad_take<MOST>(sum, most, w4_load1<BF16>(t.grad, i0 + e));
+    });
 }
 
 // Value of the lane `mask` away
@@ -118,8 +131,8 @@ __device__ __forceinline__ double grad_join(double x, double* lds) {
     return x;
 }
 
-// The last workgroup to finish joins what all have found, in the order of their numbers: equal inputs give equal bits.  The parts go
-// past the L2 caches of the XCDs (agent scope), the ticket orders them.
+// The last workgroup to finish joins what all have found, in the order of their numbers: equal inputs give equal bits.  Parts and ticket go
+// past the L2 caches of the XCDs (agent scope), and a workgroup waits for its part to arrive before it takes its ticket: a release would write back an L2 for each workgroup.
 template <bool MOST>
 __global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(GradPlan plan, float* norm) {
     __shared__ double s_join[kGradThreads / 64];
@@ -136,7 +149,9 @@ __global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(GradPlan plan, 
     const double mine = grad_join<MOST>(MOST ? double(most) : sum, s_join);
     if (threadIdx.x == 0) {
         __hip_atomic_store(&plan.head->parts[blockIdx.x], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = __hip_atomic_fetch_add(&plan.head->ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");           // for the compiler's order
+        __builtin_amdgcn_s_waitcnt(0x0070);                              // the part has arrived behind L2
+        s_last = __hip_atomic_fetch_add(&plan.head->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     }
     __syncthreads();
     if (!s_last) return;
@@ -156,29 +171,26 @@ template <bool BF16>
 __device__ __forceinline__ void grad_scale_chunk(const GradTensor& t, int number, int log_bytes, float part) {
     constexpr int N = BF16 ? 8 : 4, E = BF16 ? 2 : 4;
     const GradSpan s = grad_span<BF16>(t, number, log_bytes);
-    for (int64_t p = s.piece0 + threadIdx.x; p < s.piece1; p += kGradThreads) {
-        const int64_t i0 = p * N - s.lead;
+    grad_pieces(s, [&](int64_t p, const uint4& q) {
         float x[8];
-        grad_piece<BF16>(s.base, p, i0, t.numel, x);
-        char* out = static_cast<char*>(t.out) + i0 * E;
-        if (i0 >= 0 && i0 + N <= t.numel) {
-            if constexpr (BF16) {
-                Vec16 v;
+        grad_floats<BF16>(q, x);
+        char* out = static_cast<char*>(t.out) + (p * N - s.lead) * E;
+        if constexpr (BF16) {
+            Vec16 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v.v[e] = uint32_t(to_bf16(x[2 * e] * part)) | uint32_t(to_bf16(x[2 * e + 1] * part)) << 16;
-                *reinterpret_cast<Vec16*>(out) = v;
-            } else {
-                Vec16f v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v.v[e] = x[e] * part;
-                *reinterpret_cast<Vec16f*>(out) = v;
-            }
+            for (int e = 0; e < 4; ++e) v.v[e] = uint32_t(to_bf16(x[2 * e] * part)) | uint32_t(to_bf16(x[2 * e + 1] * part)) << 16;
+            *reinterpret_cast<Vec16*>(out) = v;
         } else {
+            Vec16f v;
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (i0 + e >= 0 && i0 + e < t.numel) w4_store1<BF16>(out, e, x[e] * part);
+            for (int e = 0; e < 4; ++e) v.v[e] = x[e] * part;
+            *reinterpret_cast<Vec16f*>(out) = v;
         }
-    }
+    }, [&](int64_t p) {
+        const int64_t i0 = p * N - s.lead;
+        for (int e = 0; e < N; ++e)
+            if (i0 + e >= 0 && i0 + e < t.numel) w4_store1<BF16>(t.out, i0 + e, w4_load1<BF16>(t.grad, i0 + e) * part);
+    });
 }
 
 // Chunks from the last to the first: what the norm has read last is still in the cache.
