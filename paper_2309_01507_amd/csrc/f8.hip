@@ -311,7 +311,7 @@ int lpmm_f8_train_backward(const void* dy, int dtype, int64_t t, int64_t dy_stri
     if (!want_x && !want_w) return LPMM_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* at = static_cast<char*>(workspace);
-    const F8Mat q = carve(at, t, n, 1), qt = want_w ? carve(at, n, t, 1) : F8Mat{};
+    const F8Mat q = want_x ? carve(at, t, n, 1) : F8Mat{}, qt = want_w ? carve(at, n, t, 1) : F8Mat{};
     char* keep = static_cast<char*>(const_cast<void*>(kept));
     const F8Mat qwt = want_x ? carve(keep, k, n, 128) : F8Mat{}, qxt = want_w ? carve(keep, k, t, 1) : F8Mat{};
     LPMM_TRY(quant_into(dy, dtype, dy_stride, t, n, 1, q, qt, s));

