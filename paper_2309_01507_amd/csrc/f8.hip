@@ -89,11 +89,12 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t blocks, bool fast) {
     else if (tiles(128, 128) >= 250 && (fast || m <= 128)) p.tile = Tile::k128;       // fp32 gains by these, with few rows alone
     else if (tiles(64, 128) >= 280) p.tile = Tile::k64x128;
     const int64_t small = tiles(64, 64);
-    // A block takes a tile of 64 x 64 some 0.28 us (fp32 0.45), the join 2.5 us and 0.2 more for each part: parts pay where most CUs have nothing to do (us without and
-    // with 4: 16 x 4096 x 4096 12, 9.6; 128 x 4096 x 4096 13.0, 13.9; 300 x 300 x 16000 with 8 17.6)
+    // A block takes a tile of 64 x 64 some 0.28 us (fp32 0.45), the join 2.5 us and 0.2 more for each part: parts pay where CUs have less than two workgroups, and two parts
+    // for long sums where they have no more than two (us without parts and with, bf16: 17 x 8192 x 4096 20.3, 13.5; 17 x 8192 x 8192 35, 18; 17 x 11008 x 4096 20.9, 16.6; 64 x
+    // 16384 x 4096 23.0, 20.9; 128 x 4096 x 11008 47, 24; 200 x 4096 x 4096 20.7, 21.2; 333 x 4096 x 11008 50, 39; with three where two are taken 128 x 4096 x 4096 17.8, 19.7)
     const double whole = double(blocks) * (fast ? 0.28 : 0.45);
-    if (p.tile == Tile::k64 && small <= 96 && whole >= 6.0) {
-        const int64_t want = std::min<int64_t>(512 / small, int64_t(std::sqrt(whole / 0.2)));
+    if (p.tile == Tile::k64 && small <= 512 && whole >= 6.0) {
+        const int64_t want = std::min<int64_t>(std::max<int64_t>(512 / small, whole >= 20.0 ? 2 : 1), int64_t(std::sqrt(whole / 0.2)));
         p.per = int(div_up(blocks, std::max<int64_t>(1, want)));
         p.splits = int(div_up(blocks, p.per));
     }
@@ -120,7 +121,7 @@ int launch_product(const F8Mat& a, const F8Mat& b, void* c, int dtype, int64_t s
 #undef LPMM_TILE
     LPMM_HIP(hipGetLastError());
     if (parts) {
-        const dim3 groups{unsigned(div_up(int64_t(a.rows) * b.rows, 256))};        // at most 96 tiles of 64 x 64
+        const dim3 groups{unsigned(div_up(int64_t(a.rows) * b.rows, 256))};        // at most 512 tiles of 64 x 64
         if (fast) hipLaunchKernelGGL(f8_join_kernel<true>, groups, dim3(256), 0, s, parts, p.splits, a.rows, b.rows, c, stride);
         else hipLaunchKernelGGL(f8_join_kernel<false>, groups, dim3(256), 0, s, parts, p.splits, a.rows, b.rows, c, stride);
         LPMM_HIP(hipGetLastError());

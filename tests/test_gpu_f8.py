@@ -132,6 +132,12 @@ def test_tiles_of_every_size(m, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(17, 8100, 4100), (200, 2100, 8300), (330, 4100, 9300), (512, 4096, 9250)])
+def test_sums_in_parts(m, n, k, dtype):
+    product_of(m, n, k, dtype, (1, 128), m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("t,n,k", [(1, 16384, 130), (3, 16400, 260), (16, 20001, 515), (2, 70000, 40)])
 def test_few_tokens_and_many_rows(t, n, k, dtype):
     x, w = matrix(t, k, dtype, t, 0.7), matrix(n, k, F32, n, 0.7)
