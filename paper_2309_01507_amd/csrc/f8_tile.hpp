@@ -249,8 +249,9 @@ constexpr int kF8FewTokens = 16, kF8FewBytes = 65536;          // codes of x tha
 // as long as there are any.  Codes of W come from memory into the registers that are the operand, AHEAD blocks in front of their use; the first
 // are on their way while the workgroup brings x to 8 bits.  The waves' sums of a row meet in LDS.
 //
-// Bound by reading W: one token through 32000 x 4096 bf16 22 us, 6.0 TB/s, through 11008 x 4096 10.3 us, 4.4, through 4096 x 4096 5.3 us, 3.2 (one round trip to memory, x and the
-// join).  Every workgroup brings the same x to 8 bits, which a kernel in front would do once, for a launch (so it began: 1 x 4096 x 4096 9.9 us).
+// Bound by reading W: one token through 32000 x 4096 bf16 22 us, 6.0 TB/s, through 11008 x 4096 9.6 us, 4.7, through 4096 x 4096 5.3 us, 3.2 (one round trip to memory, x and the
+// join).  Every workgroup brings the same x to 8 bits, which a kernel in front would do once, for a launch (so it began: 1 x 4096 x 4096 9.9 us);
+// each token more costs 0.4 us of conversions.  Loads of four units at once took as long.
 template <bool BF16, int WK, int WN, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const void* x, int t, int k, int64_t x_stride, void* y, int64_t y_stride) {
     constexpr int THREADS = 64 * WK * WN, ROWS = WN * NT * 16, PART = NT * 4 * 64;
@@ -284,8 +285,15 @@ __global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const voi
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) load(i);
     }
-    for (int unit = threadIdx.x >> 4; unit < t * blocks; unit += THREADS / 16) {       // 16 lanes a block of a token
-        const int block = unit / t, token = unit - block * t, d = threadIdx.x & 15, at = block * kF8Block + d * 8;
+    constexpr int AT_ONCE = THREADS / 16;                                 // 16 lanes a block of a token
+    const int more_blocks = AT_ONCE / t, more_tokens = AT_ONCE - more_blocks * t;
+    int block = int(threadIdx.x >> 4) / t, token = int(threadIdx.x >> 4) - block * t;
+    for (; block < blocks; block += more_blocks, token += more_tokens) {
+        if (token >= t) {
+            token -= t;
+            if (++block >= blocks) break;
+        }
+        const int d = threadIdx.x & 15, at = block * kF8Block + d * 8;
         const int64_t row = int64_t(token) * x_stride;
         float v[8];
         w4_load8<BF16>(x, row + at, row + k, v);
@@ -298,7 +306,7 @@ __global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const voi
         c.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
         c.y = f8_codes4(v[4], v[5], v[6], v[7], inverse);
         reinterpret_cast<uint2*>(s_x + block * t * 8)[lds_piece<3>(token, d >> 1) * 2 + (d & 1)] = c;
-        if (d == 0) s_scale[unit] = uint8_t(scale);
+        if (d == 0) s_scale[block * t + token] = uint8_t(scale);
     }
     __syncthreads();
     int parity = 0;
