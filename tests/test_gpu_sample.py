@@ -259,3 +259,44 @@ def test_extreme_temperatures(t, v, dtype):
         z[5, 7] = z[5, 70] = INF
         for options in ({}, {"top_p": 0.7}, {"top_p": 0.9, "min_p": 0.3}, {"top_k": 50, "top_p": 0.9}):
             run(z, u, temperature=heat, what=f"{heat} {options}", **options)
+
+
+@pytest.mark.parametrize("t,v", [(3, 900), (2, 20000)])
+def test_rows_far_apart(t, v):
+    """Rows that begin beyond 2^32 bytes"""
+    z, u = logits(t, v, BF16, 80 + v)
+    room = torch.empty(2**31 + v, dtype=BF16, device=DEV)
+    far = room.as_strided((t, v), (2**31 // (t - 1), 1))
+    far.copy_(z)
+    for options in ({"top_p": 0.9}, {"top_k": 20, "min_p": 0.01}):
+        run(z, u, what=f"{v} {options}", on_gpu=far, **options)
+
+
+def test_many_rows():
+    """More rows than a launch's second dimension could hold, each like that of a small call"""
+    z, u = logits(7, 33, F32, 90)
+    want = run(z, u, top_p=0.8, what="small")
+    many = 10001
+    tokens, logprob = lpmm.lpmm_sample(z.to(DEV).repeat(many, 1), u.to(DEV).repeat(many), top_p=0.8)
+    assert torch.equal(tokens, want[0].repeat(many)) and torch.equal(logprob, want[1].repeat(many))
+
+
+def test_one_workspace_for_two_graphs():
+    """Replayed one after the other, as calls on one stream"""
+    sets = [logits(3, 18000, F32, 91), logits(5, 30001, BF16, 92)]
+    sets = [(z.to(DEV), u.to(DEV)) for z, u in sets]
+    want = [lpmm.lpmm_sample(z, u, top_k=30, top_p=0.9) for z, u in sets]
+    room = torch.empty(max(lpmm.lib().lpmm_sample_workspace_bytes(*z.shape) for z, _ in sets), dtype=torch.uint8, device=DEV)
+    outs = [(torch.empty(z.shape[0], dtype=torch.int64, device=DEV), torch.empty(z.shape[0], device=DEV)) for z, _ in sets]
+    graphs = []
+    for (z, u), o in zip(sets, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            lpmm.lpmm_sample(z, u, top_k=30, top_p=0.9, tokens=o[0], logprob=o[1], workspace=room)
+    for _ in range(3):
+        for g, o in zip(graphs, outs):
+            o[0].zero_()
+            g.replay()
+        room.fill_(255)
+        for o, w in zip(outs, want):
+            assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
