@@ -492,9 +492,9 @@ struct SampleRow {
     }
     static __device__ __forceinline__ float of_key(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-    // Largest logit, with its lowest index if WHERE, and the smallest, with top_k the smallest finite one, of logits from .. to; false if there is a NaN or nothing
+    // Largest logit, with its lowest index if WHERE, and the smallest, if FINITE the smallest finite one, of logits from .. to; false if there is a NaN or nothing
     // above -infinity
-    template <bool WHERE>
+    template <bool WHERE, bool FINITE>
     __device__ __forceinline__ bool extremes(int from, int to, int& where, float& least) {
         float best = -__builtin_inff(), low = __builtin_inff();
         int at = 0x7FFFFFFF;
@@ -514,7 +514,7 @@ struct SampleRow {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     best = __builtin_elementwise_maximum(best, x[e]);
-                    low = __builtin_elementwise_minimum(low, x[e]);
+                    low = __builtin_elementwise_minimum(low, FINITE && x[e] == -__builtin_inff() ? low : x[e]);
                 }
             }
         });
@@ -705,13 +705,54 @@ struct SampleRow {
         return true;
     }
 
+    // With top_k, and with min_p below 1: the list has all logits down to the bin that holds the k-th, `count` of them, and everything else is done in it
+    __device__ __forceinline__ void draw_listed(int row, const Options& o, int count) {
+        const float low = o.share > 0.0f && o.share < 1.0f ? least_kept(o) : -__builtin_inff();
+        int at, n = min(o.k, count);
+        u64 before, target;
+        sort(count);
+        for (int j = threadIdx.x; j < n; j += THREADS) s.bin[j] = weight(of_key(s.key[j]));
+        __syncthreads();
+        if (o.p < 1.0f) {
+            crossing<false>(n, [&](u64 sum) { return part_of(o.p, sum); }, at, before, target);
+            n = at + 1;
+        }
+        // the first of the list stays, and of the others what min_p leaves, by index: behind these what it does not
+        __syncthreads();
+        for (int j = threadIdx.x; j < n; j += THREADS) s.key[j] = j == 0 || of_key(s.key[j]) >= low ? ~uint32_t(s.index[j]) : 0u;
+        __syncthreads();
+        sort(n);
+        for (int j = threadIdx.x; j < n; j += THREADS) s.bin[j] = s.key[j] ? weight(z(s.index[j])) : 0;
+        __syncthreads();
+        const u64 all = crossing<false>(n, [&](u64 sum) { return place_of(o.u, sum); }, at, before, target);
+        if (threadIdx.x == 0) say_drawn(row, o, s.index[at], all);
+    }
+    // False: too many logits in that bin
+    __device__ __forceinline__ bool draw_first(int row, const Options& o, float least) {
+        const float per = kSampleBins / reach(top, least);
+        auto coarse = [&](float x) { return int(fminf((top - x) * per, float(kSampleBins - 1))); };
+        bins_clear();
+        each([&](int, float x) { atomicAdd(&s.bin[coarse(x)], u64(1)); });           // what lies behind the row's end is behind the k-th
+        __syncthreads();
+        int bin;
+        u64 before, target;
+        crossing<true>(kSampleBins, [&](u64) { return u64(o.k); }, bin, before, target);
+        each([&](int i, float x) { enlist(coarse(x) <= bin && i < v, i, x); });
+        __syncthreads();
+        const int count = s.count;
+        __syncthreads();
+        if (count > kSampleList) return false;
+        draw_listed(row, o, count);
+        return true;
+    }
+
     __device__ __forceinline__ void draw(int row) {
         const Options o = options(row);
         int first;
         float least;
         // the index is for the least of probabilities from 1 up and the temperature 0; top_k needs the smallest finite logit
-        const bool simple = !o.k && !(o.share >= 1.0f) && o.heat > 0.0f;
-        if (!(simple ? extremes<false>(0, v, first, least) : extremes<true>(0, v, first, least))) {
+        const bool simple = !(o.share >= 1.0f) && o.heat > 0.0f;
+        if (!(!simple ? extremes<true, true>(0, v, first, least) : o.k ? extremes<false, true>(0, v, first, least) : extremes<false, false>(0, v, first, least))) {
             if (threadIdx.x == 0) say(row, -1, __builtin_nanf(""));
             return;
         }
@@ -720,7 +761,7 @@ struct SampleRow {
             return;
         }
         measure(o);
-        if (simple && top < __builtin_inff() && draw_once(row, o, least)) return;
+        if (simple && (o.k ? draw_first(row, o, least) : top < __builtin_inff() && draw_once(row, o, least))) return;
         SampleEnd end{-__builtin_inff(), 0x7FFFFFFF};
         if (o.k) end = last_of<false, true>(end, reach(top, least), [&](u64 all) { return min(u64(o.k), all); });
         if (o.p < 1.0f) {
@@ -809,7 +850,7 @@ struct SampleShare : SampleRow<BF16, kSampleShareThreads> {
         for (int j = part * T + threadIdx.x; j < kSampleBins; j += parts * T) w.bin[j] = 0;
         int at;
         float low;
-        Row::template extremes<true>(from, to, at, low);
+        Row::template extremes<true, true>(from, to, at, low);
         if (threadIdx.x == 0) {
             w.top[part] = top;
             w.at[part] = at;
@@ -951,29 +992,8 @@ struct SampleShare : SampleRow<BF16, kSampleShareThreads> {
             s.index[j] = far_load(&w.index[j]);
         }
         __syncthreads();
-        u64 all;
         if (o.k) {
-            Row::sort(count);
-            int n = min(o.k, count);
-            for (int j = threadIdx.x; j < n; j += T) s.bin[j] = Row::weight(Row::of_key(s.key[j]));
-            __syncthreads();
-            if (o.p < 1.0f) {
-                int at;
-                u64 before, target;
-                Row::template crossing<false>(n, [&](u64 sum) { return Row::part_of(o.p, sum); }, at, before, target);
-                n = at + 1;
-            }
-            // the first of the list stays, and of the others what min_p leaves, by index: behind these what it does not
-            __syncthreads();
-            for (int j = threadIdx.x; j < n; j += T) s.key[j] = j == 0 || Row::of_key(s.key[j]) >= low ? ~uint32_t(s.index[j]) : 0u;
-            __syncthreads();
-            Row::sort(n);
-            for (int j = threadIdx.x; j < n; j += T) s.bin[j] = s.key[j] ? Row::weight(Row::z(s.index[j])) : 0;
-            __syncthreads();
-            int at;
-            u64 before, target;
-            all = Row::template crossing<false>(n, [&](u64 sum) { return Row::place_of(o.u, sum); }, at, before, target);
-            if (threadIdx.x == 0) Row::say_drawn(row, o, s.index[at], all);
+            Row::draw_listed(row, o, count);
             return;
         }
         SampleEnd end{-__builtin_inff(), 0x7FFFFFFF};
@@ -993,7 +1013,7 @@ struct SampleShare : SampleRow<BF16, kSampleShareThreads> {
         __syncthreads();
         int line;
         u64 before, target;
-        all = Row::template crossing<false>(lines, [&](u64 sum) { return Row::place_of(o.u, sum); }, line, before, target);
+        const u64 all = Row::template crossing<false>(lines, [&](u64 sum) { return Row::place_of(o.u, sum); }, line, before, target);
         if (threadIdx.x < 64) {
             const int at = line * LINE + lane * E;
             u64 y[E], sum = 0;
