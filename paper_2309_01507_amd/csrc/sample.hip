@@ -12,12 +12,12 @@ namespace {
 
 using namespace lpmm;
 
-// Workgroups of a row; 1: one does it all.  Sharing costs two launches and the handing over, and takes from the four readings of a row.  One workgroup against several,
-// us, fp32 with top_p 0.95: 1 x 8000 19 and 24, 1 x 16000 27 and 26, 1 x 32000 36 and 27, 1 x 131072 110 and 34; 16 x 16000 28 and 27, 16 x 50257 51 and 35;
-// 64 x 16000 28 and 32, 64 x 32000 39 and 39, 64 x 50257 52 and 46; 128 x 50257 57 and 62 (there the workgroups of a row each wait for a CU).  512 for all rows
-// together: with 256 16 to 64 rows take up to a fourth longer, with 1024 64 x 32000 takes 45.
+// Workgroups of a row; 1: one does it all.  Sharing costs two launches and the handing over, and takes from the readings of a row.  One workgroup against several, us, bf16, with top_p
+// 0.95, and with top_k 50 and top_p 0.9: 1 x 18000 23 and 25, 17 and 24; 1 x 32000 29 and 25, 20 and 24; 1 x 50257 38 and 26, 24 and 24; 1 x 131072 74 and 33, 43 and 27; 16 x 32000
+// 30 and 28, 21 and 26; 16 x 50257 40 and 31, 26 and 29; 64 x 50257 45 and 43, 26 and 36; 64 x 131072 80 and 64, 44 and 46; 128 x 131072 81 and 95 (there the workgroups of a row wait for CUs).
+// 512 for all rows together: with 256 16 to 64 rows take up to a fourth longer, with 1024 64 x 32000 takes a sixth longer.
 int sample_shares(int64_t t, int64_t v) {
-    if (t < 1 || t > 64 || v < 16384 + 256 * t || v > int64_t(kSampleBins) * 256) return 1;
+    if (t < 1 || t > 64 || v < 24576 + 512 * t || v > int64_t(kSampleBins) * 256) return 1;
     return int(std::min<int64_t>(std::min<int64_t>(kSampleShares, 512 / t), div_up(v, 2048)));
 }
 
@@ -74,9 +74,9 @@ int lpmm_sample(const void* z, int z_dtype, int64_t t, int64_t v, int64_t z_stri
         return LPMM_OK;
     }
     const dim3 rows{unsigned(t)};
-    // Threads of a row: as many as speed up its passes, as few as leave room for other rows (us with 256, 512, 1024, bf16 with top_p: 1 x 1000 13.5, 14.2, 17.2;
-    // 1 x 16000 26, 22, 22; 256 x 32000 48, 38, 38, with top_k too 72, 50, 45; 256 x 131072 168, 110, 95; 300 x 32000 54, 45, 48; 768 x 32000 69, 66, 77;
-    // 2048 x 32000 150, 147, 184; 2000 x 16000 82, 88, 124; 2000 x 4000 38, 49, 85)
+    // Threads of a row: as many as speed up its passes, as few as leave room for other rows (us with 256, 512, 1024, bf16 with top_p: 1 x 1000 13.0, 14.1, 16.5;
+    // 1 x 16000 27, 22, 22; 256 x 32000 43, 34, 32; 128 x 131072 126, 89, 81; 300 x 32000 52, 45, 58; 768 x 32000 69, 64, 92; 2048 x 32000 150, 147, 184;
+    // 2000 x 16000 84, 91, 165; 2000 x 4000 39, 51, 117; with top_k too 256 x 32000 32, 22, 22; 300 x 32000 39, 30, 39; 2000 x 4000 33, 37, 92)
 #define LPMM_SAMPLE(T) { if (z_dtype == LPMM_BF16) hipLaunchKernelGGL((sample_kernel<true, T>), rows, dim3(T), 0, s, a); \
                          else hipLaunchKernelGGL((sample_kernel<false, T>), rows, dim3(T), 0, s, a); }
     if (v <= 2048 || (t > 1024 && v <= 16384)) LPMM_SAMPLE(256)
