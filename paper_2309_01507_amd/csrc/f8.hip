@@ -250,7 +250,7 @@ int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     if (few(t, mw.bytes)) {
         const size_t lds = up16(size_t(t) * (mw.bytes + mw.bytes / kF8Block));
         // 16 waves share the blocks of 16 rows; where rows abound, two those of 32 (us, 1 token, each: 4096 x 4096 5.3, 18; 11008 x 4096 9.6, 18; 32000 x 4096 23, 22;
-        // 50257 x 1024 11.5, 11.2).  Two workgroups a CU while x leaves room for them (16 tokens 11008 x 4096 one 16.7, two 24)
+        // 50257 x 1024 11.5, 11.2).  Two workgroups a CU while x leaves room for them (16 tokens 11008 x 4096 one 16.1, two 24)
         const int64_t most = lds <= 32768 ? 512 : 256;
 #define LPMM_FEW(B, K, N, T) hipLaunchKernelGGL((f8_few_kernel<B, K, N, T, 2>), dim3(unsigned(std::min<int64_t>(most, div_up(mw.rows, 16 * T * N)))), dim3(64 * K * N), lds, \
                                                 s, mw, x, int(t), int(w->cols), x_stride, y, y_stride)

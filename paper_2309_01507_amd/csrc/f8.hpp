@@ -58,6 +58,21 @@ __device__ __forceinline__ uint32_t umax16(uint32_t x) {
     return x;
 }
 
+// The largest finite magnitude's bits of a block that 16 lanes hold: all lanes look at what is not finite only where there is such
+__device__ __forceinline__ uint32_t f8_top16(const float v[8]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = umax32(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    top = umax16(top);
+    if (top >= 0x7F800000u) {
+        top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = umax32(top, f8_magnitude(v[e]));
+        top = umax16(top);
+    }
+    return top;
+}
+
 // ---- to 8 bits ---------------------------------------------------------------------------------------------------------------------
 
 // Blocks of 1 x 128: 16 lanes a block, 8 elements each; a wave takes four blocks of a row, a workgroup of four rows.  rows_up: rows rounded up to a
@@ -75,10 +90,7 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t st
     const int at = block * kF8Block + d * 8;
     float v[8];
     w4_load8<BF16>(x, int64_t(row) * stride + at, int64_t(row) * stride + cols, v);
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = umax32(top, f8_magnitude(v[e]));
-    const uint32_t scale = f8_scale(umax16(top));
+    const uint32_t scale = f8_scale(f8_top16(v));
     const float inverse = f8_inverse(scale);
     uint2 w;
     w.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);

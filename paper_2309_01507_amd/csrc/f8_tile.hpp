@@ -251,7 +251,7 @@ constexpr int kF8FewTokens = 16, kF8FewBytes = 65536;          // codes of x tha
 //
 // Bound by reading W: one token through 32000 x 4096 bf16 22 us, 6.0 TB/s, through 11008 x 4096 9.6 us, 4.7, through 4096 x 4096 5.3 us, 3.2 (one round trip to memory, x and the
 // join).  Every workgroup brings the same x to 8 bits, which a kernel in front would do once, for a launch (so it began: 1 x 4096 x 4096 9.9 us);
-// each token more costs 0.4 us of conversions.  Loads of four units at once took as long.
+// each token more costs 0.35 us of conversions.  Loads of four units at once took as long.
 template <bool BF16, int WK, int WN, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const void* x, int t, int k, int64_t x_stride, void* y, int64_t y_stride) {
     constexpr int THREADS = 64 * WK * WN, ROWS = WN * NT * 16, PART = NT * 4 * 64;
@@ -297,10 +297,7 @@ __global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const voi
         const int64_t row = int64_t(token) * x_stride;
         float v[8];
         w4_load8<BF16>(x, row + at, row + k, v);
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = umax32(top, f8_magnitude(v[e]));
-        const uint32_t scale = f8_scale(umax16(top));
+        const uint32_t scale = f8_scale(f8_top16(v));
         const float inverse = f8_inverse(scale);
         uint2 c;
         c.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
