@@ -2,7 +2,7 @@
 //
 // Results of 16 bits: v_mfma_scale_f32_32x32x64_f8f6f4 multiplies codes and applies both blocks' powers.  It adds up the 64 products of a step
 // with terms cut off some 2^-13 below the largest (measured: 1.5e-5 of the result's size, for every fp8 form), which is far below the
-// half step of 2^-9 that rounding to bf16 costs.  Results of 32 bits: the codes times their powers become bf16, which holds them
+// half step of up to 2^-8 that rounding to bf16 costs.  Results of 32 bits: the codes times their powers become bf16, which holds them
 // exactly, and v_mfma_f32_32x32x16_bf16 adds them up in fp32, at half the rate.
 //
 // Operand layout of v_mfma_scale_f32_32x32x64_f8f6f4: lane l holds, of row (A) or column (B) l % 32, 32 bytes of the half l / 32 of the
