@@ -606,7 +606,7 @@ int lpmm_f8_train_backward(const void* dy, int dtype, int64_t t, int64_t dy_stri
  *   min_p   and of these those with w_i >= min_p (0: all).  The first in the order is kept always.
  *   token   the lowest index at which the running sum, by rising index, of the kept weights exceeds u times their sum
  *   logprob log(w_token / that sum), float[t]
- * temperature 0: the first in the order, logprob 0.  Weights and sums are held in 64 bits.  Each option is one value for all rows or, where the pointer is not null,
+ * temperature 0: the first in the order, logprob 0; infinity: weights of 1, but for -infinity.  Weights and sums are held in 64 bits.  Each option is one value for all rows or, where the pointer is not null,
  * an array on the device with one for each row.  Values for all rows are refused where they are NaN, or temperature or top_k negative;
  * a row's own are taken as they come: a temperature that is not above 0 as 0, top_k below 1 and a top_p of NaN as all, a min_p of NaN as 0.
  * -infinity is never drawn; where the largest logit is +infinity, only those that are it are.  A row with a NaN, or with nothing

@@ -557,6 +557,7 @@ struct SampleRow {
         Options o{a.temperatures ? a.temperatures[row] : a.temperature, a.top_ps ? a.top_ps[row] : a.top_p, a.min_ps ? a.min_ps[row] : a.min_p, a.u[row],
                   a.top_ks ? a.top_ks[row] : a.top_k};
         if (!(o.k > 0 && o.k < v)) o.k = 0;
+        if (o.heat == __builtin_inff() && o.share <= 1.0f) o.share = 0.0f;           // all weights are 1: min_p leaves them (and infinity plus heat log(share) would be no border)
         return o;
     }
     // top is known

@@ -300,3 +300,27 @@ def test_one_workspace_for_two_graphs():
         room.fill_(255)
         for o, w in zip(outs, want):
             assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,v", [(8, 700), (8, 3000), (8, 29000), (1, 24577 + 511)])
+def test_infinite_logits_at_any_temperature(t, v, dtype):
+    """Only they are drawn, whatever min_p says alone, with top_k and with top_p; in lists, by lines, and where several workgroups share a row"""
+    for n, heat in enumerate((1.0, 3e38, INF)):
+        z, u = logits(t, v, dtype, 900 + n)
+        z[0, 3] = z[0, 41] = z[0, v - 1] = INF
+        if t > 1:
+            z[1, ::2] = INF
+            z[2] = INF
+            z[3, 77], z[3, ::3] = INF, -INF
+            z[4, -1] = INF
+        for options in ({"min_p": 0.3}, {"min_p": 1e-30}, {"min_p": 0.999, "top_p": 0.6}, {"min_p": 0.5, "top_k": 2}, {"min_p": 0.5, "top_k": 600}, {"min_p": 0.1, "top_k": 50, "top_p": 0.7},
+                        {"min_p": 1.0}, {"min_p": 1.0, "top_k": 5}):
+            progress(f"sample {t} x {v} {heat} {options}")
+            if options["min_p"] == 1.0 and heat < INF:
+                # exp(x) is below 1 for every x below 0, where 64 bits round it to 1 for those near 0: what is kept of the first top_k are those that equal the largest, with weights of 1
+                same = torch.where(z == z.amax(1, keepdim=True), z, torch.full_like(z, -INF))
+                got = lpmm.lpmm_sample(z.to(DEV), u.to(DEV), heat, **options)
+                ref.check(same, u, heat, options.get("top_k", 0), 1.0, 0.0, *got, f"{heat} {options}")
+            else:
+                run(z, u, temperature=heat, what=f"{heat} {options}", **options)
