@@ -72,21 +72,22 @@ __device__ __forceinline__ double fma_by(double a, double b, double c) {
     return r;
 }
 
-// 2^bits times 2^y for y <= 0, -infinity included, to a whole number, to some 2^-47 of 1: y = n + f with |f| <= 1/2, the series of 2^f up to the 11th power (what is
-// left is below 7e-15), and the sum with 2^52, which is returned, rounds to a whole number in its low bits.
+// 2^bits times 2^y for y <= 0, -infinity included, to a whole number, off by some 2^-47 of 1, the rounding to it: y = n + f with |f| <= 1/2, and 2^f = 1 + f q(f), where q, of the 9th power,
+// meets (2^f - 1) / f at the ten points cos((2 i + 1) pi / 20) / 2: within 4.4e-16 of 2^f (the first ten powers of the exponential series are 2.2e-13 off).  The sum with 2^52, which is
+// returned, rounds to a whole number in its low bits.
 __device__ __forceinline__ double sample_rounded(double y, int bits) {
     y = fmax(y, -100.0);
     const double shifted = y + 0x1.8p52, f = y - (shifted - 0x1.8p52);
     const int n = int(uint32_t(u64(__double_as_longlong(shifted))));
-    double p = fma_by(f, 7.0549116208011209e-09, 1.0178086009239699e-07);       // ln(2)^k / k!
-    p = fma_by(p, f, 1.3215486790144307e-06);
-    p = fma_by(p, f, 1.5252733804059838e-05);
-    p = fma_by(p, f, 1.5403530393381606e-04);
-    p = fma_by(p, f, 1.3333558146428441e-03);
-    p = fma_by(p, f, 9.6181291076284769e-03);
-    p = fma_by(p, f, 5.5504108664821576e-02);
-    p = fma_by(p, f, 2.4022650695910069e-01);
-    p = fma_by(p, f, 6.9314718055994529e-01);
+    double p = fma_by(f, 7.0709778665081391e-09, 1.0205905413765595e-07);
+    p = fma_by(p, f, 1.3215451633221434e-06);
+    p = fma_by(p, f, 1.5252672924850737e-05);
+    p = fma_by(p, f, 1.5403530424776529e-04);
+    p = fma_by(p, f, 1.3333558200794592e-03);
+    p = fma_by(p, f, 9.6181291076186653e-03);
+    p = fma_by(p, f, 5.5504108664651669e-02);
+    p = fma_by(p, f, 2.4022650695910075e-01);
+    p = fma_by(p, f, 6.9314718055994617e-01);
     p = __builtin_fma(p, f, 1.0);
     const double power = __hiloint2double((1023 + bits + n) << 20, 0);
     return fma_by(p, power, 0x1p52);

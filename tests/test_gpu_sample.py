@@ -1,4 +1,6 @@
 """Tokens drawn from logits on the GPU against a plain 64-bit form: every token, and its log-probability."""
+import decimal
+
 import pytest
 import torch
 
@@ -324,3 +326,36 @@ def test_infinite_logits_at_any_temperature(t, v, dtype):
                 ref.check(same, u, heat, options.get("top_k", 0), 1.0, 0.0, *got, f"{heat} {options}")
             else:
                 run(z, u, temperature=heat, what=f"{heat} {options}", **options)
+
+
+# N logits whose weight w has its binary logarithm next to -1/2, where a series for powers of two is farthest from them, and M of weight 1.  u: the sum of the N comes just before u times
+# that of all.  p: of them all, largest first, p leaves the M and a tenth of the N, whose sum just reaches p times that of all.
+NEAR = [("u", F32, 608, 397, "-0x1.62c51ep-2", "1", "0x1.0a34f6p-1"), ("u", F32, 15063, 14528, "-0x1.6270fcp-2", "1", "0x1.b146e0p-2"),
+        ("u", F32, 13792, 15699, "-0x1.62c69ap-2", "1", "0x1.8866bep-2"), ("u", BF16, 807, 805, "-1", "0x1.71a71ap+1", "0x1.a8d8bap-2"),
+        ("u", BF16, 665, 811, "-1", "0x1.718dacp+1", "0x1.77dee6p-2"), ("u", BF16, 475, 312, "-1", "0x1.71b0acp+1", "0x1.097a34p-1"),
+        ("p", F32, 14785, 15177, "-0x1.62a798p-2", "1", "0x1.440446p-1"), ("p", F32, 15406, 14305, "-0x1.62b674p-2", "1", "0x1.38c32ep-1"),
+        ("p", F32, 13495, 15529, "-0x1.626bb8p-2", "1", "0x1.508ee4p-1"), ("p", F32, 783, 714, "-0x1.628a4cp-2", "1", "0x1.369ddcp-1"),
+        ("p", F32, 300, 362, "-0x1.62723ap-2", "1", "0x1.55b210p-1")]
+
+
+@pytest.mark.parametrize("what,dtype,low,high,z,heat,number", NEAR)
+def test_weights_whose_errors_add_up(what, dtype, low, high, z, heat, number):
+    """Each weight may be off by 2^-47 and a little, all of them in the same direction: a border may move by (low + high) 2^-47, and is at least four times that away."""
+    z, heat, number = (float.fromhex(x) if "0x" in x else float(x) for x in (z, heat, number))
+    with decimal.localcontext() as exact:
+        exact.prec = 50
+        w = (decimal.Decimal(z) / decimal.Decimal(heat)).exp()
+        ahead = low * w if what == "u" else high + low // 10 * w
+        off = decimal.Decimal(number) * (high + low * w) - ahead
+    v = low + high
+    assert 4 * v * 2.0 ** -47 < (off if what == "u" else -off) < v * 2.0 ** -43
+    parts = [torch.full((low,), z), torch.zeros(high)]
+    row = torch.cat(parts if what == "u" else parts[::-1])
+    last = 1 - 2.0 ** -24                                       # draws the last one that is kept: the sum of thousands of weights lacks less than one of them
+    token = low if what == "u" else high + low // 10 - 1
+    for t in (1, 66):                                           # long rows by several workgroups, or one
+        for listed in ((False, True) if v < 1024 else (False,)):
+            logits = torch.cat([row, torch.full((1,), -INF)]).to(dtype).repeat(t, 1).to(DEV)
+            u = torch.full((t,), number if what == "u" else last, device=DEV)
+            tokens, _ = lpmm.lpmm_sample(logits, u, heat, v if listed else 0, 1.0 if what == "u" else number)
+            assert tokens.tolist() == [token] * t, f"{t} rows, {listed}"
