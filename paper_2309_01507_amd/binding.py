@@ -1177,11 +1177,16 @@ class GradPlanHost(ctypes.Structure):
 
 @dataclass
 class GradPlan:
-    """Gradients that are measured and scaled together; refers to them (and holds them) by address.  Two calls on one plan must not overlap."""
+    """Gradients that are measured and scaled together; refers to them by address, and holds them (by_address: no longer).  Two calls on one plan must not overlap."""
     grads: "object"
     outs: "object"
     memory: "object"
     host: GradPlanHost
+
+    def by_address(self) -> "GradPlan":
+        """Lets go of the tensors: from now on whoever calls sees to it that gradients and outputs are where they were, and to telling autograd of what was written."""
+        self.grads = self.outs = ()
+        return self
 
 
 def new_grad_plan(grads, outs=None, stream=None) -> GradPlan:

@@ -98,9 +98,12 @@ class _PlanOptimizer:
         kind = _norm_kind(norm_type)
         self._ensure_plan()
         with torch.cuda.device(self.device):
+            grads = [p.grad for p in self.params]
             if self._grad_plan is None:
-                self._grad_plan = _b.new_grad_plan([p.grad for p in self.params])
-            return _b.lpmm_grad_norm_clip(self._grad_plan, max_norm, kind)
+                self._grad_plan = _b.new_grad_plan(grads).by_address()       # held, they would outlive zero_grad(set_to_none=True)
+            norm = _b.lpmm_grad_norm_clip(self._grad_plan, max_norm, kind)
+            _b._written_all(grads)
+            return norm
 
     @torch.no_grad()
     def step(self):

@@ -1,5 +1,6 @@
 """A training step of 8-bit products, clipped gradients and the 4-bit optimizer, and tokens drawn from what it trains: each through the modules, and together."""
 import math
+import weakref
 
 import pytest
 import torch
@@ -181,3 +182,29 @@ def test_recovery_with_clipping_and_drawing(kind):
     from paper_2309_01507_amd import w4_recovery
     before, after, off = w4_recovery.recover(3, student_kind=kind, max_norm=0.1, temperature=0.9, top_p=0.95)
     assert all(math.isfinite(v) for v in (before, after, off))
+
+
+@pytest.mark.parametrize("how", ["max_norm", "method"])
+def test_gradients_are_let_go(how):
+    """After a clipped step, zero_grad(set_to_none=True) frees the gradients; the next ones may get the same addresses; and autograd knows of what the optimizer's clip wrote"""
+    ps = parameters()
+    opt = lpmm.AdamW4bit(ps, lr=1e-3, max_norm=0.5 if how == "max_norm" else None)
+    for step in range(3):
+        for p in ps:
+            p.grad = torch.randn(p.shape, device=DEV) + step
+        if how == "method":
+            opt.clip_grad_norm(0.5)
+        opt.step()
+        assert abs(norm64([p.grad for p in ps]) - 0.5) < 1e-5
+        old, size = [weakref.ref(p.grad) for p in ps], sum(p.grad.numel() * 4 for p in ps)
+        before = torch.cuda.memory_allocated()
+        opt.zero_grad(set_to_none=True)
+        assert all(r() is None for r in old) and torch.cuda.memory_allocated() <= before - size
+    x = torch.randn(ps[0].shape, device=DEV, requires_grad=True)
+    for p in ps:
+        p.grad = torch.randn(p.shape, device=DEV)
+    for again in range(2):
+        y = (x * ps[0].grad).sum()
+        opt.clip_grad_norm(0.1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
