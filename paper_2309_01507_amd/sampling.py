@@ -17,7 +17,7 @@ def sample(logits: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
     top_k int32) of the leading dimensions.  u: random numbers from [0, 1), float32, of the leading dimensions; drawn with `generator` if not given."""
     lead = logits.shape[:-1]
     if u is None:
-        u = torch.rand(lead, device=logits.device, generator=generator)
+        u = torch.rand(lead, dtype=torch.float32, device=logits.device, generator=generator)
     elif u.shape != lead:
         raise ValueError(f"sample: u must be {tuple(lead)}, like the logits")
 

@@ -111,3 +111,15 @@ def test_modules_refuse():
     p.grad = torch.ones_like(z)
     with pytest.raises(ValueError, match="GPU"):
         lpmm.clip_grad_norm([p], 1.0)
+
+
+@pytest.mark.parametrize("default", [torch.float64, torch.bfloat16])
+def test_numbers_under_another_default_type(default):
+    """sample() draws its own in float32, whatever torch's default type is: what is refused is that these logits are not on a GPU"""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        with pytest.raises(ValueError, match="GPU"):
+            lpmm.sample(torch.zeros(2, 10, dtype=torch.float32))
+    finally:
+        torch.set_default_dtype(before)
