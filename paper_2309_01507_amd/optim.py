@@ -192,7 +192,7 @@ class AdamW4bit(_PlanOptimizer):
         # into a graph and replayed (run one step eagerly first: the plan is built then); change the rate with set_lr
         self.capturable = capturable
         if capturable:
-            self.lr_dev = torch.full((1,), float(lr), device=self.device)
+            self.lr_dev = torch.full((1,), float(lr), dtype=torch.float32, device=self.device)
             self.step_dev = torch.zeros(1, dtype=torch.int64, device=self.device)
 
     def set_lr(self, lr: float):
@@ -203,7 +203,7 @@ class AdamW4bit(_PlanOptimizer):
     def _new_state(self, p):
         n = p.numel()
         if n <= QUANT_MIN_NUMEL:
-            return (torch.zeros(n, device=p.device), torch.zeros(n, device=p.device))
+            return (torch.zeros(n, dtype=torch.float32, device=p.device), torch.zeros(n, dtype=torch.float32, device=p.device))
         if p.ndim <= 1 or self.second_moment == "b128":
             return _b.new_state_b128(n, p.device)
         rows, cols = p.shape[0], n // p.shape[0]
@@ -237,7 +237,7 @@ class SGDM4bit(_PlanOptimizer):
 
     def _new_state(self, p):
         n = p.numel()
-        return torch.zeros(n, device=p.device) if n <= QUANT_MIN_NUMEL else _b.new_state_sgdm(n, p.device)
+        return torch.zeros(n, dtype=torch.float32, device=p.device) if n <= QUANT_MIN_NUMEL else _b.new_state_sgdm(n, p.device)
 
     def _desc(self, p, g, st):
         return _b.make_desc_sgdm(p, g, st, p.numel())

@@ -208,3 +208,24 @@ def test_gradients_are_let_go(how):
         opt.clip_grad_norm(0.1)
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             y.backward()
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+@pytest.mark.parametrize("make", [lambda ps: lpmm.AdamW4bit(ps, lr=1e-2), lambda ps: lpmm.AdamW4bit(ps, lr=1e-2, capturable=True), lambda ps: lpmm.SGDM4bit(ps, lr=1e-2)])
+def test_optimizers_under_another_default_type(make, default):
+    """States and rates that kernels take as float32 are that whatever torch's default type is: the same bits"""
+    mine, theirs = parameters(), parameters()
+    b = make(theirs)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        a = make(mine)
+        for _ in range(2):
+            a.step()
+    finally:
+        torch.set_default_dtype(before)
+    for _ in range(2):
+        b.step()
+    assert all(torch.equal(p, q) for p, q in zip(mine, theirs))
+    floats = [x for st in a.state_buffers() for x in a._tensors_of(st).values() if x.is_floating_point()]
+    assert floats and all(x.dtype == torch.float32 for x in floats)
