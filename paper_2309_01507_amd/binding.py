@@ -1236,7 +1236,9 @@ def _written_all(tensors) -> None:
 
 
 def lpmm_grad_clip(plan: GradPlan, norm, limit: float, stream=None) -> None:
-    """Scales the gradients by min(1, limit / (norm + 1e-6)) into the plan's outputs."""
+    """Scales the gradients by min(1, limit / (norm + 1e-6)) into the plan's outputs.  norm: a tensor of one float32, as lpmm_grad_norm gives it."""
+    if norm is None:
+        raise ValueError("lpmm_grad_clip: needs a norm")
     norm = _grad_norm_out(plan, norm, stream, "lpmm_grad_clip")
     _check((_lib or lib()).lpmm_grad_clip(ctypes.addressof(plan.host), norm.data_ptr(), limit, _stream(stream)), "lpmm_grad_clip")
     _written_all(plan.outs)

@@ -123,3 +123,13 @@ def test_numbers_under_another_default_type(default):
             lpmm.sample(torch.zeros(2, 10, dtype=torch.float32))
     finally:
         torch.set_default_dtype(before)
+
+
+def test_clipping_without_a_norm():
+    """None is not a norm to be allocated, whose value would be whatever was there"""
+    plan = lpmm.GradPlan([], [], torch.zeros(256, dtype=torch.uint8), B.GradPlanHost(256, 0, 0, 12, 1))
+    with pytest.raises(ValueError, match="norm"):
+        lpmm.lpmm_grad_clip(plan, None, 1.0)
+    for bad in (torch.zeros(2), torch.zeros(1, dtype=torch.float64), torch.zeros(())):
+        with pytest.raises(ValueError, match="norm"):
+            lpmm.lpmm_grad_clip(plan, bad, 1.0)
