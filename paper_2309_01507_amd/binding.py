@@ -1190,7 +1190,8 @@ class GradPlan:
 
 
 def new_grad_plan(grads, outs=None, stream=None) -> GradPlan:
-    """Gradients (float32 or bfloat16, contiguous, on the current GPU) as one vector; `outs`: where lpmm_grad_clip writes, in place by default."""
+    """Gradients (float32 or bfloat16, contiguous, on the current GPU) as one vector; `outs`: where lpmm_grad_clip writes, in place by default.
+    The call waits until the plan is there, so that any stream may use it; a plan that another stream still uses is kept until that is done."""
     torch = _torch or _load_torch()
     grads = list(grads)
     outs = grads if outs is None else list(outs)
@@ -1213,7 +1214,8 @@ def new_grad_plan(grads, outs=None, stream=None) -> GradPlan:
         raise LpmmError("lpmm_grad_plan_bytes: invalid tensor list")
     memory = torch.empty(need, dtype=torch.uint8, device=f"cuda:{here}")
     host = GradPlanHost()
-    _check(L.lpmm_grad_plan_build(ctypes.addressof(descs), len(grads), memory.data_ptr(), need, _stream(stream), ctypes.addressof(host)),
+    # on the stream that the memory is from, whichever is given: what that stream still does with it as its last owner's comes first
+    _check(L.lpmm_grad_plan_build(ctypes.addressof(descs), len(grads), memory.data_ptr(), need, _stream(None), ctypes.addressof(host)),
            "lpmm_grad_plan_build")
     return GradPlan(grads, outs, memory, host)
 

@@ -187,3 +187,25 @@ def test_a_tensor_listed_twice_on_the_gpu():
             lpmm.new_grad_plan(grads, outs)
     out = torch.empty(200, device=DEV)
     check_norm(lpmm.lpmm_grad_norm(lpmm.new_grad_plan([g, g], [out[:100], out[100:]])), norm_of([g, g], 0), "read twice")
+
+
+def test_a_plan_in_memory_that_is_still_written():
+    """Memory that torch hands on may still be written by its last owner's kernels, on torch's current stream: a plan that is asked for on another stream comes behind these"""
+    grads = tensors((50001, 7), (F32,), 11)
+    s = torch.cuda.Stream()
+    need = lpmm.new_grad_plan(grads).memory.numel()
+    x = torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    owner = torch.empty(need, dtype=torch.uint8, device=DEV)
+    for _ in range(8):
+        y = x @ x
+    owner.fill_(0)
+    del owner                                                   # the block that fits the plan
+    plan = lpmm.new_grad_plan(grads, stream=s)
+    torch.cuda.synchronize()
+    assert int(plan.memory.count_nonzero()) > 0, "overwritten"
+    norm = torch.empty(1, device=DEV)
+    torch.cuda.synchronize()
+    lpmm.lpmm_grad_norm(plan, norm=norm, stream=s)
+    s.synchronize()
+    check_norm(norm, norm_of(grads, 0), "on a stream")
