@@ -564,7 +564,7 @@ typedef struct lpmm_f8 {
 int lpmm_f8_sizes(int64_t rows, int64_t cols, int tile, size_t sizes[2]);
 
 /* x, out->rows x out->cols of dtype, into 8 bits; and x together with its transpose from one reading: out_t is cols x rows of the same tile, its blocks of 1 x 128
- * lie along the rows of x (rows >= 1, at most 128 * 65535, as for tile 128). */
+ * lie along the rows of x (1 <= rows <= 2^22, as its columns are). */
 int lpmm_f8_quant(const void* x, int dtype, int64_t stride, const lpmm_f8* out, void* stream);
 int lpmm_f8_quant_both(const void* x, int dtype, int64_t stride, const lpmm_f8* out, const lpmm_f8* out_t, void* stream);
 

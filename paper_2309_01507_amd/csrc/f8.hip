@@ -41,9 +41,7 @@ int check_f8(const lpmm_f8* f, F8Mat* m) {
 
 int launch_quant(const void* x, int dtype, int64_t stride, const F8Mat& m, int64_t cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
     const int blocks = m.bytes / kF8Block;
-    const int64_t groups = div_up(m.rows, 4) * div_up(blocks, 4);
-    if (groups > kMaxBlocks) return LPMM_EINVAL;
-    const dim3 grid{unsigned(groups)};
+    const dim3 grid{unsigned(std::min(div_up(m.rows, 4) * div_up(blocks, 4), kMaxBlocks))};          // of at most 2^24: 2^33 codes
     if (dtype == LPMM_BF16)
         hipLaunchKernelGGL(f8_quant_kernel<true>, grid, dim3(256), 0, s, x, stride, m.rows, int(cols), blocks, codes, scales, m.scale_bytes);
     else

@@ -75,28 +75,31 @@ __device__ __forceinline__ uint32_t f8_top16(const float v[8]) {
 
 // ---- to 8 bits ---------------------------------------------------------------------------------------------------------------------
 
-// Blocks of 1 x 128: 16 lanes a block, 8 elements each; a wave takes four blocks of a row, a workgroup of four rows.  rows_up: rows rounded up to a
-// multiple of 4, so that the rest of a row of scales is written too.  Bound by memory: 4096 x 11008 bf16 22.7 us, 5.9 TB/s.
+// Blocks of 1 x 128: 16 lanes a block, 8 elements each; a wave takes four blocks of a row, a workgroup of four rows, and goes on to others where a launch cannot have so many.
+// rows_up: rows rounded up to a multiple of 4, so that the rest of a row of scales is written too.  Bound by memory: 4096 x 11008 bf16 22.7 us, 5.9 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t stride, int rows, int cols, int blocks, uint8_t* codes, uint8_t* scales,
                                                        int rows_up) {
-    const int across = (blocks + 3) >> 2, group = int(blockIdx.x / uint32_t(across)), d = threadIdx.x & 15;
-    const int row = group * 4 + (threadIdx.x >> 6), block = int(blockIdx.x % uint32_t(across)) * 4 + (threadIdx.x >> 4 & 3);
-    if (block >= blocks) return;                                          // 16 lanes at a time
-    if (row >= rows) {
-        if (d == 0) scales[int64_t(block) * rows_up + row] = 0;
-        return;
+    const uint32_t across = uint32_t(blocks + 3) >> 2, groups = uint32_t(rows_up >> 2) * across;
+    const int d = threadIdx.x & 15;
+    for (uint32_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int row = int(group / across) * 4 + (threadIdx.x >> 6), block = int(group % across) * 4 + (threadIdx.x >> 4 & 3);
+        if (block >= blocks) continue;                                    // 16 lanes at a time
+        if (row >= rows) {
+            if (d == 0) scales[int64_t(block) * rows_up + row] = 0;
+            continue;
+        }
+        const int at = block * kF8Block + d * 8;
+        float v[8];
+        w4_load8<BF16>(x, int64_t(row) * stride + at, int64_t(row) * stride + cols, v);
+        const uint32_t scale = f8_scale(f8_top16(v));
+        const float inverse = f8_inverse(scale);
+        uint2 w;
+        w.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
+        w.y = f8_codes4(v[4], v[5], v[6], v[7], inverse);
+        *reinterpret_cast<uint2*>(codes + (int64_t(row) * blocks + block) * kF8Block + d * 8) = w;
+        if (d == 0) scales[int64_t(block) * rows_up + row] = uint8_t(scale);
     }
-    const int at = block * kF8Block + d * 8;
-    float v[8];
-    w4_load8<BF16>(x, int64_t(row) * stride + at, int64_t(row) * stride + cols, v);
-    const uint32_t scale = f8_scale(f8_top16(v));
-    const float inverse = f8_inverse(scale);
-    uint2 w;
-    w.x = f8_codes4(v[0], v[1], v[2], v[3], inverse);
-    w.y = f8_codes4(v[4], v[5], v[6], v[7], inverse);
-    *reinterpret_cast<uint2*>(codes + (int64_t(row) * blocks + block) * kF8Block + d * 8) = w;
-    if (d == 0) scales[int64_t(block) * rows_up + row] = uint8_t(scale);
 }
 
 // A tile of 128 x 128 a workgroup, for 128 x 128 blocks and for a matrix together with its transpose.  A thread takes 8 rows by 8

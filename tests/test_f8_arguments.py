@@ -103,3 +103,15 @@ def test_a_cast_of_the_layer():
     assert layer.weight.dtype == torch.float32 and layer.bfloat16().weight.dtype == torch.bfloat16
     copy = lpmm.F8Linear.from_weight(layer.weight)
     assert copy.weight is not layer.weight and copy.weight.requires_grad and (copy.in_features, copy.out_features) == (100, 30)
+
+
+def test_the_largest_matrices():
+    """As the header states them: 2^33 codes, 2^22 columns, and of a matrix with its transpose 2^22 rows"""
+    assert lpmm.lpmm_f8_sizes(2 ** 26, 128) == [2 ** 33, 2 ** 26] and lpmm.lpmm_f8_sizes(2 ** 11, 2 ** 22) == [2 ** 33, 2 ** 26]
+    for bad in ((2 ** 26 + 1, 128, 1), (2 ** 11 + 1, 2 ** 22, 1), (2 ** 26 + 1, 1, 128)):
+        with pytest.raises(lpmm.LpmmError):
+            lpmm.lpmm_f8_sizes(*bad)
+    L, at = lpmm.lib(), ctypes.addressof
+    long = 2 ** 22 + 1
+    assert L.lpmm_f8_quant_both(None, 0, 1, at(f8(long, 1, 1)), at(f8(1, long, 1)), None) == -1
+    assert L.lpmm_f8_quant_both(None, 0, 1, at(f8(long, 1, 128)), at(f8(1, long, 128)), None) == -1

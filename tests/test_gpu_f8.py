@@ -447,3 +447,19 @@ def test_layer_shapes_and_states():
     assert one.shape == (33,)
     with pytest.raises(ValueError):
         layer(torch.randn(5, 99, device=DEV))
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """Every matrix that lpmm_f8_sizes takes is brought to 8 bits: beyond 2^25 rows of one block, which end within a workgroup's four"""
+    rows = 4 * 2 ** 23 + 5
+    i = torch.arange(rows, device=DEV)
+    x = ((i % 7 + 1).float() * torch.exp2((i % 11 - 5).float())).to(BF16)[:, None].expand(rows, 2).contiguous()
+    x[-1, 1] = 448 * 2.0 ** 9
+    q = lpmm.lpmm_f8_quant(x)
+    assert torch.equal(lpmm.lpmm_f8_dequant(q, BF16)[:-1], x[:-1])
+    for part in (slice(0, 9), slice(rows // 2, rows // 2 + 9), slice(rows - 9, rows)):
+        want, scales = ref.quantize(x[part].cpu(), 1)
+        assert torch.equal(q.scales[0, part].cpu().long(), scales[:, 0])
+        assert ref.same(lpmm.lpmm_f8_dequant(lpmm.lpmm_f8_quant(x[part]), F32).cpu().double(), want)
+        assert torch.equal(q.codes[part], lpmm.lpmm_f8_quant(x[part]).codes)
+    assert q.scales[0, rows:].tolist() == [0, 0, 0] and bool((q.codes[:, 2:] == 0).all())
