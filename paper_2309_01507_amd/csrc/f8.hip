@@ -127,7 +127,13 @@ int launch_product(const F8Mat& a, const F8Mat& b, void* c, int dtype, int64_t s
     return LPMM_OK;
 }
 
+// Up to 16 tokens whose codes LDS holds have a kernel of their own
 bool few(int64_t t, int64_t bytes) { return t <= kF8FewTokens && t * bytes <= kF8FewBytes; }
+// but not for results in bf16 where every workgroup brings so much to 8 bits that one is all a CU has room for, and W has many rows, up to 2^28 codes (us, that kernel and the
+// tiles, bf16: 16 tokens 24576 x 4096 24.9, 21.5; 28672 x 4096 27.3, 22.0; 32000 x 4096 29.3, 27.5; 50257 x 4096 40.8, 34.3; 65536 x 4096 48.4, 44.2; 50257 x 2560
+// 29.3, 24.1; 12 tokens 24576 x 4096 23.5, 21.5; 32000 x 4096 27.9, 27.4; 36864 x 4096 29.0, 29.4; 50257 x 5120 45.4, 44.8; where it stays 8 tokens 32000 x 4096 26.5, 27.3; 16 tokens
+// 16384 x 2560 13.3, 15.3; 20000 x 4096 22.1, 21.1; 100000 x 4096 80.5, 86.2; 32000 x 2048 15.5, 17.6; fp32 16 tokens 32000 x 4096 30.0, 35.9)
+bool few_by_tiles(int64_t t, int64_t rows, int64_t bytes) { return t >= 12 && t * bytes > 32768 && rows >= 24576 && rows * bytes <= int64_t(1) << 28; }
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
@@ -232,7 +238,7 @@ int lpmm_f8_matmul(const lpmm_f8* a, const lpmm_f8* b, void* c, int dtype, int64
 
 size_t lpmm_f8_linear_workspace_bytes(int64_t t, int64_t n, int64_t k) {
     F8Mat x{}, w{};
-    if (t < 1 || t > kMaxTokens || check_f8(t, k, 1, &x) || check_f8(n, k, 128, &w) || n < 1 || few(t, x.bytes)) return 0;
+    if (t < 1 || t > kMaxTokens || check_f8(t, k, 1, &x) || check_f8(n, k, 128, &w) || n < 1 || (few(t, x.bytes) && !few_by_tiles(t, n, x.bytes))) return 0;
     return up16(size_t(t) * x.bytes) + up16(size_t(scale_rows(x)) * x.scale_bytes) + lpmm_f8_matmul_workspace_bytes(t, n, k);
 }
 
@@ -245,14 +251,17 @@ int lpmm_f8_linear(const void* x, int dtype, int64_t t, int64_t x_stride, const 
     LPMM_TRY(check_rows(y, dtype, w->rows ? t : 0, w->rows, y_stride));
     if (t == 0 || mw.rows == 0) return LPMM_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (few(t, mw.bytes)) {
+    if (few(t, mw.bytes) && !(dtype == LPMM_BF16 && few_by_tiles(t, mw.rows, mw.bytes))) {
         const size_t lds = up16(size_t(t) * (mw.bytes + mw.bytes / kF8Block));
-        // 16 waves share the blocks of 16 rows; where rows abound, two those of 32 (us, 1 token, each: 4096 x 4096 5.3, 18; 11008 x 4096 9.6, 18; 32000 x 4096 23, 22;
-        // 50257 x 1024 11.5, 11.2).  Two workgroups a CU while x leaves room for them (16 tokens 11008 x 4096 one 16.1, two 24)
+        // 16 waves share the blocks of 16 rows; of rows of about 4096 two share those of 32 where tiles of 128 rows are one a CU, nearly (us, 1 token bf16, each: 4096 x 4096 5.3, 18;
+        // 16384 x 4096 13.0, 18.2; 24576 x 4096 20.3, 18.5; 28672 x 4096 22.5, 19.9; 32000 x 4096 24.7, 21.7, 8 tokens 26.5, 25.9, 16 tokens 29.3, 30.2; 36864 x 4096 25.6, 34.4; 50257 x
+        // 4096 34.6, 35.3; 32000 x 5120 25.0, 26.3; 32000 x 2048 11.9, 13.7; 50257 x 1024 10.6, 11.5).  Two workgroups a CU while x leaves room for them (16 tokens 11008 x 4096 one 16.1, two 24)
         const int64_t most = lds <= 32768 ? 512 : 256;
+        const int blocks = mw.bytes / kF8Block;
+        const bool wide = t <= 8 && blocks >= 32 && blocks < 40 && mw.rows >= 24576 && mw.rows <= 32768;
 #define LPMM_FEW(B, K, N, T) hipLaunchKernelGGL((f8_few_kernel<B, K, N, T, 2>), dim3(unsigned(std::min<int64_t>(most, div_up(mw.rows, 16 * T * N)))), dim3(64 * K * N), lds, \
                                                 s, mw, x, int(t), int(w->cols), x_stride, y, y_stride)
-        if (mw.rows >= 16384) { if (dtype == LPMM_BF16) LPMM_FEW(true, 2, 4, 2); else LPMM_FEW(false, 2, 4, 2); }
+        if (wide) { if (dtype == LPMM_BF16) LPMM_FEW(true, 2, 4, 2); else LPMM_FEW(false, 2, 4, 2); }
         else { if (dtype == LPMM_BF16) LPMM_FEW(true, 16, 1, 1); else LPMM_FEW(false, 16, 1, 1); }
 #undef LPMM_FEW
         LPMM_HIP(hipGetLastError());

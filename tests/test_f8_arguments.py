@@ -115,3 +115,11 @@ def test_the_largest_matrices():
     long = 2 ** 22 + 1
     assert L.lpmm_f8_quant_both(None, 0, 1, at(f8(long, 1, 1)), at(f8(1, long, 1)), None) == -1
     assert L.lpmm_f8_quant_both(None, 0, 1, at(f8(long, 1, 128)), at(f8(1, long, 128)), None) == -1
+
+
+def test_workspace_of_few_tokens():
+    """None where a kernel of their own takes them for either type; that of the tiles next to where results in bf16 take these"""
+    need = lpmm.lib().lpmm_f8_linear_workspace_bytes
+    assert need(1, 32000, 4096) == need(11, 24576, 4096) == need(12, 24575, 4096) == need(16, 24576, 2048) == need(12, 65537, 4096) == 0
+    for t, n, k in ((12, 24576, 4096), (16, 32000, 4096), (16, 65536, 4096), (13, 50257, 2560), (12, 30000, 5120)):
+        assert need(t, n, k) >= t * (k + k // 128)

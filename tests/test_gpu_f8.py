@@ -463,3 +463,18 @@ def test_more_rows_than_a_launch_has_workgroups():
         assert ref.same(lpmm.lpmm_f8_dequant(lpmm.lpmm_f8_quant(x[part]), F32).cpu().double(), want)
         assert torch.equal(q.codes[part], lpmm.lpmm_f8_quant(x[part]).codes)
     assert q.scales[0, rows:].tolist() == [0, 0, 0] and bool((q.codes[:, 2:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,n,k", [(1, 24576, 4100), (8, 24575, 4096), (8, 24577, 5000), (9, 32768, 4096), (3, 32769, 4001), (11, 24576, 4096), (12, 24576, 4096), (16, 24575, 4000), (16, 24577, 4000),
+                                   (16, 65536, 4096), (16, 65537, 4096), (13, 50257, 2560), (5, 16384, 8192)])
+def test_few_tokens_next_to_the_rules_borders(t, n, k, dtype):
+    """Whichever kernel takes them, rows of W at the start, at the end, and where tiles meet"""
+    progress(f"{t} x {n} x {k} {dtype}")
+    x, w = matrix(t, k, dtype, t + k, 0.7), matrix(n, k, BF16, n, 0.7)
+    q = lpmm.lpmm_f8_quant(w.to(DEV), 128)
+    y = lpmm.lpmm_f8_linear(x.to(DEV), q)
+    some = torch.cat([torch.arange(40), torch.arange(n // 2, n // 2 + 300), torch.arange(n - 70, n)]).to(DEV)
+    values = lpmm.lpmm_f8_dequant(q)[some].cpu().double()
+    ref.check_product(y[:, some], ref.quantize(x, 1)[0], values, f"{t} x {n} x {k}")
+    assert torch.equal(y, lpmm.lpmm_f8_linear(x.to(DEV), q)) and bool(torch.isfinite(y).all())
