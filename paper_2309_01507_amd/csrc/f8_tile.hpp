@@ -1,8 +1,9 @@
 // The product of two matrices in 8 bits: c[i][j] = sum_k a[i][k] b[j][k].
 //
-// Results of 16 bits: v_mfma_scale_f32_32x32x64_f8f6f4 multiplies codes and applies both blocks' powers.  It adds up the 64 products of a step
-// with terms cut off some 2^-13 below the largest (measured: 1.5e-5 of the result's size, for every fp8 form), which is far below the
-// half step of up to 2^-8 that rounding to bf16 costs.  Results of 32 bits: the codes times their powers become bf16, which holds them
+// Results of 16 bits: v_mfma_scale_f32_32x32x64_f8f6f4 multiplies codes and applies both blocks' powers.  It adds up eight neighbouring products at once, each cut off at 2^-13 of the
+// largest 2^(ea + eb) among them (exponents of the codes, -6 for those below the normal numbers; measured, for v_mfma_scale_f32_16x16x128_f8f6f4 as well), and goes on in fp32.  That
+// is at most 2^-10 of the products' magnitudes (2^-7 where the largest of eight has a code below the normal numbers); of normally distributed operands it takes 1.5e-5 of the result's
+// norm, where rounding to bf16 takes 1.7e-3, and is taken for twice the rate.  Results of 32 bits: the codes times their powers become bf16, which holds them
 // exactly, and v_mfma_f32_32x32x16_bf16 adds them up in fp32, at half the rate.
 //
 // Operand layout of v_mfma_scale_f32_32x32x64_f8f6f4: lane l holds, of row (A) or column (B) l % 32, 32 bytes of the half l / 32 of the

@@ -478,3 +478,57 @@ def test_few_tokens_next_to_the_rules_borders(t, n, k, dtype):
     values = lpmm.lpmm_f8_dequant(q)[some].cpu().double()
     ref.check_product(y[:, some], ref.quantize(x, 1)[0], values, f"{t} x {n} x {k}")
     assert torch.equal(y, lpmm.lpmm_f8_linear(x.to(DEV), q)) and bool(torch.isfinite(y).all())
+
+
+def cut_off(a, b):
+    """How much the matrix instructions on 8 bits may lose of each of a's rows times each of b's, from the codes: of each eight neighbouring products, up to seven times 2^-13 of the largest
+    2^(ea + eb), with the exponents of the codes, -6 for those below the normal numbers, and of products that are not 0"""
+    def exponents(m):
+        codes = m.codes.cpu().long() & 127
+        scales = m.scales.cpu().double()
+        scales = scales[:, :m.rows].t() if m.tile == 1 else scales[:, :codes.shape[1] // 128].repeat_interleave(128, 0)[:m.rows]
+        e = ((codes >> 3).clamp(min=1) - 7).double() + (scales - 127).repeat_interleave(128, 1)
+        return torch.where(codes > 0, e, torch.full_like(e, -INF))
+    ea, eb = exponents(a), exponents(b)
+    return torch.stack([torch.exp2((ea[i] + eb).view(b.rows, -1, 8).amax(2) - 13).sum(1) * 7 for i in range(a.rows)])
+
+
+def check_cut(x, w, what):
+    """x: in bf16 too.  Few tokens and tiles; rounding to bf16, what is cut off, and a rounding of fp32 for each term"""
+    w = w.to(DEV)
+    b = lpmm.lpmm_f8_quant(w, 128)
+    a = lpmm.lpmm_f8_quant(x.to(DEV))
+    va, vb = ref.unpack(a)[0], ref.unpack(b)[0]
+    want, size = va @ vb.t().contiguous(), va.abs() @ vb.abs().t().contiguous()
+    lost = cut_off(a, b)
+    for form, got in (("tiles", lpmm.lpmm_f8_matmul(a, b)), ("linear", lpmm.lpmm_f8_linear(x.to(DEV).bfloat16(), b))):
+        ref.assert_within(got, want, 2.0 ** -8 * want.abs() + (1 + 2.0 ** -8) * (lost + x.shape[1] * 2.0 ** -24 * size), f"{what} {form}")
+    ref.check_product(lpmm.lpmm_f8_matmul(a, b, F32), va, vb, f"{what} fp32")
+    return want, lost
+
+
+@pytest.mark.parametrize("m,n,k,spread", [(3, 70, 1000, 1.0), (16, 33, 515, 4.0), (40, 70, 640, 4.0), (40, 50, 300, 8.0)])
+def test_what_results_of_16_bits_lose(m, n, k, spread):
+    """Elements that spread over codes below the normal numbers, with zeros among them"""
+    g = torch.Generator().manual_seed(m + n)
+    x, w = (torch.randn(r, k, generator=g) * (spread * torch.randn(r, k, generator=g)).exp() for r in (m, n))
+    x[x < 0] = 0.0
+    check_cut(x.bfloat16().float(), w, f"{m} x {n} x {k} {spread}")
+
+
+@pytest.mark.parametrize("t", [2, 20])
+def test_the_most_that_results_of_16_bits_lose(t):
+    """Of a product whose code is the least of all, 2^-9 times 256, and seven of just below 2^-11 beside it these are lost, 2^-7.3 of the sum; a block's largest codes meet zeros.  And sums
+    that cancel: nothing of them is left but what fp32 keeps."""
+    x, w = torch.zeros(t, 256), torch.zeros(5, 256)
+    x[:, 8], w[:, 8] = 2.0 ** -9, 256.0
+    x[:, 9:16], w[:, 9:16] = 1.875 * 2.0 ** -6, 2.0 ** -6
+    x[:, 100], w[:, 120] = 448.0, 448.0
+    want, lost = check_cut(x, w, "least code")
+    assert 2.0 ** -8 < float((lost / want)[0, 0]) < 2.0 ** -7
+    x, w = torch.zeros(t, 256), torch.zeros(5, 256)
+    x[:, :8], w[:, 2:8] = 2.0 ** -7, 2.0 ** -7
+    x[:, 0] = x[:, 1] = w[:, 0] = 16.0
+    w[:, 1] = -16.0
+    want, lost = check_cut(x, w, "cancels")
+    assert bool((want == 6 * 2.0 ** -14).all()) and bool((lost > want).all())
