@@ -532,3 +532,10 @@ def test_the_most_that_results_of_16_bits_lose(t):
     w[:, 1] = -16.0
     want, lost = check_cut(x, w, "cancels")
     assert bool((want == 6 * 2.0 ** -14).all()) and bool((lost > want).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("blocks", [1, 2, 4, 5, 9, 10])
+def test_large_tiles_of_any_number_of_blocks(blocks, dtype):
+    """256 x 256: the loop over two blocks a turn not at all, once and many times, and one or two blocks behind it"""
+    product_of(4100, 2600, 128 * blocks - 3, dtype, (1, 128), blocks)
