@@ -663,7 +663,8 @@ int lpmm_grad_plan_build(const lpmm_grad_desc* descs, int64_t n, void* device, s
 int lpmm_grad_norm(const lpmm_grad_plan* plan, int kind, float* norm, void* stream);
 
 /* out = grad * min(1, limit / (norm[0] + 1e-6)), the factor rounded to fp32, the product to the gradient's type.  A factor of 1 writes nothing in
- * place.  norm: device memory.  limit >= 0, infinity included, which is factor 1; a NaN norm makes all gradients NaN, an infinite one makes finite gradients 0. */
+ * place.  norm: device memory.  limit >= 0; infinity is factor 1 whatever the norm.  Else a NaN norm makes
+ * all gradients NaN, an infinite one makes finite gradients 0. */
 int lpmm_grad_clip(const lpmm_grad_plan* plan, const float* norm, float limit, void* stream);
 /* Both, one after the other. */
 int lpmm_grad_norm_clip(const lpmm_grad_plan* plan, int kind, float limit, float* norm, void* stream);

@@ -209,3 +209,13 @@ def test_a_plan_in_memory_that_is_still_written():
     lpmm.lpmm_grad_norm(plan, norm=norm, stream=s)
     s.synchronize()
     check_norm(norm, norm_of(grads, 0), "on a stream")
+
+
+@pytest.mark.parametrize("value", [NAN, INF])
+def test_an_infinite_limit_limits_nothing(value):
+    """Not even where the norm is no number or infinite: what is finite stays as it is"""
+    g = torch.arange(1.0, 101.0, device=DEV)
+    g[7] = value
+    before, plan = g.clone(), lpmm.new_grad_plan([g])
+    assert not math.isfinite(float(lpmm.lpmm_grad_norm_clip(plan, INF)))
+    assert torch.equal(g.nan_to_num(-1.0), before.nan_to_num(-1.0))
