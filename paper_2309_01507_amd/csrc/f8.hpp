@@ -76,7 +76,8 @@ __device__ __forceinline__ uint32_t f8_top16(const float v[8]) {
 // ---- to 8 bits ---------------------------------------------------------------------------------------------------------------------
 
 // Blocks of 1 x 128: 16 lanes a block, 8 elements each; a wave takes four blocks of a row, a workgroup of four rows, and goes on to others where a launch cannot have so many.
-// rows_up: rows rounded up to a multiple of 4, so that the rest of a row of scales is written too.  Bound by memory: 4096 x 11008 bf16 22.7 us, 5.9 TB/s.
+// rows_up: rows rounded up to a multiple of 4, so that the rest of a row of scales is written too.  Bound by memory: 4096 x 11008 bf16 27.5 us, 4.9
+// TB/s, of inputs that no cache holds, 22.9 of one that was just read.
 template <bool BF16>
 __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t stride, int rows, int cols, int blocks, uint8_t* codes, uint8_t* scales,
                                                        int rows_up) {
@@ -104,8 +105,8 @@ __global__ __launch_bounds__(256) void f8_quant_kernel(const void* x, int64_t st
 
 // A tile of 128 x 128 a workgroup, for 128 x 128 blocks and for a matrix together with its transpose.  A thread takes 8 rows by 8
 // columns: the maxima of rows, columns or all go over lanes and LDS, the transposed codes through LDS, 8 rows a piece.
-// TILE: rows of a block, 1 or 128.  codes or codes_t may be null.  Bound by memory: 4096 x 11008 bf16 and its transpose 37.8 us, 4.8 TB/s (53 where what it reads was not just
-// written); 4096 x 4096 fp32 in blocks of 128 x 128 16.9 us, 6.0 TB/s.
+// TILE: rows of a block, 1 or 128.  codes or codes_t may be null.  Bound by memory: 4096 x 11008 bf16 and its transpose 50 us, 3.6 TB/s, of inputs
+// that no cache holds (a workgroup loads, waits, writes and ends), 37.6 of one that was just written; 4096 x 4096 fp32 in blocks of 128 x 128 18.2 us, 4.6 TB/s, and 16.9.
 template <bool BF16, int TILE>
 __global__ __launch_bounds__(256) void f8_quant_tile_kernel(const void* x, int64_t stride, int rows, int cols, int across, uint8_t* codes, uint8_t* scales,
                                                             int code_bytes, int scale_bytes, uint8_t* codes_t, uint8_t* scales_t, int code_bytes_t,
@@ -230,7 +231,8 @@ __device__ __forceinline__ void f8_values4(uint32_t w, float power, float out[4]
     out[0] = lo.x * power; out[1] = lo.y * power; out[2] = hi.x * power; out[3] = hi.y * power;
 }
 
-// 16 lanes a block: 8 neighbours each, in fp32 two times 4, so that a wave's stores of 16 bytes are next to each other.  Bound by memory: 4096 x 11008 to bf16 22 us, 6.2 TB/s.
+// 16 lanes a block: 8 neighbours each, in fp32 two times 4, so that a wave's stores of 16 bytes are next to each other.  Bound by memory: 4096 x 11008 to bf16
+// 26.9 us, 5.0 TB/s, of codes that no cache holds, 22.3 of those just written.
 template <bool BF16>
 __global__ __launch_bounds__(256) void f8_dequant_kernel(F8Mat m, int cols, int blocks, void* out, int64_t stride) {
     const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);

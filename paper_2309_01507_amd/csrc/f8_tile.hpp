@@ -94,8 +94,8 @@ __device__ __forceinline__ void f8_store(void* out, int64_t at, int left, const 
 // A workgroup of WM x WN waves takes WM MT 32 rows of a and WN NT 32 rows of b; blocks of 128 go through LDS, one ahead.  FAST: results of 16
 // bits.  blockIdx.y: which of the reduction's parts of `per` blocks; their sums go to parts[y][row][column] as fp32 where there are several.
 //
-// Bound by the matrix unit and by what it waits for: 8192^3 to bf16 420 us, 2.6 PFLOP/s (with both operands kept in registers 275, with the meetings left out 356, with the loads
-// left out 384); 4096 x 11008 x 4096 164 us, 2.25 PFLOP/s, fp32 4096^3 109 us, 1.26 (the bf16 unit's half rate; a conversion for each 8 codes of each wave).  256 x 256 reads each
+// Bound by the matrix unit and by what it waits for: from a graph of 20 calls 8192^3 to bf16 426 us, 2.6 PFLOP/s (with both operands kept in registers 275, with the meetings left out 356, with the loads
+// left out 384); 4096 x 11008 x 4096 162 us, 2.28 PFLOP/s, and 168 to 195, behind the kernel that brings x to 8 bits, by the profiler; fp32 4096^3 110 us, 1.25 (the bf16 unit's half rate; a conversion for each 8 codes of each wave).  256 x 256 reads each
 // code from LDS a fourth as often as it is multiplied with 64.  Codes go straight into LDS, one block ahead: through registers 64 x 64 tiles took 242 us for the first, and two
 // blocks ahead, or halves of a block between meetings, spilled or gained nothing.  Scales are one byte a row and block, loaded a block ahead without a condition: a
 // conditional load makes the wave wait for all others, and bytes that stand a row of blocks apart take a line each.
@@ -250,8 +250,8 @@ constexpr int kF8FewTokens = 16, kF8FewBytes = 65536;          // codes of x tha
 // as long as there are any.  Codes of W come from memory into the registers that are the operand, AHEAD blocks in front of their use; the first
 // are on their way while the workgroup brings x to 8 bits.  The waves' sums of a row meet in LDS.
 //
-// Bound by reading W: one token through 32000 x 4096 bf16 22 us, 6.0 TB/s, through 11008 x 4096 9.6 us, 4.7, through 4096 x 4096 5.3 us, 3.2 (one round trip to memory, x and the
-// join).  Every workgroup brings the same x to 8 bits, which a kernel in front would do once, for a launch (so it began: 1 x 4096 x 4096 9.9 us);
+// Bound by reading W: one token through 32000 x 4096 bf16 22 us, 6.0 TB/s, through 11008 x 4096 9.6 us, 4.7, through 4096 x 4096 4.9 us, 3.4 (one round trip to memory, x and the
+// join), with W behind L2 but not out of the memory's own cache.  Every workgroup brings the same x to 8 bits, which a kernel in front would do once, for a launch (so it began: 1 x 4096 x 4096 9.9 us);
 // each token more costs 0.35 us of conversions.  Loads of four units at once took as long.
 template <bool BF16, int WK, int WN, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * WK * WN) void f8_few_kernel(F8Mat w, const void* x, int t, int k, int64_t x_stride, void* y, int64_t y_stride) {

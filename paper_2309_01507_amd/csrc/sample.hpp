@@ -791,8 +791,9 @@ struct SampleRow {
 };
 
 // Bound by the vector units: of 62 instructions for a logit the weight in 64 bits is 25, the sums and comparisons beside it 8, the search in 32 bits 12 and the largest 3
-// (the rest is by row), 91 percent of the time; the row is read three times, mostly from behind L2.  2048 x 32000 bf16, top_p 0.98: 149 us, 880 GB/s of logits (with two
-// passes in 64 bits, one for the bins of the border and one for the sums, 211); without top_p 93; with top_k 50 83.  1 x 16000 22 us, by the waits between the steps.  A row
+// (the rest is by row), 91 percent of the time; the row is read three times, mostly from behind L2.  2048 x 32000 bf16, top_p 0.98: 130 us from a graph of 20 calls, 1.0 TB/s
+// of logits; without top_p 84; with top_k 50 77, 500 143.  (The profiler's kernel time is 151; with two passes in 64 bits, one for the bins of the border and one for the sums, it was 211.)
+// 1 x 16000 20 us, by the waits between the steps.  A row
 // kept in LDS was 5 percent faster with one row a CU, and 1.4 times slower with many; in registers it spilled.  512 threads are held to 64 registers, so that four workgroups
 // run on a CU (151 us without).
 template <bool BF16, int THREADS>
@@ -804,7 +805,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 : 1) void sample_kernel
 
 // ---- few rows: several workgroups a row -------------------------------------------------------------------------------------------
 //
-// Three launches, with the whole row read in each (1 x 32000 fp32 22 us, 1 x 131072 bf16 32, 16 x 50257 bf16 31: bound by the waits of the last workgroups, of
+// Three launches, with the whole row read in each (1 x 32000 fp32 23 us, 1 x 131072 bf16 32, 16 x 50257 bf16 30: bound by the waits of the last workgroups, of
 // one row 8.5 us for the bins and 10 for the end): the largest logit; the bins, from which the last workgroup of a row to finish finds the one in question; the sums of the lines
 // above it and the list of its logits, from which the last one draws.  With top_k the list is of all logits down to the bin.  Lists that are too long, and min_p of 1
 // and more, are left to the last workgroup as a whole.
